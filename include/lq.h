@@ -344,6 +344,104 @@ lq_status lq_rot_apply(const lq_config *cfg, const float *L, const float *R, con
 /* Copy parts of the state out (device to device). */
 lq_status lq_rot_unpack(const lq_config *cfg, const void *state, const lq_rot_view *out, void *stream);
 
+/* ---- Low-rank adapters of many requests beside a shared projection -----------------------------------------------
+   Row m of a batch belongs to the adapter ids[m] of a pool; its low-rank product is added to what the shared projection gave:
+       Y[m] = Yin[m] + scale_a (X[m] A_a^T) B_a^T ,   a = ids[m] ;   Y[m] = Yin[m] for ids[m] outside [0, slots).
+   Training: with dY the derivative of a loss with respect to Y, and U[m] = scale_a dY[m] B_a,
+       dX[m] = dXin[m] + U[m] A_a ,   dA_a = sum of U[m]^T X[m] ,   dB_a = scale_a sum of dY[m]^T (X[m] A_a^T)   over the rows of a;
+   the gradients of an adapter without rows, and of the ranks that an adapter does not have, are zero.
+   X, dX, dXin: cfg.x_dtype.  Yin, Y, dY, A, B: bf16.  The products X A^T and dY B are held in fp32; outputs are rounded once.  Where an
+   output is bf16 they enter the second product as two bf16 terms (2^-16 of the value), where it is fp32 as three (all of it).
+   Rows may come in any order; a row's result does not depend on the other rows of the batch.  In this section X, Yin, dY and dXin may hold
+   infinities and NaN: they stay in their row (and in the gradients of its adapter). */
+typedef struct {
+    int64_t N, K;       /* of the shared projection: multiples of 64                                      */
+    int32_t rank;       /* of the pool's arrays: a multiple of 8, 8 .. 128                                */
+    int32_t slots;      /* adapters in the pool, 1 .. 1024                                                */
+    int32_t x_dtype;    /* lq_dtype of X, dXin, dX                                                        */
+    int32_t flags;      /* 0                                                                              */
+} lq_adapter_config;
+
+typedef struct {        /* device memory of the caller                                                    */
+    const void *A;      /* slots x rank x K   bf16, dense, 16-byte aligned                                */
+    const void *B;      /* slots x N x rank   bf16, dense, 16-byte aligned                                */
+    const int32_t *ranks; /* slots   rank of each adapter, 0 .. rank (others are taken as the nearer end); what the arrays hold
+                           beyond it is not used                                                          */
+    const float *scales;  /* slots                                                                        */
+} lq_adapter_pool;
+
+/* The grouping of a batch: the rows in the order of their adapters (stable), in tiles of up to 64 rows of one adapter.  It depends on
+   ids (device, M int32) and slots alone: made once for a batch, it serves every projection that the batch goes through.  1 <= slots <=
+   1024, 0 <= M <= 2^24.  plan: device, 256-byte aligned, at least plan_bytes of lq_adapter_plan_sizes (host-only). */
+lq_status lq_adapter_plan_sizes(int64_t M, int32_t slots, size_t *plan_bytes);
+lq_status lq_adapter_plan(int32_t slots, const int32_t *ids, int64_t M, void *plan, size_t plan_bytes, void *stream);
+
+/* Bytes of `inter` (X A^T of every row in fp32: forward's workspace, which the backward of the same batch reads) and of the
+   backward's workspace `work`; either pointer may be NULL.  Host-only. */
+lq_status lq_adapter_sizes(const lq_adapter_config *cfg, int64_t M, size_t *inter_bytes, size_t *work_bytes);
+
+/* Forward.  X: M x K, row stride ldx elements; Yin, Y: M x N, row strides ldyin, ldy; 16-byte aligned pointers, strides a multiple of 16
+   bytes and at most 2^22 elements.  Y may be Yin (same pointer and stride: rows without an adapter are then not touched) and must not overlap it
+   otherwise.  plan: of lq_adapter_plan for the same M and slots. */
+lq_status lq_adapter_fwd(const lq_adapter_config *cfg, const void *plan, size_t plan_bytes, const lq_adapter_pool *pool, const void *X,
+                         int64_t ldx, const void *Yin, int64_t ldyin, void *Y, int64_t ldy, int64_t M, void *inter, size_t inter_bytes,
+                         void *stream);
+
+/* Backward.  inter: as lq_adapter_fwd left it for the same plan, pool and X.  dXin: the gradient that comes through the shared
+   projection, or NULL for none; dX may be dXin (same pointer and stride).  dA: slots x rank x K, dB: slots x N x rank, fp32, dense, 16-byte aligned, overwritten
+   (for M = 0 with zeros).  Sums over rows are fixed in their order: repeated calls give identical bits. */
+lq_status lq_adapter_bwd(const lq_adapter_config *cfg, const void *plan, size_t plan_bytes, const lq_adapter_pool *pool, const void *X,
+                         int64_t ldx, const void *inter, size_t inter_bytes, const void *dY, int64_t lddy, const void *dXin,
+                         int64_t lddxin, void *dX, int64_t lddx, float *dA, float *dB, int64_t M, void *work, size_t work_bytes,
+                         void *stream);
+
+/* ---- Norm of queries and keys for each head, with the rotation by positions of several axes in the same pass -----
+   x is one head of one token (head_dim values), w the weight of queries or of keys:
+       n = x / sqrt(mean(x^2) + eps) * w                     (LQ_NORM_RMS;  LQ_NORM_NONE: n = x)
+       (n_a, n_b) of pair p  ->  (n_a cos t - n_b sin t,  n_a sin t + n_b cos t) ,   t = pos[m][axis of p] * inv_freq[p] .
+   Pairs are numbered axis by axis: the first pairs[0] belong to axis 0, the next pairs[1] to axis 1, ...; P = their sum, 2 P <= head_dim.
+   LQ_PAIR_HALF: pair p is the values p and p + P; LQ_PAIR_ADJACENT: 2 p and 2 p + 1.  Values from 2 P on are not rotated.  axes = 0:
+   the norm alone.  Angles are taken from the exact product of the two fp32 numbers, everything else is held in fp32 and rounded once.
+   Token m has row m % pos_rows of pos (pos_rows x axes, fp32, dense): a batch of equal grids needs one grid's positions. */
+typedef enum { LQ_PAIR_HALF = 0, LQ_PAIR_ADJACENT = 1 } lq_pairing;
+typedef enum { LQ_NORM_NONE = 0, LQ_NORM_RMS = 1 } lq_norm;
+
+typedef struct {
+    int32_t heads_q, heads_k;  /* either may be 0 (its views are then not looked at), not both; sum <= 4096     */
+    int32_t head_dim;          /* even, 2 .. 256                                                              */
+    int32_t axes;              /* 0 .. 4                                                                      */
+    int32_t pairs[4];          /* rotated pairs of each axis, >= 0; those past `axes` must be 0                */
+    int32_t pairing, norm;     /* lq_pairing, lq_norm                                                         */
+    int32_t dtype;             /* lq_dtype of queries, keys and their gradients                               */
+    int32_t flags;             /* 0                                                                           */
+    float eps;                 /* > 0 (LQ_NORM_RMS)                                                           */
+} lq_qk_config;
+
+/* Heads of M tokens: value j of head h of token m is p[m * ld + h * hs + j], strides in elements, below 2^40 in size, not negative; p aligned to its type. */
+typedef struct {
+    void *p;
+    int64_t ld, hs;
+} lq_heads;
+
+/* q, k -> qo, ko.  An output may be its input (same pointer and strides: in place, as in the rows of a fused QKV projection) and must not
+   overlap an input otherwise.  wq, wk: head_dim fp32, or NULL for ones.  pos, inv_freq (P fp32): may be NULL with axes = 0. */
+lq_status lq_qk_norm_rope_fwd(const lq_qk_config *cfg, const lq_heads *q, const lq_heads *k, const float *wq, const float *wk,
+                              const float *pos, int64_t pos_rows, const float *inv_freq, const lq_heads *qo, const lq_heads *ko, int64_t M,
+                              void *stream);
+
+/* Bytes of the backward's workspace.  Host-only. */
+lq_status lq_qk_work_sizes(const lq_qk_config *cfg, int64_t M, size_t *work_bytes);
+
+/* Gradients: with g the rotation's transpose applied to the derivative with respect to the output, xh = x / sqrt(mean(x^2) + eps):
+       dw = sum over tokens and heads of g * xh ,   dx = (g w - xh mean(g w xh)) / sqrt(mean(x^2) + eps)        (LQ_NORM_NONE: dx = g).
+   q, k: the forward's inputs (not looked at with LQ_NORM_NONE); dqo, dko: derivatives with respect to its outputs; dq, dk may be dqo, dko
+   (same pointer and strides).  dwq, dwk: head_dim fp32 each, overwritten (zeros without tokens or heads), both or neither NULL; looked at with LQ_NORM_RMS only.  Sums are fixed in their
+   order: repeated calls give identical bits. */
+lq_status lq_qk_norm_rope_bwd(const lq_qk_config *cfg, const lq_heads *q, const lq_heads *k, const float *wq, const float *wk,
+                              const float *pos, int64_t pos_rows, const float *inv_freq, const lq_heads *dqo, const lq_heads *dko,
+                              const lq_heads *dq, const lq_heads *dk, float *dwq, float *dwk, int64_t M, void *work, size_t work_bytes,
+                              void *stream);
+
 #ifdef __cplusplus
 }
 #endif

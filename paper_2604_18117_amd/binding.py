@@ -4,7 +4,7 @@ PyTorch is used for device memory and the current stream, nothing else: every st
 path runs in the library's kernels.  Importing this module fails loudly when the HIP library
 has not been built (``python paper_2604_18117_amd/build.py``); there is no CPU fallback.
 
-The entry points of a program's loops (activation step, forward, hand-off, packing, calibration and rotation steps) hand their arguments to the
+The entry points of a program's loops (activation step, forward, hand-off, packing, calibration and rotation steps, adapters, norm and rotation of queries and keys) hand their arguments to the
 native module ``_call`` (csrc/lq_call.cpp) as they are; it makes the call where they are of the ordinary kind (status >= 0) and does
 nothing otherwise (-1).  The checks and the ctypes call below each of them then decide, as for every other entry point.  ``_call`` belongs to
 one build of torch; where it cannot be loaded a warning says so and every call takes the ctypes route, which needs liblq.so alone.
@@ -94,10 +94,35 @@ class lq_rot_view(C.Structure):
     _fields_ = [(k, C.c_void_p) for k in ("Omega", "Mom", "G", "E1", "E2")]
 
 
+class lq_adapter_config(C.Structure):
+    _fields_ = [("N", C.c_int64), ("K", C.c_int64)] + [(k, C.c_int32) for k in ("rank", "slots", "x_dtype", "flags")]
+
+
+class lq_adapter_pool(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("A", "B", "ranks", "scales")]
+
+
+LQ_PAIR_HALF, LQ_PAIR_ADJACENT = 0, 1
+LQ_NORM_NONE, LQ_NORM_RMS = 0, 1
+
+
+class lq_qk_config(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("heads_q", "heads_k", "head_dim", "axes")] + [("pairs", C.c_int32 * 4)] + \
+               [(k, C.c_int32) for k in ("pairing", "norm", "dtype", "flags")] + [("eps", C.c_float)]
+
+
+class lq_heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64), ("hs", C.c_int64)]
+
+
+_call.set_operator_config_types(lq_adapter_config, lq_qk_config)
+
 EXPORTS = ["lq_status_string", "lq_packed_sizes", "lq_pack_weights", "lq_verify_blob", "lq_set_smoothing", "lq_act_sizes", "lq_quantize_act",
            "lq_linear_lowrank_fwd", "lq_handoff_sizes", "lq_linear_lowrank_fwd_handoff", "lq_branch_from_codes",
            "lq_unpack_weights", "lq_unpack_act", "lq_calib_sizes", "lq_calib_init", "lq_calib_step",
-           "lq_calib_unpack", "lq_rot_sizes", "lq_rot_init", "lq_rot_step", "lq_rot_step_static", "lq_rot_apply", "lq_rot_unpack"]
+           "lq_calib_unpack", "lq_rot_sizes", "lq_rot_init", "lq_rot_step", "lq_rot_step_static", "lq_rot_apply", "lq_rot_unpack",
+           "lq_adapter_plan_sizes", "lq_adapter_plan", "lq_adapter_sizes", "lq_adapter_fwd", "lq_adapter_bwd",
+           "lq_qk_norm_rope_fwd", "lq_qk_work_sizes", "lq_qk_norm_rope_bwd"]
 
 _lib.lq_calib_sizes.argtypes = [C.POINTER(lq_config), C.POINTER(C.c_size_t)]
 _lib.lq_calib_init.argtypes = [C.POINTER(lq_config), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -131,6 +156,20 @@ _lib.lq_branch_from_codes.argtypes = [C.POINTER(lq_config), C.c_void_p, C.c_size
                                       C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lq_unpack_weights.argtypes = [C.POINTER(lq_config), C.c_void_p, C.POINTER(lq_weights_view), C.c_void_p]
 _lib.lq_unpack_act.argtypes = [C.POINTER(lq_config), C.c_void_p, C.c_int64, C.POINTER(lq_act_view), C.c_void_p]
+_lib.lq_adapter_plan_sizes.argtypes = [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+_lib.lq_adapter_plan.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_adapter_sizes.argtypes = [C.POINTER(lq_adapter_config), C.c_int64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
+_lib.lq_adapter_fwd.argtypes = [C.POINTER(lq_adapter_config), C.c_void_p, C.c_size_t, C.POINTER(lq_adapter_pool), C.c_void_p, C.c_int64, C.c_void_p,
+                                C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_adapter_bwd.argtypes = [C.POINTER(lq_adapter_config), C.c_void_p, C.c_size_t, C.POINTER(lq_adapter_pool), C.c_void_p, C.c_int64, C.c_void_p,
+                                C.c_size_t, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                C.c_void_p, C.c_size_t, C.c_void_p]
+_H = C.POINTER(lq_heads)
+_lib.lq_qk_norm_rope_fwd.argtypes = [C.POINTER(lq_qk_config), _H, _H, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, _H, _H, C.c_int64,
+                                     C.c_void_p]
+_lib.lq_qk_work_sizes.argtypes = [C.POINTER(lq_qk_config), C.c_int64, C.POINTER(C.c_size_t)]
+_lib.lq_qk_norm_rope_bwd.argtypes = [C.POINTER(lq_qk_config), _H, _H, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, _H, _H, _H, _H,
+                                     C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
 
 
 class LqError(RuntimeError):
@@ -526,3 +565,215 @@ def lq_rot_unpack(cfg: lq_config, state: torch.Tensor, names=("Omega",)) -> dict
     view = lq_rot_view(**{k: (out[k].data_ptr() if k in out else None) for k in shapes})
     _check(_lib.lq_rot_unpack(C.byref(cfg), _ptr(state), C.byref(view), _stream()), "lq_rot_unpack")
     return out
+
+
+# ---- low-rank adapters of many requests beside a shared projection (argument marshalling only) -------------------------
+
+def make_adapter_config(N: int, K: int, rank: int, slots: int, x_dtype: str = "bf16") -> lq_adapter_config:
+    """A pool of `slots` adapters of a K -> N projection; rank: of its arrays, a multiple of 8 (each adapter has its own up to it)."""
+    return lq_adapter_config(N, K, rank, slots, {"bf16": LQ_BF16, "f32": LQ_F32}[x_dtype], 0)
+
+
+def lq_adapter_plan_sizes(M: int, slots: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.lq_adapter_plan_sizes(M, slots, C.byref(n)), "lq_adapter_plan_sizes")
+    return int(n.value)
+
+
+def lq_adapter_sizes(cfg: lq_adapter_config, M: int):
+    """(bytes of inter, bytes of the backward's work) for M rows."""
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    _check(_lib.lq_adapter_sizes(C.byref(cfg), M, C.byref(a), C.byref(b)), "lq_adapter_sizes")
+    return int(a.value), int(b.value)
+
+
+def _blob_arg(t: torch.Tensor) -> torch.Tensor:
+    assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous(), "workspaces are contiguous uint8 CUDA tensors"
+    return t
+
+
+def lq_adapter_plan(slots: int, ids: torch.Tensor, plan: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """ids: int32 CUDA, one per row: its adapter, or a number outside [0, slots) for none.  Returns the grouping of the batch."""
+    st = _call.adapter_plan(slots, ids, plan)
+    if st >= 0:
+        _check(st, "lq_adapter_plan")
+        return plan
+    assert ids.is_cuda and ids.dtype == torch.int32 and ids.dim() == 1 and ids.is_contiguous()
+    if plan is None:
+        plan = torch.empty(lq_adapter_plan_sizes(ids.shape[0], slots), dtype=torch.uint8, device=ids.device)
+    _check(_lib.lq_adapter_plan(slots, _ptr(ids), ids.shape[0], _ptr(_blob_arg(plan)), plan.numel(), _stream()), "lq_adapter_plan")
+    return plan
+
+
+def _adapter_x_dtype(cfg: lq_adapter_config):
+    return torch.bfloat16 if cfg.x_dtype == LQ_BF16 else torch.float32
+
+
+def _rows_arg(t: torch.Tensor, dtype, M: int, cols: int, what: str) -> torch.Tensor:
+    assert t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape == (M, cols) and t.stride(1) == 1, f"{what}: {M} x {cols} {dtype} CUDA rows"
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])  # (the stride of a single row says nothing)
+
+
+def _adapter_pool(cfg: lq_adapter_config, A: torch.Tensor, B: torch.Tensor, ranks: torch.Tensor, scales: torch.Tensor) -> lq_adapter_pool:
+    for t, shape in ((A, (cfg.slots, cfg.rank, cfg.K)), (B, (cfg.slots, cfg.N, cfg.rank))):
+        assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and tuple(t.shape) == shape, "pool shapes must match cfg"
+    for t, dtype in ((ranks, torch.int32), (scales, torch.float32)):
+        assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == (cfg.slots,), "one rank and one scale per adapter"
+    return lq_adapter_pool(_ptr(A), _ptr(B), _ptr(ranks), _ptr(scales))
+
+
+def lq_adapter_fwd(cfg: lq_adapter_config, plan: torch.Tensor, X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ranks: torch.Tensor,
+                   scales: torch.Tensor, Yin: torch.Tensor, Y: Optional[torch.Tensor] = None, inter: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = Yin + scale (X A^T) B^T of each row's adapter.  X: M x K of cfg's type; A: slots x rank x K, B: slots x N x rank bf16; ranks int32 and
+    scales fp32, one per slot; Yin: M x N bf16, the shared projection's output (Y may be Yin).  inter: workspace that lq_adapter_bwd reads."""
+    st = _call.adapter_fwd(cfg, plan, X, A, B, ranks, scales, Yin, Y, inter)
+    if st >= 0:
+        _check(st, "lq_adapter_fwd")
+        return Y
+    M = X.shape[0]
+    _rows_arg(X, _adapter_x_dtype(cfg), M, cfg.K, "X")
+    _rows_arg(Yin, torch.bfloat16, M, cfg.N, "Yin")
+    pool = _adapter_pool(cfg, A, B, ranks, scales)
+    if Y is None:
+        Y = torch.empty((M, cfg.N), dtype=torch.bfloat16, device=X.device)
+    if inter is None:
+        inter = torch.empty(lq_adapter_sizes(cfg, M)[0], dtype=torch.uint8, device=X.device)
+    _rows_arg(Y, torch.bfloat16, M, cfg.N, "Y")
+    _check(_lib.lq_adapter_fwd(C.byref(cfg), _ptr(_blob_arg(plan)), plan.numel(), C.byref(pool), _ptr(X), _ld(X), _ptr(Yin), _ld(Yin), _ptr(Y), _ld(Y), M,
+                               _ptr(_blob_arg(inter)), inter.numel(), _stream()), "lq_adapter_fwd")
+    return Y
+
+
+def lq_adapter_bwd(cfg: lq_adapter_config, plan: torch.Tensor, X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, ranks: torch.Tensor,
+                   scales: torch.Tensor, inter: torch.Tensor, dY: torch.Tensor, dXin: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
+                   dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None):
+    """(dX, dA, dB) of lq_adapter_fwd, whose `inter` is read.  dY: M x N bf16; dXin: the gradient through the shared projection, or None; dX of cfg's
+    type (may be dXin); dA, dB: fp32, of A's and B's shapes."""
+    st = _call.adapter_bwd(cfg, plan, X, A, B, ranks, scales, inter, dY, dXin, dX, dA, dB, work)
+    if st >= 0:
+        _check(st, "lq_adapter_bwd")
+        return dX, dA, dB
+    M, dtype = X.shape[0], _adapter_x_dtype(cfg)
+    _rows_arg(X, dtype, M, cfg.K, "X")
+    _rows_arg(dY, torch.bfloat16, M, cfg.N, "dY")
+    pool = _adapter_pool(cfg, A, B, ranks, scales)
+    if dX is None:
+        dX = torch.empty((M, cfg.K), dtype=dtype, device=X.device)
+    if dA is None:
+        dA = torch.empty(A.shape, dtype=torch.float32, device=X.device)
+    if dB is None:
+        dB = torch.empty(B.shape, dtype=torch.float32, device=X.device)
+    if work is None:
+        work = torch.empty(lq_adapter_sizes(cfg, M)[1], dtype=torch.uint8, device=X.device)
+    _rows_arg(dX, dtype, M, cfg.K, "dX")
+    if dXin is not None:
+        _rows_arg(dXin, dtype, M, cfg.K, "dXin")
+    for t, like in ((dA, A), (dB, B)):
+        assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == like.shape, "gradient shapes must match the pool"
+    _check(_lib.lq_adapter_bwd(C.byref(cfg), _ptr(_blob_arg(plan)), plan.numel(), C.byref(pool), _ptr(X), _ld(X), _ptr(_blob_arg(inter)), inter.numel(),
+                               _ptr(dY), _ld(dY), _ptr(dXin), _ld(dXin) if dXin is not None else 0, _ptr(dX), _ld(dX), _ptr(dA), _ptr(dB), M,
+                               _ptr(_blob_arg(work)), work.numel(), _stream()), "lq_adapter_bwd")
+    return dX, dA, dB
+
+
+# ---- norm of queries and keys for each head, rotation by positions of several axes (argument marshalling only) ---------
+
+def make_qk_config(heads_q: int, heads_k: int, head_dim: int, pairs=(), pairing: str = "half", norm: bool = True, eps: float = 1e-6,
+                   dtype: str = "bf16") -> lq_qk_config:
+    """pairs: rotated pairs of each axis (up to 4 axes; 2 sum(pairs) <= head_dim).  pairing: "half" (p, p + P) or "adjacent" (2p, 2p + 1)."""
+    pairs = list(pairs)
+    if len(pairs) > 4:
+        raise ValueError("up to 4 axes")
+    return lq_qk_config(heads_q, heads_k, head_dim, len(pairs), (C.c_int32 * 4)(*pairs, *[0] * (4 - len(pairs))),
+                        {"half": LQ_PAIR_HALF, "adjacent": LQ_PAIR_ADJACENT}[pairing], LQ_NORM_RMS if norm else LQ_NORM_NONE,
+                        {"bf16": LQ_BF16, "f32": LQ_F32}[dtype], 0, eps)
+
+
+def lq_qk_work_sizes(cfg: lq_qk_config, M: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.lq_qk_work_sizes(C.byref(cfg), M, C.byref(n)), "lq_qk_work_sizes")
+    return int(n.value)
+
+
+def _qk_dtype(cfg: lq_qk_config):
+    return torch.bfloat16 if cfg.dtype == LQ_BF16 else torch.float32
+
+
+def _heads(cfg: lq_qk_config, t: Optional[torch.Tensor], M: int, heads: int, what: str):
+    if heads == 0:
+        return None
+    assert t.is_cuda and t.dtype == _qk_dtype(cfg) and t.shape == (M, heads, cfg.head_dim) and t.stride(2) == 1, f"{what}: {M} x {heads} x {cfg.head_dim}"
+    return C.byref(lq_heads(_ptr(t), t.stride(0), t.stride(1)))
+
+
+def _qk_vectors(cfg: lq_qk_config, wq, wk, pos, inv_freq):
+    for w in (wq, wk):
+        assert w is None or (w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.numel() == cfg.head_dim), "weights: head_dim fp32 values"
+    P = sum(cfg.pairs)
+    if P:
+        assert pos.is_cuda and pos.dtype == torch.float32 and pos.is_contiguous() and pos.dim() == 2 and pos.shape[1] == cfg.axes, "positions: rows x axes fp32"
+        assert inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.is_contiguous() and inv_freq.numel() == P, "one inverse frequency per pair"
+
+
+def _qk_tokens(q, k) -> int:
+    return (q if q is not None else k).shape[0]
+
+
+def lq_qk_norm_rope_fwd(cfg: lq_qk_config, q: Optional[torch.Tensor], k: Optional[torch.Tensor], wq: Optional[torch.Tensor], wk: Optional[torch.Tensor],
+                        pos: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], qo: Optional[torch.Tensor] = None,
+                        ko: Optional[torch.Tensor] = None):
+    """(qo, ko): the heads of q (M x heads_q x head_dim) and k normalised and rotated.  Any strides of tokens and heads, as of views of a fused QKV
+    projection's rows; qo may be q, ko may be k.  wq, wk: head_dim fp32 or None for ones; pos: rows x axes fp32, token m has row m % rows;
+    inv_freq: fp32, one per pair."""
+    st = _call.qk_norm_rope_fwd(cfg, q, k, wq, wk, pos, inv_freq, qo, ko)
+    if st >= 0:
+        _check(st, "lq_qk_norm_rope_fwd")
+        return qo, ko
+    M = _qk_tokens(q, k)
+    _qk_vectors(cfg, wq, wk, pos, inv_freq)
+    if qo is None and cfg.heads_q:
+        qo = torch.empty((M, cfg.heads_q, cfg.head_dim), dtype=_qk_dtype(cfg), device=q.device)
+    if ko is None and cfg.heads_k:
+        ko = torch.empty((M, cfg.heads_k, cfg.head_dim), dtype=_qk_dtype(cfg), device=k.device)
+    _check(_lib.lq_qk_norm_rope_fwd(C.byref(cfg), _heads(cfg, q, M, cfg.heads_q, "q"), _heads(cfg, k, M, cfg.heads_k, "k"), _ptr(wq), _ptr(wk), _ptr(pos),
+                                    0 if pos is None else pos.shape[0], _ptr(inv_freq), _heads(cfg, qo, M, cfg.heads_q, "qo"),
+                                    _heads(cfg, ko, M, cfg.heads_k, "ko"), M, _stream()), "lq_qk_norm_rope_fwd")
+    return qo, ko
+
+
+def lq_qk_norm_rope_bwd(cfg: lq_qk_config, q: Optional[torch.Tensor], k: Optional[torch.Tensor], wq: Optional[torch.Tensor], wk: Optional[torch.Tensor],
+                        pos: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], dqo: Optional[torch.Tensor], dko: Optional[torch.Tensor],
+                        dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None, dwq: Optional[torch.Tensor] = None,
+                        dwk: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None):
+    """(dq, dk, dwq, dwk) of lq_qk_norm_rope_fwd from its inputs and the derivatives with respect to its outputs; dq may be dqo, dk may be dko.  dwq,
+    dwk: head_dim fp32 (None without the norm)."""
+    st = _call.qk_norm_rope_bwd(cfg, q, k, wq, wk, pos, inv_freq, dqo, dko, dq, dk, dwq, dwk, work)
+    if st >= 0:
+        _check(st, "lq_qk_norm_rope_bwd")
+        return dq, dk, dwq, dwk
+    M = _qk_tokens(dqo, dko)
+    device = (dqo if dqo is not None else dko).device
+    _qk_vectors(cfg, wq, wk, pos, inv_freq)
+    if dq is None and cfg.heads_q:
+        dq = torch.empty((M, cfg.heads_q, cfg.head_dim), dtype=_qk_dtype(cfg), device=device)
+    if dk is None and cfg.heads_k:
+        dk = torch.empty((M, cfg.heads_k, cfg.head_dim), dtype=_qk_dtype(cfg), device=device)
+    if cfg.norm == LQ_NORM_RMS:
+        dwq = torch.empty(cfg.head_dim, dtype=torch.float32, device=device) if dwq is None else dwq
+        dwk = torch.empty(cfg.head_dim, dtype=torch.float32, device=device) if dwk is None else dwk
+        for w in (dwq, dwk):
+            assert w.is_cuda and w.dtype == torch.float32 and w.is_contiguous() and w.numel() == cfg.head_dim
+        if work is None:
+            work = torch.empty(lq_qk_work_sizes(cfg, M), dtype=torch.uint8, device=device)
+        _blob_arg(work)
+    norm = cfg.norm == LQ_NORM_RMS
+    _check(_lib.lq_qk_norm_rope_bwd(C.byref(cfg), _heads(cfg, q, M, cfg.heads_q, "q") if norm else None,
+                                    _heads(cfg, k, M, cfg.heads_k, "k") if norm else None, _ptr(wq), _ptr(wk), _ptr(pos),
+                                    0 if pos is None else pos.shape[0], _ptr(inv_freq), _heads(cfg, dqo, M, cfg.heads_q, "dqo"),
+                                    _heads(cfg, dko, M, cfg.heads_k, "dko"), _heads(cfg, dq, M, cfg.heads_q, "dq"), _heads(cfg, dk, M, cfg.heads_k, "dk"),
+                                    _ptr(dwq), _ptr(dwk), M, _ptr(work), 0 if work is None else work.numel(), _stream()), "lq_qk_norm_rope_bwd")
+    return dq, dk, dwq, dwk

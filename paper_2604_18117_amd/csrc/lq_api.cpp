@@ -531,4 +531,202 @@ lq_status lq_rot_unpack(const lq_config* cfg, const void* state, const lq_rot_vi
     return launch_rot_unpack(d, (const uint8_t*)state, out, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
 }
 
+static lq_status adapter_check(const lq_adapter_config* c)
+{
+    if (!c) return LQ_ERR_NULL;
+    if (c->flags != 0 || (c->x_dtype != LQ_F32 && c->x_dtype != LQ_BF16)) return LQ_ERR_UNSUPPORTED;
+    if (c->N <= 0 || c->K <= 0 || c->N > (1 << 22) || c->K > (1 << 22) || c->N % 64 != 0 || c->K % 64 != 0) return LQ_ERR_SHAPE;
+    if (c->rank < 8 || c->rank > 128 || c->rank % 8 != 0 || c->slots < 1 || c->slots > 1024) return LQ_ERR_SHAPE;
+    if ((int64_t)c->slots * c->rank * (c->N + c->K) >= ((int64_t)1 << 32)) return LQ_ERR_UNSUPPORTED;  // (launches stay below 2^32 threads)
+    return LQ_OK;
+}
+static lq_status adapter_batch_check(const lq_adapter_config* c, int64_t M)
+{
+    if (M < 0 || M > (1 << 24)) return LQ_ERR_SHAPE;
+    const int64_t wide = ((c->N > c->K ? c->N : c->K) + 255) / 256;  // a workgroup of 256 threads per tile and 256 columns
+    return (M / 64 + c->slots + 1) * wide * 256 >= ((int64_t)1 << 32) ? LQ_ERR_UNSUPPORTED : LQ_OK;
+}
+// rows of `len` values of `elem` bytes
+static lq_status rows_check(const void* p, int64_t ld, int64_t len, int elem)
+{
+    if (ld < len || ld > (1 << 22)) return LQ_ERR_SHAPE;
+    return aligned(p, 16) && ld * elem % 16 == 0 ? LQ_OK : LQ_ERR_ALIGN;
+}
+static lq_status pool_check(const lq_adapter_pool* p)
+{
+    if (!p || !p->A || !p->B || !p->ranks || !p->scales) return LQ_ERR_NULL;
+    return aligned(p->A, 16) && aligned(p->B, 16) && aligned(p->ranks, 4) && aligned(p->scales, 4) ? LQ_OK : LQ_ERR_ALIGN;
+}
+static size_t adapter_inter_bytes(const lq_adapter_config* c, int64_t M) { return align256((size_t)M * ((c->rank + 15) / 16 * 16) * 4); }
+
+lq_status lq_adapter_plan_sizes(int64_t M, int32_t slots, size_t* plan_bytes)
+{
+    if (!plan_bytes) return LQ_ERR_NULL;
+    if (M < 0 || M > (1 << 24) || slots < 1 || slots > 1024) return LQ_ERR_SHAPE;
+    *plan_bytes = adapter_plan_layout(M, slots).total;
+    return LQ_OK;
+}
+
+lq_status lq_adapter_plan(int32_t slots, const int32_t* ids, int64_t M, void* plan, size_t plan_bytes, void* stream)
+{
+    size_t need;
+    lq_status st = lq_adapter_plan_sizes(M, slots, &need);
+    if (st != LQ_OK) return st;
+    if (!plan || (M > 0 && !ids)) return LQ_ERR_NULL;
+    if (!aligned(plan, 256) || !aligned(ids, 4)) return LQ_ERR_ALIGN;
+    if (plan_bytes < need) return LQ_ERR_BUFFER_TOO_SMALL;
+    return launch_adapter_plan(slots, ids, M, (uint8_t*)plan, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_adapter_sizes(const lq_adapter_config* cfg, int64_t M, size_t* inter_bytes, size_t* work_bytes)
+{
+    lq_status st = adapter_check(cfg);
+    if (st != LQ_OK) return st;
+    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if (inter_bytes) *inter_bytes = adapter_inter_bytes(cfg, M);
+    if (work_bytes) *work_bytes = adapter_work_layout(cfg, M).total;
+    return LQ_OK;
+}
+
+lq_status lq_adapter_fwd(const lq_adapter_config* cfg, const void* plan, size_t plan_bytes, const lq_adapter_pool* pool, const void* X,
+                         int64_t ldx, const void* Yin, int64_t ldyin, void* Y, int64_t ldy, int64_t M, void* inter, size_t inter_bytes,
+                         void* stream)
+{
+    lq_status st = adapter_check(cfg);
+    if (st != LQ_OK) return st;
+    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if (M == 0) return LQ_OK;  // an empty batch
+    if (!plan || !X || !Yin || !Y || !inter) return LQ_ERR_NULL;
+    if ((st = pool_check(pool)) != LQ_OK) return st;
+    if ((st = rows_check(X, ldx, cfg->K, cfg->x_dtype == LQ_F32 ? 4 : 2)) != LQ_OK || (st = rows_check(Yin, ldyin, cfg->N, 2)) != LQ_OK ||
+        (st = rows_check(Y, ldy, cfg->N, 2)) != LQ_OK)
+        return st;
+    if (!aligned(plan, 256) || !aligned(inter, 256)) return LQ_ERR_ALIGN;
+    if (plan_bytes < adapter_plan_layout(M, cfg->slots).total || inter_bytes < adapter_inter_bytes(cfg, M)) return LQ_ERR_BUFFER_TOO_SMALL;
+    return launch_adapter_fwd(cfg, (const uint8_t*)plan, pool, X, ldx, Yin, ldyin, Y, ldy, M, (uint8_t*)inter, (hipStream_t)stream) == hipSuccess
+               ? LQ_OK
+               : LQ_ERR_DEVICE;
+}
+
+lq_status lq_adapter_bwd(const lq_adapter_config* cfg, const void* plan, size_t plan_bytes, const lq_adapter_pool* pool, const void* X,
+                         int64_t ldx, const void* inter, size_t inter_bytes, const void* dY, int64_t lddy, const void* dXin,
+                         int64_t lddxin, void* dX, int64_t lddx, float* dA, float* dB, int64_t M, void* work, size_t work_bytes,
+                         void* stream)
+{
+    lq_status st = adapter_check(cfg);
+    if (st != LQ_OK) return st;
+    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if (!dA || !dB) return LQ_ERR_NULL;
+    if (!aligned(dA, 16) || !aligned(dB, 16)) return LQ_ERR_ALIGN;
+    if (M == 0) return launch_adapter_zero(cfg, dA, dB, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+    if (!plan || !X || !inter || !dY || !dX || !work) return LQ_ERR_NULL;
+    if ((st = pool_check(pool)) != LQ_OK) return st;
+    const int elem = cfg->x_dtype == LQ_F32 ? 4 : 2;
+    if ((st = rows_check(X, ldx, cfg->K, elem)) != LQ_OK || (st = rows_check(dY, lddy, cfg->N, 2)) != LQ_OK ||
+        (st = rows_check(dX, lddx, cfg->K, elem)) != LQ_OK || (dXin && (st = rows_check(dXin, lddxin, cfg->K, elem)) != LQ_OK))
+        return st;
+    if (!aligned(plan, 256) || !aligned(inter, 256) || !aligned(work, 256)) return LQ_ERR_ALIGN;
+    if (plan_bytes < adapter_plan_layout(M, cfg->slots).total || inter_bytes < adapter_inter_bytes(cfg, M) ||
+        work_bytes < adapter_work_layout(cfg, M).total)
+        return LQ_ERR_BUFFER_TOO_SMALL;
+    return launch_adapter_bwd(cfg, (const uint8_t*)plan, pool, X, ldx, (const uint8_t*)inter, dY, lddy, dXin, lddxin, dX, lddx, dA, dB, M,
+                              (uint8_t*)work, (hipStream_t)stream) == hipSuccess
+               ? LQ_OK
+               : LQ_ERR_DEVICE;
+}
+
+static lq_status qk_check(const lq_qk_config* c, int64_t M)
+{
+    if (!c) return LQ_ERR_NULL;
+    if (c->flags != 0 || (c->dtype != LQ_F32 && c->dtype != LQ_BF16) || (c->pairing != LQ_PAIR_HALF && c->pairing != LQ_PAIR_ADJACENT) ||
+        (c->norm != LQ_NORM_NONE && c->norm != LQ_NORM_RMS) || (c->norm == LQ_NORM_RMS && !(c->eps > 0.f)))
+        return LQ_ERR_UNSUPPORTED;
+    if (c->heads_q < 0 || c->heads_k < 0 || c->heads_q > 4096 || c->heads_k > 4096 || c->heads_q + c->heads_k < 1 ||
+        c->heads_q + c->heads_k > 4096 || c->head_dim < 2 || c->head_dim > 256 || c->head_dim % 2 != 0 || c->axes < 0 || c->axes > 4)
+        return LQ_ERR_SHAPE;
+    int sum = 0;
+    for (int k = 0; k < 4; ++k) {
+        if (c->pairs[k] < 0 || c->pairs[k] > 128 || (k >= c->axes && c->pairs[k] != 0)) return LQ_ERR_SHAPE;
+        sum += c->pairs[k];
+    }
+    if (2 * sum > c->head_dim || M < 0 || M > (1 << 24)) return LQ_ERR_SHAPE;
+    return LQ_OK;
+}
+static lq_status heads_check(const lq_qk_config* c, const lq_heads* h, int heads, lq_heads* out)
+{
+    if (heads == 0) return LQ_OK;  // not looked at
+    if (!h || !h->p) return LQ_ERR_NULL;
+    if (h->ld < 0 || h->hs < 0 || h->ld >= ((int64_t)1 << 40) || h->hs >= ((int64_t)1 << 40)) return LQ_ERR_SHAPE;
+    if (!aligned(h->p, c->dtype == LQ_F32 ? 4 : 2)) return LQ_ERR_ALIGN;
+    *out = *h;
+    return LQ_OK;
+}
+static lq_status positions_check(const lq_qk_config* c, const float* pos, int64_t pos_rows, const float* inv_freq)
+{
+    if (c->pairs[0] + c->pairs[1] + c->pairs[2] + c->pairs[3] == 0) return LQ_OK;
+    if (!pos || !inv_freq) return LQ_ERR_NULL;
+    if (pos_rows < 1 || pos_rows > (1 << 24)) return LQ_ERR_SHAPE;
+    return aligned(pos, 4) && aligned(inv_freq, 4) ? LQ_OK : LQ_ERR_ALIGN;
+}
+
+lq_status lq_qk_norm_rope_fwd(const lq_qk_config* cfg, const lq_heads* q, const lq_heads* k, const float* wq, const float* wk,
+                              const float* pos, int64_t pos_rows, const float* inv_freq, const lq_heads* qo, const lq_heads* ko, int64_t M,
+                              void* stream)
+{
+    lq_status st = qk_check(cfg, M);
+    if (st != LQ_OK) return st;
+    if (M == 0) return LQ_OK;  // an empty batch
+    QkTensors t{};
+    if ((st = heads_check(cfg, q, cfg->heads_q, &t.q[0])) != LQ_OK || (st = heads_check(cfg, k, cfg->heads_k, &t.q[1])) != LQ_OK ||
+        (st = heads_check(cfg, qo, cfg->heads_q, &t.out[0])) != LQ_OK || (st = heads_check(cfg, ko, cfg->heads_k, &t.out[1])) != LQ_OK ||
+        (st = positions_check(cfg, pos, pos_rows, inv_freq)) != LQ_OK)
+        return st;
+    if (!aligned(wq, 4) || !aligned(wk, 4)) return LQ_ERR_ALIGN;
+    t.w[0] = wq;
+    t.w[1] = wk;
+    t.pos = pos;
+    t.pos_rows = pos_rows;
+    t.inv_freq = inv_freq;
+    return launch_qk_fwd(cfg, t, M, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_qk_work_sizes(const lq_qk_config* cfg, int64_t M, size_t* work_bytes)
+{
+    if (!cfg || !work_bytes) return LQ_ERR_NULL;
+    lq_status st = qk_check(cfg, M);
+    if (st != LQ_OK) return st;
+    *work_bytes = qk_work_bytes(cfg, M);
+    return LQ_OK;
+}
+
+lq_status lq_qk_norm_rope_bwd(const lq_qk_config* cfg, const lq_heads* q, const lq_heads* k, const float* wq, const float* wk,
+                              const float* pos, int64_t pos_rows, const float* inv_freq, const lq_heads* dqo, const lq_heads* dko,
+                              const lq_heads* dq, const lq_heads* dk, float* dwq, float* dwk, int64_t M, void* work, size_t work_bytes,
+                              void* stream)
+{
+    lq_status st = qk_check(cfg, M);
+    if (st != LQ_OK) return st;
+    const bool norm = cfg->norm == LQ_NORM_RMS;
+    if (norm && (!dwq) != (!dwk)) return LQ_ERR_NULL;
+    QkTensors t{};
+    if (M > 0) {
+        if ((norm && ((st = heads_check(cfg, q, cfg->heads_q, &t.q[0])) != LQ_OK || (st = heads_check(cfg, k, cfg->heads_k, &t.q[1])) != LQ_OK)) ||
+            (st = heads_check(cfg, dqo, cfg->heads_q, &t.grad[0])) != LQ_OK || (st = heads_check(cfg, dko, cfg->heads_k, &t.grad[1])) != LQ_OK ||
+            (st = heads_check(cfg, dq, cfg->heads_q, &t.out[0])) != LQ_OK || (st = heads_check(cfg, dk, cfg->heads_k, &t.out[1])) != LQ_OK ||
+            (st = positions_check(cfg, pos, pos_rows, inv_freq)) != LQ_OK)
+            return st;
+        if (norm && dwq && !work) return LQ_ERR_NULL;
+        if (norm && dwq && work_bytes < qk_work_bytes(cfg, M)) return LQ_ERR_BUFFER_TOO_SMALL;
+    }
+    if (!aligned(wq, 4) || !aligned(wk, 4) || (norm && (!aligned(dwq, 4) || !aligned(dwk, 4) || !aligned(work, 256)))) return LQ_ERR_ALIGN;
+    t.w[0] = wq;
+    t.w[1] = wk;
+    t.pos = pos;
+    t.pos_rows = pos_rows;
+    t.inv_freq = inv_freq;
+    t.dw[0] = dwq;
+    t.dw[1] = dwk;
+    return launch_qk_bwd(cfg, t, M, (uint8_t*)work, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
 }  // extern "C"

@@ -219,6 +219,42 @@ hipError_t launch_rot_apply(const Dims& d, const float* L, const float* R, const
                             hipStream_t s);
 hipError_t launch_rot_unpack(const Dims& d, const uint8_t* state, const lq_rot_view* out, hipStream_t s);
 
+// Adapters of many requests (lq_adapter.hip).  Plan: rows in the order of their adapters; first row and first tile of each adapter (slots + 2
+// entries: the rows without an adapter come last, then the ends); tiles {first row, rows, adapter, 0}; counts for the plan's own kernels.
+struct AdapterPlanLayout {
+    int chunks, tiles;
+    size_t off_base, off_tbase, off_tiles, off_rows, off_total, off_hist, total;
+};
+AdapterPlanLayout adapter_plan_layout(int64_t M, int slots);
+struct AdapterWorkLayout {  // of the backward
+    size_t off_dT;            // dY B of every row, fp32
+    size_t off_At, off_Bt;    // transposed factors
+    size_t off_part;          // parts of the factors' gradients
+    size_t total;
+    int64_t part_stride;      // floats of a part
+    int per, groups;          // tiles of a group, groups
+};
+AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M);
+hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t* plan, hipStream_t s);
+hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, const lq_adapter_pool* pool, const void* X, int64_t ldx,
+                              const void* Yin, int64_t ldyin, void* Y, int64_t ldy, int64_t M, uint8_t* inter, hipStream_t s);
+hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, const lq_adapter_pool* pool, const void* X, int64_t ldx,
+                              const uint8_t* inter, const void* dY, int64_t lddy, const void* dXin, int64_t lddxin, void* dX, int64_t lddx,
+                              float* dA, float* dB, int64_t M, uint8_t* work, hipStream_t s);
+hipError_t launch_adapter_zero(const lq_adapter_config* c, float* dA, float* dB, hipStream_t s);  // the gradients of no rows
+
+// Norm and rotation of queries and keys (lq_qk.hip).
+struct QkTensors {
+    lq_heads q[2], out[2], grad[2];  // queries, keys: inputs, results, derivatives with respect to the forward's results
+    const float* w[2];
+    const float *pos, *inv_freq;
+    int64_t pos_rows;
+    float* dw[2];
+};
+size_t qk_work_bytes(const lq_qk_config* c, int64_t M);
+hipError_t launch_qk_fwd(const lq_qk_config* c, const QkTensors& t, int64_t M, hipStream_t s);
+hipError_t launch_qk_bwd(const lq_qk_config* c, const QkTensors& t, int64_t M, uint8_t* work, hipStream_t s);
+
 int compute_units();  // of the current device
 
 // Form of the activation steps with a block-scaled floating-point branch (mxb_act_kernel, mx6_act_kernel; every form sums T in the same
