@@ -16,254 +16,443 @@ struct QkArgs {
     int axis_end[4];  // first pair past each axis
     int lanes_log2;   // lanes of a head
     int tokens;       // of a workgroup at a time
-    float eps;
+    int turn_k[2], turn_h[2];  // tokens and heads from one turn of a lane to its next
+    unsigned magic[2], half_magic;  // 2^32 / heads, 2^32 / (dim / 2), rounded up: quotients of small numbers
+    float eps, inv_dim;
     float* part;      // [workgroup][2][dim] sums of dw
 };
 
-// N consecutive values at p, as fp32 (N * sizeof(T) bytes of alignment)
-template <typename T, int N>
-__device__ __forceinline__ void load(const T* p, float (&v)[N])
-{
-    typedef T vt __attribute__((ext_vector_type(N)));
-    if constexpr (N == 1) {
-        v[0] = (float)*p;
-    } else {
-        const vt r = *(const vt*)p;
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = (float)r[j];
-    }
-}
-template <typename T, int N>
-__device__ __forceinline__ void store(T* p, const float (&v)[N])
-{
-    typedef T vt __attribute__((ext_vector_type(N)));
-    if constexpr (N == 1) {
-        *p = (T)v[0];
-    } else {
-        vt r;
-#pragma unroll
-        for (int j = 0; j < N; ++j) r[j] = (T)v[j];
-        *(vt*)p = r;
-    }
-}
+__device__ __forceinline__ int quotient(int i, unsigned magic) { return magic ? (int)__umulhi((unsigned)i, magic) : i; }
 
-// Pair vectors: vector t of a head is the members a, b of V pairs.  Halves: a = x[tV ..], b = x[P + tV ..]; adjacent: 2V consecutive values.
-// What is not rotated (values from 2P on) is cut into vectors of 2V consecutive values.
-template <typename T, int V, bool HALF>
-__device__ __forceinline__ void load_pairs(const T* x, int t, int P, float (&a)[V], float (&b)[V])
+// cos and sin of the angle of pair p (ones and zeros for the values that are not rotated).  The product of two fp32 numbers is exact in 64 bits; whole
+// turns are taken off there, what is left fits 32.
+__device__ __forceinline__ float2 turn(const QkArgs& a, unsigned row, int p)
 {
-    if (HALF) {
-        const bool rot = t * V < P;
-        load<T, V>(x + (rot ? t * V : 2 * t * V), a);
-        load<T, V>(x + (rot ? P + t * V : 2 * t * V + V), b);
-    } else {
-        float v[2 * V];
-        load<T, 2 * V>(x + 2 * t * V, v);
-#pragma unroll
-        for (int j = 0; j < V; ++j) a[j] = v[2 * j], b[j] = v[2 * j + 1];
+    float2 v = make_float2(1.0f, 0.0f);
+    if (p < a.pairs) {
+        const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
+        const double turns = (double)a.t.pos[(size_t)row * a.axes + axis] * (double)a.t.inv_freq[p] * 0.15915494309189533577;
+        const float r = (float)(turns - rint(turns));
+        sincospif(2.0f * r, &v.y, &v.x);
     }
+    return v;
 }
-template <typename T, int V, bool HALF>
-__device__ __forceinline__ void store_pairs(T* x, int t, int P, const float (&a)[V], const float (&b)[V])
+// row of pos of token m0 + k; first = m0 % pos_rows
+__device__ __forceinline__ unsigned pos_row(const QkArgs& a, unsigned first, int k)
 {
-    if (HALF) {
-        const bool rot = t * V < P;
-        store<T, V>(x + (rot ? t * V : 2 * t * V), a);
-        store<T, V>(x + (rot ? P + t * V : 2 * t * V + V), b);
-    } else {
-        float v[2 * V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[2 * j] = a[j], v[2 * j + 1] = b[j];
-        store<T, 2 * V>(x + 2 * t * V, v);
-    }
+    const unsigned row = first + k;
+    return row < (unsigned)a.t.pos_rows ? row : row % (unsigned)a.t.pos_rows;
 }
+__device__ __forceinline__ unsigned first_pos(const QkArgs& a, int m0) { return a.pairs ? (unsigned)m0 % (unsigned)a.t.pos_rows : 0u; }
 
-// cos and sin of the angles of `n` tokens from m0 on: cs[token][pair of the head], ones and zeros for the values that are not rotated.  The
-// product of two fp32 numbers is exact in 64 bits; whole turns are taken off there, what is left fits 32.
-__device__ __forceinline__ void turn_table(const QkArgs& a, int64_t m0, int n, float2* cs)
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v)
 {
-    const int H = a.dim / 2;
-    for (int o = threadIdx.x; o < n * H; o += blockDim.x) {
-        const int k = o / H, p = o - k * H;
-        float2 v = make_float2(1.0f, 0.0f);
-        if (p < a.pairs) {
-            const int axis = (p >= a.axis_end[0]) + (p >= a.axis_end[1]) + (p >= a.axis_end[2]);
-            const double turns = (double)a.t.pos[((m0 + k) % a.t.pos_rows) * a.axes + axis] * (double)a.t.inv_freq[p] * 0.15915494309189533577;
-            const float r = (float)(turns - rint(turns));
-            sincospif(2.0f * r, &v.y, &v.x);
-        }
-        cs[o] = v;
-    }
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
 }
-
-__device__ __forceinline__ float sum_lanes(float v, int lanes_log2)
+// sum over groups of 2^k lanes, in all of them
+__device__ __forceinline__ float sum_lanes(float v, int k)
 {
-    for (int k = 0; k < lanes_log2; ++k) v += __shfl_xor(v, 1 << k);
+    if (k > 0) v = add_dpp<0xB1>(v);   // quad_perm [1,0,3,2]
+    if (k > 1) v = add_dpp<0x4E>(v);   // quad_perm [2,3,0,1]
+    if (k > 2) v = add_dpp<0x141>(v);  // row_half_mirror
+    if (k > 3) v = add_dpp<0x140>(v);  // row_mirror
+    if (k > 4) v += __shfl_xor(v, 16);
+    if (k > 5) v += __shfl_xor(v, 32);
     return v;
 }
 
-// GRAD: x is the forward's input (NORM only), g the derivative of its output.
-template <typename T, int V, int NV, bool HALF, bool NORM, bool GRAD>
-__global__ void __launch_bounds__(256) qk_kernel(QkArgs a)
+// Each of N values: the sum over the lanes of a wavefront with the same place in their group of 2^k, valid in the first group.  (Values inside, steps
+// outside: a uniform branch per step, not per step and value.)
+template <int N>
+__device__ __forceinline__ void sum_groups(float (&v)[N], int k)
 {
-    extern __shared__ float2 cs[];
-    const int ln = 1 << a.lanes_log2, lane = threadIdx.x & (ln - 1), group = threadIdx.x >> a.lanes_log2, groups = 256 >> a.lanes_log2;
-    const int vectors = a.dim / (2 * V), H = a.heads[0] + a.heads[1];
-    float wa[2][NV][V], wb[2][NV][V], da[2][NV][V], db[2][NV][V];
-    bool has[NV];
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-        const int t = lane + u * ln;
-        has[u] = t < vectors;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int j = 0; j < V; ++j) wa[s][u][j] = wb[s][u][j] = 1.0f, da[s][u][j] = db[s][u][j] = 0.0f;
-        if (NORM && has[u])
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                if (a.t.w[s]) {
-                    const float* w = a.t.w[s];
-                    const bool rot = HALF && t * V < a.pairs;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        wa[s][u][j] = w[HALF ? (rot ? t * V + j : 2 * t * V + j) : 2 * (t * V + j)];
-                        wb[s][u][j] = w[HALF ? (rot ? a.pairs + t * V + j : 2 * t * V + V + j) : 2 * (t * V + j) + 1];
-                    }
-                }
+#define STEP(K, EXPR) \
+    if (k < K) { \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = EXPR; \
     }
-    for (int64_t m0 = (int64_t)blockIdx.x * a.tokens; m0 < a.M; m0 += (int64_t)gridDim.x * a.tokens) {
-        const int n = (int)(a.M - m0 < a.tokens ? a.M - m0 : a.tokens);
-        __syncthreads();
-        turn_table(a, m0, n, cs);
-        __syncthreads();
-        for (int it = group; it < n * H; it += groups) {
-            const int k = it / H, h = it - k * H;
-            const int s = h >= a.heads[0];
-            const int64_t m = m0 + k;
-            const int hh = s ? h - a.heads[0] : h;
-            float xa[NV][V], xb[NV][V], ga[NV][V], gb[NV][V];
-            float ss = 0.0f;
-            if (NORM || !GRAD) {
-                const T* x = (const T*)a.t.q[s].p + m * a.t.q[s].ld + hh * a.t.q[s].hs;
+    STEP(1, add_dpp<0xB1>(v[i]))
+    STEP(2, add_dpp<0x4E>(v[i]))
+    STEP(3, add_dpp<0x124>(v[i]))  // row_ror:4
+    STEP(4, add_dpp<0x128>(v[i]))  // row_ror:8
+#undef STEP
+    if (k < 5) {
 #pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u]) {
-                        load_pairs<T, V, HALF>(x, lane + u * ln, a.pairs, xa[u], xb[u]);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) ss += xa[u][j] * xa[u][j] + xb[u][j] * xb[u][j];
-                    }
-            }
-            if (GRAD) {
-                const T* g = (const T*)a.t.grad[s].p + m * a.t.grad[s].ld + hh * a.t.grad[s].hs;
-#pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u]) load_pairs<T, V, HALF>(g, lane + u * ln, a.pairs, ga[u], gb[u]);
-            }
-            float rstd = 1.0f;
-            if (NORM) rstd = 1.0f / sqrtf(sum_lanes(ss, a.lanes_log2) / (float)a.dim + a.eps);
-            T* out = (T*)a.t.out[s].p + m * a.t.out[s].ld + hh * a.t.out[s].hs;
-            const float2* c = cs + k * (a.dim / 2);
-            if (!GRAD) {
-#pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u]) {
-                        float ya[V], yb[V];
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const float2 e = c[(lane + u * ln) * V + j];
-                            const float na = NORM ? xa[u][j] * rstd * (s ? wa[1][u][j] : wa[0][u][j]) : xa[u][j];
-                            const float nb = NORM ? xb[u][j] * rstd * (s ? wb[1][u][j] : wb[0][u][j]) : xb[u][j];
-                            ya[j] = na * e.x - nb * e.y;
-                            yb[j] = na * e.y + nb * e.x;
-                        }
-                        store_pairs<T, V, HALF>(out, lane + u * ln, a.pairs, ya, yb);
-                    }
-            } else {
-                float dot = 0.0f;
-#pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u])
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const float2 e = c[(lane + u * ln) * V + j];
-                            const float ra = ga[u][j] * e.x + gb[u][j] * e.y, rb = gb[u][j] * e.x - ga[u][j] * e.y;
-                            if (NORM) {
-                                xa[u][j] *= rstd;
-                                xb[u][j] *= rstd;
-                                const float pa = ra * xa[u][j], pb = rb * xb[u][j];
-                                da[0][u][j] += s ? 0.0f : pa, db[0][u][j] += s ? 0.0f : pb;
-                                da[1][u][j] += s ? pa : 0.0f, db[1][u][j] += s ? pb : 0.0f;
-                                const float w0 = s ? wa[1][u][j] : wa[0][u][j], w1 = s ? wb[1][u][j] : wb[0][u][j];
-                                dot += pa * w0 + pb * w1;
-                                ga[u][j] = ra * w0;
-                                gb[u][j] = rb * w1;
-                            } else {
-                                ga[u][j] = ra;
-                                gb[u][j] = rb;
-                            }
-                        }
-                const float mean = NORM ? sum_lanes(dot, a.lanes_log2) / (float)a.dim : 0.0f;
-#pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u]) {
-                        float ya[V], yb[V];
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            ya[j] = NORM ? rstd * (ga[u][j] - xa[u][j] * mean) : ga[u][j];
-                            yb[j] = NORM ? rstd * (gb[u][j] - xb[u][j] * mean) : gb[u][j];
-                        }
-                        store_pairs<T, V, HALF>(out, lane + u * ln, a.pairs, ya, yb);
-                    }
-            }
+        for (int i = 0; i < N; ++i) {
+            const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+            v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
         }
     }
-    if constexpr (GRAD && NORM) {  // the groups' sums, one group after another
-        if (!a.part) return;
-        float* acc = (float*)cs;  // [2][dim]
-        for (int o = 0; o < groups; ++o) {
-            __syncthreads();
-            if (group == o)
+    if (k < 6) {
 #pragma unroll
-                for (int u = 0; u < NV; ++u)
-                    if (has[u]) {
-                        const int t = lane + u * ln;
-                        const bool rot = HALF && t * V < a.pairs;
-#pragma unroll
-                        for (int s = 0; s < 2; ++s)
-#pragma unroll
-                            for (int j = 0; j < V; ++j) {
-                                const int ia = s * a.dim + (HALF ? (rot ? t * V + j : 2 * t * V + j) : 2 * (t * V + j));
-                                const int ib = s * a.dim + (HALF ? (rot ? a.pairs + t * V + j : 2 * t * V + V + j) : 2 * (t * V + j) + 1);
-                                acc[ia] = o ? acc[ia] + da[s][u][j] : da[s][u][j];
-                                acc[ib] = o ? acc[ib] + db[s][u][j] : db[s][u][j];
-                            }
-                    }
+        for (int i = 0; i < N; ++i) {
+            const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i]), false, false);
+            v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
         }
-        __syncthreads();
-        for (int o = threadIdx.x; o < 2 * a.dim; o += 256) a.part[(int64_t)blockIdx.x * 2 * a.dim + o] = acc[o];
     }
 }
 
-// dw: the workgroups' sums in their order; 16 values to a workgroup, 16 shares of the sums each
-__global__ void __launch_bounds__(256) qk_weight_sum(const float* part, int n, int dim, float* dwq, float* dwk)
+// V consecutive values, aligned to themselves in memory
+template <typename T, int V>
+struct Vec {
+    typedef T type __attribute__((ext_vector_type(V)));
+};
+template <typename T>
+struct Vec<T, 1> {
+    typedef T type;
+};
+template <int V, typename VT>
+__device__ __forceinline__ float part(const VT& v, int j)
 {
-    __shared__ float sh[16][17];
+    if constexpr (V == 1) return (float)v;
+    else return (float)v[j];
+}
+
+// The members a, b of V pairs of a head as they lie in memory: two vectors of V (halves), or one of 2 V
+template <typename T, int V, bool HALF>
+struct Raw {
+    typename Vec<T, HALF ? V : 2 * V>::type v[HALF ? 2 : 1];
+    __device__ __forceinline__ void fetch(const T* x, int oa, int ob)
+    {
+        v[0] = *(const decltype(&v[0]))(x + oa);
+        if constexpr (HALF) v[1] = *(const decltype(&v[0]))(x + ob);
+    }
+    __device__ __forceinline__ void get(float (&a)[V], float (&b)[V]) const
+    {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if constexpr (HALF) a[j] = part<V>(v[0], j), b[j] = part<V>(v[1], j);
+            else a[j] = part<2 * V>(v[0], 2 * j), b[j] = part<2 * V>(v[0], 2 * j + 1);
+        }
+    }
+};
+template <typename T, int V, bool HALF>
+__device__ __forceinline__ void put(T* x, int oa, int ob, const float (&a)[V], const float (&b)[V])
+{
+    if constexpr (HALF && V == 1) {
+        x[oa] = (T)a[0];
+        x[ob] = (T)b[0];
+    } else if constexpr (HALF) {
+        typename Vec<T, V>::type va, vb;
+#pragma unroll
+        for (int j = 0; j < V; ++j) va[j] = (T)a[j], vb[j] = (T)b[j];
+        *(decltype(&va))(x + oa) = va;
+        *(decltype(&va))(x + ob) = vb;
+    } else {
+        typename Vec<T, 2 * V>::type w;
+#pragma unroll
+        for (int j = 0; j < V; ++j) w[2 * j] = (T)a[j], w[2 * j + 1] = (T)b[j];
+        *(decltype(&w))(x + oa) = w;
+    }
+}
+
+// A lane's way through the heads of a chunk of tokens: head h of token k, in the same steps at every turn, so that a turn costs no division and
+// no product.  at: offset of the head in a tensor, or of the token's cosines in their table.
+struct Walk {
+    int h;
+    int64_t at, turn, wrap;  // of a turn; what is added where the next token begins
+    __device__ __forceinline__ Walk(int h0, int k0, int dh, int dk, int H, int64_t ld, int64_t hs)
+        : h(h0), at(k0 * ld + h0 * hs), turn(dk * ld + dh * hs), wrap(ld - H * hs)
+    {
+    }
+    __device__ __forceinline__ void next(int dh, int H)
+    {
+        h += dh;
+        at += turn;
+        if (h >= H) h -= H, at += wrap;
+    }
+};
+
+// What a lane knows of its NV pair vectors: offsets of the members in a head, first pair; lanes past the head's end repeat vector 0 and store nothing.
+template <int V, int NV, bool HALF>
+struct Lane {
+    static constexpr int WS = HALF ? 1 : 2;  // from one member to the next of its kind
+    bool has[NV];
+    int oa[NV], ob[NV], oc[NV];
+    __device__ __forceinline__ Lane(const QkArgs& a, int lane, int ln)
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int t = lane + v * ln;
+            has[v] = t < a.dim / (2 * V);
+            const int u = has[v] ? t : 0;
+            const bool rot = HALF && u * V < a.pairs;
+            oa[v] = rot ? u * V : 2 * u * V;
+            ob[v] = rot ? a.pairs + u * V : 2 * u * V + (HALF ? V : 1);
+            oc[v] = u * V;
+        }
+    }
+};
+
+// Forward.  The table holds, for queries and for keys, {cos wa, sin wb, sin wa, cos wb} of every pair: a pair is then four products, and
+// the norm's factor two.  A lane works on one head of the queries and one of the keys at a time, with the next ones already requested; the first are
+// requested before the table is made.
+template <typename T, int V, int NV, bool HALF, bool NORM>
+__global__ void __launch_bounds__(256) qk_fwd_kernel(QkArgs a)
+{
+    extern __shared__ v4f table[];  // [queries, keys][token][pair]
+    const int ln = 1 << a.lanes_log2, lane = threadIdx.x & (ln - 1), group = threadIdx.x >> a.lanes_log2, groups = 256 >> a.lanes_log2;
+    const int half = a.dim / 2;
+    const Lane<V, NV, HALF> L(a, lane, ln);
+    const int m0 = blockIdx.x * a.tokens, n = min((int)a.M - m0, a.tokens);
+    int k0[2], h0[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) k0[s] = quotient(group, a.magic[s]), h0[s] = group - k0[s] * a.heads[s];
+#define WALK(NAME, S, TENSOR) Walk NAME(h0[S], k0[S], a.turn_h[S], a.turn_k[S], a.heads[S], a.t.TENSOR[S].ld, a.t.TENSOR[S].hs)
+    WALK(xq, 0, q);
+    WALK(xk, 1, q);
+    WALK(yq, 0, out);
+    WALK(yk, 1, out);
+#undef WALK
+    const T* xp[2] = {(const T*)a.t.q[0].p + m0 * a.t.q[0].ld, (const T*)a.t.q[1].p + m0 * a.t.q[1].ld};
+    T* yp[2] = {(T*)a.t.out[0].p + m0 * a.t.out[0].ld, (T*)a.t.out[1].p + m0 * a.t.out[1].ld};
+    int at[2] = {k0[0] * half, k0[1] * half};  // of the token's part of the table
+    const int items[2] = {n * a.heads[0], n * a.heads[1]};
+    Raw<T, V, HALF> raw[2][NV];
+    auto request = [&](int it) {
+        if (it < items[0])
+#pragma unroll
+            for (int v = 0; v < NV; ++v) raw[0][v].fetch(xp[0] + xq.at, L.oa[v], L.ob[v]);
+        if (it < items[1])
+#pragma unroll
+            for (int v = 0; v < NV; ++v) raw[1][v].fetch(xp[1] + xk.at, L.oa[v], L.ob[v]);
+        xq.next(a.turn_h[0], a.heads[0]);
+        xk.next(a.turn_h[1], a.heads[1]);
+    };
+    request(group);
+    const unsigned first = first_pos(a, m0);
+    for (int o = threadIdx.x; o < n * half; o += 256) {
+        const int k = quotient(o, a.half_magic), p = o - k * half;
+        const float2 e = turn(a, pos_row(a, first, k), p);
+        // members of pair p of the head (what is not rotated: as a lane's vectors of it are cut)
+        int ia = 2 * p, ib = 2 * p + 1;
+        if (HALF) {
+            const bool rot = p < a.pairs;
+            ia = rot ? p : 2 * (p / V) * V + p % V;
+            ib = rot ? a.pairs + p : ia + V;
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const float* w = a.t.w[s];
+            const float wa = NORM && w ? w[ia] : 1.0f, wb = NORM && w ? w[ib] : 1.0f;
+            table[s * a.tokens * half + o] = v4f{e.x * wa, e.y * wb, e.y * wa, e.x * wb};
+        }
+    }
+    __syncthreads();
+    const int most = max(items[0], items[1]);
+    for (int it = group; it < most; it += groups) {
+        float xa[2][NV][V], xb[2][NV][V];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) raw[s][v].get(xa[s][v], xb[s][v]);
+        if (it + groups < most) request(it + groups);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            if (it < items[s]) {
+                const v4f* c = table + s * a.tokens * half + at[s];
+                T* y = yp[s] + (s ? yk.at : yq.at);
+                float rstd = 1.0f;
+                if constexpr (NORM) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        float t = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < V; ++j) t = fmaf(xa[s][v][j], xa[s][v][j], fmaf(xb[s][v][j], xb[s][v][j], t));
+                        ss += L.has[v] ? t : 0.0f;
+                    }
+                    rstd = __builtin_amdgcn_rsqf(fmaf(sum_lanes(ss, a.lanes_log2), a.inv_dim, a.eps));
+                }
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float ya[V], yb[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const v4f e = c[L.oc[v] + j];
+                        ya[j] = fmaf(xa[s][v][j], e[0], -(xb[s][v][j] * e[1]));
+                        yb[j] = fmaf(xa[s][v][j], e[2], xb[s][v][j] * e[3]);
+                        if (NORM) ya[j] *= rstd, yb[j] *= rstd;
+                    }
+                    if (L.has[v]) put<T, V, HALF>(y, L.oa[v], L.ob[v], ya, yb);
+                }
+            }
+            at[s] += a.turn_k[s] * half;
+            if ((s ? yk.h : yq.h) + a.turn_h[s] >= a.heads[s]) at[s] += half;
+        }
+        yq.next(a.turn_h[0], a.heads[0]);
+        yk.next(a.turn_h[1], a.heads[1]);
+    }
+}
+
+// Gradient: x is the forward's input (NORM only), g the derivative of its output.  Queries, then keys, one head at a time with the next one already
+// requested; dw is summed in registers, then over the wavefront, then over the workgroup's four, into the workgroup's part.
+template <typename T, int V, int NV, bool HALF, bool NORM>
+__global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a)
+{
+    extern __shared__ float2 cs[];  // [token][pair]; with NORM then [wavefront][dim] floats
+    const int ln = 1 << a.lanes_log2, lane = threadIdx.x & (ln - 1), group = threadIdx.x >> a.lanes_log2, groups = 256 >> a.lanes_log2;
+    const int half = a.dim / 2;
+    const Lane<V, NV, HALF> L(a, lane, ln);
+    const int m0 = blockIdx.x * a.tokens, n = min((int)a.M - m0, a.tokens);
+    float* sums = (float*)(cs + a.tokens * half);
+    bool made = false;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int H = a.heads[s], items = n * H, dh = a.turn_h[s], dk = a.turn_k[s];
+        float dw[2 * NV * V], wa[NV][V], wb[NV][V];
+#pragma unroll
+        for (int v = 0; v < 2 * NV * V; ++v) dw[v] = 0.0f;
+        if (H > 0) {
+            const int k0 = quotient(group, a.magic[s]), h0 = group - k0 * H;
+            Walk wx(h0, k0, dh, dk, H, a.t.q[s].ld, a.t.q[s].hs), wg(h0, k0, dh, dk, H, a.t.grad[s].ld, a.t.grad[s].hs);
+            Walk wy(h0, k0, dh, dk, H, a.t.out[s].ld, a.t.out[s].hs), wc(h0, k0, dh, dk, H, half, 0);
+            const T* xp = (const T*)a.t.q[s].p + m0 * a.t.q[s].ld;
+            const T* gp = (const T*)a.t.grad[s].p + m0 * a.t.grad[s].ld;
+            T* yp = (T*)a.t.out[s].p + m0 * a.t.out[s].ld;
+            Raw<T, V, HALF> rx[NV], rg[NV];
+            auto request = [&](int it) {
+                if (it < items)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        if constexpr (NORM) rx[v].fetch(xp + wx.at, L.oa[v], L.ob[v]);
+                        rg[v].fetch(gp + wg.at, L.oa[v], L.ob[v]);
+                    }
+                wx.next(dh, H);
+                wg.next(dh, H);
+            };
+            request(group);
+            if constexpr (NORM) {
+                const float* w = a.t.w[s];
+                if (w) {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) wa[v][j] = w[L.oa[v] + L.WS * j], wb[v][j] = w[L.ob[v] + L.WS * j];
+                } else {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) wa[v][j] = wb[v][j] = 1.0f;
+                }
+            }
+            if (!made) {
+                const unsigned first = first_pos(a, m0);
+                for (int o = threadIdx.x; o < n * half; o += 256) {
+                    const int k = quotient(o, a.half_magic);
+                    cs[o] = turn(a, pos_row(a, first, k), o - k * half);
+                }
+                __syncthreads();
+                made = true;
+            }
+            for (int it = group; it < items; it += groups) {
+                float xa[NV][V], xb[NV][V], ga[NV][V], gb[NV][V];
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    if constexpr (NORM) rx[v].get(xa[v], xb[v]);
+                    rg[v].get(ga[v], gb[v]);
+                }
+                request(it + groups);
+                const float2* c = cs + wc.at;
+                T* y = yp + wy.at;
+                float rstd = 1.0f;
+                if constexpr (NORM) {
+                    float ss = 0.0f;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        float t = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < V; ++j) t = fmaf(xa[v][j], xa[v][j], fmaf(xb[v][j], xb[v][j], t));
+                        ss += L.has[v] ? t : 0.0f;
+                    }
+                    rstd = __builtin_amdgcn_rsqf(fmaf(sum_lanes(ss, a.lanes_log2), a.inv_dim, a.eps));
+                }
+                float dot = 0.0f;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float d = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float2 e = c[L.oc[v] + j];
+                        const float ra = fmaf(ga[v][j], e.x, gb[v][j] * e.y), rb = fmaf(gb[v][j], e.x, -(ga[v][j] * e.y));
+                        ga[v][j] = ra;
+                        gb[v][j] = rb;
+                        if constexpr (NORM) {
+                            xa[v][j] *= rstd;
+                            xb[v][j] *= rstd;
+                            float &da = dw[(v * V + j) * 2], &db = dw[(v * V + j) * 2 + 1];
+                            da = fmaf(ra, xa[v][j], da);
+                            db = fmaf(rb, xb[v][j], db);
+                            ga[v][j] *= wa[v][j];
+                            gb[v][j] *= wb[v][j];
+                            d = fmaf(ga[v][j], xa[v][j], fmaf(gb[v][j], xb[v][j], d));
+                        }
+                    }
+                    dot += L.has[v] ? d : 0.0f;
+                }
+                float mean = 0.0f;
+                if constexpr (NORM) mean = sum_lanes(dot, a.lanes_log2) * a.inv_dim;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    if constexpr (NORM)
+#pragma unroll
+                        for (int j = 0; j < V; ++j) {
+                            ga[v][j] = rstd * fmaf(-xa[v][j], mean, ga[v][j]);
+                            gb[v][j] = rstd * fmaf(-xb[v][j], mean, gb[v][j]);
+                        }
+                    if (L.has[v]) put<T, V, HALF>(y, L.oa[v], L.ob[v], ga[v], gb[v]);
+                }
+                wy.next(dh, H);
+                wc.next(dh, H);
+            }
+        }
+        if constexpr (NORM) {
+            if (a.part) {
+                sum_groups(dw, a.lanes_log2);
+                float* mine = sums + (threadIdx.x >> 6) * a.dim;
+                if ((threadIdx.x & 63) < ln)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+                        if (L.has[v])
+#pragma unroll
+                            for (int j = 0; j < V; ++j) mine[L.oa[v] + L.WS * j] = dw[(v * V + j) * 2], mine[L.ob[v] + L.WS * j] = dw[(v * V + j) * 2 + 1];
+                __syncthreads();
+                for (int o = threadIdx.x; o < a.dim; o += 256)
+                    a.part[((int64_t)blockIdx.x * 2 + s) * a.dim + o] = (sums[o] + sums[a.dim + o]) + (sums[2 * a.dim + o] + sums[3 * a.dim + o]);
+                __syncthreads();
+            }
+        }
+    }
+}
+
+// dw: the workgroups' sums in their order; 16 values to a workgroup, 64 shares of the sums each
+__global__ void __launch_bounds__(1024) qk_weight_sum(const float* part, int n, int dim, float* dwq, float* dwk)
+{
+    __shared__ float sh[64][17];
     const int v = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
     float t = 0.0f;
-    if (v < 2 * dim)
-        for (int i = r; i < n; i += 16) t += part[(int64_t)i * 2 * dim + v];
+    if (v < 2 * dim) {
+#pragma unroll 8
+        for (int i = r; i < n; i += 64) t += part[(int64_t)i * 2 * dim + v];
+    }
     sh[r][threadIdx.x & 15] = t;
     __syncthreads();
     if (r == 0 && v < 2 * dim) {
-        for (int k = 1; k < 16; ++k) t += sh[k][threadIdx.x];
+        for (int k = 1; k < 64; ++k) t += sh[k][threadIdx.x];
         (v < dim ? dwq : dwk)[v < dim ? v : v - dim] = t;
     }
 }
 
 // ---- host ---------------------------------------------------------------------------------------
 
-constexpr int QK_MAX_GROUPS = 1024;  // workgroups of the gradient, each of which leaves a part of dw
+// Tokens of a workgroup of the gradient, each of which leaves a part of dw: two workgroups to a compute unit are what its registers allow (us by the number
+// of workgroups, 8192 tokens of 16 + 16 heads of 72: 256 37.9, 512 35.9, 1024 39.4, 2048 49.3), one while they have little to do (1000 tokens: 256 13.5,
+// 512 14.7).  The table of cosines takes up to 48 KB of the LDS.
+static int qk_grad_tokens(const lq_qk_config* c, int64_t M)
+{
+    const int64_t most = 12288 / c->head_dim, groups = M < 4096 ? 256 : 512, t = (M + groups - 1) / groups;
+    return (int)(t < 1 ? 1 : t > most ? most : t);
+}
 
 struct QkShape {
     int V, NV, lanes_log2, tokens, lds;
@@ -275,7 +464,7 @@ static bool fits(const lq_heads& h, int heads, int64_t M, int elem, int bytes)
 {
     return ((uintptr_t)h.p % bytes) == 0 && (M < 2 || h.ld * elem % bytes == 0) && (heads < 2 || h.hs * elem % bytes == 0);
 }
-static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, int64_t max_grid)
+static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, bool grad)
 {
     const int P = c->pairs[0] + c->pairs[1] + c->pairs[2] + c->pairs[3], elem = c->dtype == LQ_F32 ? 4 : 2;
     const int heads[2] = {c->heads_q, c->heads_k};
@@ -291,19 +480,29 @@ static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, in
                      (!t->grad[k].p || fits(t->grad[k], heads[k], M, elem, bytes));
         if (ok) break;
     }
+    // two or three vectors to a lane, on the fewest lanes: what a turn costs beside its vectors is shared, and three fill 9 of 12 places of a
+    // head of 72 where one or two fill 9 of 16
     const int vectors = c->head_dim / (2 * s.V);
     s.lanes_log2 = 0;
-    while ((1 << s.lanes_log2) < vectors && s.lanes_log2 < 6) ++s.lanes_log2;
-    s.NV = (vectors + (1 << s.lanes_log2) - 1) >> s.lanes_log2;
-    const int H = heads[0] + heads[1], groups = 256 >> s.lanes_log2;
-    s.tokens = (2 * groups + H - 1) / H;
-    s.tokens = s.tokens < 1 ? 1 : s.tokens > 16 ? 16 : s.tokens;
+    while ((3 << s.lanes_log2) < vectors) ++s.lanes_log2;
+    s.NV = vectors <= (2 << s.lanes_log2) ? 2 : 3;
+    if (grad) {
+        s.tokens = qk_grad_tokens(c, M);
+    } else {
+        // two heads of each kind to a lane, while there are 1024 workgroups (us by the number of workgroups: 8192 tokens of 16 + 16 heads of 72: 512 25.4, 1024
+        // 24.9, 4096 27.6; 16380 of 20 + 20 of 112, two heads with 8192: 1024 62.6, 4096 59.4, 8192 59.2); up to 32 KB of the LDS for the table
+        const int groups = 256 >> s.lanes_log2, H = heads[0] > heads[1] ? heads[0] : heads[1];
+        const int64_t two = (2 * groups + H - 1) / H, share = M / 1024, most = 2048 / c->head_dim;
+        s.tokens = (int)(two < share ? two : share);
+        s.tokens = s.tokens < 1 ? 1 : s.tokens > most ? (int)most : s.tokens;
+    }
     s.grid = (M + s.tokens - 1) / s.tokens;
-    s.grid = s.grid > max_grid ? max_grid : s.grid;
-    const int table = s.tokens * c->head_dim / 2 * 8, sums = 2 * c->head_dim * 4;
-    s.lds = table > sums ? table : sums;
+    s.lds = s.tokens * c->head_dim / 2 * (grad ? 8 : 32) + (grad ? 4 * c->head_dim * 4 : 0);
     return s;
 }
+
+// floor(i / d) = floor(i m / 2^32) for i d < 2^32; 0 stands for d = 1, whose factor does not fit
+static unsigned quotient_magic(int d) { return d > 1 ? (unsigned)((((uint64_t)1 << 32) + d - 1) / d) : 0; }
 
 static QkArgs qk_args(const lq_qk_config* c, const QkTensors& t, int64_t M, const QkShape& s)
 {
@@ -317,23 +516,42 @@ static QkArgs qk_args(const lq_qk_config* c, const QkTensors& t, int64_t M, cons
     for (int k = 0; k < 4; ++k) a.axis_end[k] = a.pairs += c->pairs[k];
     a.lanes_log2 = s.lanes_log2;
     a.tokens = s.tokens;
+    const int groups = 256 >> s.lanes_log2;
+    for (int k = 0; k < 2; ++k) {
+        a.magic[k] = quotient_magic(a.heads[k]);
+        a.turn_k[k] = a.heads[k] ? groups / a.heads[k] : 0;
+        a.turn_h[k] = a.heads[k] ? groups % a.heads[k] : 0;
+    }
+    a.half_magic = quotient_magic(c->head_dim / 2);
     a.eps = c->eps;
+    a.inv_dim = 1.0f / (float)c->head_dim;
     return a;
 }
 
 template <typename T, int V, int NV, bool HALF, bool GRAD>
 static void qk_run(const QkArgs& a, bool norm, const QkShape& s, hipStream_t stream)
 {
-    if (norm) hipLaunchKernelGGL((qk_kernel<T, V, NV, HALF, true, GRAD>), dim3((unsigned)s.grid), dim3(256), s.lds, stream, a);
-    else hipLaunchKernelGGL((qk_kernel<T, V, NV, HALF, false, GRAD>), dim3((unsigned)s.grid), dim3(256), s.lds, stream, a);
+    const dim3 grid((unsigned)s.grid), block(256);
+    if constexpr (GRAD) {
+        if (norm) hipLaunchKernelGGL((qk_bwd_kernel<T, V, NV, HALF, true>), grid, block, s.lds, stream, a);
+        else hipLaunchKernelGGL((qk_bwd_kernel<T, V, NV, HALF, false>), grid, block, s.lds, stream, a);
+    } else {
+        if (norm) hipLaunchKernelGGL((qk_fwd_kernel<T, V, NV, HALF, true>), grid, block, s.lds, stream, a);
+        else hipLaunchKernelGGL((qk_fwd_kernel<T, V, NV, HALF, false>), grid, block, s.lds, stream, a);
+    }
+}
+template <typename T, int V, bool HALF, bool GRAD>
+static void qk_run_nv(const QkArgs& a, bool norm, const QkShape& s, hipStream_t stream)
+{
+    if (s.NV == 2) qk_run<T, V, 2, HALF, GRAD>(a, norm, s, stream);
+    else qk_run<T, V, 3, HALF, GRAD>(a, norm, s, stream);
 }
 template <typename T, bool HALF, bool GRAD>
 static void qk_run_v(const QkArgs& a, bool norm, const QkShape& s, hipStream_t stream)
 {
-    if (s.V == 4) qk_run<T, 4, 1, HALF, GRAD>(a, norm, s, stream);
-    else if (s.V == 2) qk_run<T, 2, 1, HALF, GRAD>(a, norm, s, stream);
-    else if (s.NV == 1) qk_run<T, 1, 1, HALF, GRAD>(a, norm, s, stream);
-    else qk_run<T, 1, 2, HALF, GRAD>(a, norm, s, stream);
+    if (s.V == 4) qk_run_nv<T, 4, HALF, GRAD>(a, norm, s, stream);
+    else if (s.V == 2) qk_run_nv<T, 2, HALF, GRAD>(a, norm, s, stream);
+    else qk_run_nv<T, 1, HALF, GRAD>(a, norm, s, stream);
 }
 template <bool GRAD>
 static hipError_t qk_run_all(const lq_qk_config* c, const QkArgs& a, const QkShape& s, hipStream_t stream)
@@ -351,26 +569,26 @@ static hipError_t qk_run_all(const lq_qk_config* c, const QkArgs& a, const QkSha
 
 size_t qk_work_bytes(const lq_qk_config* c, int64_t M)
 {
-    const int64_t groups = M < QK_MAX_GROUPS ? M : QK_MAX_GROUPS;
-    return c->norm == LQ_NORM_RMS ? align256((size_t)groups * 2 * c->head_dim * 4) : 0;
+    const int tokens = qk_grad_tokens(c, M);
+    return c->norm == LQ_NORM_RMS ? align256((size_t)((M + tokens - 1) / tokens) * 2 * c->head_dim * 4) : 0;
 }
 
 hipError_t launch_qk_fwd(const lq_qk_config* c, const QkTensors& t, int64_t M, hipStream_t s)
 {
-    const QkShape sh = qk_shape(c, &t, M, 1 << 20);
+    const QkShape sh = qk_shape(c, &t, M, false);
     return qk_run_all<false>(c, qk_args(c, t, M, sh), sh, s);
 }
 
 hipError_t launch_qk_bwd(const lq_qk_config* c, const QkTensors& t, int64_t M, uint8_t* work, hipStream_t s)
 {
-    const QkShape sh = qk_shape(c, &t, M, QK_MAX_GROUPS);
+    const QkShape sh = qk_shape(c, &t, M, true);
     QkArgs a = qk_args(c, t, M, sh);
     const bool dw = c->norm == LQ_NORM_RMS && t.dw[0];
     a.part = dw ? (float*)work : nullptr;
     hipError_t e = hipSuccess;
     if (M > 0) e = qk_run_all<true>(c, a, sh, s);
     if (e != hipSuccess || !dw) return e;
-    hipLaunchKernelGGL(qk_weight_sum, dim3((2 * c->head_dim + 15) / 16), dim3(256), 0, s, (const float*)work, M > 0 ? (int)sh.grid : 0, c->head_dim, t.dw[0], t.dw[1]);
+    hipLaunchKernelGGL(qk_weight_sum, dim3((2 * c->head_dim + 15) / 16), dim3(1024), 0, s, (const float*)work, M > 0 ? (int)sh.grid : 0, c->head_dim, t.dw[0], t.dw[1]);
     return hipGetLastError();
 }
 
