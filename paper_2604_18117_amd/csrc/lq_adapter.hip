@@ -204,6 +204,16 @@ __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
 
+// Column e of a block of 8 rows of 8 bf16 values, as the 8 consecutive values that a product takes.
+__device__ __forceinline__ v4i column(const v4i (&rows)[8], int e)
+{
+    v4i t;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+        t[d] = (int)__builtin_amdgcn_perm((uint32_t)rows[2 * d + 1][e / 2], (uint32_t)rows[2 * d][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+    return t;
+}
+
 struct AdapterView {  // of the plan, and the pool's per-adapter numbers
     const int *rows, *tbase;
     const int4* tiles;
@@ -219,82 +229,166 @@ __device__ __forceinline__ int rank_of(const AdapterView& v, int slot) { return 
 struct ShrinkArgs {
     AdapterView v;
     const void* X;  // rows of `depth` values
-    const uint16_t* W;  // [adapter][rank][depth]
+    const uint16_t* W;  // [adapter][rank][depth], or [adapter][depth][rank]
     float* T;       // [row of the plan][rp]
     int64_t ldx;
     int depth;
 };
 
-// A workgroup of 8 wavefronts: 32 rows of a tile, 16 * RT of the rank, the wavefronts' 64-deep pieces of K in turn.  A lane of the 16 x 16
-// x 32 product holds 8 values of K; it reads 16 consecutive ones, the first and second half for two products, so that four lanes
-// read 128 bytes of a row.
-template <bool F32, int RT>
-__global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
+// Orders the LDS accesses of one wavefront on memory of its own (they complete in order; the compiler must not move them either).
+__device__ __forceinline__ void wave_sync()
 {
-    __shared__ float red[8][32][RT * 16];
-    const int4 tile = a.v.tiles[blockIdx.x >> 1];
-    const int h = (blockIdx.x & 1) * 32, n = min(tile.y - h, 32), rank = rank_of(a.v, tile.z), r0 = blockIdx.y * (RT * 16);
-    if (n <= 0 || rank == 0) return;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    constexpr int XV = F32 ? 4 : 2, ES = F32 ? 4 : 2;
-    const uint8_t* x[2];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A wavefront's piece of a product: 64 values of K of 16 * MT rows of X and 16 * RT of the factor.  The 16 x 16 x 32 product wants 16 rows in 16
+// consecutive lanes; read like that from memory, every 16 bytes are a cache line of their own (40 us for 8191 x 2240, rank 128, whatever was
+// in flight).  So 8 (fp32: 16) lanes read a row's 128 (256) consecutive bytes, and the rows go through the wavefront's part of the LDS: unit p of 16
+// bytes of row r stands at r * units + (p ^ r % 16), free of bank conflicts both ways.
+// TW: the factor is given as [depth][rank]; a lane reads blocks of 8 x 8 and turns them on the way to the LDS.
+template <bool F32, bool TW, int MT, int RT>
+struct ShrinkPiece {
+    static constexpr int XU = F32 ? 16 : 8;            // units of a row of X
+    static constexpr int XL = MT * 16 * XU / 64, WL = TW ? 8 : RT * 16 * 8 / 64, WP = TW ? 1 : WL;
+    static constexpr int UNITS = MT * 16 * XU + RT * 16 * 8;
+    v4i x[XL], w[WL];
+    static __device__ __forceinline__ int place(int r, int p) { return MT * 16 * XU + r * 8 + (p ^ ((r + (r >> 3)) & 7)); }
+    __device__ __forceinline__ void fetch(const uint8_t* const (&xp)[XL], const uint8_t* const (&wp)[WP], int64_t c, int rank)
+    {
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-        const int row = a.v.rows[tile.x + h + min(mt * 16 + i, n - 1)];
-        x[mt] = (const uint8_t*)a.X + ((int64_t)row * a.ldx + q * 16) * ES;
+        for (int u = 0; u < XL; ++u) x[u] = *(const v4i*)(xp[u] + c * (XU * 16));
+#pragma unroll
+        for (int u = 0; u < WL; ++u) w[u] = TW ? *(const v4i*)(wp[0] + (c * 64 + u) * (rank * 2)) : *(const v4i*)(wp[TW ? 0 : u] + c * 128);
     }
-    const uint8_t* wt[RT];
+    __device__ __forceinline__ void put(v4i* lds, int lane) const
+    {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-        wt[rt] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.v.rank + min(r0 + rt * 16 + i, a.v.rank - 1)) * a.depth + q * 16);
-    v4f acc[2][RT];
+        for (int u = 0; u < XL; ++u) {
+            const int r = u * (64 / XU) + lane / XU, p = lane % XU;
+            lds[r * XU + (p ^ (r & (XU - 1)))] = x[u];
+        }
+        if constexpr (TW) {
+            if (lane < 16 * RT)
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+                for (int e = 0; e < 8; ++e) lds[place(lane % (2 * RT) * 8 + e, lane / (2 * RT))] = column(w, e);
+        } else {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = v4f{0, 0, 0, 0};
-    for (int c = w; c < a.depth / 64; c += 8) {
-        v4i xv[2][XV], wv[RT][2];
+            for (int u = 0; u < WL; ++u) lds[place(u * 8 + lane / 8, lane % 8)] = w[u];
+        }
+    }
+    static __device__ __forceinline__ void multiply(const v4i* lds, int i, int q, v4f (&acc)[MT][RT])
+    {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int u = 0; u < 2; ++u) {
+            v4i wv[RT];
 #pragma unroll
-            for (int u = 0; u < XV; ++u) xv[mt][u] = ((const v4i*)(x[mt] + (int64_t)c * 64 * ES))[u];
+            for (int rt = 0; rt < RT; ++rt) wv[rt] = lds[place(rt * 16 + i, u * 4 + q)];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) wv[rt][u] = ((const v4i*)(wt[rt] + (int64_t)c * 128))[u];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
+            for (int mt = 0; mt < MT; ++mt) {
+                const v4i* row = lds + (mt * 16 + i) * XU;
                 if constexpr (F32) {
                     float v[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = __int_as_float(xv[mt][2 * u + j / 4][j % 4]);
+                    for (int h = 0; h < 2; ++h) {
+                        const v4i r = row[(2 * (u * 4 + q) + h) ^ i];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[4 * h + j] = __int_as_float(r[j]);
+                    }
                     v4i t[3];
                     split8<3>(v, t);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-                        for (int k = 2; k >= 0; --k) acc[mt][rt] = mfma(t[k], wv[rt][u], acc[mt][rt]);
+                        for (int k = 2; k >= 0; --k) acc[mt][rt] = mfma(t[k], wv[rt], acc[mt][rt]);
                 } else {
+                    const v4i x = row[(u * 4 + q) ^ (i & 7)];
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = mfma(xv[mt][u], wv[rt][u], acc[mt][rt]);
+                    for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = mfma(x, wv[rt], acc[mt][rt]);
                 }
             }
+        }
     }
+};
+
+// A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next two
+// requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
+template <bool F32, bool TW, int MT, int RT>
+__global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
+{
+    typedef ShrinkPiece<F32, TW, MT, RT> Piece;
+    constexpr int PARTS = TILE / (16 * MT);  // workgroups of a tile
+    extern __shared__ v4i lds[];             // a piece per wavefront; then [wavefront][row][rank] sums
+    const int4 tile = a.v.tiles[blockIdx.x / PARTS];
+    const int h = (blockIdx.x % PARTS) * (16 * MT), n = min(tile.y - h, 16 * MT), rank = rank_of(a.v, tile.z), r0 = blockIdx.y * (RT * 16);
+    if (n <= 0 || rank == 0) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const uint8_t *xp[Piece::XL], *wp[Piece::WP];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int u = 0; u < Piece::XL; ++u) {
+        const int row = a.v.rows[tile.x + h + min(u * (64 / Piece::XU) + lane / Piece::XU, n - 1)];
+        xp[u] = (const uint8_t*)a.X + (int64_t)row * a.ldx * (F32 ? 4 : 2) + lane % Piece::XU * 16;
+    }
+    // (ranks past the pool's are read from its last and not stored)
+    if constexpr (TW) {
+        const int block = min(lane / (2 * RT), 7), r = min(r0 + lane % (2 * RT) * 8, a.v.rank - 8);
+        wp[0] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.depth + block * 8) * a.v.rank + r);
+    } else {
+#pragma unroll
+        for (int u = 0; u < Piece::WL; ++u)
+            wp[u] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.v.rank + min(r0 + u * 8 + lane / 8, a.v.rank - 1)) * a.depth) + lane % 8 * 16;
+    }
+    v4f acc[MT][RT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = v4f{0, 0, 0, 0};
+    const int pieces = a.depth / 64;
+    v4i* mine = lds + w * Piece::UNITS;
+    if constexpr (Piece::XL + Piece::WL <= 14 && !(TW && MT == 2 && RT == 4)) {
+        Piece p0, p1;
+        if (w < pieces) p0.fetch(xp, wp, w, a.v.rank);
+        if (w + 8 < pieces) p1.fetch(xp, wp, w + 8, a.v.rank);
+        for (int c = w; c < pieces; c += 16) {
+            wave_sync();
+            p0.put(mine, lane);
+            wave_sync();
+            if (c + 16 < pieces) p0.fetch(xp, wp, c + 16, a.v.rank);
+            Piece::multiply(mine, i, q, acc);
+            if (c + 8 >= pieces) break;
+            wave_sync();
+            p1.put(mine, lane);
+            wave_sync();
+            if (c + 24 < pieces) p1.fetch(xp, wp, c + 24, a.v.rank);
+            Piece::multiply(mine, i, q, acc);
+        }
+    } else {  // (two would not fit the registers)
+        Piece p;
+        if (w < pieces) p.fetch(xp, wp, w, a.v.rank);
+        for (int c = w; c < pieces; c += 8) {
+            wave_sync();
+            p.put(mine, lane);
+            wave_sync();
+            if (c + 8 < pieces) p.fetch(xp, wp, c + 8, a.v.rank);
+            Piece::multiply(mine, i, q, acc);
+        }
+    }
+    constexpr int ROW = RT * 16, ALL = MT * 16 * ROW;
+    float* red = (float*)lds;
+    __syncthreads();
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) red[w][mt * 16 + q * 4 + e][rt * 16 + i] = acc[mt][rt][e];
+            for (int e = 0; e < 4; ++e) red[w * ALL + (mt * 16 + q * 4 + e) * ROW + rt * 16 + i] = acc[mt][rt][e];
     __syncthreads();
-    for (int o = threadIdx.x; o < 32 * RT * 16; o += 512) {
-        const int m = o / (RT * 16), r = o % (RT * 16);
+    for (int o = threadIdx.x; o < ALL; o += 512) {
+        const int m = o / ROW, r = r0 + o % ROW;
         float t = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += red[k][m][r];
-        if (m < n && r0 + r < a.v.rp) a.T[(int64_t)(tile.x + h + m) * a.v.rp + r0 + r] = r0 + r < rank ? t : 0.0f;
+        for (int k = 0; k < 8; ++k) t += red[k * ALL + o];
+        if (m < n && r < a.v.rp) a.T[(int64_t)(tile.x + h + m) * a.v.rp + r] = r < rank ? t : 0.0f;
     }
 }
 
@@ -303,264 +397,321 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
 struct ExpandArgs {
     AdapterView v;
     const float* T;
-    const uint16_t* W;  // [adapter][width][rank]
+    const uint16_t* W;  // [adapter][width][rank], or [adapter][rank][width]
     const void* Yin;    // or NULL: zeros
     void* Y;
     int64_t ldyin, ldy;
     int width;
     int in_place;
+    int per;              // pieces of 128 columns of a workgroup
+    unsigned unit_magic;  // 2^32 / (rank / 8), rounded up; 0 for rank 8
 };
 
-// 16 consecutive values of a row, as fp32
-template <bool F32>
-__device__ __forceinline__ void load16(const void* p, int64_t at, float (&v)[16])
-{
-    if constexpr (F32) {
+// 8 consecutive values of a row as they lie in memory, at a uniform base and a lane's offset of OFF bytes: with 32 bits an access needs one register
+// for its address.
+template <bool F32, typename OFF>
+struct Row8 {
+    v4i v[F32 ? 2 : 1];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const v4f t = ((const v4f*)((const float*)p + at))[u];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * u + e] = t[e];
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const v4i t = ((const v4i*)((const uint16_t*)p + at))[u];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[8 * u + 2 * e] = __uint_as_float((uint32_t)t[e] << 16);
-                v[8 * u + 2 * e + 1] = __uint_as_float((uint32_t)t[e] & 0xFFFF0000u);
-            }
-        }
+        for (int u = 0; u < (F32 ? 2 : 1); ++u) v[u] = v4i{0, 0, 0, 0};
     }
-}
+    __device__ __forceinline__ void fetch(const uint8_t* base, OFF off)
+    {
+#pragma unroll
+        for (int u = 0; u < (F32 ? 2 : 1); ++u) v[u] = ((const v4i*)(base + off))[u];
+    }
+    __device__ __forceinline__ float get(int j) const
+    {
+        if constexpr (F32) return __int_as_float(v[j / 4][j % 4]);
+        else return __uint_as_float(j & 1 ? (uint32_t)v[0][j / 2] & 0xFFFF0000u : (uint32_t)v[0][j / 2] << 16);
+    }
+    __device__ __forceinline__ void store(uint8_t* base, OFF off) const
+    {
+#pragma unroll
+        for (int u = 0; u < (F32 ? 2 : 1); ++u) ((v4i*)(base + off))[u] = v[u];
+    }
+};
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)  // round to nearest even
 {
     typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
     const v2bf v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
 }
-template <bool F32>
-__device__ __forceinline__ void store16(void* p, int64_t at, const float (&v)[16])
+// Clears what lies beyond an adapter's rank in 8 values of it, `left` of which it has.
+__device__ __forceinline__ v4i keep(v4i t, int left)
 {
-    if constexpr (F32) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) ((v4f*)((float*)p + at))[u] = v4f{v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]};
-    } else {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            v4i t;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = (int)pack_bf16(v[8 * u + 2 * e], v[8 * u + 2 * e + 1]);
-            ((v4i*)((uint16_t*)p + at))[u] = t;
-        }
-    }
+    for (int d = 0; d < 4; ++d) t[d] = left >= 2 * d + 2 ? t[d] : left == 2 * d + 1 ? t[d] & 0xFFFF : 0;
+    return t;
 }
 
-// A workgroup of 4 wavefronts: a tile, 64 columns each.  T's rows are the second operand, so that a lane's four sums are four columns of one
-// row; the factor's rows are dealt to the four products so that these are 16 consecutive columns.
-template <bool F32, int KS>
+// A workgroup of 4 wavefronts: a tile, 16 rows each, and `per` pieces of 128 columns one after another.  Bound by memory, so it is laid out for its
+// accesses: product j of 8 has columns 8 i + j in lane i, so that a lane's sums of the 8 products are 8 consecutive columns of a row and 16 lanes
+// read and write 256 consecutive bytes (with 16 rows in 16 lanes every 16 bytes are a cache line of their own).  The factor's 128
+// rows are read in order, too, by all four wavefronts, and go through the LDS (unit (j, ks, q, i) of 16 bytes in the order of its
+// readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
+// TW: the factor is given as [rank][width]; a thread reads blocks of 8 x 8 and turns them on the way to the LDS.
+template <bool F32, bool TW, int KS, typename OFF>
 __global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
 {
+    constexpr int ES = F32 ? 4 : 2;
     constexpr int TERMS = F32 ? 3 : 2;
-    __shared__ v4i top[4][KS][TERMS][64];
-    const int4 tile = a.v.tiles[blockIdx.x];
+    constexpr int WL = TW ? 8 : KS * 2;       // units of 16 bytes that a thread reads of a piece of the factor: 128 * 4 KS / 256
+    constexpr int BUFFERS = KS <= 2 ? 2 : 1;  // (two of the larger ones leave room for two workgroups on a compute unit, one for four)
+    __shared__ v4i wl[BUFFERS][8 * KS * 64];
+    const int4 tile = a.v.tiles[blockIdx.y];
     const int n = tile.y, rank = rank_of(a.v, tile.z);
     if (n <= 0 || (rank == 0 && a.in_place)) return;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const int col = (blockIdx.y * 4 + w) * 64;
-    const int subs = (n + 15) >> 4;
-    if (rank > 0) {
-        if (w < subs) {
-            const float s = a.v.scales[tile.z];
-            const float* T = a.T + (int64_t)(tile.x + min(w * 16 + i, n - 1)) * a.v.rp;
+    const int c0 = blockIdx.x * a.per, c1 = min(c0 + a.per, (a.width + 127) / 128);
+    const int pr = a.v.rank / 8;  // units of a row of the factor
+    const uint16_t* W = a.W + (int64_t)tile.z * a.width * a.v.rank;
+    v4i wr[WL];
+    auto request_w = [&](int c) {
+        if constexpr (TW) {  // thread (p, i): ranks 8 p .., columns 8 i ..
+            const int r = (int)threadIdx.x / 16 * 8, x = (int)threadIdx.x % 16 * 8;
+            const uint16_t* src = W + c * 128 + (x < a.width - c * 128 ? x : 0);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int k = ks * 32 + q * 8;
-                float v[8];
+            for (int u = 0; u < 8; ++u) wr[u] = *(const v4i*)(src + (int64_t)min(r + u, a.v.rank - 1) * a.width);
+        } else {
+            const int units = min(128, a.width - c * 128) * pr;
+            const uint8_t* src = (const uint8_t*)(W + (int64_t)c * 128 * a.v.rank);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const v4f t = *(const v4f*)(T + min(k, a.v.rp - 8) + 4 * u);
+            for (int u = 0; u < WL; ++u) wr[u] = *(const v4i*)(src + (uint32_t)min(u * 256 + (int)threadIdx.x, units - 1) * 16u);
+        }
+    };
+    if (rank > 0) request_w(c0);
+    // this lane's four rows of the output
+    // (rows and columns past the tile's and the matrix's are read from the last or first ones and not stored; so no load has a branch around it)
+    OFF yin[4], yout[4];
+    const int mine = n - (w * 16 + q * 4);  // how many of them the tile has
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[4 * u + e] = k < rank ? t[e] * s : 0.0f;
+    for (int e = 0; e < 4; ++e) {
+        const int row = a.v.rows[tile.x + (e < mine ? w * 16 + q * 4 + e : n - 1)];
+        yin[e] = ((OFF)row * (OFF)a.ldyin + 8 * i) * ES;
+        yout[e] = ((OFF)row * (OFF)a.ldy + 8 * i) * ES;
+    }
+    Row8<F32, OFF> y[4];
+    auto request_y = [&](int c) {
+        const OFF wrap = 8 * i < a.width - c * 128 ? 0 : 8 * i * ES;
+        if (a.Yin) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e].fetch((const uint8_t*)a.Yin + (int64_t)c * 128 * ES, yin[e] - wrap);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e].clear();
+        }
+    };
+    request_y(c0);
+    if (rank == 0) {
+        for (int c = c0; c < c1; ++c) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e < mine && 8 * i < a.width - c * 128) y[e].store((uint8_t*)a.Y + (int64_t)c * 128 * ES, yout[e]);
+            if (c + 1 < c1) request_y(c + 1);
+        }
+        return;
+    }
+    v4i tt[KS][TERMS];
+    {
+        const float s = a.v.scales[tile.z];
+        const float* T = a.T + (int64_t)(tile.x + min(w * 16 + i, n - 1)) * a.v.rp;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            float t[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const v4f x = *(const v4f*)(T + min(ks * 32 + q * 8, a.v.rp - 8) + 4 * u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
+            }
+            split8<TERMS>(t, tt[ks]);
+        }
+    }
+    // the units that no row of the factor fills (ranks that are no multiple of 32)
+    if (!TW && pr < KS * 4) {
+        for (int o = threadIdx.x; o < BUFFERS * 8 * KS * 64; o += 256) wl[0][o] = v4i{0, 0, 0, 0};
+        __syncthreads();
+    }
+    for (int c = c0; c < c1; ++c) {
+        const int rows = min(128, a.width - c * 128);
+        v4i* buf = wl[(c - c0) % BUFFERS];
+        if (BUFFERS == 1 && c > c0) __syncthreads();  // (the present piece has been read)
+        if constexpr (TW) {
+            const int p = (int)threadIdx.x / 16, x = (int)threadIdx.x % 16;
+            if (p < KS * 4) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u)  // (ranks that the adapter does not have, whatever the pool holds there)
+                    if (8 * p + u >= rank) wr[u] = v4i{0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) buf[(j * KS + (p >> 2)) * 64 + (p & 3) * 16 + (x ^ ((p & 3) + 4 * (((p >> 2) + j) & 1)))] = column(wr, j);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < WL; ++u) {
+                const int f = u * 256 + (int)threadIdx.x, r = a.unit_magic ? (int)__umulhi((unsigned)f, a.unit_magic) : f, p = f - r * pr;
+                if (f < rows * pr) {
+                    const int j = r & 7, k = p >> 2, qq = p & 3;
+                    buf[(j * KS + k) * 64 + qq * 16 + ((r >> 3) ^ (qq + 4 * ((k + j) & 1)))] = rank < a.v.rank ? keep(wr[u], rank - 8 * p) : wr[u];
                 }
-                v4i t[TERMS];
-                split8<TERMS>(v, t);
-#pragma unroll
-                for (int k2 = 0; k2 < TERMS; ++k2) top[w][ks][k2][lane] = t[k2];
             }
         }
         __syncthreads();
-    }
-    if (col >= a.width) return;
-    // a lane's part of the factor: rows (i / 4) * 16 + 4 j + i % 4 of the 64, 8 values of the rank from 32 ks + 8 q on
-    v4i wv[4][KS];
-    if (rank > 0) {
-        const uint16_t* W = a.W + ((int64_t)tile.z * a.width + col + (i >> 2) * 16 + (i & 3)) * a.v.rank;
+        if (c + 1 < c1) request_w(c + 1);
+        // a bf16 output's sums start from it (rounded to 8 bits in the end); an fp32 one takes them when they are complete
+        v4f acc[8];
+        Row8<F32, OFF> o[F32 ? 4 : 1];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int k = ks * 32 + q * 8, left = rank - k;  // values that the adapter has; the others are cleared whatever they hold
+        for (int j = 0; j < 8; ++j) acc[j] = F32 ? v4f{0, 0, 0, 0} : v4f{y[0].get(j), y[1].get(j), y[2].get(j), y[3].get(j)};
+        if constexpr (F32)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v4i t = *(const v4i*)(W + (int64_t)(4 * j) * a.v.rank + min(k, a.v.rank - 8));
+            for (int e = 0; e < 4; ++e) o[e] = y[e];
+        if (c + 1 < c1) request_y(c + 1);
+        if (w * 16 >= n) continue;
 #pragma unroll
-                for (int d = 0; d < 4; ++d) t[d] = left >= 2 * d + 2 ? t[d] : left == 2 * d + 1 ? t[d] & 0xFFFF : 0;
-                wv[j][ks] = t;
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const v4i wv = buf[(j * KS + ks) * 64 + q * 16 + (i ^ (q + 4 * ((ks + j) & 1)))];
+#pragma unroll
+                for (int k = TERMS - 1; k >= 0; --k) acc[j] = mfma(tt[ks][k], wv, acc[j]);
             }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            Row8<F32, OFF> z;
+            if constexpr (F32) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z.v[j / 4][j % 4] = __float_as_int(o[e].get(j) + acc[j][e]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z.v[0][j] = (int)pack_bf16(acc[2 * j][e], acc[2 * j + 1][e]);
+            }
+            if (e < mine && 8 * i < rows) z.store((uint8_t*)a.Y + (int64_t)c * 128 * ES, yout[e]);
         }
-    }
-#pragma unroll
-    for (int sub = 0; sub < 4; ++sub) {
-        if (sub >= subs) break;
-        const int m = sub * 16 + i;
-        const bool ok = m < n;
-        const int64_t row = a.v.rows[tile.x + min(m, n - 1)];
-        float y[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) y[e] = 0.0f;
-        if (ok && a.Yin) load16<F32>(a.Yin, row * a.ldyin + col + q * 16, y);
-        if (rank > 0) {
-            v4f acc[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = v4f{0, 0, 0, 0};
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-                for (int k = TERMS - 1; k >= 0; --k) {
-                    const v4i t = top[sub][ks][k][lane];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = mfma(wv[j][ks], t, acc[j]);
-                }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y[4 * j + e] += acc[j][e];
-        }
-        if (ok) store16<F32>(a.Y, row * a.ldy + col + q * 16, y);
     }
 }
 
 // ---- gradients of the factors -----------------------------------------------------------------
 
-// The factors transposed, zeros in the ranks that an adapter does not have: At [adapter][K][rank], Bt [adapter][rank][N].  64 x 64 squares
-// through the LDS; adapters without rows are skipped.
-__global__ void __launch_bounds__(256) adapter_transpose(AdapterView v, const uint16_t* A, const uint16_t* B, uint16_t* At, uint16_t* Bt, int N, int K)
-{
-    __shared__ uint16_t sq[64][65];
-    const int slot = blockIdx.z;
-    if (v.tbase[slot] == v.tbase[slot + 1]) return;
-    const int rank = rank_of(v, slot), r0 = blockIdx.y * 64, kb = K / 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    const bool isA = (int)blockIdx.x < kb;
-    const int c0 = (isA ? (int)blockIdx.x : (int)blockIdx.x - kb) * 64;
-    if (isA) {
-        for (int y = ty; y < 64; y += 4)
-            if (r0 + y < v.rank) sq[y][tx] = r0 + y < rank ? A[((int64_t)slot * v.rank + r0 + y) * K + c0 + tx] : 0;
-        __syncthreads();
-        for (int y = ty; y < 64; y += 4)
-            if (r0 + tx < v.rank) At[((int64_t)slot * K + c0 + y) * v.rank + r0 + tx] = sq[tx][y];
-    } else {
-        for (int y = ty; y < 64; y += 4)
-            if (r0 + tx < v.rank) sq[tx][y] = r0 + tx < rank ? B[((int64_t)slot * N + c0 + y) * v.rank + r0 + tx] : 0;
-        __syncthreads();
-        for (int y = ty; y < 64; y += 4)
-            if (r0 + y < v.rank) Bt[((int64_t)slot * v.rank + r0 + y) * N + c0 + tx] = sq[y][tx];
-    }
-}
-
 struct WgradArgs {
     AdapterView v;
-    const float* T;  // [row of the plan][rp]
-    const void* Q;   // rows of `width` values
-    float* out;      // [adapter][rank * width]
-    float* part;     // [2 * group + (0 | 1)][part_stride]
-    int64_t ldq, part_stride;
-    int width, per;  // per: tiles of a group
+    const float *T, *dT;   // [row of the plan][rp]
+    const void *dY, *X;    // rows of N, of K values
+    float *dA, *dB;        // [adapter][rank][K], [adapter][N][rank]
+    float* part;           // [2 * group + (0 | 1)][part_stride]: N x rank of dB, then rank x K of dA
+    int64_t lddy, ldx, part_stride;
+    int N, K, per;         // per: tiles of a group
 };
 
-// out = s T^T Q over the rows of an adapter, for 128 columns of Q and 16 * RT of the rank.  The tiles of the plan are dealt to groups of `per`;
-// an adapter that lies within a group is finished there, one that does not leaves a part in each (2 g where it has the group's first tile, 2 g + 1
-// where it starts within), which adapter_wgrad_sum adds up.  The four wavefronts of a workgroup take tiles in turn.
-// Both operands need 8 rows of one column in a lane: a lane loads 8 columns of 8 rows and pairs up the halves of the dwords, which gives
-// the operands of 8 products, the c-th with columns 8 i + c.
+// One group's part of out = s T^T Q, for 128 columns of Q and 16 * RT of the rank (see adapter_wgrad).
 // COLS_FIRST: the columns are the first operand (out is [rank][width], a lane's sums are consecutive columns), else the second ([width][rank]).
 template <bool F32, int RT, bool COLS_FIRST>
-__global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
+__device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T, const void* Q, int64_t ldq, float* whole_out, float* part, int64_t part_stride,
+                                            int width, int per, int block, v4f (*red)[8 * RT][64])
 {
     constexpr int QT = F32 ? 3 : 1;
-    __shared__ v4f red[2][8 * RT][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const int c0 = blockIdx.x * 128, r0 = blockIdx.z * (RT * 16), g = blockIdx.y;
-    const int col = c0 + 8 * i < a.width ? c0 + 8 * i : c0;  // (lanes past the width repeat the first columns and store nothing)
-    const int last = min((g + 1) * a.per, a.v.tbase[a.v.slots]);
-    for (int t0 = g * a.per; t0 < last;) {
-        const int slot = a.v.tiles[t0].z, s0 = a.v.tbase[slot], s1 = a.v.tbase[slot + 1], t1 = min(s1, last);
+    const int c0 = block * 128, r0 = blockIdx.z * (RT * 16), g = blockIdx.y;
+    const int col = c0 + 8 * i < width ? c0 + 8 * i : c0;  // (lanes past the width repeat the first columns and store nothing)
+    const int last = min((g + 1) * per, v.tbase[v.slots]);
+    for (int t0 = g * per; t0 < last;) {
+        const int slot = v.tiles[t0].z, s0 = v.tbase[slot], s1 = v.tbase[slot + 1], t1 = min(s1, last);
         v4f acc[8][RT];
 #pragma unroll
         for (int c = 0; c < 8; ++c)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) acc[c][rt] = v4f{0, 0, 0, 0};
-        for (int t = t0 + w; t < t1; t += 4) {
-            const int4 tile = a.v.tiles[t];
-            for (int h = 0; h < tile.y; h += 32) {
-                const int left = tile.y - h - q * 8;  // rows that this lane's 8 have
-                v4i qr[8][F32 ? 2 : 1];
-                float tv[RT][8];
+        // steps of 32 rows, two to a tile, dealt to the wavefronts; the next step's rows are looked up, and Q requested, under the products of this one
+        const int steps = 2 * (t1 - t0);
+        v4i qn[8][F32 ? 2 : 1];
+        int pn = 0, left_n = 0;  // first row of the plan, and how many rows the lane's 8 have
+        int64_t rows_n[8];
+        auto look = [&](int st) {
+            const int4 tile = v.tiles[t0 + min(st, steps - 1) / 2];
+            const int h = (min(st, steps - 1) & 1) * 32 + q * 8;
+            left_n = st < steps ? tile.y - h : 0;
+            pn = tile.x + h;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int pos = tile.x + (j < left ? h + q * 8 + j : tile.y - 1);
-                    const int64_t row = a.v.rows[pos];
-                    if constexpr (F32) {
+            for (int j = 0; j < 8; ++j) rows_n[j] = v.rows[j < left_n ? pn + j : tile.x];
+        };
+        auto request = [&] {
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) qr[j][u] = ((const v4i*)((const float*)a.Q + row * a.ldq + col))[u];
-                    } else {
-                        qr[j][0] = *(const v4i*)((const uint16_t*)a.Q + row * a.ldq + col);
-                    }
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (F32) {
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        const int r = min(r0 + rt * 16 + i, a.v.rp - 1);
-                        const float t1v = a.T[(int64_t)pos * a.v.rp + r];
-                        tv[rt][j] = j < left ? t1v : 0.0f;
-                    }
-                }
-                v4i tt[RT][3];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) split8<3>(tv[rt], tt[rt]);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    v4i qt[QT];
-                    if constexpr (F32) {
-                        float v[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = __int_as_float(qr[j][c / 4][c % 4]);
-                        split8<3>(v, qt);
-                    } else {
-#pragma unroll
-                        for (int d = 0; d < 4; ++d)
-                            qt[0][d] = (int)__builtin_amdgcn_perm((uint32_t)qr[2 * d + 1][0][c / 2], (uint32_t)qr[2 * d][0][c / 2],
-                                                                   c & 1 ? 0x07060302u : 0x05040100u);
-                    }
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int k = 2; k >= 0; --k)
-#pragma unroll
-                            for (int u = QT - 1; u >= 0; --u)
-                                if (k + u < 3)  // (what is left out is below 2^-24 of the product)
-                                    acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
+                    for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + rows_n[j] * ldq + col))[u];
+                } else {
+                    qn[j][0] = *(const v4i*)((const uint16_t*)Q + rows_n[j] * ldq + col);
                 }
             }
+        };
+        if (w < steps) {
+            look(w);
+            request();
         }
-        // wavefronts 2 and 3 to 0 and 1, then 1 to 0
+        for (int st = w; st < steps; st += 4) {
+            v4i qr[8][F32 ? 2 : 1];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
+            const int left = left_n, pos = pn;
+            float tv[RT][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) tv[rt][j] = T[(int64_t)(j < left ? pos + j : 0) * v.rp + min(r0 + rt * 16 + i, v.rp - 1)];
+            look(st + 4);
+            v4i tt[RT][3];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) tv[rt][j] = j < left ? tv[rt][j] : 0.0f;
+                split8<3>(tv[rt], tt[rt]);
+            }
+            // (rows past the adapter's last: the row that stands in for them must not reach the sums through an infinity of its own, 0 * inf)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = j < left ? qr[j][u] : v4i{0, 0, 0, 0};
+            if (st + 4 < steps) request();
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                v4i qt[QT];
+                if constexpr (F32) {
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = __int_as_float(qr[j][c / 4][c % 4]);
+                    split8<3>(x, qt);
+                } else {
+                    v4i rows8[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) rows8[j] = qr[j][0];
+                    qt[0] = column(rows8, c);
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int k = 2; k >= 0; --k)
+#pragma unroll
+                        for (int u = QT - 1; u >= 0; --u)
+                            if (k + u < 3)  // (what is left out is below 2^-22 of the product)
+                                acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
+            }
+        }
+        // wavefronts 2 and 3 to 0 and 1, then 1 to 0 (those that had steps)
         __syncthreads();
 #pragma unroll
         for (int d = 2; d >= 1; d >>= 1) {
-            if (w >= d && w < 2 * d)
+            if (w >= d && w < 2 * d && w < steps)
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) red[w - d][c * RT + rt][lane] = acc[c][rt];
             __syncthreads();
-            if (w < d)
+            if (w < d && w + d < steps)
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
 #pragma unroll
@@ -568,10 +719,10 @@ __global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
             __syncthreads();
         }
         if (w == 0) {
-            const int rank = rank_of(a.v, slot);
-            const float s = a.v.scales[slot];
-            const bool whole = s0 >= g * a.per && s1 <= (g + 1) * a.per;
-            float* out = whole ? a.out + (int64_t)slot * a.v.rank * a.width : a.part + (int64_t)(2 * g + (s0 > g * a.per)) * a.part_stride;
+            const int rank = rank_of(v, slot);
+            const float s = v.scales[slot];
+            const bool whole = s0 >= g * per && s1 <= (g + 1) * per;
+            float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(2 * g + (s0 > g * per)) * part_stride;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 if constexpr (COLS_FIRST) {
@@ -579,30 +730,44 @@ __global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int k = c0 + 8 * (q * 4 + e);
-                        if (r < a.v.rank && k < a.width)
+                        if (r < v.rank && k < width)
 #pragma unroll
                             for (int u = 0; u < 2; ++u) {
                                 v4f o;
 #pragma unroll
                                 for (int c = 0; c < 4; ++c) o[c] = r < rank ? acc[4 * u + c][rt][e] * s : 0.0f;
-                                *(v4f*)(out + (int64_t)r * a.width + k + 4 * u) = o;
+                                *(v4f*)(out + (int64_t)r * width + k + 4 * u) = o;
                             }
                     }
                 } else {
                     const int r = r0 + rt * 16 + q * 4;
-                    if (r < a.v.rank && c0 + 8 * i < a.width)
+                    if (r < v.rank && c0 + 8 * i < width)
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             v4f o;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) o[e] = r + e < rank ? acc[c][rt][e] * s : 0.0f;
-                            *(v4f*)(out + (int64_t)(c0 + 8 * i + c) * a.v.rank + r) = o;
+                            *(v4f*)(out + (int64_t)(c0 + 8 * i + c) * v.rank + r) = o;
                         }
                 }
             }
         }
         t0 = t1;
     }
+}
+
+// dB = s dY^T T and dA = (s dY B)^T X in one launch, 128 columns of dY or X and 16 * RT of the rank to a workgroup.  The tiles of the plan are dealt
+// to groups of `per`; an adapter that lies within a group is finished there, one that does not leaves a part in each (2 g where it has the group's
+// first tile, 2 g + 1 where it starts within), which adapter_wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
+// a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
+// products, the c-th with columns 8 i + c.
+template <bool F32, int RT>
+__global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
+{
+    __shared__ v4f red[2][8 * RT][64];
+    const int nb = (a.N + 127) / 128;
+    if ((int)blockIdx.x < nb) wgrad_group<false, RT, false>(a.v, a.T, a.dY, a.lddy, a.dB, a.part, a.part_stride, a.N, a.per, blockIdx.x, red);
+    else wgrad_group<F32, RT, true>(a.v, a.dT, a.X, a.ldx, a.dA, a.part + (int64_t)a.v.rank * a.N, a.part_stride, a.K, a.per, blockIdx.x - nb, red);
 }
 
 // Adapters without rows: zeros.  Adapters of more than one group: their parts in the order of the groups.  nb, na: quads of dB and dA.
@@ -614,6 +779,7 @@ __global__ void __launch_bounds__(256) adapter_wgrad_sum(AdapterView v, const fl
     for (int64_t o = (int64_t)blockIdx.x * 256 + threadIdx.x; o < nb + na; o += (int64_t)gridDim.x * 256) {
         v4f t = {0, 0, 0, 0};
         if (s0 < s1)
+#pragma unroll 8
             for (int g = g0; g <= g1; ++g) t += ((const v4f*)(part + (int64_t)(2 * g + (s0 > g * per)) * part_stride))[o];
         if (o < nb) dB[(int64_t)slot * nb + o] = t;
         else dA[(int64_t)slot * na + o - nb] = t;
@@ -647,13 +813,10 @@ AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
     int64_t groups = 1024 / units;
     groups = groups < 1 ? 1 : groups;
     l.per = (int)((tiles + groups - 1) / groups);
-    l.per = l.per < 4 ? 4 : l.per;
     l.groups = (tiles + l.per - 1) / l.per;
     l.part_stride = (int64_t)c->rank * (c->N + c->K);
     size_t o = 0;
     l.off_dT = o, o += align256((size_t)M * rp * 4);
-    l.off_At = o, o += align256((size_t)c->slots * c->rank * c->K * 2);
-    l.off_Bt = o, o += align256((size_t)c->slots * c->rank * c->N * 2);
     l.off_part = o, o += l.groups > 1 ? align256((size_t)(2 * l.groups) * l.part_stride * 4) : 0;
     l.total = o;
     return l;
@@ -666,61 +829,77 @@ static AdapterView view_of(const lq_adapter_config* c, const lq_adapter_pool* po
             c->slots, c->rank, (c->rank + 15) / 16 * 16, (int)M};
 }
 
-static hipError_t run_shrink(const ShrinkArgs& a, bool f32, int tiles, hipStream_t s)
+template <bool F32, bool TW, int MT, int RT>
+static hipError_t run_shrink_form(const ShrinkArgs& a, int tiles, int groups, hipStream_t s)
+{
+    const int pieces = 8 * ShrinkPiece<F32, TW, MT, RT>::UNITS * 16, sums = 8 * MT * 16 * RT * 16 * 4, lds = pieces > sums ? pieces : sums;
+    const hipError_t e = allow_lds<adapter_shrink<F32, TW, MT, RT>>(lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((adapter_shrink<F32, TW, MT, RT>), dim3(tiles * (TILE / (16 * MT)), groups), dim3(512), lds, s, a);
+    return hipGetLastError();
+}
+template <bool F32, bool TW, int MT>
+static hipError_t run_shrink_ranks(const ShrinkArgs& a, int tiles, hipStream_t s)
 {
     const RankSplit rs = rank_split(a.v.rank);
-    const dim3 grid(2 * tiles, rs.groups), block(512);
-#define SHRINK(RT) \
-    if (f32) hipLaunchKernelGGL((adapter_shrink<true, RT>), grid, block, 0, s, a); \
-    else hipLaunchKernelGGL((adapter_shrink<false, RT>), grid, block, 0, s, a)
     switch (rs.rt) {
-        case 1: SHRINK(1); break;
-        case 2: SHRINK(2); break;
-        case 3: SHRINK(3); break;
-        default: SHRINK(4); break;
+        case 1: return run_shrink_form<F32, TW, MT, 1>(a, tiles, rs.groups, s);
+        case 2: return run_shrink_form<F32, TW, MT, 2>(a, tiles, rs.groups, s);
+        case 3: return run_shrink_form<F32, TW, MT, 3>(a, tiles, rs.groups, s);
+        default: return run_shrink_form<F32, TW, MT, 4>(a, tiles, rs.groups, s);
     }
-#undef SHRINK
-    return hipGetLastError();
 }
-
-static hipError_t run_expand(const ExpandArgs& a, bool f32, int tiles, hipStream_t s)
+// 16 rows to a workgroup while that leaves two workgroups to a compute unit or fewer, 32 beyond (us, 16 / 32: 301 x 1152 fp32 rank 24 6.0 / 8.0, 300 x 1152 rank
+// 64 5.9 / 6.8, 64 x 1152 rank 32 4.8 / 5.2, 8192 x 1152 rank 32 8.5 / 8.4, 8191 x 2240 rank 128 40 / 32).
+template <bool F32, bool TW>
+static hipError_t run_shrink(const ShrinkArgs& a, int tiles, hipStream_t s)
 {
-    const dim3 grid(tiles, (a.width + 255) / 256), block(256);
-#define EXPAND(KS) \
-    if (f32) hipLaunchKernelGGL((adapter_expand<true, KS>), grid, block, 0, s, a); \
-    else hipLaunchKernelGGL((adapter_expand<false, KS>), grid, block, 0, s, a)
+    return (int64_t)tiles * (TILE / 16) * rank_split(a.v.rank).groups <= 2 * compute_units() ? run_shrink_ranks<F32, TW, 1>(a, tiles, s)
+                                                                                             : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
+}
+
+template <bool F32, bool TW, typename OFF>
+static void run_expand_ranks(const ExpandArgs& a, dim3 grid, hipStream_t s)
+{
     switch ((a.v.rank + 31) / 32) {
-        case 1: EXPAND(1); break;
-        case 2: EXPAND(2); break;
-        case 3: EXPAND(3); break;
-        default: EXPAND(4); break;
+        case 1: hipLaunchKernelGGL((adapter_expand<F32, TW, 1, OFF>), grid, dim3(256), 0, s, a); break;
+        case 2: hipLaunchKernelGGL((adapter_expand<F32, TW, 2, OFF>), grid, dim3(256), 0, s, a); break;
+        case 3: hipLaunchKernelGGL((adapter_expand<F32, TW, 3, OFF>), grid, dim3(256), 0, s, a); break;
+        default: hipLaunchKernelGGL((adapter_expand<F32, TW, 4, OFF>), grid, dim3(256), 0, s, a); break;
     }
-#undef EXPAND
+}
+template <bool F32, bool TW>
+static hipError_t run_expand(ExpandArgs a, int tiles, hipStream_t s)
+{
+    // pieces of a workgroup: 2048 workgroups, or three pieces each where the factor's part of the work is large and 768 workgroups are left
+    const int pieces = (a.width + 127) / 128;
+    const int64_t all = (int64_t)tiles * pieces, want = all / 2048;
+    a.per = (int)(want < 1 ? 1 : want);
+    if (a.per < 3 && a.v.rank > 64 && all >= 3 * 768) a.per = 3;
+    a.per = a.per > pieces ? pieces : a.per;
+    a.unit_magic = a.v.rank > 8 ? (unsigned)((((uint64_t)1 << 32) + a.v.rank / 8 - 1) / (a.v.rank / 8)) : 0;
+    const dim3 grid((pieces + a.per - 1) / a.per, tiles);
+    // offsets of 32 bits where the last row's fit
+    const int64_t ld = a.ldyin > a.ldy ? a.ldyin : a.ldy;
+    if (((int64_t)a.v.M * ld + a.width) * (F32 ? 4 : 2) < ((int64_t)1 << 32)) run_expand_ranks<F32, TW, uint32_t>(a, grid, s);
+    else run_expand_ranks<F32, TW, int64_t>(a, grid, s);
     return hipGetLastError();
 }
 
-template <bool COLS_FIRST>
 static hipError_t run_wgrad(const WgradArgs& a, bool f32, int groups, hipStream_t s)
 {
     const RankSplit rs = rank_split(a.v.rank);
-    const dim3 grid((a.width + 127) / 128, groups, rs.groups), block(256);
-    if constexpr (COLS_FIRST) {
-        if (f32) {
-            switch (rs.rt) {
-                case 1: hipLaunchKernelGGL((adapter_wgrad<true, 1, true>), grid, block, 0, s, a); break;
-                case 2: hipLaunchKernelGGL((adapter_wgrad<true, 2, true>), grid, block, 0, s, a); break;
-                case 3: hipLaunchKernelGGL((adapter_wgrad<true, 3, true>), grid, block, 0, s, a); break;
-                default: hipLaunchKernelGGL((adapter_wgrad<true, 4, true>), grid, block, 0, s, a); break;
-            }
-            return hipGetLastError();
-        }
-    }
+    const dim3 grid((a.N + 127) / 128 + (a.K + 127) / 128, groups, rs.groups), block(256);
+#define WGRAD(RT) \
+    if (f32) hipLaunchKernelGGL((adapter_wgrad<true, RT>), grid, block, 0, s, a); \
+    else hipLaunchKernelGGL((adapter_wgrad<false, RT>), grid, block, 0, s, a)
     switch (rs.rt) {
-        case 1: hipLaunchKernelGGL((adapter_wgrad<false, 1, COLS_FIRST>), grid, block, 0, s, a); break;
-        case 2: hipLaunchKernelGGL((adapter_wgrad<false, 2, COLS_FIRST>), grid, block, 0, s, a); break;
-        case 3: hipLaunchKernelGGL((adapter_wgrad<false, 3, COLS_FIRST>), grid, block, 0, s, a); break;
-        default: hipLaunchKernelGGL((adapter_wgrad<false, 4, COLS_FIRST>), grid, block, 0, s, a); break;
+        case 1: WGRAD(1); break;
+        case 2: WGRAD(2); break;
+        case 3: WGRAD(3); break;
+        default: WGRAD(4); break;
     }
+#undef WGRAD
     return hipGetLastError();
 }
 
@@ -729,9 +908,10 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
 {
     const AdapterView v = view_of(c, pool, plan, M);
     const int tiles = adapter_plan_layout(M, c->slots).tiles;
-    hipError_t e = run_shrink({v, X, (const uint16_t*)pool->A, (float*)inter, ldx, (int)c->K}, c->x_dtype == LQ_F32, tiles, s);
+    const ShrinkArgs a{v, X, (const uint16_t*)pool->A, (float*)inter, ldx, (int)c->K};
+    const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
-    return run_expand({v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy}, false, tiles, s);
+    return run_expand<false, false>({v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy}, tiles, s);
 }
 
 hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, const lq_adapter_pool* pool, const void* X, int64_t ldx,
@@ -742,23 +922,18 @@ hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, c
     const AdapterWorkLayout l = adapter_work_layout(c, M);
     const int tiles = adapter_plan_layout(M, c->slots).tiles;
     const bool f32 = c->x_dtype == LQ_F32;
-    float* dT = (float*)(work + l.off_dT);
-    uint16_t *At = (uint16_t*)(work + l.off_At), *Bt = (uint16_t*)(work + l.off_Bt);
-    float* part = (float*)(work + l.off_part);
-    hipError_t e;
-    hipLaunchKernelGGL(adapter_transpose, dim3((unsigned)((c->K + c->N) / 64), (c->rank + 63) / 64, c->slots), dim3(256), 0, s, v,
-                       (const uint16_t*)pool->A, (const uint16_t*)pool->B, At, Bt, (int)c->N, (int)c->K);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if ((e = run_shrink({v, dY, Bt, dT, lddy, (int)c->N}, false, tiles, s)) != hipSuccess) return e;
-    // dA before dX: X may be read before a caller's dX, which may be its own buffer for dXin only, is written
-    if ((e = run_wgrad<false>({v, (const float*)inter, dY, dB, part, lddy, l.part_stride, (int)c->N, l.per}, false, l.groups, s)) != hipSuccess) return e;
-    if ((e = run_wgrad<true>({v, dT, X, dA, part + (int64_t)c->rank * c->N, ldx, l.part_stride, (int)c->K, l.per}, f32, l.groups, s)) != hipSuccess) return e;
+    float *dT = (float*)(work + l.off_dT), *part = (float*)(work + l.off_part);
+    hipError_t e = run_shrink<false, true>({v, dY, (const uint16_t*)pool->B, dT, lddy, (int)c->N}, tiles, s);
+    if (e != hipSuccess) return e;
+    if ((e = run_wgrad({v, (const float*)inter, dT, dY, X, dA, dB, part, lddy, ldx, l.part_stride, (int)c->N, (int)c->K, l.per}, f32, l.groups, s)) != hipSuccess)
+        return e;
     const int64_t nb = (int64_t)c->rank * c->N / 4, na = (int64_t)c->rank * c->K / 4;
-    int64_t blocks = (nb + na + 1023) / 1024;
-    blocks = blocks > 1024 ? 1024 : blocks;
+    int64_t blocks = (nb + na + 255) / 256;
+    blocks = blocks > 2048 ? 2048 : blocks;
     hipLaunchKernelGGL(adapter_wgrad_sum, dim3((unsigned)blocks, c->slots), dim3(256), 0, s, v, part, l.part_stride, l.per, (v4f*)dB, (v4f*)dA, nb, na);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    return run_expand({v, dT, At, dXin, dX, lddxin, lddx, (int)c->K, dXin == dX && lddxin == lddx}, f32, tiles, s);
+    const ExpandArgs x{v, dT, (const uint16_t*)pool->A, dXin, dX, lddxin, lddx, (int)c->K, dXin == dX && lddxin == lddx};
+    return f32 ? run_expand<true, true>(x, tiles, s) : run_expand<false, true>(x, tiles, s);
 }
 
 hipError_t launch_adapter_zero(const lq_adapter_config* c, float* dA, float* dB, hipStream_t s)

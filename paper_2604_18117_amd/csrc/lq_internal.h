@@ -228,7 +228,6 @@ struct AdapterPlanLayout {
 AdapterPlanLayout adapter_plan_layout(int64_t M, int slots);
 struct AdapterWorkLayout {  // of the backward
     size_t off_dT;            // dY B of every row, fp32
-    size_t off_At, off_Bt;    // transposed factors
     size_t off_part;          // parts of the factors' gradients
     size_t total;
     int64_t part_stride;      // floats of a part
