@@ -98,7 +98,26 @@ __global__ void __launch_bounds__(256) adapter_plan_scan(int chunks, PlanPtrs p)
     if (threadIdx.x == 0) p.total[blockIdx.x] = run;
 }
 
-// first row and first tile of every adapter, and the tiles {first row, rows, adapter, 0} (rows 0: none); one workgroup
+// The tiles {first row, rows, adapter, 0} (rows 0: none), from first rows and first tiles in the LDS, by 1024 threads.
+__device__ __forceinline__ void write_tiles(int slots, int cap, int tiles, const int* bs, const int* tb, int4* out)
+{
+    for (int t = threadIdx.x; t < cap; t += 1024) {
+        int4 v = make_int4(0, 0, slots, 0);
+        if (t < tiles) {
+            int lo = 0, hi = slots;  // the last adapter whose first tile is at or before t has it: later ones with the same first tile have rows, earlier have none
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (tb[mid] <= t) lo = mid;
+                else hi = mid - 1;
+            }
+            const int r0 = bs[lo] + (t - tb[lo]) * TILE;
+            v = make_int4(r0, min(TILE, bs[lo + 1] - r0), lo, 0);
+        }
+        out[t] = v;
+    }
+}
+
+// first row and first tile of every adapter, and the tiles; one workgroup
 __global__ void __launch_bounds__(1024) adapter_plan_tiles(int slots, int cap, PlanPtrs p)
 {
     __shared__ int lds[16], tb[1026], bs[1026];
@@ -113,20 +132,18 @@ __global__ void __launch_bounds__(1024) adapter_plan_tiles(int slots, int cap, P
     }
     if (threadIdx.x == 0) bs[slots + 1] = p.base[slots + 1] = row, tb[slots + 1] = p.tbase[slots + 1] = tile;
     __syncthreads();
-    for (int t = threadIdx.x; t < cap; t += 1024) {
-        int4 v = make_int4(0, 0, slots, 0);
-        if (t < tile) {
-            int lo = 0, hi = slots;  // the last adapter whose first tile is at or before t has it: later ones with the same first tile have rows, earlier have none
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (tb[mid] <= t) lo = mid;
-                else hi = mid - 1;
-            }
-            const int r0 = bs[lo] + (t - tb[lo]) * TILE;
-            v = make_int4(r0, min(TILE, bs[lo + 1] - r0), lo, 0);
-        }
-        p.tiles[t] = v;
+    write_tiles(slots, cap, tile, bs, tb, p.tiles);
+}
+
+// The lanes of a wavefront (of those in `ok`) with the same adapter s < 2048: a ballot per bit of its number.
+__device__ __forceinline__ unsigned long long same_lanes(int s, bool ok, int bits)
+{
+    unsigned long long same = __ballot(ok);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long one = __ballot(s >> b & 1);
+        same &= s >> b & 1 ? one : ~one;
     }
+    return same;
 }
 
 // rows in the order of their adapters, in their own order within one: the wavefronts take turns, and a lane's place among the 64 rows of a
@@ -142,11 +159,7 @@ __global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, 
             const int m = blockIdx.x * PLAN_CHUNK + g * 64 + lane;
             const bool ok = m < M;
             const int s = ok ? slot_of(ids[m], slots) : 0;
-            unsigned long long same = __ballot(ok);
-            for (int b = 0; b < 11; ++b) {
-                const unsigned long long one = __ballot(s >> b & 1);
-                same &= s >> b & 1 ? one : ~one;
-            }
+            const unsigned long long same = same_lanes(s, ok, 11);
             const int at = next[s];
             if (ok) p.rows[at + __popcll(same & ((1ull << lane) - 1))] = m;
             // every lane has read before one writes
@@ -158,19 +171,75 @@ __global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, 
     }
 }
 
+// The whole plan in one workgroup: its 16 wavefronts take consecutive sixteenths of the batch, count their rows of each adapter (twice: for the adapters'
+// first rows, then on the way to every row's place).
+constexpr int PLAN_ONE = 8192;  // rows up to which it is taken (us, 32 adapters: 64 rows 5.1, 8192 13.7, 16384 23.3; four launches 17.3)
+__global__ void __launch_bounds__(1024) adapter_plan_one(const int* ids, int M, int slots, int bits, int cap, PlanPtrs p)
+{
+    extern __shared__ int mem[];  // first rows, first tiles (slots + 2 each), then [wavefront][adapter] counts of 16 bits
+    __shared__ int lds[16];
+    int *bs = mem, *tb = mem + slots + 2;
+    uint16_t* count = (uint16_t*)(mem + 2 * (slots + 2));
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = ((M + 1023) >> 10) << 6, m0 = w * per, m1 = min(M, m0 + per);
+    for (int o = threadIdx.x; o < 16 * (slots + 1); o += 1024) count[o] = 0;
+    __syncthreads();
+    uint16_t* mine = count + w * (slots + 1);
+    for (int m = m0; m < m1; m += 64) {
+        const bool ok = m + lane < m1;
+        const int s = ok ? slot_of(ids[m + lane], slots) : 0;
+        const unsigned long long same = same_lanes(s, ok, bits);
+        if (ok && (same >> lane) == 1) mine[s] += (uint16_t)__popcll(same);  // the last lane of each adapter
+    }
+    __syncthreads();
+    int row = 0, tile = 0;
+    for (int s0 = 0; s0 <= slots; s0 += 1024) {
+        const int s = s0 + (int)threadIdx.x;
+        int n = 0;
+        if (s <= slots)
+            for (int k = 0; k < 16; ++k) {  // counts become the rows of earlier wavefronts
+                const int c = count[k * (slots + 1) + s];
+                count[k * (slots + 1) + s] = (uint16_t)n;
+                n += c;
+            }
+        int sn, st;
+        const int b = row + block_scan(n, lds, &sn), t = tile + block_scan((n + TILE - 1) / TILE, lds, &st);
+        if (s <= slots) bs[s] = p.base[s] = b, tb[s] = p.tbase[s] = t;
+        row += sn;
+        tile += st;
+    }
+    if (threadIdx.x == 0) bs[slots + 1] = p.base[slots + 1] = row, tb[slots + 1] = p.tbase[slots + 1] = tile;
+    __syncthreads();
+    write_tiles(slots, cap, tile, bs, tb, p.tiles);
+    for (int m = m0; m < m1; m += 64) {
+        const bool ok = m + lane < m1;
+        const int s = ok ? slot_of(ids[m + lane], slots) : 0;
+        const unsigned long long same = same_lanes(s, ok, bits);
+        const int at = mine[s];
+        if (ok) p.rows[bs[s] + at + __popcll(same & ((1ull << lane) - 1))] = m + lane;
+        // every lane has read before one writes
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (ok && (same >> lane) == 1) mine[s] = (uint16_t)(at + __popcll(same));
+    }
+}
+
 hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t* plan, hipStream_t s)
 {
     const AdapterPlanLayout l = adapter_plan_layout(M, slots);
     const PlanPtrs p = plan_ptrs(l, plan);
-    hipError_t e;
-    if (l.chunks) {
-        hipLaunchKernelGGL(adapter_plan_count, dim3(l.chunks), dim3(256), 0, s, ids, (int)M, slots, l.chunks, p);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (M <= PLAN_ONE) {
+        int bits = 1;
+        while (slots >> bits) ++bits;
+        hipLaunchKernelGGL(adapter_plan_one, dim3(1), dim3(1024), (2 * (slots + 2)) * 4 + 16 * (slots + 1) * 2, s, ids, (int)M, slots, bits, l.tiles, p);
+        return hipGetLastError();
     }
+    hipError_t e;
+    hipLaunchKernelGGL(adapter_plan_count, dim3(l.chunks), dim3(256), 0, s, ids, (int)M, slots, l.chunks, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(adapter_plan_scan, dim3(slots + 1), dim3(256), 0, s, l.chunks, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(adapter_plan_tiles, dim3(1), dim3(1024), 0, s, slots, l.tiles, p);
-    if ((e = hipGetLastError()) != hipSuccess || !l.chunks) return e;
+    if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(adapter_plan_rows, dim3(l.chunks), dim3(256), 0, s, ids, (int)M, slots, l.chunks, p);
     return hipGetLastError();
 }
@@ -311,13 +380,14 @@ struct ShrinkPiece {
     }
 };
 
-// A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next two
-// requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
+// A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next ones (up to four, as
+// the registers allow) requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
 template <bool F32, bool TW, int MT, int RT>
 __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
 {
     typedef ShrinkPiece<F32, TW, MT, RT> Piece;
     constexpr int PARTS = TILE / (16 * MT);  // workgroups of a tile
+    constexpr int UNITS = Piece::XL + Piece::WL, AHEAD = UNITS <= 6 ? 4 : UNITS <= 14 && !(TW && MT == 2 && RT == 4) ? 2 : 1;
     extern __shared__ v4i lds[];             // a piece per wavefront; then [wavefront][row][rank] sums
     const int4 tile = a.v.tiles[blockIdx.x / PARTS];
     const int h = (blockIdx.x % PARTS) * (16 * MT), n = min(tile.y - h, 16 * MT), rank = rank_of(a.v, tile.z), r0 = blockIdx.y * (RT * 16);
@@ -345,31 +415,19 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
         for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = v4f{0, 0, 0, 0};
     const int pieces = a.depth / 64;
     v4i* mine = lds + w * Piece::UNITS;
-    if constexpr (Piece::XL + Piece::WL <= 14 && !(TW && MT == 2 && RT == 4)) {
-        Piece p0, p1;
-        if (w < pieces) p0.fetch(xp, wp, w, a.v.rank);
-        if (w + 8 < pieces) p1.fetch(xp, wp, w + 8, a.v.rank);
-        for (int c = w; c < pieces; c += 16) {
+    Piece p[AHEAD];
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+        if (w + 8 * d < pieces) p[d].fetch(xp, wp, w + 8 * d, a.v.rank);
+    for (int c0 = w; c0 < pieces; c0 += 8 * AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            const int c = c0 + 8 * d;
+            if (c >= pieces) break;
             wave_sync();
-            p0.put(mine, lane);
+            p[d].put(mine, lane);
             wave_sync();
-            if (c + 16 < pieces) p0.fetch(xp, wp, c + 16, a.v.rank);
-            Piece::multiply(mine, i, q, acc);
-            if (c + 8 >= pieces) break;
-            wave_sync();
-            p1.put(mine, lane);
-            wave_sync();
-            if (c + 24 < pieces) p1.fetch(xp, wp, c + 24, a.v.rank);
-            Piece::multiply(mine, i, q, acc);
-        }
-    } else {  // (two would not fit the registers)
-        Piece p;
-        if (w < pieces) p.fetch(xp, wp, w, a.v.rank);
-        for (int c = w; c < pieces; c += 8) {
-            wave_sync();
-            p.put(mine, lane);
-            wave_sync();
-            if (c + 8 < pieces) p.fetch(xp, wp, c + 8, a.v.rank);
+            if (c + 8 * AHEAD < pieces) p[d].fetch(xp, wp, c + 8 * AHEAD, a.v.rank);
             Piece::multiply(mine, i, q, acc);
         }
     }
@@ -832,7 +890,7 @@ static AdapterView view_of(const lq_adapter_config* c, const lq_adapter_pool* po
 template <bool F32, bool TW, int MT, int RT>
 static hipError_t run_shrink_form(const ShrinkArgs& a, int tiles, int groups, hipStream_t s)
 {
-    const int pieces = 8 * ShrinkPiece<F32, TW, MT, RT>::UNITS * 16, sums = 8 * MT * 16 * RT * 16 * 4, lds = pieces > sums ? pieces : sums;
+    constexpr int pieces = 8 * ShrinkPiece<F32, TW, MT, RT>::UNITS * 16, sums = 8 * MT * 16 * RT * 16 * 4, lds = pieces > sums ? pieces : sums;
     const hipError_t e = allow_lds<adapter_shrink<F32, TW, MT, RT>>(lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((adapter_shrink<F32, TW, MT, RT>), dim3(tiles * (TILE / (16 * MT)), groups), dim3(512), lds, s, a);
@@ -849,13 +907,17 @@ static hipError_t run_shrink_ranks(const ShrinkArgs& a, int tiles, hipStream_t s
         default: return run_shrink_form<F32, TW, MT, 4>(a, tiles, rs.groups, s);
     }
 }
-// 16 rows to a workgroup while that leaves two workgroups to a compute unit or fewer, 32 beyond (us, 16 / 32: 301 x 1152 fp32 rank 24 6.0 / 8.0, 300 x 1152 rank
-// 64 5.9 / 6.8, 64 x 1152 rank 32 4.8 / 5.2, 8192 x 1152 rank 32 8.5 / 8.4, 8191 x 2240 rank 128 40 / 32).
+// 16 rows and 16 of the rank to a workgroup while there are compute units for all (the time is a wavefront's chain of pieces, and reading the factor through
+// few compute units), then 16 rows up to two workgroups a compute unit, then 32 (us of a forward, the three forms: 1 x 4608 -> 1152 rank 128 10.2 / 14.6 / 16.3,
+// 300 x 1152 -> 2304 rank 64 9.2 / 10.8 / 11.4, 1024 x 1152 -> 3456 rank 32 10.6 / 11.0 / 11.7, 2048 of them 15.0 / 14.2 / 14.8; the kernel alone, 8191 x 2240 rank
+// 128 - / 40 / 32).
 template <bool F32, bool TW>
 static hipError_t run_shrink(const ShrinkArgs& a, int tiles, hipStream_t s)
 {
-    return (int64_t)tiles * (TILE / 16) * rank_split(a.v.rank).groups <= 2 * compute_units() ? run_shrink_ranks<F32, TW, 1>(a, tiles, s)
-                                                                                             : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
+    const int64_t parts = a.v.M / 16 + a.v.slots + 1, cus = compute_units();  // (of 16 rows, at most)
+    const int ranks = (a.v.rank + 15) / 16;
+    if (parts * ranks <= cus) return run_shrink_form<F32, TW, 1, 1>(a, tiles, ranks, s);
+    return parts * rank_split(a.v.rank).groups <= 2 * cus ? run_shrink_ranks<F32, TW, 1>(a, tiles, s) : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
 }
 
 template <bool F32, bool TW, typename OFF>
@@ -909,9 +971,10 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
     const AdapterView v = view_of(c, pool, plan, M);
     const int tiles = adapter_plan_layout(M, c->slots).tiles;
     const ShrinkArgs a{v, X, (const uint16_t*)pool->A, (float*)inter, ldx, (int)c->K};
+    const ExpandArgs x{v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy};
     const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
-    return run_expand<false, false>({v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy}, tiles, s);
+    return run_expand<false, false>(x, tiles, s);
 }
 
 hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, const lq_adapter_pool* pool, const void* X, int64_t ldx,

@@ -494,7 +494,9 @@ static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, bo
         const int groups = 256 >> s.lanes_log2, H = heads[0] > heads[1] ? heads[0] : heads[1];
         const int64_t two = (2 * groups + H - 1) / H, share = M / 1024, most = 2048 / c->head_dim;
         s.tokens = (int)(two < share ? two : share);
-        s.tokens = s.tokens < 1 ? 1 : s.tokens > most ? (int)most : s.tokens;
+        s.tokens = s.tokens > most ? (int)most : s.tokens;
+        const int least = M > (1 << 23) ? 2 : 1;  // (a launch stays below 2^32 threads)
+        s.tokens = s.tokens < least ? least : s.tokens;
     }
     s.grid = (M + s.tokens - 1) / s.tokens;
     s.lds = s.tokens * c->head_dim / 2 * (grad ? 8 : 32) + (grad ? 4 * c->head_dim * 4 : 0);

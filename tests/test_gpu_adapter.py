@@ -178,6 +178,26 @@ def test_not_a_number_stays_in_its_row(lq):
     assert torch.isnan(Y[one]).all() and torch.isnan(dA[2]).any()
 
 
+@pytest.mark.parametrize("M,slots", [(1, 1), (63, 5), (1000, 1024), (1025, 3), (8192, 1024), (8193, 64), (20011, 1024), (40000, 2)])
+def test_plans_of_every_size(lq, M, slots):
+    """Batches on both sides of the plan's forms: every row's output is its own adapter's, with runs of one adapter and single rows mixed."""
+    g = _gen(M + slots)
+    ids = torch.randint(-1, slots, (M,), generator=g, device="cuda")
+    ids[M // 3: M // 2] = slots - 1
+    d = make(M, 64, 64, 8, slots, "bf16", seed=M, ids=ids, ranks="full", garbage=False)
+    cfg = lq.make_adapter_config(64, 64, 8, slots)
+    Y = lq.lq_adapter_fwd(cfg, lq.lq_adapter_plan(slots, d["ids"]), d["X"], *pool(d), d["Yin"])
+    A, B = d["A"].double(), d["B"].double()
+    own = ids.clamp(min=0)
+    T = (d["X"].double()[:, None, :] * A[own]).sum(-1)
+    delta = (T[:, None, :] * B[own]).sum(-1) * d["scales"].double()[own, None] * (ids >= 0)[:, None]
+    Tabs = (d["X"].double().abs()[:, None, :] * A[own].abs()).sum(-1)
+    off = ((72 * ref.U * Tabs + 2.0 ** -16 * T.abs())[:, None, :] * B[own].abs()).sum(-1) * d["scales"].double().abs()[own, None] * (1 + 30 * ref.U)
+    want = d["Yin"].double() + delta
+    off = off + 30 * ref.U * (Tabs[:, None, :] * B[own].abs()).sum(-1) * d["scales"].double().abs()[own, None] + 4 * ref.U * d["Yin"].double().abs()
+    ref.check(Y, (want, off + ref.ROUND[torch.bfloat16] * (want.abs() + off)), f"{M} rows, {slots} adapters")
+
+
 def test_empty_batch(lq):
     d = make(0, 128, 64, 8, 3, "bf16", ids=torch.zeros(0))
     Y, dX, dA, dB = run(lq, d, "bf16")
