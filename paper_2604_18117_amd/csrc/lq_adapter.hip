@@ -274,7 +274,7 @@ __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c)
 }
 
 // Column e of a block of 8 rows of 8 bf16 values, as the 8 consecutive values that a product takes.
-__device__ __forceinline__ v4i column(const v4i (&rows)[8], int e)
+__device__ __forceinline__ v4i column(const v4i* rows, int e)
 {
     v4i t;
 #pragma unroll
@@ -289,7 +289,7 @@ struct AdapterView {  // of the plan, and the pool's per-adapter numbers
     const int32_t* ranks;
     const float* scales;
     int slots, rank, rp;  // rank of the arrays, and rounded up to 16
-    int M;
+    int M, cap;           // rows; entries of `tiles`
 };
 __device__ __forceinline__ int rank_of(const AdapterView& v, int slot) { return slot < v.slots ? min(max(v.ranks[slot], 0), v.rank) : 0; }
 
@@ -319,7 +319,8 @@ __device__ __forceinline__ void wave_sync()
 template <bool F32, bool TW, int MT, int RT>
 struct ShrinkPiece {
     static constexpr int XU = F32 ? 16 : 8;            // units of a row of X
-    static constexpr int XL = MT * 16 * XU / 64, WL = TW ? 8 : RT * 16 * 8 / 64, WP = TW ? 1 : WL;
+    static constexpr int BLOCKS = (RT + 3) / 4;        // TW: blocks of 8 x 8 of a lane
+    static constexpr int XL = MT * 16 * XU / 64, WL = TW ? 8 * BLOCKS : RT * 16 * 8 / 64, WP = TW ? BLOCKS : WL;
     static constexpr int UNITS = MT * 16 * XU + RT * 16 * 8;
     v4i x[XL], w[WL];
     static __device__ __forceinline__ int place(int r, int p) { return MT * 16 * XU + r * 8 + (p ^ ((r + (r >> 3)) & 7)); }
@@ -328,7 +329,7 @@ struct ShrinkPiece {
 #pragma unroll
         for (int u = 0; u < XL; ++u) x[u] = *(const v4i*)(xp[u] + c * (XU * 16));
 #pragma unroll
-        for (int u = 0; u < WL; ++u) w[u] = TW ? *(const v4i*)(wp[0] + (c * 64 + u) * (rank * 2)) : *(const v4i*)(wp[TW ? 0 : u] + c * 128);
+        for (int u = 0; u < WL; ++u) w[u] = TW ? *(const v4i*)(wp[u / 8] + (c * 64 + u % 8) * (rank * 2)) : *(const v4i*)(wp[TW ? 0 : u] + c * 128);
     }
     __device__ __forceinline__ void put(v4i* lds, int lane) const
     {
@@ -338,9 +339,13 @@ struct ShrinkPiece {
             lds[r * XU + (p ^ (r & (XU - 1)))] = x[u];
         }
         if constexpr (TW) {
-            if (lane < 16 * RT)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) lds[place(lane % (2 * RT) * 8 + e, lane / (2 * RT))] = column(w, e);
+            for (int k = 0; k < BLOCKS; ++k) {
+                const int b = lane + 64 * k;
+                if (b < 16 * RT)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) lds[place(b % (2 * RT) * 8 + e, b / (2 * RT))] = column(w + 8 * k, e);
+            }
         } else {
 #pragma unroll
             for (int u = 0; u < WL; ++u) lds[place(u * 8 + lane / 8, lane % 8)] = w[u];
@@ -401,8 +406,11 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
     }
     // (ranks past the pool's are read from its last and not stored)
     if constexpr (TW) {
-        const int block = min(lane / (2 * RT), 7), r = min(r0 + lane % (2 * RT) * 8, a.v.rank - 8);
-        wp[0] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.depth + block * 8) * a.v.rank + r);
+#pragma unroll
+        for (int k = 0; k < Piece::BLOCKS; ++k) {
+            const int b = lane + 64 * k, block = min(b / (2 * RT), 7), r = min(r0 + b % (2 * RT) * 8, a.v.rank - 8);
+            wp[k] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.depth + block * 8) * a.v.rank + r);
+        }
     } else {
 #pragma unroll
         for (int u = 0; u < Piece::WL; ++u)
@@ -462,6 +470,7 @@ struct ExpandArgs {
     int width;
     int in_place;
     int per;              // pieces of 128 columns of a workgroup
+    unsigned runs;        // workgroups of a tile
     unsigned unit_magic;  // 2^32 / (rank / 8), rounded up; 0 for rank 8
 };
 
@@ -512,18 +521,18 @@ __device__ __forceinline__ v4i keep(v4i t, int left)
 // readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
 // TW: the factor is given as [rank][width]; a thread reads blocks of 8 x 8 and turns them on the way to the LDS.
 template <bool F32, bool TW, int KS, typename OFF>
-__global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
+__device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
 {
     constexpr int ES = F32 ? 4 : 2;
     constexpr int TERMS = F32 ? 3 : 2;
     constexpr int WL = TW ? 8 : KS * 2;       // units of 16 bytes that a thread reads of a piece of the factor: 128 * 4 KS / 256
     constexpr int BUFFERS = KS <= 2 ? 2 : 1;  // (two of the larger ones leave room for two workgroups on a compute unit, one for four)
     __shared__ v4i wl[BUFFERS][8 * KS * 64];
-    const int4 tile = a.v.tiles[blockIdx.y];
+    const int4 tile = a.v.tiles[t];
     const int n = tile.y, rank = rank_of(a.v, tile.z);
     if (n <= 0 || (rank == 0 && a.in_place)) return;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    const int c0 = blockIdx.x * a.per, c1 = min(c0 + a.per, (a.width + 127) / 128);
+    const int c0 = run * a.per, c1 = min(c0 + a.per, (a.width + 127) / 128);
     const int pr = a.v.rank / 8;  // units of a row of the factor
     const uint16_t* W = a.W + (int64_t)tile.z * a.width * a.v.rank;
     v4i wr[WL];
@@ -667,74 +676,86 @@ struct WgradArgs {
 // COLS_FIRST: the columns are the first operand (out is [rank][width], a lane's sums are consecutive columns), else the second ([width][rank]).
 template <bool F32, int RT, bool COLS_FIRST>
 __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T, const void* Q, int64_t ldq, float* whole_out, float* part, int64_t part_stride,
-                                            int width, int per, int block, v4f (*red)[8 * RT][64])
+                                            int width, int per, int block, v4f (*red)[8 * RT * 64])
 {
     constexpr int QT = F32 ? 3 : 1;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int c0 = block * 128, r0 = blockIdx.z * (RT * 16), g = blockIdx.y;
     const int col = c0 + 8 * i < width ? c0 + 8 * i : c0;  // (lanes past the width repeat the first columns and store nothing)
-    const int last = min((g + 1) * per, v.tbase[v.slots]);
-    for (int t0 = g * per; t0 < last;) {
-        const int slot = v.tiles[t0].z, s0 = v.tbase[slot], s1 = v.tbase[slot + 1], t1 = min(s1, last);
+    // the group's first and last tile and the ones beside it, requested together: mostly they say all (one adapter), and every lookup that waits for
+    // another is half a microsecond of a workgroup that lives for ten
+    const int g0 = g * per, g1 = min(g0 + per, v.cap);
+    const int before = g0 > 0 ? v.tiles[g0 - 1].z : -1, after = g1 < v.cap ? v.tiles[g1].z : -1, with = v.tbase[v.slots];
+    int4 first = v.tiles[g0];
+    const int4 end = v.tiles[g1 - 1];
+    const int last = min(g1, with);
+    for (int t0 = g0; t0 < last;) {
+        const int slot = first.z;
+        const int t1 = end.z == slot ? g1 : min(v.tbase[slot + 1], last);
         v4f acc[8][RT];
 #pragma unroll
         for (int c = 0; c < 8; ++c)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) acc[c][rt] = v4f{0, 0, 0, 0};
-        // steps of 32 rows, two to a tile, dealt to the wavefronts; the next step's rows are looked up, and Q requested, under the products of this one
-        const int steps = 2 * (t1 - t0);
+        // Steps of 32 rows of the plan, dealt to the wavefronts.  Under the products of one, Q and T of the next are requested, and the rows of the one
+        // after are looked up: a step that began with its own lookups took three dependent round trips.
+        const int4 final = t1 == g1 ? end : v.tiles[t1 - 1];
+        const int p0 = first.x, p1 = final.x + final.y, steps = (p1 - p0 + 31) / 32;
         v4i qn[8][F32 ? 2 : 1];
-        int pn = 0, left_n = 0;  // first row of the plan, and how many rows the lane's 8 have
-        int64_t rows_n[8];
+        float tn[RT][8];
+        int rows_n[8];
         auto look = [&](int st) {
-            const int4 tile = v.tiles[t0 + min(st, steps - 1) / 2];
-            const int h = (min(st, steps - 1) & 1) * 32 + q * 8;
-            left_n = st < steps ? tile.y - h : 0;
-            pn = tile.x + h;
+            typedef int v4u __attribute__((ext_vector_type(4), aligned(4)));
+            const int at = p0 + st * 32 + q * 8;  // (up to 31 past the adapter's last, inside the plan)
+            if (st < steps) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) rows_n[j] = v.rows[j < left_n ? pn + j : tile.x];
+                for (int u = 0; u < 2; ++u) {
+                    const v4u r = *(const v4u*)(v.rows + at + 4 * u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) rows_n[4 * u + e] = r[e];
+                }
+            }
         };
-        auto request = [&] {
+        auto request = [&](int st) {
+            const int at = p0 + st * 32 + q * 8;
+            const int first = v.rows[p0];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                const int64_t row = at + j < p1 ? rows_n[j] : first;
                 if constexpr (F32) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + rows_n[j] * ldq + col))[u];
+                    for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + row * ldq + col))[u];
                 } else {
-                    qn[j][0] = *(const v4i*)((const uint16_t*)Q + rows_n[j] * ldq + col);
+                    qn[j][0] = *(const v4i*)((const uint16_t*)Q + row * ldq + col);
                 }
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) tn[rt][j] = T[(int64_t)min(at + j, p1 - 1) * v.rp + min(r0 + rt * 16 + i, v.rp - 1)];
             }
         };
         if (w < steps) {
             look(w);
-            request();
+            request(w);
+            look(w + 4);
         }
         for (int st = w; st < steps; st += 4) {
-            v4i qr[8][F32 ? 2 : 1];
+            const int left = p1 - (p0 + st * 32 + q * 8);
+            // rows past the adapter's last: zeros on both sides (what stands in for them must not reach the sums through an infinity of its own)
+            v4i qr[8][F32 ? 2 : 1], tt[RT][3];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
-            const int left = left_n, pos = pn;
-            float tv[RT][8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) tv[rt][j] = T[(int64_t)(j < left ? pos + j : 0) * v.rp + min(r0 + rt * 16 + i, v.rp - 1)];
-            look(st + 4);
-            v4i tt[RT][3];
+                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = j < left ? qn[j][u] : v4i{0, 0, 0, 0};
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
+                float t[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) tv[rt][j] = j < left ? tv[rt][j] : 0.0f;
-                split8<3>(tv[rt], tt[rt]);
+                for (int j = 0; j < 8; ++j) t[j] = j < left ? tn[rt][j] : 0.0f;
+                split8<3>(t, tt[rt]);
             }
-            // (rows past the adapter's last: the row that stands in for them must not reach the sums through an infinity of its own, 0 * inf)
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = j < left ? qr[j][u] : v4i{0, 0, 0, 0};
-            if (st + 4 < steps) request();
+            if (st + 4 < steps) {
+                request(st + 4);
+                look(st + 8);
+            }
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 v4i qt[QT];
@@ -759,88 +780,109 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                                 acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
             }
         }
-        // wavefronts 2 and 3 to 0 and 1, then 1 to 0 (those that had steps)
+        // the wavefronts' sums, in their order: each adds up and stores a quarter of the columns (product c: columns 8 i + c)
+        const int waves = min(steps, 4);
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                if (w < waves) red[w][(c * RT + rt) * 64 + lane] = acc[c][rt];
+        const int rank = rank_of(v, slot);
+        const float s = v.scales[slot];
+        const bool whole = (t0 > g0 || before != slot) && (t1 < g1 || after != slot);
+        float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(2 * g + (t0 > g0)) * part_stride;
         __syncthreads();
-#pragma unroll
-        for (int d = 2; d >= 1; d >>= 1) {
-            if (w >= d && w < 2 * d && w < steps)
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) red[w - d][c * RT + rt][lane] = acc[c][rt];
-            __syncthreads();
-            if (w < d && w + d < steps)
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) acc[c][rt] += red[w][c * RT + rt][lane];
-            __syncthreads();
-        }
-        if (w == 0) {
-            const int rank = rank_of(v, slot);
-            const float s = v.scales[slot];
-            const bool whole = s0 >= g * per && s1 <= (g + 1) * per;
-            float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(2 * g + (s0 > g * per)) * part_stride;
+        if constexpr (COLS_FIRST) {  // 2 columns and 16 consecutive ranks' rows: lane (i, q) has rank i, columns 8 (4 q + e) + c
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                if constexpr (COLS_FIRST) {
-                    const int r = r0 + rt * 16 + i;
+                v4f t[2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int k = c0 + 8 * (q * 4 + e);
-                        if (r < v.rank && k < width)
+                for (int u = 0; u < 2; ++u) {
+                    t[u] = red[0][((2 * w + u) * RT + rt) * 64 + lane];
+                    for (int k = 1; k < waves; ++k) t[u] += red[k][((2 * w + u) * RT + rt) * 64 + lane];
+                }
+                const int r = r0 + rt * 16 + i;
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                v4f o;
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) o[c] = r < rank ? acc[4 * u + c][rt][e] * s : 0.0f;
-                                *(v4f*)(out + (int64_t)r * width + k + 4 * u) = o;
-                            }
-                    }
-                } else {
-                    const int r = r0 + rt * 16 + q * 4;
-                    if (r < v.rank && c0 + 8 * i < width)
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            v4f o;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = r + e < rank ? acc[c][rt][e] * s : 0.0f;
-                            *(v4f*)(out + (int64_t)(c0 + 8 * i + c) * v.rank + r) = o;
-                        }
+                for (int e = 0; e < 4; ++e) {
+                    const int k = c0 + 8 * (q * 4 + e) + 2 * w;
+                    typedef float v2f __attribute__((ext_vector_type(2)));
+                    if (r < v.rank && k < width) *(v2f*)(out + (int64_t)r * width + k) = r < rank ? v2f{t[0][e] * s, t[1][e] * s} : v2f{0, 0};
                 }
             }
+        } else {  // lane (i, q) has columns 8 i + c, ranks 4 q ..
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    v4f t = red[0][((2 * w + u) * RT + rt) * 64 + lane];
+                    for (int k = 1; k < waves; ++k) t += red[k][((2 * w + u) * RT + rt) * 64 + lane];
+                    const int r = r0 + rt * 16 + q * 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[e] = r + e < rank ? t[e] * s : 0.0f;
+                    if (r < v.rank && c0 + 8 * i < width) *(v4f*)(out + (int64_t)(c0 + 8 * i + 2 * w + u) * v.rank + r) = t;
+                }
         }
         t0 = t1;
+        if (t0 < last) {
+            first = v.tiles[t0];
+            __syncthreads();
+        }
     }
 }
 
 // dB = s dY^T T and dA = (s dY B)^T X in one launch, 128 columns of dY or X and 16 * RT of the rank to a workgroup.  The tiles of the plan are dealt
 // to groups of `per`; an adapter that lies within a group is finished there, one that does not leaves a part in each (2 g where it has the group's
-// first tile, 2 g + 1 where it starts within), which adapter_wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
+// first tile, 2 g + 1 where it starts within), which wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
 // a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
 // products, the c-th with columns 8 i + c.
 template <bool F32, int RT>
 __global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
 {
-    __shared__ v4f red[2][8 * RT][64];
+    __shared__ v4f red[4][8 * RT * 64];
     const int nb = (a.N + 127) / 128;
     if ((int)blockIdx.x < nb) wgrad_group<false, RT, false>(a.v, a.T, a.dY, a.lddy, a.dB, a.part, a.part_stride, a.N, a.per, blockIdx.x, red);
     else wgrad_group<F32, RT, true>(a.v, a.dT, a.X, a.ldx, a.dA, a.part + (int64_t)a.v.rank * a.N, a.part_stride, a.K, a.per, blockIdx.x - nb, red);
 }
 
-// Adapters without rows: zeros.  Adapters of more than one group: their parts in the order of the groups.  nb, na: quads of dB and dA.
-__global__ void __launch_bounds__(256) adapter_wgrad_sum(AdapterView v, const float* part, int64_t part_stride, int per, v4f* dB, v4f* dA, int64_t nb, int64_t na)
+// What adapter_wgrad leaves to do, a share of 256 quads at a time.  Adapters without rows: zeros.  Adapters of more than one group: their parts in the order
+// of the groups.  nb, na: quads of dB and dA.
+struct WgradSumArgs {
+    const float* part;
+    v4f *dB, *dA;
+    int64_t part_stride, nb, na;
+    int per, shares;  // shares of an adapter
+};
+__device__ __forceinline__ void wgrad_sum(const AdapterView& v, const WgradSumArgs& a, int slot, int share)
 {
-    const int slot = blockIdx.y, s0 = v.tbase[slot], s1 = v.tbase[slot + 1];
-    const int g0 = s0 / per, g1 = (s1 - 1) / per;
+    if (slot >= v.slots) return;
+    const int s0 = v.tbase[slot], s1 = v.tbase[slot + 1], g0 = s0 / a.per, g1 = (s1 - 1) / a.per;
     if (s0 < s1 && g0 == g1) return;
-    for (int64_t o = (int64_t)blockIdx.x * 256 + threadIdx.x; o < nb + na; o += (int64_t)gridDim.x * 256) {
+    for (int64_t o = (int64_t)share * 256 + threadIdx.x; o < a.nb + a.na; o += (int64_t)a.shares * 256) {
         v4f t = {0, 0, 0, 0};
         if (s0 < s1)
 #pragma unroll 8
-            for (int g = g0; g <= g1; ++g) t += ((const v4f*)(part + (int64_t)(2 * g + (s0 > g * per)) * part_stride))[o];
-        if (o < nb) dB[(int64_t)slot * nb + o] = t;
-        else dA[(int64_t)slot * na + o - nb] = t;
+            for (int g = g0; g <= g1; ++g) t += ((const v4f*)(a.part + (int64_t)(2 * g + (s0 > g * a.per)) * a.part_stride))[o];
+        if (o < a.nb) a.dB[(int64_t)slot * a.nb + o] = t;
+        else a.dA[(int64_t)slot * a.na + o - a.nb] = t;
+    }
+}
+
+template <bool F32, int KS, typename OFF>
+__global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
+{
+    const unsigned t = blockIdx.x / a.runs;
+    expand_tile<F32, false, KS, OFF>(a, (int)(blockIdx.x - t * a.runs), (int)t);
+}
+// The backward's last launch: dX = dXin + s dT A, and beside its tiles what is left of dA and dB.
+template <bool F32, int KS, typename OFF>
+__global__ void __launch_bounds__(256) adapter_bwd_last(ExpandArgs a, WgradSumArgs g, int tiles)
+{
+    const unsigned t = blockIdx.x / a.runs;
+    if (t < (unsigned)tiles) {
+        expand_tile<F32, true, KS, OFF>(a, (int)(blockIdx.x - t * a.runs), (int)t);
+    } else {
+        const int o = (int)(blockIdx.x - tiles * a.runs);
+        wgrad_sum(a.v, g, o / g.shares, o % g.shares);
     }
 }
 
@@ -851,13 +893,15 @@ __global__ void __launch_bounds__(256) adapter_zero(v4f* p, int64_t n)
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Ranks are dealt to workgroups in groups of up to 64.
+// Ranks are dealt to workgroups in groups of up to 64, in the factors' gradients of up to 32 (their sums are 8 times 4 registers for 16 of them; us of a
+// training step by 16, 32, 48 and 64: 3000 x 2240 -> 11200 rank 128 258 / 220 / 279 / 247, 13066 x 512 -> 768 rank 96 104 / 102 / 118 / 118).
+constexpr int WGRAD_RANKS = 2;
 struct RankSplit {
     int groups, rt;
 };
-static RankSplit rank_split(int rank)
+static RankSplit rank_split(int rank, int most = 4)
 {
-    const int tiles = (rank + 15) / 16, groups = (tiles + 3) / 4;
+    const int tiles = (rank + 15) / 16, groups = (tiles + most - 1) / most;
     return {groups, (tiles + groups - 1) / groups};
 }
 
@@ -866,9 +910,10 @@ AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
     AdapterWorkLayout l;
     const int64_t rp = (c->rank + 15) / 16 * 16;
     const int tiles = (int)(M / TILE) + c->slots + 1;
-    // groups of tiles: about 1024 workgroups over all column blocks, so that the card is full and there are few parts
-    const int64_t units = ((c->N + 127) / 128 + (c->K + 127) / 128) * rank_split(c->rank).groups;
-    int64_t groups = 1024 / units;
+    // groups of tiles: about 512 workgroups over all column blocks, two to a compute unit, so that there are few parts (us of a training step of 8192 x 1152 ->
+    // 3456 rank 32 by 256, 512, 1024: 113 / 108 / 115)
+    const int64_t units = ((c->N + 127) / 128 + (c->K + 127) / 128) * rank_split(c->rank, WGRAD_RANKS).groups;
+    int64_t groups = 512 / units;
     groups = groups < 1 ? 1 : groups;
     l.per = (int)((tiles + groups - 1) / groups);
     l.groups = (tiles + l.per - 1) / l.per;
@@ -884,7 +929,7 @@ static AdapterView view_of(const lq_adapter_config* c, const lq_adapter_pool* po
 {
     const AdapterPlanLayout l = adapter_plan_layout(M, c->slots);
     return {(const int*)(plan + l.off_rows), (const int*)(plan + l.off_tbase), (const int4*)(plan + l.off_tiles), pool->ranks, pool->scales,
-            c->slots, c->rank, (c->rank + 15) / 16 * 16, (int)M};
+            c->slots, c->rank, (c->rank + 15) / 16 * 16, (int)M, l.tiles};
 }
 
 template <bool F32, bool TW, int MT, int RT>
@@ -899,6 +944,11 @@ static hipError_t run_shrink_form(const ShrinkArgs& a, int tiles, int groups, hi
 template <bool F32, bool TW, int MT>
 static hipError_t run_shrink_ranks(const ShrinkArgs& a, int tiles, hipStream_t s)
 {
+    if constexpr (!F32 && MT == 2) {
+        // (us in one group and in two: rank 80 of 5000 x 3456 23.2 / 28.7, 96 of 8191 x 3456 42.7 / 45.3, 128 of 8191 x 2240 34.6 / 31.1)
+        if (a.v.rank > 64 && a.v.rank <= 80) return run_shrink_form<F32, TW, MT, 5>(a, tiles, 1, s);
+        if (a.v.rank > 80 && a.v.rank <= 96) return run_shrink_form<F32, TW, MT, 6>(a, tiles, 1, s);
+    }
     const RankSplit rs = rank_split(a.v.rank);
     switch (rs.rt) {
         case 1: return run_shrink_form<F32, TW, MT, 1>(a, tiles, rs.groups, s);
@@ -920,18 +970,25 @@ static hipError_t run_shrink(const ShrinkArgs& a, int tiles, hipStream_t s)
     return parts * rank_split(a.v.rank).groups <= 2 * cus ? run_shrink_ranks<F32, TW, 1>(a, tiles, s) : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
 }
 
+// sum: in the backward; NULL in the forward
+template <bool F32, bool TW, int KS, typename OFF>
+static void run_expand_form(const ExpandArgs& a, int tiles, const WgradSumArgs* sum, hipStream_t s)
+{
+    if constexpr (TW) hipLaunchKernelGGL((adapter_bwd_last<F32, KS, OFF>), dim3(tiles * a.runs + a.v.slots * sum->shares), dim3(256), 0, s, a, *sum, tiles);
+    else hipLaunchKernelGGL((adapter_expand<F32, KS, OFF>), dim3(tiles * a.runs), dim3(256), 0, s, a);
+}
 template <bool F32, bool TW, typename OFF>
-static void run_expand_ranks(const ExpandArgs& a, dim3 grid, hipStream_t s)
+static void run_expand_ranks(const ExpandArgs& a, int tiles, const WgradSumArgs* sum, hipStream_t s)
 {
     switch ((a.v.rank + 31) / 32) {
-        case 1: hipLaunchKernelGGL((adapter_expand<F32, TW, 1, OFF>), grid, dim3(256), 0, s, a); break;
-        case 2: hipLaunchKernelGGL((adapter_expand<F32, TW, 2, OFF>), grid, dim3(256), 0, s, a); break;
-        case 3: hipLaunchKernelGGL((adapter_expand<F32, TW, 3, OFF>), grid, dim3(256), 0, s, a); break;
-        default: hipLaunchKernelGGL((adapter_expand<F32, TW, 4, OFF>), grid, dim3(256), 0, s, a); break;
+        case 1: run_expand_form<F32, TW, 1, OFF>(a, tiles, sum, s); break;
+        case 2: run_expand_form<F32, TW, 2, OFF>(a, tiles, sum, s); break;
+        case 3: run_expand_form<F32, TW, 3, OFF>(a, tiles, sum, s); break;
+        default: run_expand_form<F32, TW, 4, OFF>(a, tiles, sum, s); break;
     }
 }
 template <bool F32, bool TW>
-static hipError_t run_expand(ExpandArgs a, int tiles, hipStream_t s)
+static hipError_t run_expand(ExpandArgs a, int tiles, const WgradSumArgs* sum, hipStream_t s)
 {
     // pieces of a workgroup: 2048 workgroups, or three pieces each where the factor's part of the work is large and 768 workgroups are left
     const int pieces = (a.width + 127) / 128;
@@ -940,27 +997,23 @@ static hipError_t run_expand(ExpandArgs a, int tiles, hipStream_t s)
     if (a.per < 3 && a.v.rank > 64 && all >= 3 * 768) a.per = 3;
     a.per = a.per > pieces ? pieces : a.per;
     a.unit_magic = a.v.rank > 8 ? (unsigned)((((uint64_t)1 << 32) + a.v.rank / 8 - 1) / (a.v.rank / 8)) : 0;
-    const dim3 grid((pieces + a.per - 1) / a.per, tiles);
+    a.runs = (unsigned)((pieces + a.per - 1) / a.per);
     // offsets of 32 bits where the last row's fit
     const int64_t ld = a.ldyin > a.ldy ? a.ldyin : a.ldy;
-    if (((int64_t)a.v.M * ld + a.width) * (F32 ? 4 : 2) < ((int64_t)1 << 32)) run_expand_ranks<F32, TW, uint32_t>(a, grid, s);
-    else run_expand_ranks<F32, TW, int64_t>(a, grid, s);
+    if (((int64_t)a.v.M * ld + a.width) * (F32 ? 4 : 2) < ((int64_t)1 << 32)) run_expand_ranks<F32, TW, uint32_t>(a, tiles, sum, s);
+    else run_expand_ranks<F32, TW, int64_t>(a, tiles, sum, s);
     return hipGetLastError();
 }
 
 static hipError_t run_wgrad(const WgradArgs& a, bool f32, int groups, hipStream_t s)
 {
-    const RankSplit rs = rank_split(a.v.rank);
+    const RankSplit rs = rank_split(a.v.rank, WGRAD_RANKS);
     const dim3 grid((a.N + 127) / 128 + (a.K + 127) / 128, groups, rs.groups), block(256);
 #define WGRAD(RT) \
     if (f32) hipLaunchKernelGGL((adapter_wgrad<true, RT>), grid, block, 0, s, a); \
     else hipLaunchKernelGGL((adapter_wgrad<false, RT>), grid, block, 0, s, a)
-    switch (rs.rt) {
-        case 1: WGRAD(1); break;
-        case 2: WGRAD(2); break;
-        case 3: WGRAD(3); break;
-        default: WGRAD(4); break;
-    }
+    if (rs.rt == 1) WGRAD(1);
+    else WGRAD(2);
 #undef WGRAD
     return hipGetLastError();
 }
@@ -974,7 +1027,7 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
     const ExpandArgs x{v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy};
     const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
-    return run_expand<false, false>(x, tiles, s);
+    return run_expand<false, false>(x, tiles, nullptr, s);
 }
 
 hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, const lq_adapter_pool* pool, const void* X, int64_t ldx,
@@ -990,13 +1043,10 @@ hipError_t launch_adapter_bwd(const lq_adapter_config* c, const uint8_t* plan, c
     if (e != hipSuccess) return e;
     if ((e = run_wgrad({v, (const float*)inter, dT, dY, X, dA, dB, part, lddy, ldx, l.part_stride, (int)c->N, (int)c->K, l.per}, f32, l.groups, s)) != hipSuccess)
         return e;
-    const int64_t nb = (int64_t)c->rank * c->N / 4, na = (int64_t)c->rank * c->K / 4;
-    int64_t blocks = (nb + na + 255) / 256;
-    blocks = blocks > 2048 ? 2048 : blocks;
-    hipLaunchKernelGGL(adapter_wgrad_sum, dim3((unsigned)blocks, c->slots), dim3(256), 0, s, v, part, l.part_stride, l.per, (v4f*)dB, (v4f*)dA, nb, na);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t nb = (int64_t)c->rank * c->N / 4, na = (int64_t)c->rank * c->K / 4, shares = (nb + na + 255) / 256;
+    const WgradSumArgs sum{part, (v4f*)dB, (v4f*)dA, l.part_stride, nb, na, l.per, (int)(shares > 2048 ? 2048 : shares)};
     const ExpandArgs x{v, dT, (const uint16_t*)pool->A, dXin, dX, lddxin, lddx, (int)c->K, dXin == dX && lddxin == lddx};
-    return f32 ? run_expand<true, true>(x, tiles, s) : run_expand<false, true>(x, tiles, s);
+    return f32 ? run_expand<true, true>(x, tiles, &sum, s) : run_expand<false, true>(x, tiles, &sum, s);
 }
 
 hipError_t launch_adapter_zero(const lq_adapter_config* c, float* dA, float* dB, hipStream_t s)

@@ -540,11 +540,9 @@ static lq_status adapter_check(const lq_adapter_config* c)
     if ((int64_t)c->slots * c->rank * (c->N + c->K) >= ((int64_t)1 << 32)) return LQ_ERR_UNSUPPORTED;  // (launches stay below 2^32 threads)
     return LQ_OK;
 }
-static lq_status adapter_batch_check(const lq_adapter_config* c, int64_t M)
+static lq_status adapter_batch_check(int64_t M)
 {
-    if (M < 0 || M > (1 << 24)) return LQ_ERR_SHAPE;
-    const int64_t wide = ((c->N > c->K ? c->N : c->K) + 255) / 256;  // a workgroup of 256 threads per tile and 256 columns
-    return (M / 64 + c->slots + 1) * wide * 256 >= ((int64_t)1 << 32) ? LQ_ERR_UNSUPPORTED : LQ_OK;
+    return M < 0 || M > (1 << 24) ? LQ_ERR_SHAPE : LQ_OK;
 }
 // rows of `len` values of `elem` bytes
 static lq_status rows_check(const void* p, int64_t ld, int64_t len, int elem)
@@ -582,7 +580,7 @@ lq_status lq_adapter_sizes(const lq_adapter_config* cfg, int64_t M, size_t* inte
 {
     lq_status st = adapter_check(cfg);
     if (st != LQ_OK) return st;
-    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if ((st = adapter_batch_check(M)) != LQ_OK) return st;
     if (inter_bytes) *inter_bytes = adapter_inter_bytes(cfg, M);
     if (work_bytes) *work_bytes = adapter_work_layout(cfg, M).total;
     return LQ_OK;
@@ -594,7 +592,7 @@ lq_status lq_adapter_fwd(const lq_adapter_config* cfg, const void* plan, size_t 
 {
     lq_status st = adapter_check(cfg);
     if (st != LQ_OK) return st;
-    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if ((st = adapter_batch_check(M)) != LQ_OK) return st;
     if (M == 0) return LQ_OK;  // an empty batch
     if (!plan || !X || !Yin || !Y || !inter) return LQ_ERR_NULL;
     if ((st = pool_check(pool)) != LQ_OK) return st;
@@ -615,7 +613,7 @@ lq_status lq_adapter_bwd(const lq_adapter_config* cfg, const void* plan, size_t 
 {
     lq_status st = adapter_check(cfg);
     if (st != LQ_OK) return st;
-    if ((st = adapter_batch_check(cfg, M)) != LQ_OK) return st;
+    if ((st = adapter_batch_check(M)) != LQ_OK) return st;
     if (!dA || !dB) return LQ_ERR_NULL;
     if (!aligned(dA, 16) || !aligned(dB, 16)) return LQ_ERR_ALIGN;
     if (M == 0) return launch_adapter_zero(cfg, dA, dB, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;

@@ -55,9 +55,8 @@ def test_adapter_configuration(call, field, value, status):
     assert lq.raw().lq_adapter_sizes(C.byref(cfg), 10, C.byref(n), None) == want
 
 
-def test_adapter_pools_and_batches_beyond_a_launch():
+def test_adapter_pools_beyond_a_launch():
     assert _fwd(_acfg(N=1 << 22, K=1 << 22, rank=128, slots=16), M=0) == lq.LQ_ERR_UNSUPPORTED
-    assert _fwd(_acfg(N=1 << 22, rank=8, slots=1), M=1 << 24) == lq.LQ_ERR_UNSUPPORTED
     assert _fwd(M=-1) == lq.LQ_ERR_SHAPE and _bwd(M=(1 << 24) + 1) == lq.LQ_ERR_SHAPE
 
 
@@ -280,7 +279,7 @@ def test_nothing_is_launched_after_a_failed_launch(run, name, args):
 
 def test_launches_stay_below_two_to_the_32_threads(run):
     """The largest batches and pools that are not refused."""
-    jobs = [("plan", (1024, 1 << 24), -1), ("fwd", (1 << 16, 64, 128, 256, 1, 1 << 21), -1), ("bwd", (1 << 16, 1 << 16, 128, 255, 0, 1 << 20), -1),
+    jobs = [("plan", (1024, 1 << 24), -1), ("fwd", (1 << 16, 64, 128, 256, 1, 1 << 24), -1), ("fwd", (1 << 22, 1 << 22, 128, 3, 0, 1 << 24), -1), ("bwd", (1 << 22, 1 << 22, 128, 3, 1, 1 << 24), -1), ("bwd", (1 << 16, 1 << 16, 128, 255, 0, 1 << 20), -1),
             ("bwd", (1 << 18, 1 << 18, 8, 1023, 1, 1000), -1), ("bwd", (1 << 22, 64, 128, 4, 1, 1 << 14), -1), ("qk", (2048, 2048, 256, (128,), 0, 1, 1, 1 << 24), -1),
             ("qk_bwd", (1, 1, 2, (1,), 1, 1, 1, 1 << 24), -1)]
     for job, (st, names, threads) in zip(jobs, run(jobs)):
