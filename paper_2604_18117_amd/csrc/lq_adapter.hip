@@ -873,6 +873,73 @@ __global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
     const unsigned t = blockIdx.x / a.runs;
     expand_tile<F32, false, KS, OFF>(a, (int)(blockIdx.x - t * a.runs), (int)t);
 }
+// The forward's second product where adapters have few rows each (single tokens): a wavefront takes a piece of 128 columns by itself and reads its part of
+// the factor straight into the products' operands, 16 rows of the tile at a time.  The same bits as adapter_expand.
+template <int KS>
+__global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
+{
+    const unsigned at = blockIdx.x / a.runs;
+    const int4 tile = a.v.tiles[at];
+    const int n = tile.y, rank = rank_of(a.v, tile.z);
+    if (n <= 0 || (rank == 0 && a.in_place)) return;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int c = (int)(blockIdx.x - at * a.runs) * 4 + w, rows = min(128, a.width - c * 128);
+    if (rows <= 0) return;
+    const bool in = 8 * i < rows;  // (columns past the width are read from the piece's first and not stored)
+    v4i wv[8][KS];
+    if (rank > 0) {
+        const uint16_t* W = a.W + ((int64_t)tile.z * a.width + c * 128 + (in ? 8 * i : 0)) * a.v.rank;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) wv[j][ks] = *(const v4i*)(W + (int64_t)j * a.v.rank + min(ks * 32 + q * 8, a.v.rank - 8));
+    }
+    for (int h = 0; h < n; h += 16) {
+        Row8<false, int64_t> y[4];
+        int64_t out[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t row = a.v.rows[tile.x + min(h + q * 4 + e, n - 1)];
+            const int col = c * 128 + (in ? 8 * i : 0);
+            y[e].fetch((const uint8_t*)a.Yin, (row * a.ldyin + col) * 2);
+            out[e] = (row * a.ldy + col) * 2;
+        }
+        if (rank > 0) {
+            const float s = a.v.scales[tile.z];
+            const float* T = a.T + (int64_t)(tile.x + min(h + i, n - 1)) * a.v.rp;
+            v4i tt[KS][2];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                float t[8];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const v4f x = *(const v4f*)(T + min(ks * 32 + q * 8, a.v.rp - 8) + 4 * u);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
+                }
+                split8<2>(t, tt[ks]);
+            }
+            v4f acc[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                acc[j] = v4f{y[0].get(j), y[1].get(j), y[2].get(j), y[3].get(j)};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    const v4i b = rank < a.v.rank ? keep(wv[j][ks], rank - ks * 32 - q * 8) : wv[j][ks];
+                    acc[j] = mfma(tt[ks][1], b, acc[j]);
+                    acc[j] = mfma(tt[ks][0], b, acc[j]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[e].v[0][j] = (int)pack_bf16(acc[2 * j][e], acc[2 * j + 1][e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (h + q * 4 + e < n && in) y[e].store((uint8_t*)a.Y, out[e]);
+    }
+}
 // The backward's last launch: dX = dXin + s dT A, and beside its tiles what is left of dA and dB.
 template <bool F32, int KS, typename OFF>
 __global__ void __launch_bounds__(256) adapter_bwd_last(ExpandArgs a, WgradSumArgs g, int tiles)
@@ -1005,6 +1072,19 @@ static hipError_t run_expand(ExpandArgs a, int tiles, const WgradSumArgs* sum, h
     return hipGetLastError();
 }
 
+static hipError_t run_expand_few(ExpandArgs a, int tiles, hipStream_t s)
+{
+    a.runs = (unsigned)((a.width + 511) / 512);
+    const dim3 grid(tiles * a.runs), block(256);
+    switch ((a.v.rank + 31) / 32) {
+        case 1: hipLaunchKernelGGL(adapter_expand_few<1>, grid, block, 0, s, a); break;
+        case 2: hipLaunchKernelGGL(adapter_expand_few<2>, grid, block, 0, s, a); break;
+        case 3: hipLaunchKernelGGL(adapter_expand_few<3>, grid, block, 0, s, a); break;
+        default: hipLaunchKernelGGL(adapter_expand_few<4>, grid, block, 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
 static hipError_t run_wgrad(const WgradArgs& a, bool f32, int groups, hipStream_t s)
 {
     const RankSplit rs = rank_split(a.v.rank, WGRAD_RANKS);
@@ -1027,6 +1107,9 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
     const ExpandArgs x{v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy};
     const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
+    // (us of a forward, few / other form: 64 rows over 32 adapters 1152 -> 3456 rank 32 9.1 / 9.5, 300 over 64 12.0 / 13.7, 1000 over 64 rank 64 19.9 / 21.4, 16 over 16
+    // 1152 -> 4608 rank 128 12.6 / 14.7; where the other form's workgroups all fit at once it is ahead: 64 over 4 8.3 / 6.5, 1 x 4608 -> 1152 rank 128 12.6 / 10.9)
+    if (M <= 16 * (int64_t)c->slots && (int64_t)tiles * ((c->N + 127) / 128) >= 512) return run_expand_few(x, tiles, s);
     return run_expand<false, false>(x, tiles, nullptr, s);
 }
 

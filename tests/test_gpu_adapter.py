@@ -155,6 +155,26 @@ def test_rows_do_not_depend_on_each_other(lq):
         assert torch.equal(Y2, Y[pick]) and torch.equal(dX2, dX[pick]), n
 
 
+@pytest.mark.parametrize("R", [8, 40, 96, 128])
+def test_many_adapters_of_few_rows(lq, R):
+    """Enough adapters for the form with a wavefront per 128 columns (one of them with more than 16 rows, some with none), with the other form's bits."""
+    M, K, N, slots = 130, 128, 1088, 70
+    g = _gen(R)
+    ids = torch.randint(-1, slots, (M,), generator=g, device="cuda")
+    ids[:40] = 7
+    d = make(M, K, N, R, slots, "bf16", seed=R, ids=ids, pad=8)
+    cfg = lq.make_adapter_config(N, K, R, slots)
+    Y = lq.lq_adapter_fwd(cfg, lq.lq_adapter_plan(slots, d["ids"]), d["X"], *pool(d), d["Yin"])
+    ref.check(Y, ref.adapter_fwd(d["X"], d["Yin"], *pool(d), d["ids"]), "Y")
+    one = make(40, K, N, R, 8, "bf16", ids=7, garbage=False)
+    e = dict(one, X=d["X"][:40], Yin=d["Yin"][:40], A=d["A"][:8].contiguous(), B=d["B"][:8].contiguous(), ranks=d["ranks"][:8].contiguous(), scales=d["scales"][:8].contiguous())
+    alone = lq.lq_adapter_fwd(lq.make_adapter_config(N, K, R, 8), lq.lq_adapter_plan(8, one["ids"]), e["X"], *pool(e), e["Yin"])
+    assert torch.equal(alone, Y[:40])
+    inplace = _strided(d["Yin"], 8)
+    lq.lq_adapter_fwd(cfg, lq.lq_adapter_plan(slots, d["ids"]), d["X"], *pool(d), inplace, Y=inplace)
+    assert torch.equal(inplace, Y) and _untouched(inplace)
+
+
 def test_not_a_number_stays_in_its_row(lq):
     """Infinities and NaN in rows without an adapter are carried over as they are and reach nothing else; in rows with one they reach that adapter alone."""
     d = make(300, 128, 192, 24, 4, "f32", seed=6, ranks="full", garbage=False)
