@@ -667,19 +667,20 @@ struct WgradArgs {
     const float *T, *dT;   // [row of the plan][rp]
     const void *dY, *X;    // rows of N, of K values
     float *dA, *dB;        // [adapter][rank][K], [adapter][N][rank]
-    float* part;           // [2 * group + (0 | 1)][part_stride]: N x rank of dB, then rank x K of dA
+    float* part;           // [2 * group + (0 | 1)][part_stride] (groups of one tile: [group]): N x rank of dB, then rank x K of dA
     int64_t lddy, ldx, part_stride;
     int N, K, per;         // per: tiles of a group
 };
 
 // One group's part of out = s T^T Q, for 128 columns of Q and 16 * RT of the rank (see adapter_wgrad).
 // COLS_FIRST: the columns are the first operand (out is [rank][width], a lane's sums are consecutive columns), else the second ([width][rank]).
-template <bool F32, int RT, bool COLS_FIRST>
+// ALONE: a wavefront makes the sums of its block by itself, all steps; else the workgroup's four share the steps of one block and join their sums in the LDS.
+template <bool F32, int RT, bool COLS_FIRST, bool ALONE>
 __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T, const void* Q, int64_t ldq, float* whole_out, float* part, int64_t part_stride,
-                                            int width, int per, int block, v4f (*red)[8 * RT * 64])
+                                            int width, int per, int block, v4f (*red)[ALONE ? 1 : 8 * RT * 64])
 {
-    constexpr int QT = F32 ? 3 : 1;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    constexpr int QT = F32 ? 3 : 1, SHARE = ALONE ? 1 : 4;  // SHARE: wavefronts of a block
+    const int lane = threadIdx.x & 63, w = ALONE ? 0 : threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int c0 = block * 128, r0 = blockIdx.z * (RT * 16), g = blockIdx.y;
     const int col = c0 + 8 * i < width ? c0 + 8 * i : c0;  // (lanes past the width repeat the first columns and store nothing)
     // the group's first and last tile and the ones beside it, requested together: mostly they say all (one adapter), and every lookup that waits for
@@ -735,9 +736,9 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
         if (w < steps) {
             look(w);
             request(w);
-            look(w + 4);
+            look(w + SHARE);
         }
-        for (int st = w; st < steps; st += 4) {
+        for (int st = w; st < steps; st += SHARE) {
             const int left = p1 - (p0 + st * 32 + q * 8);
             // rows past the adapter's last: zeros on both sides (what stands in for them must not reach the sums through an infinity of its own)
             v4i qr[8][F32 ? 2 : 1], tt[RT][3];
@@ -752,9 +753,9 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                 for (int j = 0; j < 8; ++j) t[j] = j < left ? tn[rt][j] : 0.0f;
                 split8<3>(t, tt[rt]);
             }
-            if (st + 4 < steps) {
-                request(st + 4);
-                look(st + 8);
+            if (st + SHARE < steps) {
+                request(st + SHARE);
+                look(st + 2 * SHARE);
             }
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
@@ -780,6 +781,43 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                                 acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
             }
         }
+        const int rank = rank_of(v, slot);
+        const float s = v.scales[slot];
+        const bool whole = (t0 > g0 || before != slot) && (t1 < g1 || after != slot);
+        float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(g * (per > 1 ? 2 : 1) + (t0 > g0)) * part_stride;
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                if constexpr (COLS_FIRST) {  // lane (i, q) has rank i, columns 8 (4 q + e) + c
+                    const int r = r0 + rt * 16 + i;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int k = c0 + 8 * (q * 4 + e);
+                        if (r < v.rank && k < width)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                v4f o;
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) o[c] = r < rank ? acc[4 * u + c][rt][e] * s : 0.0f;
+                                *(v4f*)(out + (int64_t)r * width + k + 4 * u) = o;
+                            }
+                    }
+                } else {  // lane (i, q) has columns 8 i + c, ranks 4 q ..
+                    const int r = r0 + rt * 16 + q * 4;
+                    if (r < v.rank && c0 + 8 * i < width)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            v4f o;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[e] = r + e < rank ? acc[c][rt][e] * s : 0.0f;
+                            *(v4f*)(out + (int64_t)(c0 + 8 * i + c) * v.rank + r) = o;
+                        }
+                }
+            }
+            t0 = t1;
+            if (t0 < last) first = v.tiles[t0];
+            continue;
+        }
         // the wavefronts' sums, in their order: each adds up and stores a quarter of the columns (product c: columns 8 i + c)
         const int waves = min(steps, 4);
 #pragma unroll
@@ -787,10 +825,6 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
                 if (w < waves) red[w][(c * RT + rt) * 64 + lane] = acc[c][rt];
-        const int rank = rank_of(v, slot);
-        const float s = v.scales[slot];
-        const bool whole = (t0 > g0 || before != slot) && (t1 < g1 || after != slot);
-        float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(2 * g + (t0 > g0)) * part_stride;
         __syncthreads();
         if constexpr (COLS_FIRST) {  // 2 columns and 16 consecutive ranks' rows: lane (i, q) has rank i, columns 8 (4 q + e) + c
 #pragma unroll
@@ -835,13 +869,13 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 // first tile, 2 g + 1 where it starts within), which wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
 // a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
 // products, the c-th with columns 8 i + c.
-template <bool F32, int RT>
+template <bool F32, int RT, bool ALONE>
 __global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
 {
-    __shared__ v4f red[4][8 * RT * 64];
-    const int nb = (a.N + 127) / 128;
-    if ((int)blockIdx.x < nb) wgrad_group<false, RT, false>(a.v, a.T, a.dY, a.lddy, a.dB, a.part, a.part_stride, a.N, a.per, blockIdx.x, red);
-    else wgrad_group<F32, RT, true>(a.v, a.dT, a.X, a.ldx, a.dA, a.part + (int64_t)a.v.rank * a.N, a.part_stride, a.K, a.per, blockIdx.x - nb, red);
+    __shared__ v4f red[ALONE ? 1 : 4][ALONE ? 1 : 8 * RT * 64];
+    const int nb = (a.N + 127) / 128, kb = (a.K + 127) / 128, block = ALONE ? (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) : (int)blockIdx.x;
+    if (block < nb) wgrad_group<false, RT, false, ALONE>(a.v, a.T, a.dY, a.lddy, a.dB, a.part, a.part_stride, a.N, a.per, block, red);
+    else if (block < nb + kb) wgrad_group<F32, RT, true, ALONE>(a.v, a.dT, a.X, a.ldx, a.dA, a.part + (int64_t)a.v.rank * a.N, a.part_stride, a.K, a.per, block - nb, red);
 }
 
 // What adapter_wgrad leaves to do, a share of 256 quads at a time.  Adapters without rows: zeros.  Adapters of more than one group: their parts in the order
@@ -861,7 +895,7 @@ __device__ __forceinline__ void wgrad_sum(const AdapterView& v, const WgradSumAr
         v4f t = {0, 0, 0, 0};
         if (s0 < s1)
 #pragma unroll 8
-            for (int g = g0; g <= g1; ++g) t += ((const v4f*)(a.part + (int64_t)(2 * g + (s0 > g * a.per)) * a.part_stride))[o];
+            for (int g = g0; g <= g1; ++g) t += ((const v4f*)(a.part + (int64_t)(g * (a.per > 1 ? 2 : 1) + (s0 > g * a.per)) * a.part_stride))[o];
         if (o < a.nb) a.dB[(int64_t)slot * a.nb + o] = t;
         else a.dA[(int64_t)slot * a.na + o - a.nb] = t;
     }
@@ -972,6 +1006,11 @@ static RankSplit rank_split(int rank, int most = 4)
     return {groups, (tiles + groups - 1) / groups};
 }
 
+// Adapters with a step of 32 rows each, about: nothing to share out among the wavefronts, and a group for every tile (us of a training step, shared / alone: 121
+// rows over 31 adapters 256 -> 4864 rank 104 148 / 93, 231 over 25 192 -> 2560 rank 48 43 / 37, 5 over 7 3456 -> 704 rank 96 40 / 31, 368 over 21 64 -> 1728 rank 48
+// 32 / 30; with more rows, 327 over 12 384 -> 832 rank 48 24.1 / 25.7).
+static bool few_rows(int slots, int64_t M) { return M <= 24 * (int64_t)slots; }
+
 AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
 {
     AdapterWorkLayout l;
@@ -983,11 +1022,12 @@ AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
     int64_t groups = 512 / units;
     groups = groups < 1 ? 1 : groups;
     l.per = (int)((tiles + groups - 1) / groups);
+    if (few_rows(c->slots, M)) l.per = 1;
     l.groups = (tiles + l.per - 1) / l.per;
     l.part_stride = (int64_t)c->rank * (c->N + c->K);
     size_t o = 0;
     l.off_dT = o, o += align256((size_t)M * rp * 4);
-    l.off_part = o, o += l.groups > 1 ? align256((size_t)(2 * l.groups) * l.part_stride * 4) : 0;
+    l.off_part = o, o += l.groups > 1 ? align256((size_t)(l.per > 1 ? 2 * l.groups : l.groups) * l.part_stride * 4) : 0;
     l.total = o;
     return l;
 }
@@ -1088,10 +1128,14 @@ static hipError_t run_expand_few(ExpandArgs a, int tiles, hipStream_t s)
 static hipError_t run_wgrad(const WgradArgs& a, bool f32, int groups, hipStream_t s)
 {
     const RankSplit rs = rank_split(a.v.rank, WGRAD_RANKS);
-    const dim3 grid((a.N + 127) / 128 + (a.K + 127) / 128, groups, rs.groups), block(256);
+    const unsigned blocks = (a.N + 127) / 128 + (a.K + 127) / 128;
+    const bool alone = few_rows(a.v.slots, a.v.M);
+    const dim3 grid(alone ? (blocks + 3) / 4 : blocks, groups, rs.groups), block(256);
 #define WGRAD(RT) \
-    if (f32) hipLaunchKernelGGL((adapter_wgrad<true, RT>), grid, block, 0, s, a); \
-    else hipLaunchKernelGGL((adapter_wgrad<false, RT>), grid, block, 0, s, a)
+    if (f32 && alone) hipLaunchKernelGGL((adapter_wgrad<true, RT, true>), grid, block, 0, s, a); \
+    else if (f32) hipLaunchKernelGGL((adapter_wgrad<true, RT, false>), grid, block, 0, s, a); \
+    else if (alone) hipLaunchKernelGGL((adapter_wgrad<false, RT, true>), grid, block, 0, s, a); \
+    else hipLaunchKernelGGL((adapter_wgrad<false, RT, false>), grid, block, 0, s, a)
     if (rs.rt == 1) WGRAD(1);
     else WGRAD(2);
 #undef WGRAD

@@ -104,7 +104,7 @@ def compare(d, out, dxin=True, what=""):
 @pytest.mark.parametrize("M,K,N,R,slots", [
     (1, 64, 64, 8, 1), (2, 1152, 1152, 16, 4), (15, 64, 128, 24, 3), (16, 192, 320, 40, 2), (17, 128, 64, 128, 1), (63, 256, 192, 72, 6),
     (64, 320, 64, 104, 2), (65, 64, 448, 32, 1), (130, 1152, 192, 64, 64), (300, 512, 640, 48, 8), (1025, 192, 320, 16, 5), (2500, 128, 192, 80, 3),
-    (700, 64, 64, 8, 1024), (4099, 64, 128, 96, 33)])
+    (700, 64, 64, 8, 1024), (4099, 64, 128, 96, 33), (150, 192, 320, 48, 9), (24, 64, 832, 128, 1), (240, 1152, 64, 24, 10), (241, 128, 192, 16, 10)])
 def test_forward_and_backward(lq, M, K, N, R, slots, x):
     d = make(M, K, N, R, slots, x, seed=M + R)
     compare(d, run(lq, d, x), what=f"{M} x {K} -> {N} rank {R} slots {slots}")
