@@ -469,7 +469,9 @@ static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, bo
     const int P = c->pairs[0] + c->pairs[1] + c->pairs[2] + c->pairs[3], elem = c->dtype == LQ_F32 ? 4 : 2;
     const int heads[2] = {c->heads_q, c->heads_k};
     QkShape s;
-    for (s.V = 4; s.V > 1; s.V /= 2) {
+    // (bf16 halves have vectors of 8, 16 bytes an access, up to heads of 128: us, 8 / 4, 8192 tokens of 18 + 18 heads of 64 21.0 / 23.8, 16380 of 20 + 20 of 112 62.2 /
+    // 70.6; of 7 + 7 of 160 23.8 / 22.6, whose 10 vectors leave 6 of 16 lanes idle)
+    for (s.V = c->dtype == LQ_BF16 && c->pairing == LQ_PAIR_HALF && c->head_dim <= 128 ? 8 : 4; s.V > 1; s.V /= 2) {
         if (c->head_dim % (2 * s.V) || P % s.V) continue;
         int bytes = c->pairing == LQ_PAIR_HALF ? s.V * elem : 2 * s.V * elem;
         bytes = bytes > 16 ? 16 : bytes;
@@ -480,12 +482,12 @@ static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, bo
                      (!t->grad[k].p || fits(t->grad[k], heads[k], M, elem, bytes));
         if (ok) break;
     }
-    // two or three vectors to a lane, on the fewest lanes: what a turn costs beside its vectors is shared, and three fill 9 of 12 places of a
+    // two or three vectors to a lane (one of the widest), on the fewest lanes: what a turn costs beside its vectors is shared, and three fill 9 of 12 places of a
     // head of 72 where one or two fill 9 of 16
     const int vectors = c->head_dim / (2 * s.V);
     s.lanes_log2 = 0;
-    while ((3 << s.lanes_log2) < vectors) ++s.lanes_log2;
-    s.NV = vectors <= (2 << s.lanes_log2) ? 2 : 3;
+    while (((s.V == 8 ? 1 : 3) << s.lanes_log2) < vectors) ++s.lanes_log2;
+    s.NV = s.V == 8 ? 1 : vectors <= (2 << s.lanes_log2) ? 2 : 3;
     if (grad) {
         s.tokens = qk_grad_tokens(c, M);
     } else {
@@ -551,6 +553,8 @@ static void qk_run_nv(const QkArgs& a, bool norm, const QkShape& s, hipStream_t 
 template <typename T, bool HALF, bool GRAD>
 static void qk_run_v(const QkArgs& a, bool norm, const QkShape& s, hipStream_t stream)
 {
+    if constexpr (HALF && sizeof(T) == 2)
+        if (s.V == 8) return qk_run<T, 8, 1, HALF, GRAD>(a, norm, s, stream);
     if (s.V == 4) qk_run_nv<T, 4, HALF, GRAD>(a, norm, s, stream);
     else if (s.V == 2) qk_run_nv<T, 2, HALF, GRAD>(a, norm, s, stream);
     else qk_run_nv<T, 1, HALF, GRAD>(a, norm, s, stream);
