@@ -667,10 +667,15 @@ struct WgradArgs {
     const float *T, *dT;   // [row of the plan][rp]
     const void *dY, *X;    // rows of N, of K values
     float *dA, *dB;        // [adapter][rank][K], [adapter][N][rank]
-    float* part;           // [2 * group + (0 | 1)][part_stride] (groups of one tile: [group]): N x rank of dB, then rank x K of dA
+    float* part;           // [part_of()][part_stride]: N x rank of dB, then rank x K of dA
     int64_t lddy, ldx, part_stride;
     int N, K, per;         // per: tiles of a group
 };
+
+// Where group g keeps its part of an adapter's sums: 2 g where the adapter has the group's first tile, 2 g + 1 where it starts within.  With groups of one
+// tile only adapters of more than 64 rows have parts; the last tile of one may hold a single row, all before are full, so that a number made of the tile's
+// first row and of which of both it is belongs to one tile, and the batch has few (not one for every adapter of the pool).
+__device__ __forceinline__ int64_t part_of(int per, int g, bool within, int row, bool last) { return per > 1 ? 2 * g + within : row / TILE * 2 + last; }
 
 // One group's part of out = s T^T Q, for 128 columns of Q and 16 * RT of the rank (see adapter_wgrad).
 // COLS_FIRST: the columns are the first operand (out is [rank][width], a lane's sums are consecutive columns), else the second ([width][rank]).
@@ -784,7 +789,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
         const int rank = rank_of(v, slot);
         const float s = v.scales[slot];
         const bool whole = (t0 > g0 || before != slot) && (t1 < g1 || after != slot);
-        float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + (int64_t)(g * (per > 1 ? 2 : 1) + (t0 > g0)) * part_stride;
+        float* out = whole ? whole_out + (int64_t)slot * v.rank * width : part + part_of(per, g, t0 > g0, p0, after != slot) * part_stride;
         if constexpr (ALONE) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -865,8 +870,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 }
 
 // dB = s dY^T T and dA = (s dY B)^T X in one launch, 128 columns of dY or X and 16 * RT of the rank to a workgroup.  The tiles of the plan are dealt
-// to groups of `per`; an adapter that lies within a group is finished there, one that does not leaves a part in each (2 g where it has the group's
-// first tile, 2 g + 1 where it starts within), which wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
+// to groups of `per`; an adapter that lies within a group is finished there, one that does not leaves a part in each, which wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
 // a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
 // products, the c-th with columns 8 i + c.
 template <bool F32, int RT, bool ALONE>
@@ -895,7 +899,8 @@ __device__ __forceinline__ void wgrad_sum(const AdapterView& v, const WgradSumAr
         v4f t = {0, 0, 0, 0};
         if (s0 < s1)
 #pragma unroll 8
-            for (int g = g0; g <= g1; ++g) t += ((const v4f*)(a.part + (int64_t)(g * (a.per > 1 ? 2 : 1) + (s0 > g * a.per)) * a.part_stride))[o];
+            for (int g = g0; g <= g1; ++g)
+                t += ((const v4f*)(a.part + part_of(a.per, g, s0 > g * a.per, a.per > 1 ? 0 : v.tiles[g].x, g == g1) * a.part_stride))[o];
         if (o < a.nb) a.dB[(int64_t)slot * a.nb + o] = t;
         else a.dA[(int64_t)slot * a.na + o - a.nb] = t;
     }
@@ -1027,7 +1032,8 @@ AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
     l.part_stride = (int64_t)c->rank * (c->N + c->K);
     size_t o = 0;
     l.off_dT = o, o += align256((size_t)M * rp * 4);
-    l.off_part = o, o += l.groups > 1 ? align256((size_t)(l.per > 1 ? 2 * l.groups : l.groups) * l.part_stride * 4) : 0;
+    const int64_t parts = l.per > 1 ? (l.groups > 1 ? 2 * l.groups : 0) : M > TILE ? 2 * (M / TILE + 1) : 0;  // (see part_of)
+    l.off_part = o, o += align256((size_t)parts * l.part_stride * 4);
     l.total = o;
     return l;
 }

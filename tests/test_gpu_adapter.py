@@ -119,6 +119,15 @@ def test_a_full_layer(lq, x):
     compare(d, run(lq, d, x), what="full layer")
 
 
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [[65, 65, 65, 129, 1, 64, 0, 65, 193], [0, 0, 129, 0, 65, 66, 127, 128, 65, 0], [700], [64, 64, 1]])
+def test_a_few_adapters_of_a_large_pool(lq, counts, x):
+    """Adapters whose last tile holds a single row, next to each other: their gradients' parts stay apart."""
+    ids = torch.repeat_interleave(torch.arange(len(counts)) + 3, torch.tensor(counts))
+    d = make(len(ids), 128, 192, 24, 100, x, seed=sum(counts), ids=ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(1))], ranks="full")
+    compare(d, run(lq, d, x), what=f"counts {counts}")
+
+
 @pytest.mark.parametrize("rank", [8, 128])
 @pytest.mark.parametrize("ids", [-1, 0, 2, 3])
 def test_one_adapter_for_all_rows(lq, ids, rank):

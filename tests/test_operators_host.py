@@ -55,6 +55,14 @@ def test_adapter_configuration(call, field, value, status):
     assert lq.raw().lq_adapter_sizes(C.byref(cfg), 10, C.byref(n), None) == want
 
 
+def test_a_few_rows_over_a_large_pool_need_little_memory():
+    """Only adapters of more than 64 rows have parts of their gradients' sums: none here, then at most two for every 64 rows."""
+    cfg, rp = _acfg(N=1152, K=1152, rank=32, slots=1024), 32
+    part = 32 * (1152 + 1152) * 4
+    assert lq.lq_adapter_sizes(cfg, 64)[1] == 64 * rp * 4
+    assert lq.lq_adapter_sizes(cfg, 1000)[1] <= 1000 * rp * 4 + 256 + 2 * 16 * part + 256
+
+
 def test_adapter_pools_beyond_a_launch():
     assert _fwd(_acfg(N=1 << 22, K=1 << 22, rank=128, slots=16), M=0) == lq.LQ_ERR_UNSUPPORTED
     assert _fwd(M=-1) == lq.LQ_ERR_SHAPE and _bwd(M=(1 << 24) + 1) == lq.LQ_ERR_SHAPE
