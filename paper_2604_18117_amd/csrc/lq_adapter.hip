@@ -2,10 +2,14 @@
 //     Y[m] = Yin[m] + s_a (X[m] A_a^T) B_a^T ,  a = ids[m]
 // and its gradients.  A grouping of the batch (the plan) lists the rows adapter by adapter in tiles of up to 64 rows; T = X A^T is held in
 // fp32 in the order of the plan ("inter").
-//   adapter_shrink   T = X A^T        a workgroup per half tile, its wavefronts share out K and add up in the LDS
-//   adapter_expand   Y = Yin + s T B^T  a wavefront per tile and 64 columns
-//   adapter_wgrad    dB = s dY^T T, dA = (s dY B)^T X   contraction over the rows of an adapter, in groups of tiles
-// The backward runs the first two on the transposed factors (dT = dY B, dX = dXin + s dT A).  No atomics: every sum has a fixed order.
+//   forward    adapter_shrink    T = X A^T             a workgroup per 16 or 32 rows of a tile; its wavefronts share out K and add up in the LDS
+//              adapter_expand    Y = Yin + s T B^T     a workgroup per tile and a few times 128 columns (single tokens: adapter_expand_few)
+//   backward   adapter_shrink    dT = dY B
+//              adapter_wgrad     dB = s dY^T T, dA = (s dT)^T X    contraction over the rows of an adapter, in groups of tiles
+//              adapter_bwd_last  dX = dXin + s dT A as adapter_expand does it, and what is left of the sums of dA and dB
+// The products are far below the matrix unit's rate: all of it is bound by memory and latency.  The backward has the factors in the other order than
+// its products want them; they are turned in registers, 8 x 8 at a time (transposed copies beforehand cost 8 us of a step of 8192 x 1152 -> 3456).
+// No atomics on memory: every sum has a fixed order, and T and Y of a row do not depend on the other rows.
 #include "lq_internal.h"
 
 namespace lq {
@@ -18,6 +22,8 @@ constexpr int TILE = 64;          // rows of a tile
 constexpr int PLAN_CHUNK = 1024;  // rows that a workgroup of the plan's kernels sorts
 
 // ---- plan ---------------------------------------------------------------------------------
+
+// The batch sorted by adapter, stably: counts, a scan over adapters and chunks, every row to its place.  Bound by the round trips of a few launches or of one.
 
 AdapterPlanLayout adapter_plan_layout(int64_t M, int slots)
 {
@@ -387,6 +393,9 @@ struct ShrinkPiece {
 
 // A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next ones (up to four, as
 // the registers allow) requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
+// Bound by a wavefront's chain of round trips and by what a compute unit's loads bring in, rows and factor alike: us and TB/s of X, traced, 8192 x 1152 rank 32
+// 8.1 and 2.3, dY 8192 x 3456 rank 32 27 and 2.1, 8191 x 2240 rank 128 32 and 1.1; of the 27, X alone takes 20 and the factor
+// alone 16.  64 rows to a workgroup halve the factor's part and the workgroups: 9.8 for 8.5.
 template <bool F32, bool TW, int MT, int RT>
 __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
 {
@@ -519,6 +528,9 @@ __device__ __forceinline__ v4i keep(v4i t, int left)
 // read and write 256 consecutive bytes (with 16 rows in 16 lanes every 16 bytes are a cache line of their own).  The factor's 128
 // rows are read in order, too, by all four wavefronts, and go through the LDS (unit (j, ks, q, i) of 16 bytes in the order of its
 // readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
+// us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 25 and 4.5, 8191 x 11200 rank 128 94-102 and 3.6-3.9; copying the same rows by the same pattern takes 23 and 76, a plain
+// copy 23 and 70.  Three or four wavefronts a SIMD by launch bounds spill (38 -> 52); non-temporal stores save 2-3 of the 25, but Y
+// has a reader, for whom it is left in the caches.
 // TW: the factor is given as [rank][width]; a thread reads blocks of 8 x 8 and turns them on the way to the LDS.
 template <bool F32, bool TW, int KS, typename OFF>
 __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
@@ -872,7 +884,9 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 // dB = s dY^T T and dA = (s dY B)^T X in one launch, 128 columns of dY or X and 16 * RT of the rank to a workgroup.  The tiles of the plan are dealt
 // to groups of `per`; an adapter that lies within a group is finished there, one that does not leaves a part in each, which wgrad_sum adds up.  The products run over rows, of which both operands need 8 of one column in
 // a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
-// products, the c-th with columns 8 i + c.
+// products, the c-th with columns 8 i + c.  T and dT are fp32, so they go in as three bf16 terms.
+// Bound by latency: 8 rows of a step are 8 loads in flight for a wavefront, and the sums leave two wavefronts a SIMD: us and TB/s of X and dY, traced, 8192 rows of
+// 1152 and 3456, rank 32: 21-24 and 3.1-3.6; 301 rows of fp32 1152 and bf16 1152, rank 24: 6.2-7.2.
 template <bool F32, int RT, bool ALONE>
 __global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
 {
@@ -913,7 +927,8 @@ __global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
     expand_tile<F32, false, KS, OFF>(a, (int)(blockIdx.x - t * a.runs), (int)t);
 }
 // The forward's second product where adapters have few rows each (single tokens): a wavefront takes a piece of 128 columns by itself and reads its part of
-// the factor straight into the products' operands, 16 rows of the tile at a time.  The same bits as adapter_expand.
+// the factor straight into the products' operands, 16 rows of the tile at a time.  The same bits as adapter_expand.  Bound by latency: two dependent
+// round trips, tile to rows to Yin (64 rows over 32 adapters, 1152 -> 3456 rank 32: 4.1-5.0 us traced for the factors' 7 MB).
 template <int KS>
 __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 {
@@ -979,7 +994,8 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
             if (h + q * 4 + e < n && in) y[e].store((uint8_t*)a.Y, out[e]);
     }
 }
-// The backward's last launch: dX = dXin + s dT A, and beside its tiles what is left of dA and dB.
+// The backward's last launch: dX = dXin + s dT A, and beside its tiles what is left of dA and dB (a launch less).  Bound by memory: 8192 x 1152 -> 3456 rank 32 over
+// two adapters 14 us traced, 38 MB of dXin and dX and about 10 MB of parts (3.4 TB/s).
 template <bool F32, int KS, typename OFF>
 __global__ void __launch_bounds__(256) adapter_bwd_last(ExpandArgs a, WgradSumArgs g, int tiles)
 {
