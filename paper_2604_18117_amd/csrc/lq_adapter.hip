@@ -24,6 +24,8 @@ constexpr int PLAN_CHUNK = 1024;  // rows that a workgroup of the plan's kernels
 // ---- plan ---------------------------------------------------------------------------------
 
 // The batch sorted by adapter, stably: counts, a scan over adapters and chunks, every row to its place.  Bound by the round trips of a few launches or of one.
+// The rows of tile t are at 64 t of `rows`, not behind those of the tile before, so that a kernel asks for a tile and for its rows at once (what lies
+// past a tile's last row is never used).
 
 AdapterPlanLayout adapter_plan_layout(int64_t M, int slots)
 {
@@ -34,7 +36,7 @@ AdapterPlanLayout adapter_plan_layout(int64_t M, int slots)
     l.off_base = o, o += align256((size_t)(slots + 2) * 4);
     l.off_tbase = o, o += align256((size_t)(slots + 2) * 4);
     l.off_tiles = o, o += align256((size_t)l.tiles * 16);
-    l.off_rows = o, o += align256((size_t)M * 4);
+    l.off_rows = o, o += align256((size_t)l.tiles * TILE * 4);
     l.off_total = o, o += align256((size_t)(slots + 1) * 4);
     l.off_hist = o, o += align256((size_t)(slots + 1) * l.chunks * 4);
     l.total = o;
@@ -157,7 +159,7 @@ __device__ __forceinline__ unsigned long long same_lanes(int s, bool ok, int bit
 __global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, int slots, int chunks, PlanPtrs p)
 {
     __shared__ int next[1025];
-    for (int s = threadIdx.x; s <= slots; s += 256) next[s] = p.base[s] + p.hist[(size_t)s * chunks + blockIdx.x];
+    for (int s = threadIdx.x; s <= slots; s += 256) next[s] = p.tbase[s] * TILE + p.hist[(size_t)s * chunks + blockIdx.x];
     __syncthreads();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     for (int g = 0; g < PLAN_CHUNK / 64; ++g) {
@@ -221,7 +223,7 @@ __global__ void __launch_bounds__(1024) adapter_plan_one(const int* ids, int M, 
         const int s = ok ? slot_of(ids[m + lane], slots) : 0;
         const unsigned long long same = same_lanes(s, ok, bits);
         const int at = mine[s];
-        if (ok) p.rows[bs[s] + at + __popcll(same & ((1ull << lane) - 1))] = m + lane;
+        if (ok) p.rows[tb[s] * TILE + at + __popcll(same & ((1ull << lane) - 1))] = m + lane;
         // every lane has read before one writes
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -309,6 +311,10 @@ struct ShrinkArgs {
     int64_t ldx;
     int depth;
 };
+
+// The rows of a tile have to be there now: keeps their loads before what depends on the tile itself, so that one round trip brings both.
+#define TOGETHER(ROWS) \
+    _Pragma("unroll") for (int& row : ROWS) asm("" : "+v"(row))
 
 // Orders the LDS accesses of one wavefront on memory of its own (they complete in order; the compiler must not move them either).
 __device__ __forceinline__ void wave_sync()
@@ -404,13 +410,19 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
     constexpr int UNITS = Piece::XL + Piece::WL, AHEAD = UNITS <= 6 ? 4 : UNITS <= 14 && !(TW && MT == 2 && RT == 4) ? 2 : 1;
     extern __shared__ v4i lds[];             // a piece per wavefront; then [wavefront][row][rank] sums
     const int4 tile = a.v.tiles[blockIdx.x / PARTS];
-    const int h = (blockIdx.x % PARTS) * (16 * MT), n = min(tile.y - h, 16 * MT), rank = rank_of(a.v, tile.z), r0 = blockIdx.y * (RT * 16);
-    if (n <= 0 || rank == 0) return;
+    const int h = (blockIdx.x % PARTS) * (16 * MT), r0 = blockIdx.y * (RT * 16);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const uint8_t *xp[Piece::XL], *wp[Piece::WP];
+    int rows[Piece::XL];
+#pragma unroll
+    for (int u = 0; u < Piece::XL; ++u) rows[u] = a.v.rows[(int)(blockIdx.x / PARTS) * TILE + h + u * (64 / Piece::XU) + lane / Piece::XU];
+    TOGETHER(rows);
+    const int n = min(tile.y - h, 16 * MT);
+    if (n <= 0 || tile.z >= a.v.slots) return;
+    const int first = __builtin_amdgcn_readfirstlane(rows[0]);
 #pragma unroll
     for (int u = 0; u < Piece::XL; ++u) {
-        const int row = a.v.rows[tile.x + h + min(u * (64 / Piece::XU) + lane / Piece::XU, n - 1)];
+        const int row = u * (64 / Piece::XU) + lane / Piece::XU < n ? rows[u] : first;
         xp[u] = (const uint8_t*)a.X + (int64_t)row * a.ldx * (F32 ? 4 : 2) + lane % Piece::XU * 16;
     }
     // (ranks past the pool's are read from its last and not stored)
@@ -436,6 +448,8 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d)
         if (w + 8 * d < pieces) p[d].fetch(xp, wp, w + 8 * d, a.v.rank);
+    const int rank = rank_of(a.v, tile.z);
+    if (rank == 0) return;
     for (int c0 = w; c0 < pieces; c0 += 8 * AHEAD) {
 #pragma unroll
         for (int d = 0; d < AHEAD; ++d) {
@@ -541,9 +555,17 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
     constexpr int BUFFERS = KS <= 2 ? 2 : 1;  // (two of the larger ones leave room for two workgroups on a compute unit, one for four)
     __shared__ v4i wl[BUFFERS][8 * KS * 64];
     const int4 tile = a.v.tiles[t];
-    const int n = tile.y, rank = rank_of(a.v, tile.z);
-    if (n <= 0 || (rank == 0 && a.in_place)) return;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    int rows4[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rows4[e] = a.v.rows[t * TILE + w * 16 + q * 4 + e];
+    int zeroth = a.v.rows[t * TILE];
+    TOGETHER(rows4);
+    asm("" : "+v"(zeroth));
+    const int n = tile.y;
+    if (n <= 0) return;
+    const int rank = rank_of(a.v, tile.z);
+    if (rank == 0 && a.in_place) return;
     const int c0 = run * a.per, c1 = min(c0 + a.per, (a.width + 127) / 128);
     const int pr = a.v.rank / 8;  // units of a row of the factor
     const uint16_t* W = a.W + (int64_t)tile.z * a.width * a.v.rank;
@@ -568,7 +590,7 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
     const int mine = n - (w * 16 + q * 4);  // how many of them the tile has
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int row = a.v.rows[tile.x + (e < mine ? w * 16 + q * 4 + e : n - 1)];
+        const int row = e < mine ? rows4[e] : zeroth;
         yin[e] = ((OFF)row * (OFF)a.ldyin + 8 * i) * ES;
         yout[e] = ((OFF)row * (OFF)a.ldy + 8 * i) * ES;
     }
@@ -719,16 +741,17 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
         // after are looked up: a step that began with its own lookups took three dependent round trips.
         const int4 final = t1 == g1 ? end : v.tiles[t1 - 1];
         const int p0 = first.x, p1 = final.x + final.y, steps = (p1 - p0 + 31) / 32;
+        const int* rows = v.rows + (t0 * TILE - p0);  // (by place in the plan, as T)
         v4i qn[8][F32 ? 2 : 1];
         float tn[RT][8];
         int rows_n[8];
         auto look = [&](int st) {
             typedef int v4u __attribute__((ext_vector_type(4), aligned(4)));
-            const int at = p0 + st * 32 + q * 8;  // (up to 31 past the adapter's last, inside the plan)
+            const int at = p0 + st * 32 + q * 8;
             if (st < steps) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const v4u r = *(const v4u*)(v.rows + at + 4 * u);
+                    const v4u r = *(const v4u*)(rows + at + 4 * u);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) rows_n[4 * u + e] = r[e];
                 }
@@ -736,10 +759,10 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
         };
         auto request = [&](int st) {
             const int at = p0 + st * 32 + q * 8;
-            const int first = v.rows[p0];
+            const int zeroth = rows[p0];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int64_t row = at + j < p1 ? rows_n[j] : first;
+                const int64_t row = at + j < p1 ? rows_n[j] : zeroth;
                 if constexpr (F32) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + row * ldq + col))[u];
@@ -934,26 +957,33 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 {
     const unsigned at = blockIdx.x / a.runs;
     const int4 tile = a.v.tiles[at];
-    const int n = tile.y, rank = rank_of(a.v, tile.z);
-    if (n <= 0 || (rank == 0 && a.in_place)) return;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
+    const int n = tile.y;
+    if (n <= 0 || (tile.z >= a.v.slots && a.in_place)) return;
+    // the rank is another round trip: with one step of it, whose registers allow it, it is waited for behind the first loads (300 rows over 64 adapters 1152 ->
+    // 3456 rank 32 11.7 -> 11.4 us); with more the loads ahead of it take a wavefront a SIMD
+    constexpr bool LATE = KS == 1;
+    int rank = LATE ? 0 : rank_of(a.v, tile.z);
+    if (!LATE && rank == 0 && a.in_place) return;
     const int c = (int)(blockIdx.x - at * a.runs) * 4 + w, rows = min(128, a.width - c * 128);
     if (rows <= 0) return;
     const bool in = 8 * i < rows;  // (columns past the width are read from the piece's first and not stored)
     v4i wv[8][KS];
-    if (rank > 0) {
-        const uint16_t* W = a.W + ((int64_t)tile.z * a.width + c * 128 + (in ? 8 * i : 0)) * a.v.rank;
+    if (LATE || rank > 0) {
+        const uint16_t* W = a.W + ((int64_t)(tile.z < a.v.slots ? tile.z : 0) * a.width + c * 128 + (in ? 8 * i : 0)) * a.v.rank;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) wv[j][ks] = *(const v4i*)(W + (int64_t)j * a.v.rank + min(ks * 32 + q * 8, a.v.rank - 8));
     }
+    if (LATE) rank = rank_of(a.v, tile.z);
+    if (LATE && rank == 0 && a.in_place) return;
     for (int h = 0; h < n; h += 16) {
         Row8<false, int64_t> y[4];
         int64_t out[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int64_t row = a.v.rows[tile.x + min(h + q * 4 + e, n - 1)];
+            const int64_t row = a.v.rows[(int)at * TILE + min(h + q * 4 + e, n - 1)];
             const int col = c * 128 + (in ? 8 * i : 0);
             y[e].fetch((const uint8_t*)a.Yin, (row * a.ldyin + col) * 2);
             out[e] = (row * a.ldy + col) * 2;
