@@ -256,7 +256,7 @@ hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t
 
 // An fp32 number as bf16 terms, each the leading bits of what the ones before leave (cut off, so that every difference is exact): two
 // carry 16 bits of it, three all 24.
-__device__ __forceinline__ uint32_t cut(float v) { return __float_as_uint(v) & 0xFFFF0000u; }
+__device__ __forceinline__ float cut(uint32_t bits) { return __uint_as_float(bits & 0xFFFF0000u); }
 template <int TERMS>
 __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[TERMS])
 {
@@ -269,8 +269,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[TERMS])
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             // the last of two terms is rounded: 2^-17 of the value is left instead of 2^-16
-            c[j] = cut(TERMS == 2 && k == 1 ? __uint_as_float(__float_as_uint(r[j]) + 0x8000u) : r[j]);
-            r[j] -= __uint_as_float(c[j]);
+            c[j] = __float_as_uint(r[j]) + (TERMS == 2 && k == 1 ? 0x8000u : 0u);
+            if (k + 1 < TERMS) r[j] -= cut(c[j]);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) t[k][d] = (int)__builtin_amdgcn_perm(c[2 * d + 1], c[2 * d], 0x07060302u);
@@ -762,15 +762,17 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
             const int zeroth = rows[p0];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int64_t row = at + j < p1 ? rows_n[j] : zeroth;
+                // (row and stride have up to 24 and 23 bits, so that one multiplication with a product of 64 will do; a place in T's fits 32)
+                const uint64_t off = (uint64_t)(uint32_t)(at + j < p1 ? rows_n[j] : zeroth) * (uint32_t)ldq + (uint32_t)col;
                 if constexpr (F32) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + row * ldq + col))[u];
+                    for (int u = 0; u < 2; ++u) qn[j][u] = ((const v4i*)((const float*)Q + off))[u];
                 } else {
-                    qn[j][0] = *(const v4i*)((const uint16_t*)Q + row * ldq + col);
+                    qn[j][0] = *(const v4i*)((const uint16_t*)Q + off);
                 }
+                const uint32_t place = __umul24(min(at + j, p1 - 1), v.rp);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) tn[rt][j] = T[(int64_t)min(at + j, p1 - 1) * v.rp + min(r0 + rt * 16 + i, v.rp - 1)];
+                for (int rt = 0; rt < RT; ++rt) tn[rt][j] = T[place + (uint32_t)min(r0 + rt * 16 + i, v.rp - 1)];
             }
         };
         if (w < steps) {
@@ -781,18 +783,23 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
         for (int st = w; st < steps; st += SHARE) {
             const int left = p1 - (p0 + st * 32 + q * 8);
             // rows past the adapter's last: zeros on both sides (what stands in for them must not reach the sums through an infinity of its own)
+            if (st == steps - 1) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j >= left) {
+#pragma unroll
+                        for (int u = 0; u < (F32 ? 2 : 1); ++u) qn[j][u] = v4i{0, 0, 0, 0};
+#pragma unroll
+                        for (int rt = 0; rt < RT; ++rt) tn[rt][j] = 0.0f;
+                    }
+            }
             v4i qr[8][F32 ? 2 : 1], tt[RT][3];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = j < left ? qn[j][u] : v4i{0, 0, 0, 0};
+                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                float t[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = j < left ? tn[rt][j] : 0.0f;
-                split8<3>(t, tt[rt]);
-            }
+            for (int rt = 0; rt < RT; ++rt) split8<3>(tn[rt], tt[rt]);
             if (st + SHARE < steps) {
                 request(st + SHARE);
                 look(st + 2 * SHARE);
