@@ -1123,17 +1123,22 @@ static hipError_t run_shrink_ranks(const ShrinkArgs& a, int tiles, hipStream_t s
         default: return run_shrink_form<F32, TW, MT, 4>(a, tiles, rs.groups, s);
     }
 }
-// 16 rows and 16 of the rank to a workgroup while there are compute units for all (the time is a wavefront's chain of pieces, and reading the factor through
-// few compute units), then 16 rows up to two workgroups a compute unit, then 32 (us of a forward, the three forms: 1 x 4608 -> 1152 rank 128 10.2 / 14.6 / 16.3,
-// 300 x 1152 -> 2304 rank 64 9.2 / 10.8 / 11.4, 1024 x 1152 -> 3456 rank 32 10.6 / 11.0 / 11.7, 2048 of them 15.0 / 14.2 / 14.8; the kernel alone, 8191 x 2240 rank
-// 128 - / 40 / 32).
+// The three forms: (a) 16 rows and 16 of the rank to a workgroup, (b) 16 rows and up to 64 of the rank, (c) 32 rows.  The first spreads the factor over many compute units, the
+// last reads it least.  `launched`: workgroups of 16 rows and all of the rank, of which an adapter's four may have no rows but take a place (the larger forms fill a compute
+// unit).  (a) with half the compute units or fewer and one for each part with rows; not with the turned factor, of whose rows it would read 32 bytes at a time.  (b) while all
+// are there at once.  us of a forward, (a) / (b) / (c): 1 x 4608 -> 1152 rank 128 10.8 / 15.2 / 16.7, 16 over 16 adapters 1152 -> 4608 rank 128 12.5 / 13.2 / 13.9, 300 x 1152 -> 2304 rank 64 8.4 /
+// 10.1 / 10.8, 1024 x 1152 -> 3456 rank 32 10.4 / 10.9 / 11.5; 64 over 32 of it 8.7 / 8.4 / 8.9, 2048 of it 14.0 / 13.2 / 13.9, 3000 16.4 / 15.7 / 16.2; 4096 21.4 / 22.0 / 20.5, 300 over 64 11.5 / 11.4 / 10.8,
+// 100 over 100 2240 -> 2240 rank 64 25.5 / 25.2 / 18.3.  Of a training step: 128 over 16 1152 -> 1152 rank 128 37.6 / 35.1 / 35.8, 40 over 20 4608 -> 1152 rank 64 47.4 / 45.0 / 47.3, 100 over 100
+// 153 / 117 / 103.
 template <bool F32, bool TW>
 static hipError_t run_shrink(const ShrinkArgs& a, int tiles, hipStream_t s)
 {
-    const int64_t parts = a.v.M / 16 + a.v.slots + 1, cus = compute_units();  // (of 16 rows, at most)
-    const int ranks = (a.v.rank + 15) / 16;
-    if (parts * ranks <= cus) return run_shrink_form<F32, TW, 1, 1>(a, tiles, ranks, s);
-    return parts * rank_split(a.v.rank).groups <= 2 * cus ? run_shrink_ranks<F32, TW, 1>(a, tiles, s) : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
+    const int64_t parts = a.v.M / 16 + a.v.slots + 1, launched = (int64_t)tiles * (TILE / 16), cus = compute_units();  // parts: with rows, at most
+    if constexpr (!TW) {
+        const int ranks = (a.v.rank + 15) / 16;
+        if (2 * launched <= cus && parts * ranks <= cus) return run_shrink_form<F32, TW, 1, 1>(a, tiles, ranks, s);
+    }
+    return launched * rank_split(a.v.rank).groups <= cus ? run_shrink_ranks<F32, TW, 1>(a, tiles, s) : run_shrink_ranks<F32, TW, 2>(a, tiles, s);
 }
 
 // sum: in the backward; NULL in the forward
@@ -1210,8 +1215,8 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
     const ExpandArgs x{v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy};
     const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
-    // (us of a forward, few / other form: 64 rows over 32 adapters 1152 -> 3456 rank 32 9.1 / 9.5, 300 over 64 12.0 / 13.7, 1000 over 64 rank 64 19.9 / 21.4, 16 over 16
-    // 1152 -> 4608 rank 128 12.6 / 14.7; where the other form's workgroups all fit at once it is ahead: 64 over 4 8.3 / 6.5, 1 x 4608 -> 1152 rank 128 12.6 / 10.9)
+    // (us of a forward, few / other form: 64 rows over 32 adapters 1152 -> 3456 rank 32 8.7 / 9.2, 300 over 64 11.5 / 13.0, 1000 over 64 rank 64 19.8 / 21.0, 16 over 16
+    // 1152 -> 4608 rank 128 12.5 / 14.4; where the other form's workgroups all fit at once it is ahead: 64 over 4 7.8 / 6.3, 1 x 4608 -> 1152 rank 128 12.5 / 10.7)
     if (M <= 16 * (int64_t)c->slots && (int64_t)tiles * ((c->N + 127) / 128) >= 512) return run_expand_few(x, tiles, s);
     return run_expand<false, false>(x, tiles, nullptr, s);
 }
