@@ -400,7 +400,7 @@ struct ShrinkPiece {
 // A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next ones (up to four, as
 // the registers allow) requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
 // Bound by a wavefront's chain of round trips and by what a compute unit's loads bring in, rows and factor alike: us and TB/s of X, traced, 8192 x 1152 rank 32
-// 8.1 and 2.3, dY 8192 x 3456 rank 32 27 and 2.1, 8191 x 2240 rank 128 32 and 1.1; of the 27, X alone takes 20 and the factor
+// 8.0 and 2.4, dY 8192 x 3456 rank 32 26 and 2.2, 8191 x 2240 rank 128 30-34 and 1.1; of the 26, X alone takes 20 and the factor
 // alone 16.  64 rows to a workgroup halve the factor's part and the workgroups: 9.8 for 8.5.
 template <bool F32, bool TW, int MT, int RT>
 __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
@@ -542,7 +542,7 @@ __device__ __forceinline__ v4i keep(v4i t, int left)
 // read and write 256 consecutive bytes (with 16 rows in 16 lanes every 16 bytes are a cache line of their own).  The factor's 128
 // rows are read in order, too, by all four wavefronts, and go through the LDS (unit (j, ks, q, i) of 16 bytes in the order of its
 // readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
-// us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 25 and 4.5, 8191 x 11200 rank 128 94-102 and 3.6-3.9; copying the same rows by the same pattern takes 23 and 76, a plain
+// us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 25 and 4.5, 8191 x 11200 rank 128 94-106 and 3.5-3.9; copying the same rows by the same pattern takes 23 and 76, a plain
 // copy 23 and 70.  Three or four wavefronts a SIMD by launch bounds spill (38 -> 52); non-temporal stores save 2-3 of the 25, but Y
 // has a reader, for whom it is left in the caches.
 // TW: the factor is given as [rank][width]; a thread reads blocks of 8 x 8 and turns them on the way to the LDS.
@@ -958,7 +958,7 @@ __global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
 }
 // The forward's second product where adapters have few rows each (single tokens): a wavefront takes a piece of 128 columns by itself and reads its part of
 // the factor straight into the products' operands, 16 rows of the tile at a time.  The same bits as adapter_expand.  Bound by latency: two dependent
-// round trips, tile to rows to Yin (64 rows over 32 adapters, 1152 -> 3456 rank 32: 4.1-5.0 us traced for the factors' 7 MB).
+// round trips, tile to rows to Yin (64 rows over 32 adapters, 1152 -> 3456 rank 32: 4.1-4.7 us traced for the factors' 7 MB).
 template <int KS>
 __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 {
