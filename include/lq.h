@@ -350,8 +350,8 @@ lq_status lq_rot_unpack(const lq_config *cfg, const void *state, const lq_rot_vi
    Training: with dY the derivative of a loss with respect to Y, and U[m] = scale_a dY[m] B_a,
        dX[m] = dXin[m] + U[m] A_a ,   dA_a = sum of U[m]^T X[m] ,   dB_a = scale_a sum of dY[m]^T (X[m] A_a^T)   over the rows of a;
    the gradients of an adapter without rows, and of the ranks that an adapter does not have, are zero.
-   X, dX, dXin: cfg.x_dtype.  Yin, Y, dY, A, B: bf16.  The products X A^T and dY B are held in fp32; outputs are rounded once.  Where an
-   output is bf16 they enter the second product as two bf16 terms (2^-16 of the value), where it is fp32 as three (all of it).
+   X, dX, dXin: cfg.x_dtype.  Yin, Y, dY, A, B: bf16.  The products X A^T and dY B are held in fp32 and enter
+   the second product as three bf16 terms (all 24 bits); outputs are rounded once.
    Rows may come in any order; a row's result does not depend on the other rows of the batch.  In this section X, Yin, dY and dXin may hold
    infinities and NaN: they stay in their row (and in the gradients of its adapter). */
 typedef struct {

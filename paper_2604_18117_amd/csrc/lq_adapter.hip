@@ -254,23 +254,21 @@ hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t
 
 // ---- terms --------------------------------------------------------------------------------
 
-// An fp32 number as bf16 terms, each the leading bits of what the ones before leave (cut off, so that every difference is exact): two
-// carry 16 bits of it, three all 24.
+// An fp32 number as three bf16 terms, each the leading bits of what the ones before leave (cut off, so that every difference is exact): they
+// carry all 24 bits of it.  (Two, enough for the rounding of a bf16 output, lose the sum where adapter and projection cancel.)
 __device__ __forceinline__ float cut(uint32_t bits) { return __uint_as_float(bits & 0xFFFF0000u); }
-template <int TERMS>
-__device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[TERMS])
+__device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[3])
 {
     float r[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) r[j] = v[j];
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k) {
+    for (int k = 0; k < 3; ++k) {
         uint32_t c[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            // the last of two terms is rounded: 2^-17 of the value is left instead of 2^-16
-            c[j] = __float_as_uint(r[j]) + (TERMS == 2 && k == 1 ? 0x8000u : 0u);
-            if (k + 1 < TERMS) r[j] -= cut(c[j]);
+            c[j] = __float_as_uint(r[j]);
+            if (k < 2) r[j] -= cut(c[j]);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) t[k][d] = (int)__builtin_amdgcn_perm(c[2 * d + 1], c[2 * d], 0x07060302u);
@@ -382,7 +380,7 @@ struct ShrinkPiece {
                         for (int j = 0; j < 4; ++j) v[4 * h + j] = __int_as_float(r[j]);
                     }
                     v4i t[3];
-                    split8<3>(v, t);
+                    split8(v, t);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -543,17 +541,20 @@ __device__ __forceinline__ v4i keep(v4i t, int left)
 // rows are read in order, too, by all four wavefronts, and go through the LDS (unit (j, ks, q, i) of 16 bytes in the order of its
 // readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
 // us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 25 and 4.5, 8191 x 11200 rank 128 94-106 and 3.5-3.9; copying the same rows by the same pattern takes 23 and 76, a plain
-// copy 23 and 70.  Three or four wavefronts a SIMD by launch bounds spill (38 -> 52); non-temporal stores save 2-3 of the 25, but Y
+// copy 23 and 70.  Registers are held by launch bounds to what keeps four wavefronts a SIMD (rank up to 32) or three without spilling; left alone, T's third
+// terms cost one each (forward of 8192 x 3456 rank 32 36.4 -> 33.9, 8191 x 11200 rank 128 137 -> 130).  Non-temporal stores save 2-3 of the 25, but Y
 // has a reader, for whom it is left in the caches.
 // TW: the factor is given as [rank][width]; a thread reads blocks of 8 x 8 and turns them on the way to the LDS.
 template <bool F32, bool TW, int KS, typename OFF>
 __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
 {
     constexpr int ES = F32 ? 4 : 2;
-    constexpr int TERMS = F32 ? 3 : 2;
     constexpr int WL = TW ? 8 : KS * 2;       // units of 16 bytes that a thread reads of a piece of the factor: 128 * 4 KS / 256
     constexpr int BUFFERS = KS <= 2 ? 2 : 1;  // (two of the larger ones leave room for two workgroups on a compute unit, one for four)
     __shared__ v4i wl[BUFFERS][8 * KS * 64];
+    // The last term or two of T wait in the LDS where their registers would spill or cost a wavefront a SIMD (each lane reads what it wrote itself).
+    constexpr int LOW = F32 || KS < (TW ? 2 : 4) ? 0 : KS == 3 ? 2 : 1;
+    __shared__ v4i low[LOW ? LOW * KS * 256 : 1];
     const int4 tile = a.v.tiles[t];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     int rows4[4];
@@ -615,7 +616,7 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
         }
         return;
     }
-    v4i tt[KS][TERMS];
+    v4i tt[KS][3];
     {
         const float s = a.v.scales[tile.z];
         const float* T = a.T + (int64_t)(tile.x + min(w * 16 + i, n - 1)) * a.v.rp;
@@ -628,7 +629,9 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
             }
-            split8<TERMS>(t, tt[ks]);
+            split8(t, tt[ks]);
+#pragma unroll
+            for (int k = 3 - LOW; k < 3; ++k) low[((k - 3 + LOW) * KS + ks) * 256 + threadIdx.x] = tt[ks][k];
         }
     }
     // the units that no row of the factor fills (ranks that are no multiple of 32)
@@ -671,14 +674,26 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
             for (int e = 0; e < 4; ++e) o[e] = y[e];
         if (c + 1 < c1) request_y(c + 1);
         if (w * 16 >= n) continue;
+        auto multiply = [&](int j, int ks, const v4i (&t)[3]) {
+            const v4i wv = buf[(j * KS + ks) * 64 + q * 16 + (i ^ (q + 4 * ((ks + j) & 1)))];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+            for (int k = 2; k >= 0; --k) acc[j] = mfma(t[k], wv, acc[j]);
+        };
+        if constexpr (LOW > 0) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const v4i wv = buf[(j * KS + ks) * 64 + q * 16 + (i ^ (q + 4 * ((ks + j) & 1)))];
+                v4i t[3];
 #pragma unroll
-                for (int k = TERMS - 1; k >= 0; --k) acc[j] = mfma(tt[ks][k], wv, acc[j]);
+                for (int k = 0; k < 3; ++k) t[k] = k < 3 - LOW ? tt[ks][k] : low[((k - 3 + LOW) * KS + ks) * 256 + threadIdx.x];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) multiply(j, ks, t);
             }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) multiply(j, ks, tt[ks]);
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             Row8<F32, OFF> z;
@@ -799,7 +814,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 #pragma unroll
                 for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) split8<3>(tn[rt], tt[rt]);
+            for (int rt = 0; rt < RT; ++rt) split8(tn[rt], tt[rt]);
             if (st + SHARE < steps) {
                 request(st + SHARE);
                 look(st + 2 * SHARE);
@@ -811,7 +826,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                     float x[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = __int_as_float(qr[j][c / 4][c % 4]);
-                    split8<3>(x, qt);
+                    split8(x, qt);
                 } else {
                     v4i rows8[8];
 #pragma unroll
@@ -951,7 +966,7 @@ __device__ __forceinline__ void wgrad_sum(const AdapterView& v, const WgradSumAr
 }
 
 template <bool F32, int KS, typename OFF>
-__global__ void __launch_bounds__(256) adapter_expand(ExpandArgs a)
+__global__ void __launch_bounds__(256, KS == 1 ? 4 : 3) adapter_expand(ExpandArgs a)
 {
     const unsigned t = blockIdx.x / a.runs;
     expand_tile<F32, false, KS, OFF>(a, (int)(blockIdx.x - t * a.runs), (int)t);
@@ -998,7 +1013,7 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
         if (rank > 0) {
             const float s = a.v.scales[tile.z];
             const float* T = a.T + (int64_t)(tile.x + min(h + i, n - 1)) * a.v.rp;
-            v4i tt[KS][2];
+            v4i tt[KS][3];
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 float t[8];
@@ -1008,7 +1023,7 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
                 }
-                split8<2>(t, tt[ks]);
+                split8(t, tt[ks]);
             }
             v4f acc[8];
 #pragma unroll
@@ -1017,8 +1032,8 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     const v4i b = rank < a.v.rank ? keep(wv[j][ks], rank - ks * 32 - q * 8) : wv[j][ks];
-                    acc[j] = mfma(tt[ks][1], b, acc[j]);
-                    acc[j] = mfma(tt[ks][0], b, acc[j]);
+#pragma unroll
+                    for (int k = 2; k >= 0; --k) acc[j] = mfma(tt[ks][k], b, acc[j]);
                 }
             }
 #pragma unroll
@@ -1034,7 +1049,7 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 // The backward's last launch: dX = dXin + s dT A, and beside its tiles what is left of dA and dB (a launch less).  Bound by memory: 8192 x 1152 -> 3456 rank 32 over
 // two adapters 14 us traced, 38 MB of dXin and dX and about 10 MB of parts (3.4 TB/s).
 template <bool F32, int KS, typename OFF>
-__global__ void __launch_bounds__(256) adapter_bwd_last(ExpandArgs a, WgradSumArgs g, int tiles)
+__global__ void __launch_bounds__(256, (F32 ? 1 : KS == 4 && sizeof(OFF) == 8 ? 2 : 3)) adapter_bwd_last(ExpandArgs a, WgradSumArgs g, int tiles)
 {
     const unsigned t = blockIdx.x / a.runs;
     if (t < (unsigned)tiles) {
