@@ -63,7 +63,7 @@ typedef enum {
     LQ_ERR_ALIGN = 4,            /* a pointer or stride is not aligned as documented     */
     LQ_ERR_BUFFER_TOO_SMALL = 5, /* caller's buffer smaller than lq_*_sizes reports       */
     LQ_ERR_DEVICE = 6,           /* the HIP runtime rejected a launch                    */
-    LQ_ERR_STALE_BLOB = 7        /* lq_verify_blob: the blob's header belongs to another configuration, token count or layout version */
+    LQ_ERR_STALE_BLOB = 7        /* lq_verify_blob, lq_adapter_verify_plan: the blob's header belongs to another configuration, token count or layout version */
 } lq_status;
 
 typedef enum { LQ_BLOB_PACKED = 1, LQ_BLOB_ACT = 2 } lq_blob_kind;
@@ -375,6 +375,11 @@ typedef struct {        /* device memory of the caller                          
    1024, 0 <= M <= 2^24.  plan: device, 256-byte aligned, at least plan_bytes of lq_adapter_plan_sizes (host-only). */
 lq_status lq_adapter_plan_sizes(int64_t M, int32_t slots, size_t *plan_bytes);
 lq_status lq_adapter_plan(int32_t slots, const int32_t *ids, int64_t M, void *plan, size_t plan_bytes, void *stream);
+
+/* A plan starts with a header that holds M and slots.  The host side of the calls below does not read it (that would synchronise); their kernels do, and a call whose M
+   or pool's slots are not the plan's, or that is given memory in which no plan was made, writes nothing.  This is the explicit check: it copies the header to the
+   host and therefore SYNCHRONISES `stream`.  LQ_ERR_STALE_BLOB for anything but a plan of M rows and `slots` adapters. */
+lq_status lq_adapter_verify_plan(int32_t slots, int64_t M, const void *plan, size_t plan_bytes, void *stream);
 
 /* Bytes of `inter` (X A^T of every row in fp32: forward's workspace, which the backward of the same batch reads) and of the
    backward's workspace `work`; either pointer may be NULL.  Host-only. */

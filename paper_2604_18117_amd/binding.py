@@ -121,7 +121,7 @@ EXPORTS = ["lq_status_string", "lq_packed_sizes", "lq_pack_weights", "lq_verify_
            "lq_linear_lowrank_fwd", "lq_handoff_sizes", "lq_linear_lowrank_fwd_handoff", "lq_branch_from_codes",
            "lq_unpack_weights", "lq_unpack_act", "lq_calib_sizes", "lq_calib_init", "lq_calib_step",
            "lq_calib_unpack", "lq_rot_sizes", "lq_rot_init", "lq_rot_step", "lq_rot_step_static", "lq_rot_apply", "lq_rot_unpack",
-           "lq_adapter_plan_sizes", "lq_adapter_plan", "lq_adapter_sizes", "lq_adapter_fwd", "lq_adapter_bwd",
+           "lq_adapter_plan_sizes", "lq_adapter_plan", "lq_adapter_verify_plan", "lq_adapter_sizes", "lq_adapter_fwd", "lq_adapter_bwd",
            "lq_qk_norm_rope_fwd", "lq_qk_work_sizes", "lq_qk_norm_rope_bwd"]
 
 _lib.lq_calib_sizes.argtypes = [C.POINTER(lq_config), C.POINTER(C.c_size_t)]
@@ -158,6 +158,7 @@ _lib.lq_unpack_weights.argtypes = [C.POINTER(lq_config), C.c_void_p, C.POINTER(l
 _lib.lq_unpack_act.argtypes = [C.POINTER(lq_config), C.c_void_p, C.c_int64, C.POINTER(lq_act_view), C.c_void_p]
 _lib.lq_adapter_plan_sizes.argtypes = [C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
 _lib.lq_adapter_plan.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_adapter_verify_plan.argtypes = [C.c_int32, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lq_adapter_sizes.argtypes = [C.POINTER(lq_adapter_config), C.c_int64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]
 _lib.lq_adapter_fwd.argtypes = [C.POINTER(lq_adapter_config), C.c_void_p, C.c_size_t, C.POINTER(lq_adapter_pool), C.c_void_p, C.c_int64, C.c_void_p,
                                 C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -603,6 +604,11 @@ def lq_adapter_plan(slots: int, ids: torch.Tensor, plan: Optional[torch.Tensor] 
         plan = torch.empty(lq_adapter_plan_sizes(ids.shape[0], slots), dtype=torch.uint8, device=ids.device)
     _check(_lib.lq_adapter_plan(slots, _ptr(ids), ids.shape[0], _ptr(_blob_arg(plan)), plan.numel(), _stream()), "lq_adapter_plan")
     return plan
+
+
+def lq_adapter_verify_plan(slots: int, M: int, plan: torch.Tensor) -> None:
+    """Raises LqError(LQ_ERR_STALE_BLOB) when `plan` is not one of M rows over `slots` adapters.  Synchronises the stream."""
+    _check(_lib.lq_adapter_verify_plan(slots, M, _ptr(_blob_arg(plan)), plan.numel(), _stream()), "lq_adapter_verify_plan")
 
 
 def _adapter_x_dtype(cfg: lq_adapter_config):

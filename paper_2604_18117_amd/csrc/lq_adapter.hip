@@ -32,7 +32,7 @@ AdapterPlanLayout adapter_plan_layout(int64_t M, int slots)
     AdapterPlanLayout l;
     l.chunks = (int)((M + PLAN_CHUNK - 1) / PLAN_CHUNK);
     l.tiles = (int)(M / TILE) + slots + 1;  // every adapter, and the rows without one, may leave one tile that is not full
-    size_t o = 0;
+    size_t o = BLOB_HEADER;
     l.off_base = o, o += align256((size_t)(slots + 2) * 4);
     l.off_tbase = o, o += align256((size_t)(slots + 2) * 4);
     l.off_tiles = o, o += align256((size_t)l.tiles * 16);
@@ -44,21 +44,23 @@ AdapterPlanLayout adapter_plan_layout(int64_t M, int slots)
 }
 
 struct PlanPtrs {
+    uint32_t* head;
     int *base, *tbase, *rows, *total, *hist;
     int4* tiles;
 };
 static PlanPtrs plan_ptrs(const AdapterPlanLayout& l, uint8_t* p)
 {
-    return {(int*)(p + l.off_base), (int*)(p + l.off_tbase), (int*)(p + l.off_rows), (int*)(p + l.off_total), (int*)(p + l.off_hist),
+    return {(uint32_t*)p, (int*)(p + l.off_base), (int*)(p + l.off_tbase), (int*)(p + l.off_rows), (int*)(p + l.off_total), (int*)(p + l.off_hist),
             (int4*)(p + l.off_tiles)};
 }
 
 __device__ __forceinline__ int slot_of(int id, int slots) { return (unsigned)id < (unsigned)slots ? id : slots; }
 
-// rows of each adapter in each chunk of the batch; hist is [adapter][chunk]
+// rows of each adapter in each chunk of the batch; hist is [adapter][chunk].  The plan is nobody's until the last of its kernels has run.
 __global__ void __launch_bounds__(256) adapter_plan_count(const int* ids, int M, int slots, int chunks, PlanPtrs p)
 {
     __shared__ int h[1025];
+    write_tag(p.head, BlobTag{});
     for (int s = threadIdx.x; s <= slots; s += 256) h[s] = 0;
     __syncthreads();
     const int m0 = blockIdx.x * PLAN_CHUNK;
@@ -156,9 +158,10 @@ __device__ __forceinline__ unsigned long long same_lanes(int s, bool ok, int bit
 
 // rows in the order of their adapters, in their own order within one: the wavefronts take turns, and a lane's place among the 64 rows of a
 // turn is the number of lower lanes with the same adapter (a ballot per bit of its number)
-__global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, int slots, int chunks, PlanPtrs p)
+__global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, int slots, int chunks, PlanPtrs p, BlobTag tag)
 {
     __shared__ int next[1025];
+    write_tag(p.head, tag);
     for (int s = threadIdx.x; s <= slots; s += 256) next[s] = p.tbase[s] * TILE + p.hist[(size_t)s * chunks + blockIdx.x];
     __syncthreads();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
@@ -182,8 +185,9 @@ __global__ void __launch_bounds__(256) adapter_plan_rows(const int* ids, int M, 
 // The whole plan in one workgroup: its 16 wavefronts take consecutive sixteenths of the batch, count their rows of each adapter (twice: for the adapters'
 // first rows, then on the way to every row's place).
 constexpr int PLAN_ONE = 8192;  // rows up to which it is taken (us, 32 adapters: 64 rows 5.1, 8192 13.7, 16384 23.3; four launches 17.3)
-__global__ void __launch_bounds__(1024) adapter_plan_one(const int* ids, int M, int slots, int bits, int cap, PlanPtrs p)
+__global__ void __launch_bounds__(1024) adapter_plan_one(const int* ids, int M, int slots, int bits, int cap, PlanPtrs p, BlobTag tag)
 {
+    write_tag(p.head, tag);
     extern __shared__ int mem[];  // first rows, first tiles (slots + 2 each), then [wavefront][adapter] counts of 16 bits
     __shared__ int lds[16];
     int *bs = mem, *tb = mem + slots + 2;
@@ -238,7 +242,8 @@ hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t
     if (M <= PLAN_ONE) {
         int bits = 1;
         while (slots >> bits) ++bits;
-        hipLaunchKernelGGL(adapter_plan_one, dim3(1), dim3(1024), (2 * (slots + 2)) * 4 + 16 * (slots + 1) * 2, s, ids, (int)M, slots, bits, l.tiles, p);
+        hipLaunchKernelGGL(adapter_plan_one, dim3(1), dim3(1024), (2 * (slots + 2)) * 4 + 16 * (slots + 1) * 2, s, ids, (int)M, slots, bits, l.tiles, p,
+                           plan_tag(M, slots));
         return hipGetLastError();
     }
     hipError_t e;
@@ -248,7 +253,7 @@ hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(adapter_plan_tiles, dim3(1), dim3(1024), 0, s, slots, l.tiles, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(adapter_plan_rows, dim3(l.chunks), dim3(256), 0, s, ids, (int)M, slots, l.chunks, p);
+    hipLaunchKernelGGL(adapter_plan_rows, dim3(l.chunks), dim3(256), 0, s, ids, (int)M, slots, l.chunks, p, plan_tag(M, slots));
     return hipGetLastError();
 }
 
@@ -290,6 +295,7 @@ __device__ __forceinline__ v4i column(const v4i* rows, int e)
 }
 
 struct AdapterView {  // of the plan, and the pool's per-adapter numbers
+    const uint32_t* head;  // its two words for the kernels
     const int *rows, *tbase;
     const int4* tiles;
     const int32_t* ranks;
@@ -297,6 +303,14 @@ struct AdapterView {  // of the plan, and the pool's per-adapter numbers
     int slots, rank, rp;  // rank of the arrays, and rounded up to 16
     int M, cap;           // rows; entries of `tiles`
 };
+// Whether the plan is one for these M rows and slots (of another one, or of memory that holds none, the rows would be numbers past the batch's).  Asked
+// where a tile comes in anyway, in the same round trip: ask_together keeps the comparison behind both loads.
+__device__ __forceinline__ uint2 plan_words(const AdapterView& v) { return *(const uint2*)v.head; }
+__device__ __forceinline__ void ask_together() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ bool planned(const AdapterView& v, const uint2& is)
+{
+    return ((is.x ^ (uint32_t)v.M) | (is.y ^ (PLAN_SLOTS + (uint32_t)v.slots))) == 0;
+}
 __device__ __forceinline__ int rank_of(const AdapterView& v, int slot) { return slot < v.slots ? min(max(v.ranks[slot], 0), v.rank) : 0; }
 
 // ---- T = X W^T ----------------------------------------------------------------------------
@@ -408,15 +422,17 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
     constexpr int UNITS = Piece::XL + Piece::WL, AHEAD = UNITS <= 6 ? 4 : UNITS <= 14 && !(TW && MT == 2 && RT == 4) ? 2 : 1;
     extern __shared__ v4i lds[];             // a piece per wavefront; then [wavefront][row][rank] sums
     const int4 tile = a.v.tiles[blockIdx.x / PARTS];
+    const uint2 is = plan_words(a.v);
     const int h = (blockIdx.x % PARTS) * (16 * MT), r0 = blockIdx.y * (RT * 16);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const uint8_t *xp[Piece::XL], *wp[Piece::WP];
     int rows[Piece::XL];
 #pragma unroll
     for (int u = 0; u < Piece::XL; ++u) rows[u] = a.v.rows[(int)(blockIdx.x / PARTS) * TILE + h + u * (64 / Piece::XU) + lane / Piece::XU];
+    ask_together();
     TOGETHER(rows);
     const int n = min(tile.y - h, 16 * MT);
-    if (n <= 0 || tile.z >= a.v.slots) return;
+    if ((n <= 0) | (tile.z >= a.v.slots) | !planned(a.v, is)) return;
     const int first = __builtin_amdgcn_readfirstlane(rows[0]);
 #pragma unroll
     for (int u = 0; u < Piece::XL; ++u) {
@@ -556,15 +572,17 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
     constexpr int LOW = F32 || KS < (TW ? 2 : 4) ? 0 : KS == 3 ? 2 : 1;
     __shared__ v4i low[LOW ? LOW * KS * 256 : 1];
     const int4 tile = a.v.tiles[t];
+    const uint2 is = plan_words(a.v);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     int rows4[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) rows4[e] = a.v.rows[t * TILE + w * 16 + q * 4 + e];
     int zeroth = a.v.rows[t * TILE];
+    ask_together();
     TOGETHER(rows4);
     asm("" : "+v"(zeroth));
     const int n = tile.y;
-    if (n <= 0) return;
+    if ((n <= 0) | !planned(a.v, is)) return;
     const int rank = rank_of(a.v, tile.z);
     if (rank == 0 && a.in_place) return;
     const int c0 = run * a.per, c1 = min(c0 + a.per, (a.width + 127) / 128);
@@ -740,10 +758,12 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
     // the group's first and last tile and the ones beside it, requested together: mostly they say all (one adapter), and every lookup that waits for
     // another is half a microsecond of a workgroup that lives for ten
     const int g0 = g * per, g1 = min(g0 + per, v.cap);
+    const uint2 is = plan_words(v);
     const int before = g0 > 0 ? v.tiles[g0 - 1].z : -1, after = g1 < v.cap ? v.tiles[g1].z : -1, with = v.tbase[v.slots];
     int4 first = v.tiles[g0];
     const int4 end = v.tiles[g1 - 1];
-    const int last = min(g1, with);
+    ask_together();
+    const int last = planned(v, is) ? min(g1, with) : 0;
     for (int t0 = g0; t0 < last;) {
         const int slot = first.z;
         const int t1 = end.z == slot ? g1 : min(v.tbase[slot + 1], last);
@@ -952,8 +972,9 @@ struct WgradSumArgs {
 __device__ __forceinline__ void wgrad_sum(const AdapterView& v, const WgradSumArgs& a, int slot, int share)
 {
     if (slot >= v.slots) return;
+    const uint2 is = plan_words(v);
     const int s0 = v.tbase[slot], s1 = v.tbase[slot + 1], g0 = s0 / a.per, g1 = (s1 - 1) / a.per;
-    if (s0 < s1 && g0 == g1) return;
+    if (!planned(v, is) | (s0 < s1 && g0 == g1)) return;
     for (int64_t o = (int64_t)share * 256 + threadIdx.x; o < a.nb + a.na; o += (int64_t)a.shares * 256) {
         v4f t = {0, 0, 0, 0};
         if (s0 < s1)
@@ -979,9 +1000,11 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 {
     const unsigned at = blockIdx.x / a.runs;
     const int4 tile = a.v.tiles[at];
+    const uint2 is = plan_words(a.v);
+    ask_together();
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
     const int n = tile.y;
-    if (n <= 0 || (tile.z >= a.v.slots && a.in_place)) return;
+    if ((n <= 0) | (tile.z >= a.v.slots && a.in_place) | !planned(a.v, is)) return;
     // the rank is another round trip: with one step of it, whose registers allow it, it is waited for behind the first loads (300 rows over 64 adapters 1152 ->
     // 3456 rank 32 11.7 -> 11.4 us); with more the loads ahead of it take a wavefront a SIMD
     constexpr bool LATE = KS == 1;
@@ -1109,7 +1132,7 @@ AdapterWorkLayout adapter_work_layout(const lq_adapter_config* c, int64_t M)
 static AdapterView view_of(const lq_adapter_config* c, const lq_adapter_pool* pool, const uint8_t* plan, int64_t M)
 {
     const AdapterPlanLayout l = adapter_plan_layout(M, c->slots);
-    return {(const int*)(plan + l.off_rows), (const int*)(plan + l.off_tbase), (const int4*)(plan + l.off_tiles), pool->ranks, pool->scales,
+    return {(const uint32_t*)plan + 6, (const int*)(plan + l.off_rows), (const int*)(plan + l.off_tbase), (const int4*)(plan + l.off_tiles), pool->ranks, pool->scales,
             c->slots, c->rank, (c->rank + 15) / 16 * 16, (int)M, l.tiles};
 }
 

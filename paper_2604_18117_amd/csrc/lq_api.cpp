@@ -576,6 +576,23 @@ lq_status lq_adapter_plan(int32_t slots, const int32_t* ids, int64_t M, void* pl
     return launch_adapter_plan(slots, ids, M, (uint8_t*)plan, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
 }
 
+lq_status lq_adapter_verify_plan(int32_t slots, int64_t M, const void* plan, size_t plan_bytes, void* stream)
+{
+    size_t need;
+    lq_status st = lq_adapter_plan_sizes(M, slots, &need);
+    if (st != LQ_OK) return st;
+    if (!plan) return LQ_ERR_NULL;
+    if (!aligned(plan, 256)) return LQ_ERR_ALIGN;
+    if (plan_bytes < need) return LQ_ERR_BUFFER_TOO_SMALL;
+    BlobTag got;
+    if (hipMemcpyAsync(&got, plan, sizeof(got), hipMemcpyDeviceToHost, (hipStream_t)stream) != hipSuccess) return LQ_ERR_DEVICE;
+    if (hipStreamSynchronize((hipStream_t)stream) != hipSuccess) return LQ_ERR_DEVICE;
+    const BlobTag want = plan_tag(M, slots);
+    for (int i = 0; i < 8; ++i)
+        if (got.w[i] != want.w[i]) return LQ_ERR_STALE_BLOB;
+    return LQ_OK;
+}
+
 lq_status lq_adapter_sizes(const lq_adapter_config* cfg, int64_t M, size_t* inter_bytes, size_t* work_bytes)
 {
     lq_status st = adapter_check(cfg);

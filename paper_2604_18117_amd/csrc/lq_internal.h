@@ -219,8 +219,15 @@ hipError_t launch_rot_apply(const Dims& d, const float* L, const float* R, const
                             hipStream_t s);
 hipError_t launch_rot_unpack(const Dims& d, const uint8_t* state, const lq_rot_view* out, hipStream_t s);
 
-// Adapters of many requests (lq_adapter.hip).  Plan: rows in the order of their adapters; first row and first tile of each adapter (slots + 2
-// entries: the rows without an adapter come last, then the ends); tiles {first row, rows, adapter, 0}; counts for the plan's own kernels.
+// Adapters of many requests (lq_adapter.hip).  Plan: a header as of the other blobs, with M and slots; rows in the order of their adapters; first row and
+// first tile of each adapter (slots + 2 entries: the rows without an adapter come last, then the ends); tiles {first row, rows, adapter, 0}; counts for the
+// plan's own kernels.  Everything behind the header stands where M and slots say, and holds numbers of rows: the kernels that read a plan compare the
+// header's last two words with their own M and slots first and end where they are another's (or of no plan: a number of slots is far below PLAN_SLOTS).
+constexpr uint32_t PLAN_KIND = 3, PLAN_VERSION = 1, PLAN_SLOTS = 0x504C414Eu;
+static inline BlobTag plan_tag(int64_t M, int slots)
+{
+    return {{BLOB_MAGIC, PLAN_VERSION, PLAN_KIND, 0, 0, 0, (uint32_t)M, PLAN_SLOTS + (uint32_t)slots}};
+}
 struct AdapterPlanLayout {
     int chunks, tiles;
     size_t off_base, off_tbase, off_tiles, off_rows, off_total, off_hist, total;
