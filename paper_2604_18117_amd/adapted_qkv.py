@@ -51,10 +51,17 @@ class AdaptedQKV:
         inter, work = lq.lq_adapter_sizes(self.adapters, M)
         self.inter, self.work = torch.empty(inter, dtype=torch.uint8, device="cuda"), torch.empty(work, dtype=torch.uint8, device="cuda")
         self.plan = torch.empty(lq.lq_adapter_plan_sizes(M, slots), dtype=torch.uint8, device="cuda")
+        self.rows = None  # of the batch that the plan is for
 
     def group(self, ids: torch.Tensor) -> None:
         """The batch's composition: the adapter of each row (-1: none).  Once per batch; every layer of a model could share it."""
+        self.rows = None
         lq.lq_adapter_plan(self.adapters.slots, ids, plan=self.plan)
+        self.rows = ids.shape[0]
+
+    def _grouped(self, X) -> None:
+        if X.shape[0] != self.rows:
+            raise ValueError(f"a batch of {X.shape[0]} rows, the last one grouped has {self.rows}")
 
     def heads_of(self, rows: torch.Tensor):
         """Views of the queries and keys in the projection's rows."""
@@ -62,6 +69,7 @@ class AdaptedQKV:
 
     def project(self, X, Y=None):
         """The adapted projection, before the norm: what the backward needs beside X."""
+        self._grouped(X)
         lq.lq_quantize_act(self.cfg, self.packed, X, act=self.act)
         Y = lq.lq_linear_lowrank_fwd(self.cfg, self.packed, self.act, X.shape[0], Y=Y)
         return lq.lq_adapter_fwd(self.adapters, self.plan, X, self.A, self.B, self.ranks, self.scales, Y, Y=Y, inter=self.inter)
@@ -75,6 +83,7 @@ class AdaptedQKV:
 
     def backward(self, X, rows, pos, grad):
         """Gradients of A, B, wq and wk.  rows: project(X); grad: the derivative with respect to the finished rows, overwritten."""
+        self._grouped(X)
         q, k = self.heads_of(rows)
         gq, gk = self.heads_of(grad)
         _, _, dwq, dwk = lq.lq_qk_norm_rope_bwd(self.qk, q, k, self.wq, self.wk, pos, self.inv_freq, gq, gk, dq=gq, dk=gk)
