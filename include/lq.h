@@ -353,7 +353,8 @@ lq_status lq_rot_unpack(const lq_config *cfg, const void *state, const lq_rot_vi
    X, dX, dXin: cfg.x_dtype.  Yin, Y, dY, A, B: bf16.  The products X A^T and dY B are held in fp32 and enter
    the second product as three bf16 terms (all 24 bits); outputs are rounded once.
    Rows may come in any order; a row's result does not depend on the other rows of the batch.  In this section X, Yin, dY and dXin may hold
-   infinities and NaN: they stay in their row (and in the gradients of its adapter). */
+   infinities and NaN: they stay in their row (and in the gradients of its adapter), and an infinity gives what the formulas give.  A, B (up to each adapter's
+   rank) and scales are finite. */
 typedef struct {
     int64_t N, K;       /* of the shared projection: multiples of 64                                      */
     int32_t rank;       /* of the pool's arrays: a multiple of 8, 8 .. 128                                */

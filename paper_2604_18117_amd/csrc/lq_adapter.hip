@@ -12,6 +12,8 @@
 // No atomics on memory: every sum has a fixed order, and T and Y of a row do not depend on the other rows.
 #include "lq_internal.h"
 
+#include <type_traits>
+
 namespace lq {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -260,8 +262,10 @@ hipError_t launch_adapter_plan(int slots, const int32_t* ids, int64_t M, uint8_t
 // ---- terms --------------------------------------------------------------------------------
 
 // An fp32 number as three bf16 terms, each the leading bits of what the ones before leave (cut off, so that every difference is exact): they
-// carry all 24 bits of it.  (Two, enough for the rounding of a bf16 output, lose the sum where adapter and projection cancel.)
+// carry all 24 bits of it.  (Two, enough for the rounding of a bf16 output, lose the sum where adapter and projection cancel.)  INF: of an infinity the
+// first term is one and nothing is left (without, what is left is not a number, and so is every sum that it enters).
 __device__ __forceinline__ float cut(uint32_t bits) { return __uint_as_float(bits & 0xFFFF0000u); }
+template <bool INF>
 __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[3])
 {
     float r[8];
@@ -273,11 +277,38 @@ __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[3])
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             c[j] = __float_as_uint(r[j]);
-            if (k < 2) r[j] -= cut(c[j]);
+            if (k < 2) r[j] = INF && k == 0 && __builtin_isinf(r[j]) ? 0.0f : r[j] - cut(c[j]);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) t[k][d] = (int)__builtin_amdgcn_perm(c[2 * d + 1], c[2 * d], 0x07060302u);
     }
+}
+// Where such terms meet an infinity, a later term of zero would make it not a number: it becomes the least number with the first one's sign (2^-126; of
+// a zero it stays zero).
+__device__ __forceinline__ void fill8(v4i (&t)[3])
+{
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            const uint32_t first = (uint32_t)t[0][d] >> h & 0xFFFFu;
+#pragma unroll
+            for (int k = 1; k < 3; ++k)
+                if ((first & 0x7FFFu) && !((uint32_t)t[k][d] >> h & 0x7FFFu)) t[k][d] = (int)(((uint32_t)t[k][d] & ~(0xFFFFu << h)) | ((first & 0x8000u) | 0x80u) << h);
+        }
+}
+// Whether a wavefront's sums hold something that is not a number.
+template <int A, int B>
+__device__ __forceinline__ bool not_numbers(const v4f (&acc)[A][B])
+{
+    bool nan = false;
+#pragma unroll
+    for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) nan |= __builtin_isunordered(acc[a][b][e], acc[a][b][e + 1]);
+    return __any(nan);
 }
 __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c)
 {
@@ -375,6 +406,7 @@ struct ShrinkPiece {
             for (int u = 0; u < WL; ++u) lds[place(u * 8 + lane / 8, lane % 8)] = w[u];
         }
     }
+    template <bool INF>
     static __device__ __forceinline__ void multiply(const v4i* lds, int i, int q, v4f (&acc)[MT][RT])
     {
 #pragma unroll
@@ -394,7 +426,7 @@ struct ShrinkPiece {
                         for (int j = 0; j < 4; ++j) v[4 * h + j] = __int_as_float(r[j]);
                     }
                     v4i t[3];
-                    split8(v, t);
+                    split8<INF>(v, t);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -433,24 +465,27 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
     TOGETHER(rows);
     const int n = min(tile.y - h, 16 * MT);
     if ((n <= 0) | (tile.z >= a.v.slots) | !planned(a.v, is)) return;
-    const int first = __builtin_amdgcn_readfirstlane(rows[0]);
+    auto point = [&](const int (&rows)[Piece::XL], int slot) {
+        const int first = __builtin_amdgcn_readfirstlane(rows[0]);
 #pragma unroll
-    for (int u = 0; u < Piece::XL; ++u) {
-        const int row = u * (64 / Piece::XU) + lane / Piece::XU < n ? rows[u] : first;
-        xp[u] = (const uint8_t*)a.X + (int64_t)row * a.ldx * (F32 ? 4 : 2) + lane % Piece::XU * 16;
-    }
-    // (ranks past the pool's are read from its last and not stored)
-    if constexpr (TW) {
-#pragma unroll
-        for (int k = 0; k < Piece::BLOCKS; ++k) {
-            const int b = lane + 64 * k, block = min(b / (2 * RT), 7), r = min(r0 + b % (2 * RT) * 8, a.v.rank - 8);
-            wp[k] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.depth + block * 8) * a.v.rank + r);
+        for (int u = 0; u < Piece::XL; ++u) {
+            const int row = u * (64 / Piece::XU) + lane / Piece::XU < n ? rows[u] : first;
+            xp[u] = (const uint8_t*)a.X + (int64_t)row * a.ldx * (F32 ? 4 : 2) + lane % Piece::XU * 16;
         }
-    } else {
+        // (ranks past the pool's are read from its last and not stored)
+        if constexpr (TW) {
 #pragma unroll
-        for (int u = 0; u < Piece::WL; ++u)
-            wp[u] = (const uint8_t*)(a.W + ((int64_t)tile.z * a.v.rank + min(r0 + u * 8 + lane / 8, a.v.rank - 1)) * a.depth) + lane % 8 * 16;
-    }
+            for (int k = 0; k < Piece::BLOCKS; ++k) {
+                const int b = lane + 64 * k, block = min(b / (2 * RT), 7), r = min(r0 + b % (2 * RT) * 8, a.v.rank - 8);
+                wp[k] = (const uint8_t*)(a.W + ((int64_t)slot * a.depth + block * 8) * a.v.rank + r);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < Piece::WL; ++u)
+                wp[u] = (const uint8_t*)(a.W + ((int64_t)slot * a.v.rank + min(r0 + u * 8 + lane / 8, a.v.rank - 1)) * a.depth) + lane % 8 * 16;
+        }
+    };
+    point(rows, tile.z);
     v4f acc[MT][RT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -473,9 +508,30 @@ __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
             p[d].put(mine, lane);
             wave_sync();
             if (c + 8 * AHEAD < pieces) p[d].fetch(xp, wp, c + 8 * AHEAD, a.v.rank);
-            Piece::multiply(mine, i, q, acc);
+            Piece::template multiply<false>(mine, i, q, acc);
         }
     }
+    // Sums that are not a number: once more, for an X with infinities.  Nothing is ahead here, and nothing is kept for it: its rows are looked up again.
+    if constexpr (F32)
+        if (not_numbers(acc)) {
+            int at = blockIdx.x / PARTS, slot = tile.z;
+            asm volatile("" : "+s"(at), "+s"(slot));
+#pragma unroll
+            for (int u = 0; u < Piece::XL; ++u) rows[u] = a.v.rows[at * TILE + h + u * (64 / Piece::XU) + lane / Piece::XU];
+            point(rows, slot);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[mt][rt] = v4f{0, 0, 0, 0};
+            for (int c = w; c < pieces; c += 8) {
+                Piece again;
+                again.fetch(xp, wp, c, a.v.rank);
+                wave_sync();
+                again.put(mine, lane);
+                wave_sync();
+                Piece::template multiply<true>(mine, i, q, acc);
+            }
+        }
     constexpr int ROW = RT * 16, ALL = MT * 16 * ROW;
     float* red = (float*)lds;
     __syncthreads();
@@ -549,6 +605,32 @@ __device__ __forceinline__ v4i keep(v4i t, int left)
 #pragma unroll
     for (int d = 0; d < 4; ++d) t[d] = left >= 2 * d + 2 ? t[d] : left == 2 * d + 1 ? t[d] & 0xFFFF : 0;
     return t;
+}
+
+// A lane's part of a row of s T as terms: ranks 32 ks + 8 q ..  Once more for infinities where there are any (one test for all of them).
+template <int KS>
+__device__ __forceinline__ void load_terms(const ExpandArgs& a, const float* T, int slot, int rank, int q, v4i (&tt)[KS][3])
+{
+    const float s = a.v.scales[slot];
+    float most = 0.0f;
+    auto load = [&](auto infinite) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            float t[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const v4f x = *(const v4f*)(T + min(ks * 32 + q * 8, a.v.rp - 8) + 4 * u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
+                    if (!infinite()) most = fmaxf(most, fabsf(t[4 * u + e]));
+                }
+            }
+            split8<infinite()>(t, tt[ks]);
+        }
+    };
+    load(std::false_type());
+    if (__any(__builtin_isinf(most))) load(std::true_type());
 }
 
 // A workgroup of 4 wavefronts: a tile, 16 rows each, and `per` pieces of 128 columns one after another.  Bound by memory, so it is laid out for its
@@ -635,23 +717,11 @@ __device__ __forceinline__ void expand_tile(const ExpandArgs& a, int run, int t)
         return;
     }
     v4i tt[KS][3];
-    {
-        const float s = a.v.scales[tile.z];
-        const float* T = a.T + (int64_t)(tile.x + min(w * 16 + i, n - 1)) * a.v.rp;
+    load_terms<KS>(a, a.T + (int64_t)(tile.x + min(w * 16 + i, n - 1)) * a.v.rp, tile.z, rank, q, tt);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            float t[8];
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const v4f x = *(const v4f*)(T + min(ks * 32 + q * 8, a.v.rp - 8) + 4 * u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
-            }
-            split8(t, tt[ks]);
-#pragma unroll
-            for (int k = 3 - LOW; k < 3; ++k) low[((k - 3 + LOW) * KS + ks) * 256 + threadIdx.x] = tt[ks][k];
-        }
-    }
+        for (int k = 3 - LOW; k < 3; ++k) low[((k - 3 + LOW) * KS + ks) * 256 + threadIdx.x] = tt[ks][k];
     // the units that no row of the factor fills (ranks that are no multiple of 32)
     if (!TW && pr < KS * 4) {
         for (int o = threadIdx.x; o < BUFFERS * 8 * KS * 64; o += 256) wl[0][o] = v4i{0, 0, 0, 0};
@@ -810,14 +880,9 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                 for (int rt = 0; rt < RT; ++rt) tn[rt][j] = T[place + (uint32_t)min(r0 + rt * 16 + i, v.rp - 1)];
             }
         };
-        if (w < steps) {
-            look(w);
-            request(w);
-            look(w + SHARE);
-        }
-        for (int st = w; st < steps; st += SHARE) {
+        // rows past the adapter's last: zeros on both sides (what stands in for them must not reach the sums through an infinity of its own)
+        auto clear_past = [&](int st) {
             const int left = p1 - (p0 + st * 32 + q * 8);
-            // rows past the adapter's last: zeros on both sides (what stands in for them must not reach the sums through an infinity of its own)
             if (st == steps - 1) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -828,25 +893,17 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                         for (int rt = 0; rt < RT; ++rt) tn[rt][j] = 0.0f;
                     }
             }
-            v4i qr[8][F32 ? 2 : 1], tt[RT][3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) split8(tn[rt], tt[rt]);
-            if (st + SHARE < steps) {
-                request(st + SHARE);
-                look(st + 2 * SHARE);
-            }
+        };
+        auto multiply = [&](const v4i (&qr)[8][F32 ? 2 : 1], const v4i (&tt)[RT][3], auto infinite) {
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                v4i qt[QT];
+                v4i qt[F32 ? 3 : 1];
                 if constexpr (F32) {
                     float x[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) x[j] = __int_as_float(qr[j][c / 4][c % 4]);
-                    split8(x, qt);
+                    split8<infinite()>(x, qt);
+                    if constexpr (infinite()) fill8(qt);
                 } else {
                     v4i rows8[8];
 #pragma unroll
@@ -861,6 +918,45 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                         for (int u = QT - 1; u >= 0; --u)
                             if (k + u < 3)  // (what is left out is below 2^-22 of the product)
                                 acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
+            }
+        };
+        if (w < steps) {
+            look(w);
+            request(w);
+            look(w + SHARE);
+        }
+        for (int st = w; st < steps; st += SHARE) {
+            clear_past(st);
+            v4i qr[8][F32 ? 2 : 1], tt[RT][3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int u = 0; u < (F32 ? 2 : 1); ++u) qr[j][u] = qn[j][u];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) split8<false>(tn[rt], tt[rt]);
+            if (st + SHARE < steps) {
+                request(st + SHARE);
+                look(st + 2 * SHARE);
+            }
+            multiply(qr, tt, std::false_type());
+        }
+        // sums that are not a number: once more, for products with an infinity (see fill8); nothing is ahead here
+        if (not_numbers(acc)) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[c][rt] = v4f{0, 0, 0, 0};
+            for (int st = w; st < steps; st += SHARE) {
+                look(st);
+                request(st);
+                clear_past(st);
+                v4i tt[RT][3];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    split8<true>(tn[rt], tt[rt]);
+                    fill8(tt[rt]);
+                }
+                multiply(qn, tt, std::true_type());
             }
         }
         const int rank = rank_of(v, slot);
@@ -953,7 +1049,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 // Bound by latency: 8 rows of a step are 8 loads in flight for a wavefront, and the sums leave two wavefronts a SIMD: us and TB/s of X and dY, traced, 8192 rows of
 // 1152 and 3456, rank 32: 21-24 and 3.1-3.6; 301 rows of fp32 1152 and bf16 1152, rank 24: 6.2-7.2.
 template <bool F32, int RT, bool ALONE>
-__global__ void __launch_bounds__(256) adapter_wgrad(WgradArgs a)
+__global__ void __launch_bounds__(256, (!F32 && RT == 1 ? 3 : 1)) adapter_wgrad(WgradArgs a)
 {
     __shared__ v4f red[ALONE ? 1 : 4][ALONE ? 1 : 8 * RT * 64];
     const int nb = (a.N + 127) / 128, kb = (a.K + 127) / 128, block = ALONE ? (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) : (int)blockIdx.x;
@@ -1034,20 +1130,8 @@ __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
             out[e] = (row * a.ldy + col) * 2;
         }
         if (rank > 0) {
-            const float s = a.v.scales[tile.z];
-            const float* T = a.T + (int64_t)(tile.x + min(h + i, n - 1)) * a.v.rp;
             v4i tt[KS][3];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                float t[8];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const v4f x = *(const v4f*)(T + min(ks * 32 + q * 8, a.v.rp - 8) + 4 * u);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) t[4 * u + e] = ks * 32 + q * 8 < rank ? x[e] * s : 0.0f;
-                }
-                split8(t, tt[ks]);
-            }
+            load_terms<KS>(a, a.T + (int64_t)(tile.x + min(h + i, n - 1)) * a.v.rp, tile.z, rank, q, tt);
             v4f acc[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
