@@ -916,7 +916,7 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
                     for (int k = 2; k >= 0; --k)
 #pragma unroll
                         for (int u = QT - 1; u >= 0; --u)
-                            if (k + u < 3)  // (what is left out is below 2^-22 of the product)
+                            if (k + u < 4)  // (what is left out is below 2^-30 of the product)
                                 acc[c][rt] = COLS_FIRST ? mfma(qt[u], tt[rt][k], acc[c][rt]) : mfma(tt[rt][k], qt[u], acc[c][rt]);
             }
         };

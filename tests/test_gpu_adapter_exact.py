@@ -66,3 +66,36 @@ def test_all_bits_of_the_backwards_first_product_reach_dx(lq, M, slots, K, R, x)
     lq.lq_adapter_fwd(cfg, plan, X, A, B, ranks, scales, dY, inter=inter)
     dX, _, _ = lq.lq_adapter_bwd(cfg, plan, X, A, B, ranks, scales, inter, dY)
     assert torch.equal(dX.float(), want)
+
+
+@pytest.mark.parametrize("M,slots,K,N,R", [(1, 1, 64, 64, 8), (40, 1, 192, 64, 40), (3000, 1, 64, 64, 24), (30, 30, 128, 64, 8), (30, 30, 64, 64, 128)])
+def test_all_bits_of_fp32_x_reach_da(lq, M, slots, K, N, R):  # noqa: F811
+    """dA of adapters with one row that has a derivative: each value is one product of two numbers of 24 bits, whose terms after the first are as large as they come.
+    It is rounded when the last of its terms' products is added (by at most 2^-23 of it, cut off or to nearest); what the additions before lose is below 2^-29."""
+    g = torch.Generator().manual_seed(M + K)
+    dY, X = torch.zeros(M, N), torch.zeros(M, K, dtype=torch.float64)
+    first = torch.zeros(slots, N, R)
+    ids = torch.arange(M) % slots
+    value = torch.zeros(slots, R, dtype=torch.float64)
+    for s in range(slots):
+        a, b, c = triples(R, g)
+        worst = torch.arange(R) % 2 == 0
+        a, b, c = [torch.where(worst, torch.tensor(float(v)), t) for v, t in ((128, a), (255, b), (255, c))]
+        first[s, :3] = torch.stack([a, b, c])
+        value[s] = a.double() * 2 ** 16 + b.double() * 2 ** 8 + c.double()
+        row = s  # the adapter's first
+        dY[row, :3] = torch.tensor([2.0 ** 16, 2.0 ** 8, 1.0])
+        x = torch.randint(2 ** 23, 2 ** 24, (K,), generator=g).double()
+        x[::3] = 128 * 2 ** 16 + 255 * 2 ** 8 + 255
+        X[row] = x * torch.where(torch.arange(K) % 5 == 0, -1.0, 1.0)
+    cfg = lq.make_adapter_config(N, K, R, slots, "f32")
+    pool = (torch.zeros(slots, R, K, dtype=torch.bfloat16, device="cuda"), first.bfloat16().cuda(), torch.full((slots,), R, dtype=torch.int32, device="cuda"),
+            torch.ones(slots, device="cuda"))
+    plan = lq.lq_adapter_plan(slots, ids.int().cuda())
+    inter = torch.empty(lq.lq_adapter_sizes(cfg, M)[0], dtype=torch.uint8, device="cuda")
+    Xg, dYg = X.float().cuda(), dY.bfloat16().cuda()
+    lq.lq_adapter_fwd(cfg, plan, Xg, *pool, dYg, inter=inter)
+    _, dA, _ = lq.lq_adapter_bwd(cfg, plan, Xg, *pool, inter, dYg)
+    want = value[:, :, None] * X[:slots][:, None, :]
+    off = (dA.double().cpu() - want).abs() / want.abs()
+    assert float(off.max()) <= 2.0 ** -23 * (1 + 2.0 ** -5), float(off.max())
