@@ -92,10 +92,17 @@ __device__ __forceinline__ void sum_groups(float (&v)[N], int k)
     }
 }
 
-// V consecutive values, aligned to themselves in memory
-template <typename T, int V>
+// What an access of V pairs is aligned to, in bytes: the whole of it up to 16, and nothing but its values where V = 1 (of adjacent pairs two at once, which any
+// strides may put anywhere).  The host's choice of V keeps to it.
+constexpr int access_align(int V, bool half, int elem)
+{
+    const int bytes = V == 1 ? elem : half ? V * elem : 2 * V * elem;
+    return bytes > 16 ? 16 : bytes;
+}
+// N consecutive values
+template <typename T, int N>
 struct Vec {
-    typedef T type __attribute__((ext_vector_type(V)));
+    typedef T type __attribute__((ext_vector_type(N)));
 };
 template <typename T>
 struct Vec<T, 1> {
@@ -111,11 +118,13 @@ __device__ __forceinline__ float part(const VT& v, int j)
 // The members a, b of V pairs of a head as they lie in memory: two vectors of V (halves), or one of 2 V
 template <typename T, int V, bool HALF>
 struct Raw {
-    typename Vec<T, HALF ? V : 2 * V>::type v[HALF ? 2 : 1];
+    typedef typename Vec<T, HALF ? V : 2 * V>::type Value;
+    typedef Value Access __attribute__((aligned(access_align(V, HALF, sizeof(T)))));
+    Value v[HALF ? 2 : 1];
     __device__ __forceinline__ void fetch(const T* x, int oa, int ob)
     {
-        v[0] = *(const decltype(&v[0]))(x + oa);
-        if constexpr (HALF) v[1] = *(const decltype(&v[0]))(x + ob);
+        v[0] = *(const Access*)(x + oa);
+        if constexpr (HALF) v[1] = *(const Access*)(x + ob);
     }
     __device__ __forceinline__ void get(float (&a)[V], float (&b)[V]) const
     {
@@ -133,16 +142,16 @@ __device__ __forceinline__ void put(T* x, int oa, int ob, const float (&a)[V], c
         x[oa] = (T)a[0];
         x[ob] = (T)b[0];
     } else if constexpr (HALF) {
-        typename Vec<T, V>::type va, vb;
+        typename Raw<T, V, HALF>::Value va, vb;
 #pragma unroll
         for (int j = 0; j < V; ++j) va[j] = (T)a[j], vb[j] = (T)b[j];
-        *(decltype(&va))(x + oa) = va;
-        *(decltype(&va))(x + ob) = vb;
+        *(typename Raw<T, V, HALF>::Access*)(x + oa) = va;
+        *(typename Raw<T, V, HALF>::Access*)(x + ob) = vb;
     } else {
-        typename Vec<T, 2 * V>::type w;
+        typename Raw<T, V, HALF>::Value w;
 #pragma unroll
         for (int j = 0; j < V; ++j) w[2 * j] = (T)a[j], w[2 * j + 1] = (T)b[j];
-        *(decltype(&w))(x + oa) = w;
+        *(typename Raw<T, V, HALF>::Access*)(x + oa) = w;
     }
 }
 
@@ -477,8 +486,7 @@ static QkShape qk_shape(const lq_qk_config* c, const QkTensors* t, int64_t M, bo
     // 70.6; of 7 + 7 of 160 23.8 / 22.6, whose 10 vectors leave 6 of 16 lanes idle)
     for (s.V = c->dtype == LQ_BF16 && c->pairing == LQ_PAIR_HALF && c->head_dim <= 128 ? 8 : 4; s.V > 1; s.V /= 2) {
         if (c->head_dim % (2 * s.V) || P % s.V) continue;
-        int bytes = c->pairing == LQ_PAIR_HALF ? s.V * elem : 2 * s.V * elem;
-        bytes = bytes > 16 ? 16 : bytes;
+        const int bytes = access_align(s.V, c->pairing == LQ_PAIR_HALF, elem);
         bool ok = true;
         for (int k = 0; t && k < 2; ++k)
             if (heads[k])
