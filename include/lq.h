@@ -423,7 +423,8 @@ typedef struct {
     float eps;                 /* > 0 (LQ_NORM_RMS)                                                           */
 } lq_qk_config;
 
-/* Heads of M tokens: value j of head h of token m is p[m * ld + h * hs + j], strides in elements, below 2^40 in size, not negative; p aligned to its type. */
+/* Heads of M tokens: value j of head h of token m is p[m * ld + h * hs + j], strides in elements, below 2^40 in size, not negative; p aligned to its type.  Inputs may
+   repeat (a stride of 0: a head shared by several); the heads of an output must lie apart (LQ_ERR_SHAPE), whichever of tokens and heads is outermost. */
 typedef struct {
     void *p;
     int64_t ld, hs;

@@ -676,6 +676,29 @@ static lq_status heads_check(const lq_qk_config* c, const lq_heads* h, int heads
     *out = *h;
     return LQ_OK;
 }
+// Whether the heads of an output lie apart: no two of them have a value in common.
+static bool heads_apart(const lq_heads& h, int64_t heads, int64_t dim, int64_t M)
+{
+    if ((heads > 1 && h.hs < dim) || (M > 1 && h.ld < dim)) return false;
+    if (heads < 2 || M < 2 || h.ld - dim >= (heads - 1) * h.hs || (h.hs - dim) / h.ld >= M - 1) return true;  // head by head in a token, or token by token in a head
+    for (int64_t b = 1; b < heads; ++b) {  // heads b apart, of tokens so far apart that their offsets are the nearest
+        const int64_t at = b * h.hs, a = at / h.ld;
+        if ((a >= 1 && a < M && at - a * h.ld < dim) || (a + 1 < M && (a + 1) * h.ld - at < dim)) return false;
+    }
+    return true;
+}
+// outputs of queries and keys
+static lq_status outputs_check(const lq_qk_config* c, const lq_heads* q, const lq_heads* k, int64_t M, lq_heads* out)
+{
+    const lq_heads* in[2] = {q, k};
+    const int heads[2] = {c->heads_q, c->heads_k};
+    for (int s = 0; s < 2; ++s) {
+        const lq_status st = heads_check(c, in[s], heads[s], &out[s]);
+        if (st != LQ_OK) return st;
+        if (heads[s] && !heads_apart(out[s], heads[s], c->head_dim, M)) return LQ_ERR_SHAPE;
+    }
+    return LQ_OK;
+}
 static lq_status positions_check(const lq_qk_config* c, const float* pos, int64_t pos_rows, const float* inv_freq)
 {
     if (c->pairs[0] + c->pairs[1] + c->pairs[2] + c->pairs[3] == 0) return LQ_OK;
@@ -693,7 +716,7 @@ lq_status lq_qk_norm_rope_fwd(const lq_qk_config* cfg, const lq_heads* q, const 
     if (M == 0) return LQ_OK;  // an empty batch
     QkTensors t{};
     if ((st = heads_check(cfg, q, cfg->heads_q, &t.q[0])) != LQ_OK || (st = heads_check(cfg, k, cfg->heads_k, &t.q[1])) != LQ_OK ||
-        (st = heads_check(cfg, qo, cfg->heads_q, &t.out[0])) != LQ_OK || (st = heads_check(cfg, ko, cfg->heads_k, &t.out[1])) != LQ_OK ||
+        (st = outputs_check(cfg, qo, ko, M, t.out)) != LQ_OK ||
         (st = positions_check(cfg, pos, pos_rows, inv_freq)) != LQ_OK)
         return st;
     if (!aligned(wq, 4) || !aligned(wk, 4)) return LQ_ERR_ALIGN;
@@ -727,7 +750,7 @@ lq_status lq_qk_norm_rope_bwd(const lq_qk_config* cfg, const lq_heads* q, const 
     if (M > 0) {
         if ((norm && ((st = heads_check(cfg, q, cfg->heads_q, &t.q[0])) != LQ_OK || (st = heads_check(cfg, k, cfg->heads_k, &t.q[1])) != LQ_OK)) ||
             (st = heads_check(cfg, dqo, cfg->heads_q, &t.grad[0])) != LQ_OK || (st = heads_check(cfg, dko, cfg->heads_k, &t.grad[1])) != LQ_OK ||
-            (st = heads_check(cfg, dq, cfg->heads_q, &t.out[0])) != LQ_OK || (st = heads_check(cfg, dk, cfg->heads_k, &t.out[1])) != LQ_OK ||
+            (st = outputs_check(cfg, dq, dk, M, t.out)) != LQ_OK ||
             (st = positions_check(cfg, pos, pos_rows, inv_freq)) != LQ_OK)
             return st;
         if (norm && dwq && !work) return LQ_ERR_NULL;
