@@ -438,21 +438,27 @@ __global__ void __launch_bounds__(256) qk_bwd_kernel(QkArgs a)
     }
 }
 
-// dw: the workgroups' sums in their order; 16 values to a workgroup, 64 shares of the sums each (512 parts of two heads of 72: 4 us traced, round trips)
+// dw: the workgroups' sums in a fixed order; 16 values to a workgroup, 64 shares of the sums each, joined in a tree (one after another their 63 additions were
+// most of dw's rounding, and no faster; 512 parts of two heads of 72: 4 us traced, round trips)
 __global__ void __launch_bounds__(1024) qk_weight_sum(const float* part, int n, int dim, float* dwq, float* dwk)
 {
-    __shared__ float sh[64][17];
+    __shared__ float sh[16][16];
     const int v = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
     float t = 0.0f;
     if (v < 2 * dim) {
 #pragma unroll 8
         for (int i = r; i < n; i += 64) t += part[(int64_t)i * 2 * dim + v];
     }
-    sh[r][threadIdx.x & 15] = t;
+    t += __shfl_xor(t, 16);
+    t += __shfl_xor(t, 32);
+    if ((threadIdx.x & 63) < 16) sh[threadIdx.x >> 6][threadIdx.x & 15] = t;
     __syncthreads();
-    if (r == 0 && v < 2 * dim) {
-        for (int k = 1; k < 64; ++k) t += sh[k][threadIdx.x];
-        (v < dim ? dwq : dwk)[v < dim ? v : v - dim] = t;
+    if (threadIdx.x < 64) {
+        const int c = threadIdx.x & 15;
+        t = (sh[r][c] + sh[r + 4][c]) + (sh[r + 8][c] + sh[r + 12][c]);
+        t += __shfl_xor(t, 16);
+        t += __shfl_xor(t, 32);
+        if (r == 0 && v < 2 * dim) (v < dim ? dwq : dwk)[v < dim ? v : v - dim] = t;
     }
 }
 

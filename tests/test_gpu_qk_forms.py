@@ -72,3 +72,15 @@ def test_gradient_with_offsets_past_32_bits(lq, x):  # noqa: F811
     for a, b in zip(want, got):
         assert torch.equal(a, b)
     check(d, lq.lq_qk_norm_rope_fwd(cfg, far[0], far[1], *at), got, pairs, "half", True, "qk")
+
+
+@pytest.mark.parametrize("M", [64, 256, 512, 4096])
+def test_sums_of_the_weights_gradients_lose_little(lq, M):  # noqa: F811
+    """Heads of ones have a norm of one, so that dw is the sum of the derivatives: 2^24, then ones.  An addition to 2^24 is off by at most 1; a value goes through at most
+    8 of them in a workgroup, 8 of workgroups' sums in a share and 6 where the shares are joined."""
+    cfg = lq.make_qk_config(1, 1, 2, (), "half", True, 1e-12, "f32")
+    x, dy = torch.ones(M, 1, 2, device="cuda"), torch.ones(M, 1, 2, device="cuda")
+    dy[0] = 2.0 ** 24
+    _, _, dwq, dwk = lq.lq_qk_norm_rope_bwd(cfg, x, x, None, None, None, None, dy, dy)
+    for dw in (dwq, dwk):
+        assert float((dw.double() - (2.0 ** 24 + M - 1)).abs().max()) <= 8 + 8 + 6, dw
