@@ -356,9 +356,9 @@ lq_status lq_rot_unpack(const lq_config *cfg, const void *state, const lq_rot_vi
    infinities and NaN: they stay in their row (and in the gradients of its adapter), and an infinity gives what the formulas give.  A, B (up to each adapter's
    rank) and scales are finite. */
 typedef struct {
-    int64_t N, K;       /* of the shared projection: multiples of 64                                      */
+    int64_t N, K;       /* of the shared projection: multiples of 64, up to 2^22 (LQ_ERR_SHAPE)           */
     int32_t rank;       /* of the pool's arrays: a multiple of 8, 8 .. 128                                */
-    int32_t slots;      /* adapters in the pool, 1 .. 1024                                                */
+    int32_t slots;      /* adapters in the pool, 1 .. 1024; slots * rank * (N + K) below 2^32 (LQ_ERR_UNSUPPORTED) */
     int32_t x_dtype;    /* lq_dtype of X, dXin, dX                                                        */
     int32_t flags;      /* 0                                                                              */
 } lq_adapter_config;

@@ -369,7 +369,8 @@ __device__ __forceinline__ void wave_sync()
 // A wavefront's piece of a product: 64 values of K of 16 * MT rows of X and 16 * RT of the factor.  The 16 x 16 x 32 product wants 16 rows in 16
 // consecutive lanes; read like that from memory, every 16 bytes are a cache line of their own (40 us for 8191 x 2240, rank 128, whatever was
 // in flight).  So 8 (fp32: 16) lanes read a row's 128 (256) consecutive bytes, and the rows go through the wavefront's part of the LDS: unit p of 16
-// bytes of row r stands at r * units + (p ^ r % 16), free of bank conflicts both ways.
+// bytes of row r stands at r * units + (p ^ r % 16), free of bank conflicts both ways (the turned
+// form's writes, two ways, and the stores of the sums at the end, four, are not: 19 % of the LDS's cycles, turned 27 %).
 // TW: the factor is given as [depth][rank]; a lane reads blocks of 8 x 8 and turns them on the way to the LDS.
 template <bool F32, bool TW, int MT, int RT>
 struct ShrinkPiece {
@@ -444,8 +445,8 @@ struct ShrinkPiece {
 // A workgroup of 8 wavefronts: 16 * MT rows of a tile, 16 * RT of the rank; the wavefronts take the pieces of K in turn, the next ones (up to four, as
 // the registers allow) requested before the present one is multiplied, and add up in the LDS.  T's bits depend on the row, the factor and K alone.
 // Bound by a wavefront's chain of round trips and by what a compute unit's loads bring in, rows and factor alike: us and TB/s of X, traced, 8192 x 1152 rank 32
-// 8.0 and 2.4, dY 8192 x 3456 rank 32 26 and 2.2, 8191 x 2240 rank 128 30-34 and 1.1; of the 26, X alone takes 20 and the factor
-// alone 16.  64 rows to a workgroup halve the factor's part and the workgroups: 9.8 for 8.5.
+// 7.8 and 2.4, dY 8192 x 3456 rank 32 26-27 and 2.2, 8191 x 2240 rank 128 30-35 and 1.1 (92 MB past the L2s for 39); of the 26, X alone takes 20 and the factor
+// alone 16 (each with the other's loads left out).  64 rows to a workgroup halve the factor's part and the workgroups: 9.8 for 8.5.
 template <bool F32, bool TW, int MT, int RT>
 __global__ void __launch_bounds__(512) adapter_shrink(ShrinkArgs a)
 {
@@ -638,7 +639,7 @@ __device__ __forceinline__ void load_terms(const ExpandArgs& a, const float* T, 
 // read and write 256 consecutive bytes (with 16 rows in 16 lanes every 16 bytes are a cache line of their own).  The factor's 128
 // rows are read in order, too, by all four wavefronts, and go through the LDS (unit (j, ks, q, i) of 16 bytes in the order of its
 // readers, i turned by what the writers differ in).  The next piece's columns are requested before the present one's are worked on.
-// us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 25 and 4.5, 8191 x 11200 rank 128 94-106 and 3.5-3.9; copying the same rows by the same pattern takes 23 and 76, a plain
+// us and TB/s of Yin and Y, traced: 8192 x 3456 rank 32 24-26 and 4.4-4.6, 8191 x 11200 rank 128 100-117 and 3.1-3.7 (299 MB read past the L2s for 199: the factor comes to every XCD more than once); copying the same rows by the same pattern takes 23 and 76, a plain
 // copy 23 and 70.  Registers are held by launch bounds to what keeps four wavefronts a SIMD (rank up to 32) or three without spilling; left alone, T's third
 // terms cost one each (forward of 8192 x 3456 rank 32 36.4 -> 33.9, 8191 x 11200 rank 128 137 -> 130).  Non-temporal stores save 2-3 of the 25, but Y
 // has a reader, for whom it is left in the caches.
@@ -1047,7 +1048,8 @@ __device__ __forceinline__ void wgrad_group(const AdapterView& v, const float* T
 // a lane: a lane loads 8 columns of 8 rows (16 lanes 256 consecutive bytes) and pairs up the halves of the dwords, which gives the operands of 8
 // products, the c-th with columns 8 i + c.  T and dT are fp32, so they go in as three bf16 terms.
 // Bound by latency: 8 rows of a step are 8 loads in flight for a wavefront, and the sums leave two wavefronts a SIMD: us and TB/s of X and dY, traced, 8192 rows of
-// 1152 and 3456, rank 32: 21-24 and 3.1-3.6; 301 rows of fp32 1152 and bf16 1152, rank 24: 6.2-7.2.
+// 1152 and 3456, rank 32: 21-25 and 3.1-3.6 (0.9 wavefronts a SIMD on the average); 301 rows of fp32 1152 and bf16 1152, rank 24: 7.3-7.8.
+// (Three wavefronts a SIMD for bf16 and 16 of the rank: what it takes without the second round for infinities, which must not cost one.)
 template <bool F32, int RT, bool ALONE>
 __global__ void __launch_bounds__(256, (!F32 && RT == 1 ? 3 : 1)) adapter_wgrad(WgradArgs a)
 {
@@ -1090,7 +1092,7 @@ __global__ void __launch_bounds__(256, KS == 1 ? 4 : 3) adapter_expand(ExpandArg
 }
 // The forward's second product where adapters have few rows each (single tokens): a wavefront takes a piece of 128 columns by itself and reads its part of
 // the factor straight into the products' operands, 16 rows of the tile at a time.  The same bits as adapter_expand.  Bound by latency: two dependent
-// round trips, tile to rows to Yin (64 rows over 32 adapters, 1152 -> 3456 rank 32: 4.1-4.7 us traced for the factors' 7 MB).
+// round trips, tile to rows to Yin (64 rows over 32 adapters, 1152 -> 3456 rank 32: 4.6-4.8 us traced for the factors' 7 MB).
 template <int KS>
 __global__ void __launch_bounds__(256) adapter_expand_few(ExpandArgs a)
 {
@@ -1186,7 +1188,7 @@ static RankSplit rank_split(int rank, int most = 4)
     return {groups, (tiles + groups - 1) / groups};
 }
 
-// Adapters with a step of 32 rows each, about: nothing to share out among the wavefronts, and a group for every tile (us of a training step, shared / alone: 121
+// Adapters with a step of 32 rows each, about, as far as the pool's size says (the host does not know which of them a batch has): nothing to share out among the wavefronts, and a group for every tile (us of a training step, shared / alone: 121
 // rows over 31 adapters 256 -> 4864 rank 104 148 / 93, 231 over 25 192 -> 2560 rank 48 43 / 37, 5 over 7 3456 -> 704 rank 96 40 / 31, 368 over 21 64 -> 1728 rank 48
 // 32 / 30; with more rows, 327 over 12 384 -> 832 rank 48 24.1 / 25.7).
 static bool few_rows(int slots, int64_t M) { return M <= 24 * (int64_t)slots; }
@@ -1337,8 +1339,10 @@ hipError_t launch_adapter_fwd(const lq_adapter_config* c, const uint8_t* plan, c
     const ExpandArgs x{v, (const float*)inter, (const uint16_t*)pool->B, Yin, Y, ldyin, ldy, (int)c->N, Yin == Y && ldyin == ldy};
     const hipError_t e = c->x_dtype == LQ_F32 ? run_shrink<true, false>(a, tiles, s) : run_shrink<false, false>(a, tiles, s);
     if (e != hipSuccess) return e;
-    // (us of a forward, few / other form: 64 rows over 32 adapters 1152 -> 3456 rank 32 8.7 / 9.2, 300 over 64 11.5 / 13.0, 1000 over 64 rank 64 19.8 / 21.0, 16 over 16
-    // 1152 -> 4608 rank 128 12.5 / 14.4; where the other form's workgroups all fit at once it is ahead: 64 over 4 7.8 / 6.3, 1 x 4608 -> 1152 rank 128 12.5 / 10.7)
+    // (us of a forward, few / other form: 64 rows over 32 adapters 1152 -> 3456 rank 32 8.6 / 9.2, 300 over 64 10.9 / 12.9, 1000 over 64 rank 64 18.6 / 19.9, 16 over 16
+    // 1152 -> 4608 rank 128 13.0 / 15.0; where the other form's workgroups all fit at once it is ahead: 64 over 4 8.1 / 6.4, 1 x 4608 -> 1152 rank 128 12.9 / 11.3.  The pool
+    // stands for the adapters of the batch, which the host does not know: a single token of a pool of 64 takes it, too, 18.8 / 17.3, and 8192 rows of one adapter of 1024
+    // 64.7 / 63.2)
     if (M <= 16 * (int64_t)c->slots && (int64_t)tiles * ((c->N + 127) / 128) >= 512) return run_expand_few(x, tiles, s);
     return run_expand<false, false>(x, tiles, nullptr, s);
 }
