@@ -410,7 +410,7 @@ lq_status lq_adapter_bwd(const lq_adapter_config *cfg, const void *plan, size_t 
    the norm alone.  Angles are taken from the exact product of the two fp32 numbers, everything else is held in fp32 and rounded once.
    Token m has row m % pos_rows of pos (pos_rows x axes, fp32, dense): a batch of equal grids needs one grid's positions. */
 typedef enum { LQ_PAIR_HALF = 0, LQ_PAIR_ADJACENT = 1 } lq_pairing;
-typedef enum { LQ_NORM_NONE = 0, LQ_NORM_RMS = 1 } lq_norm;
+typedef enum { LQ_NORM_NONE = 0, LQ_NORM_RMS = 1, LQ_NORM_LAYER = 2 /* lq_block_norm_* only */ } lq_norm;
 
 typedef struct {
     int32_t heads_q, heads_k;  /* either may be 0 (its views are then not looked at), not both; sum <= 4096     */
@@ -448,6 +448,136 @@ lq_status lq_qk_norm_rope_bwd(const lq_qk_config *cfg, const lq_heads *q, const 
                               const float *pos, int64_t pos_rows, const float *inv_freq, const lq_heads *dqo, const lq_heads *dko,
                               const lq_heads *dq, const lq_heads *dk, float *dwq, float *dwk, int64_t M, void *work, size_t work_bytes,
                               void *stream);
+
+/* ---- Product of a few rows with 4-bit weights in groups along K (weights alone are quantised) ----------------------
+   The layers beside the large projections: conditioning vectors, single tokens.
+       Y[m,n]  = bias[n] + sum_k X[m,k] c[n,k] s[n, k / group]
+       dX[m,k] = sum_n dY[m,n] s[n, k / group] c[n,k]                    (the weights are not trained)
+   c: integers -7 .. 7, s: fp32.  Codes enter the products exactly, fp32 rows with all 24 bits; sums are held in fp32 and rounded once.  A row's result does not depend on the
+   other rows; infinities and NaN stay in their row.  Sums are fixed in their order: repeated calls give identical bits.  Any N, K; rows may start anywhere (16-byte
+   aligned rows are read faster). */
+typedef struct {
+    int64_t N, K;      /* 1 .. 2^18, 1 .. 2^16 (LQ_ERR_SHAPE)                                             */
+    int32_t group;     /* values along K per scale: 32 | 64 | 128; the last group of a row may be shorter */
+    int32_t x_dtype;   /* lq_dtype of X, dX                                                               */
+    int32_t y_dtype;   /* lq_dtype of Y, dY                                                               */
+    int32_t flags;     /* 0                                                                               */
+} lq_w4_config;
+
+/* Bytes of the packed weights.  Host-only. */
+lq_status lq_w4_sizes(const lq_w4_config *cfg, size_t *packed_bytes);
+
+/* Pack W (device, N x K fp32 dense, finite) by the INT family's rule: s = amax / 7 of the group, c = rne(w 7 / amax) (s = 1 for a group of zeros).  packed: device,
+   256-byte aligned.  It depends on N, K and group alone. */
+lq_status lq_w4_pack(const lq_w4_config *cfg, const float *W, void *packed, size_t packed_bytes, void *stream);
+/* Pack codes (device, N x K int8 dense; beyond -7 .. 7 the nearer end) and scales (N x ceil(K / group) fp32 dense, finite, any sign) that are there. */
+lq_status lq_w4_pack_codes(const lq_w4_config *cfg, const int8_t *codes, const float *scales, void *packed, size_t packed_bytes, void *stream);
+/* Their plain views; either may be NULL. */
+lq_status lq_w4_unpack(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, int8_t *codes, float *scales, void *stream);
+
+/* X: M x K, row stride ldx elements (>= K), Y: M x N, row stride ldy; below 2^40; 0 <= M <= 2^14.  bias: N fp32 or NULL.  Y must not overlap X. */
+lq_status lq_w4_fwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy,
+                    int64_t M, void *stream);
+
+/* Bytes of the gradient's workspace (may be 0).  Host-only. */
+lq_status lq_w4_work_sizes(const lq_w4_config *cfg, int64_t M, size_t *work_bytes);
+/* work: 256-byte aligned; may be NULL where lq_w4_work_sizes reports 0. */
+lq_status lq_w4_bwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *dY, int64_t lddy, void *dX, int64_t lddx, int64_t M, void *work,
+                    size_t work_bytes, void *stream);
+
+/* ---- Norms before and after a block, with its gate, residual scale and modulation ---------------------------------
+   What lies between two blocks, row by row; s is the row's sequence:
+       h' = res_scale h + gate[s] post(y) w_post              (without a branch y: h' = h, which is not written)
+       x  = pre(h') w_pre (1 + scale[s]) + shift[s]            (from h' before its rounding)
+   LQ_NORM_NONE: z;  LQ_NORM_RMS: z / sqrt(mean(z^2) + eps);  LQ_NORM_LAYER: (z - mean z) / sqrt(var z + eps), var the mean of squared differences.
+   Everything is held in fp32 and rounded once.  Not a number stays in its row (and in the gradients of its sequence). */
+typedef struct {
+    int32_t dim;        /* of a row: 1 .. 16384                                                              */
+    int32_t post, pre;  /* lq_norm of the branch's output before it is added; of the sum for the next block  */
+    int32_t h_dtype;    /* lq_dtype of h, h' and their gradients                                             */
+    int32_t y_dtype;    /* lq_dtype of y, x and their gradients; fp32 with an fp32 stream only               */
+    int32_t flags;      /* 0                                                                                 */
+    float eps;          /* > 0 (with a norm)                                                                 */
+    float res_scale;    /* finite                                                                            */
+} lq_block_config;
+
+/* A vector of dim values for each sequence: that of s at p + s * ld (fp32; ld >= dim).  p = NULL: gate and scaling of 1, shift of 0; an output that is not wanted. */
+typedef struct {
+    const float *p;
+    int64_t ld;
+} lq_mod;
+typedef struct {
+    float *p;
+    int64_t ld;
+} lq_mod_out;
+
+/* Rows of M, strides in elements (>= dim, below 2^40), pointers aligned to their type.  y, ldy, ho: NULL without a branch; x: NULL where no block follows.  ho may be h, x may be y
+   (same pointer and stride); outputs must not overlap otherwise.  offsets: device, S + 1 int32: sequence s has the rows offsets[s] .. offsets[s + 1] - 1, rising; a sequence may have no
+   rows; rows before the first and behind the last sequence are left as they were.  NULL: one sequence of all rows (S = 1).  gate, scale, shift: the structures may be NULL, too.  w_post, w_pre: dim
+   fp32, or NULL for ones.  0 <= M <= 2^24, 1 <= S <= 2^20. */
+lq_status lq_block_norm_fwd(const lq_block_config *cfg, const void *h, int64_t ldh, const void *y, int64_t ldy, const int32_t *offsets, int32_t S,
+                            const lq_mod *gate, const lq_mod *scale, const lq_mod *shift, const float *w_post, const float *w_pre, void *ho,
+                            int64_t ldho, void *x, int64_t ldx, int64_t M, void *stream);
+
+/* Bytes of the gradient's workspace.  Host-only. */
+lq_status lq_block_work_sizes(const lq_block_config *cfg, int64_t M, int32_t S, size_t *work_bytes);
+
+/* Gradients.  With n = pre(h'), p = post(y) before their weights, dho the derivative of a loss with respect to h' (what comes through the stream) and dx that with respect to x:
+       G = dho + (pre's gradient at h') (dx w_pre (1 + scale[s]))
+       dh = res_scale G ,  dy = (post's gradient at y) (G gate[s] w_post)
+       dshift[s] = sum dx ,  dscale[s] = w_pre sum dx n ,  dgate[s] = w_post sum G p    over the rows of s (zeros for a sequence without rows)
+       dw_pre = sum dx (1 + scale[s]) n ,  dw_post = sum G gate[s] p                     over all rows of sequences
+   ho: the forward's h'.  dho or dx may be NULL (zero): without dx, h' is not looked at; without y, dy, dgate and dw_post must be NULL.  dh, dy and every gradient of modulation and
+   weights may be NULL.  dh may be dho, dy may be dx (same pointer and stride).  work: 256-byte aligned.  Sums are fixed in their order: repeated calls give identical bits. */
+typedef struct {
+    void *dh;
+    int64_t lddh;
+    void *dy;
+    int64_t lddy;
+    lq_mod_out dgate, dscale, dshift;
+    float *dw_post, *dw_pre;
+} lq_block_grads;
+lq_status lq_block_norm_bwd(const lq_block_config *cfg, const void *ho, int64_t ldho, const void *y, int64_t ldy, const int32_t *offsets, int32_t S,
+                            const lq_mod *gate, const lq_mod *scale, const float *w_post, const float *w_pre, const void *dho, int64_t lddho,
+                            const void *dx, int64_t lddx, const lq_block_grads *out, int64_t M, void *work, size_t work_bytes, void *stream);
+
+/* ---- AdamW step over many tensors --------------------------------------------------------------------------------
+       g = grad_scale grad ;  m = beta1 m + (1 - beta1) g ;  v = beta2 v + (1 - beta2) g^2
+       p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+   in fp32, every operation rounded by itself, rounded once more where p is bf16.  A launch for every 64 tensors.
+   state_bits = 8: m and the root of v are E4M3 elements (a byte each) times a power of two for each 256 consecutive values of a tensor, the smallest with which the largest of them is
+   448 or below (1 for zeros).  They are rounded up or down at random with their mean kept, by numbers that depend on seed, t and the value's place (tensors one after another, each
+   from a multiple of 256 on), so that a step repeated on the same state gives the same bits; a root above zero is not rounded to zero.  A gradient that is not finite makes the states of its 256
+   values NaN.  A tensor's first states are zeros, its first scales ones. */
+typedef struct {
+    int32_t p_dtype, g_dtype;  /* lq_dtype of parameters and of gradients                             */
+    int32_t state_bits;        /* 32 (fp32) | 8                                                       */
+    int32_t flags;             /* 0                                                                   */
+    double beta1, beta2;       /* in [0, 1)                                                           */
+    double eps, weight_decay;  /* > 0, >= 0                                                           */
+    uint32_t seed;             /* of the rounding                                                     */
+    uint32_t reserved;         /* 0                                                                   */
+} lq_adamw_config;
+
+typedef struct {       /* device memory, aligned to its type; n consecutive values of each         */
+    void *p;           /* parameter, updated                                                       */
+    float *master;     /* fp32 copy that is updated in its place (p receives its rounding), or NULL */
+    const void *grad;
+    void *m, *v;       /* states: fp32, or bytes                                                   */
+    float *scales;     /* state_bits = 8: ceil(n / 256) x 2 (of m, of v's root); otherwise NULL    */
+    int64_t n;         /* 0 .. 2^32                                                                */
+} lq_adamw_tensor;
+
+typedef struct {
+    double lr;                  /* used where lr_dev is NULL                                         */
+    int64_t step;               /* t: 1 for the first step (1 .. 2^31 - 1); used where step_dev is NULL */
+    const float *lr_dev;        /* device, one value each, or NULL: read by the kernels, so that a captured step can be replayed with others */
+    const int32_t *step_dev;    /* (taken as 1 below 1)                                              */
+    const float *grad_scale;    /* device, one value, or NULL for 1                                  */
+} lq_adamw_args;
+
+/* tensors: host, `count` of them (0 .. 65536).  What a call writes must not overlap (LQ_ERR_SHAPE: the same tensor twice, views that share values). */
+lq_status lq_adamw_step(const lq_adamw_config *cfg, const lq_adamw_tensor *tensors, int32_t count, const lq_adamw_args *args, void *stream);
 
 #ifdef __cplusplus
 }

@@ -103,7 +103,7 @@ class lq_adapter_pool(C.Structure):
 
 
 LQ_PAIR_HALF, LQ_PAIR_ADJACENT = 0, 1
-LQ_NORM_NONE, LQ_NORM_RMS = 0, 1
+LQ_NORM_NONE, LQ_NORM_RMS, LQ_NORM_LAYER = 0, 1, 2
 
 
 class lq_qk_config(C.Structure):
@@ -117,12 +117,47 @@ class lq_heads(C.Structure):
 
 _call.set_operator_config_types(lq_adapter_config, lq_qk_config)
 
+
+class lq_w4_config(C.Structure):
+    _fields_ = [("N", C.c_int64), ("K", C.c_int64)] + [(k, C.c_int32) for k in ("group", "x_dtype", "y_dtype", "flags")]
+
+
+class lq_block_config(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("dim", "post", "pre", "h_dtype", "y_dtype", "flags")] + [("eps", C.c_float), ("res_scale", C.c_float)]
+
+
+class lq_mod(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("ld", C.c_int64)]
+
+
+class lq_block_grads(C.Structure):
+    _fields_ = [("dh", C.c_void_p), ("lddh", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("dgate", lq_mod), ("dscale", lq_mod), ("dshift", lq_mod),
+                ("dw_post", C.c_void_p), ("dw_pre", C.c_void_p)]
+
+
+class lq_adamw_config(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("p_dtype", "g_dtype", "state_bits", "flags")] + [(k, C.c_double) for k in ("beta1", "beta2", "eps", "weight_decay")] + \
+               [("seed", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class lq_adamw_tensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("p", "master", "grad", "m", "v", "scales")] + [("n", C.c_int64)]
+
+
+class lq_adamw_args(C.Structure):
+    _fields_ = [("lr", C.c_double), ("step", C.c_int64), ("lr_dev", C.c_void_p), ("step_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
+
+
+_call.set_block_config_types(lq_w4_config, lq_block_config, lq_adamw_config)
+
 EXPORTS = ["lq_status_string", "lq_packed_sizes", "lq_pack_weights", "lq_verify_blob", "lq_set_smoothing", "lq_act_sizes", "lq_quantize_act",
            "lq_linear_lowrank_fwd", "lq_handoff_sizes", "lq_linear_lowrank_fwd_handoff", "lq_branch_from_codes",
            "lq_unpack_weights", "lq_unpack_act", "lq_calib_sizes", "lq_calib_init", "lq_calib_step",
            "lq_calib_unpack", "lq_rot_sizes", "lq_rot_init", "lq_rot_step", "lq_rot_step_static", "lq_rot_apply", "lq_rot_unpack",
            "lq_adapter_plan_sizes", "lq_adapter_plan", "lq_adapter_verify_plan", "lq_adapter_sizes", "lq_adapter_fwd", "lq_adapter_bwd",
-           "lq_qk_norm_rope_fwd", "lq_qk_work_sizes", "lq_qk_norm_rope_bwd"]
+           "lq_qk_norm_rope_fwd", "lq_qk_work_sizes", "lq_qk_norm_rope_bwd",
+           "lq_w4_sizes", "lq_w4_pack", "lq_w4_pack_codes", "lq_w4_unpack", "lq_w4_fwd", "lq_w4_work_sizes", "lq_w4_bwd",
+           "lq_block_norm_fwd", "lq_block_work_sizes", "lq_block_norm_bwd", "lq_adamw_step"]
 
 _lib.lq_calib_sizes.argtypes = [C.POINTER(lq_config), C.POINTER(C.c_size_t)]
 _lib.lq_calib_init.argtypes = [C.POINTER(lq_config), C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -171,6 +206,21 @@ _lib.lq_qk_norm_rope_fwd.argtypes = [C.POINTER(lq_qk_config), _H, _H, C.c_void_p
 _lib.lq_qk_work_sizes.argtypes = [C.POINTER(lq_qk_config), C.c_int64, C.POINTER(C.c_size_t)]
 _lib.lq_qk_norm_rope_bwd.argtypes = [C.POINTER(lq_qk_config), _H, _H, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, _H, _H, _H, _H,
                                      C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_W4, _MOD = C.POINTER(lq_w4_config), C.POINTER(lq_mod)
+_lib.lq_w4_sizes.argtypes = [_W4, C.POINTER(C.c_size_t)]
+_lib.lq_w4_pack.argtypes = [_W4, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_w4_pack_codes.argtypes = [_W4, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_w4_unpack.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.lq_w4_fwd.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
+_lib.lq_w4_work_sizes.argtypes = [_W4, C.c_int64, C.POINTER(C.c_size_t)]
+_lib.lq_w4_bwd.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.lq_block_norm_fwd.argtypes = [C.POINTER(lq_block_config), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, _MOD, _MOD, _MOD,
+                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
+_lib.lq_block_work_sizes.argtypes = [C.POINTER(lq_block_config), C.c_int64, C.c_int32, C.POINTER(C.c_size_t)]
+_lib.lq_block_norm_bwd.argtypes = [C.POINTER(lq_block_config), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, _MOD, _MOD, C.c_void_p,
+                                   C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(lq_block_grads), C.c_int64, C.c_void_p, C.c_size_t,
+                                   C.c_void_p]
+_lib.lq_adamw_step.argtypes = [C.POINTER(lq_adamw_config), C.POINTER(lq_adamw_tensor), C.c_int32, C.POINTER(lq_adamw_args), C.c_void_p]
 
 
 class LqError(RuntimeError):
@@ -783,3 +833,253 @@ def lq_qk_norm_rope_bwd(cfg: lq_qk_config, q: Optional[torch.Tensor], k: Optiona
                                     _heads(cfg, dko, M, cfg.heads_k, "dko"), _heads(cfg, dq, M, cfg.heads_q, "dq"), _heads(cfg, dk, M, cfg.heads_k, "dk"),
                                     _ptr(dwq), _ptr(dwk), M, _ptr(work), 0 if work is None else work.numel(), _stream()), "lq_qk_norm_rope_bwd")
     return dq, dk, dwq, dwk
+
+
+# ---- product of a few rows with 4-bit weights (argument marshalling only) ----------------------------------------------
+
+_DTYPES = {"bf16": LQ_BF16, "f32": LQ_F32}
+_TORCH = {LQ_BF16: torch.bfloat16, LQ_F32: torch.float32}
+
+
+def make_w4_config(N: int, K: int, group: int = 64, x_dtype: str = "bf16", y_dtype: str = "bf16") -> lq_w4_config:
+    """A K -> N layer of 4-bit weights with a scale for each `group` (32, 64, 128) values along K; x_dtype of the rows that go in (and of their gradient), y_dtype of
+    those that come out."""
+    return lq_w4_config(N, K, group, _DTYPES[x_dtype], _DTYPES[y_dtype], 0)
+
+
+def lq_w4_sizes(cfg: lq_w4_config) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.lq_w4_sizes(C.byref(cfg), C.byref(n)), "lq_w4_sizes")
+    return int(n.value)
+
+
+def lq_w4_work_sizes(cfg: lq_w4_config, M: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.lq_w4_work_sizes(C.byref(cfg), M, C.byref(n)), "lq_w4_work_sizes")
+    return int(n.value)
+
+
+def _dense_arg(t: torch.Tensor, dtype, shape, what: str) -> torch.Tensor:
+    assert t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(), f"{what}: {shape} {dtype}, contiguous"
+    return t
+
+
+def lq_w4_pack(cfg: lq_w4_config, W: torch.Tensor, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """W: N x K fp32 CUDA, contiguous.  Returns the packed weights (codes by the INT family's rule)."""
+    _dense_arg(W, torch.float32, (cfg.N, cfg.K), "W")
+    if packed is None:
+        packed = torch.empty(lq_w4_sizes(cfg), dtype=torch.uint8, device=W.device)
+    _check(_lib.lq_w4_pack(C.byref(cfg), _ptr(W), _ptr(_blob_arg(packed)), packed.numel(), _stream()), "lq_w4_pack")
+    return packed
+
+
+def lq_w4_pack_codes(cfg: lq_w4_config, codes: torch.Tensor, scales: torch.Tensor, packed: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """codes: N x K int8 (-7 .. 7), scales: N x ceil(K / group) fp32.  Returns the packed weights."""
+    _dense_arg(codes, torch.int8, (cfg.N, cfg.K), "codes")
+    _dense_arg(scales, torch.float32, (cfg.N, -(-cfg.K // cfg.group)), "scales")
+    if packed is None:
+        packed = torch.empty(lq_w4_sizes(cfg), dtype=torch.uint8, device=codes.device)
+    _check(_lib.lq_w4_pack_codes(C.byref(cfg), _ptr(codes), _ptr(scales), _ptr(_blob_arg(packed)), packed.numel(), _stream()), "lq_w4_pack_codes")
+    return packed
+
+
+def lq_w4_unpack(cfg: lq_w4_config, packed: torch.Tensor):
+    """(codes, scales) of packed weights."""
+    codes = torch.empty((cfg.N, cfg.K), dtype=torch.int8, device=packed.device)
+    scales = torch.empty((cfg.N, -(-cfg.K // cfg.group)), dtype=torch.float32, device=packed.device)
+    _check(_lib.lq_w4_unpack(C.byref(cfg), _ptr(_blob_arg(packed)), packed.numel(), _ptr(codes), _ptr(scales), _stream()), "lq_w4_unpack")
+    return codes, scales
+
+
+def lq_w4_fwd(cfg: lq_w4_config, packed: torch.Tensor, X: torch.Tensor, bias: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = X W^T + bias.  X: M x K of cfg's x type, Y: M x N of its y type (rows may be further apart); bias: N fp32."""
+    st = _call.w4_fwd(cfg, packed, X, bias, Y)
+    if st >= 0:
+        _check(st, "lq_w4_fwd")
+        return Y
+    M = X.shape[0]
+    _rows_arg(X, _TORCH[cfg.x_dtype], M, cfg.K, "X")
+    if bias is not None:
+        _dense_arg(bias, torch.float32, (cfg.N,), "bias")
+    if Y is None:
+        Y = torch.empty((M, cfg.N), dtype=_TORCH[cfg.y_dtype], device=X.device)
+    _rows_arg(Y, _TORCH[cfg.y_dtype], M, cfg.N, "Y")
+    _check(_lib.lq_w4_fwd(C.byref(cfg), _ptr(_blob_arg(packed)), packed.numel(), _ptr(X), _ld(X), _ptr(bias), _ptr(Y), _ld(Y), M, _stream()), "lq_w4_fwd")
+    return Y
+
+
+def lq_w4_bwd(cfg: lq_w4_config, packed: torch.Tensor, dY: torch.Tensor, dX: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """dX = dY W.  dY: M x N of cfg's y type, dX: M x K of its x type."""
+    st = _call.w4_bwd(cfg, packed, dY, dX, work)
+    if st >= 0:
+        _check(st, "lq_w4_bwd")
+        return dX
+    M = dY.shape[0]
+    _rows_arg(dY, _TORCH[cfg.y_dtype], M, cfg.N, "dY")
+    if dX is None:
+        dX = torch.empty((M, cfg.K), dtype=_TORCH[cfg.x_dtype], device=dY.device)
+    _rows_arg(dX, _TORCH[cfg.x_dtype], M, cfg.K, "dX")
+    if work is None:
+        work = torch.empty(lq_w4_work_sizes(cfg, M), dtype=torch.uint8, device=dY.device)
+    _check(_lib.lq_w4_bwd(C.byref(cfg), _ptr(_blob_arg(packed)), packed.numel(), _ptr(dY), _ld(dY), _ptr(dX), _ld(dX), M, _ptr(_blob_arg(work)), work.numel(),
+                          _stream()), "lq_w4_bwd")
+    return dX
+
+
+# ---- norms before and after a block (argument marshalling only) --------------------------------------------------------
+
+_NORMS = {"none": LQ_NORM_NONE, "rms": LQ_NORM_RMS, "layer": LQ_NORM_LAYER}
+
+
+def make_block_config(dim: int, post: str = "none", pre: str = "layer", eps: float = 1e-6, res_scale: float = 1.0, h_dtype: str = "bf16",
+                      y_dtype: str = "bf16") -> lq_block_config:
+    """post, pre: norm of a block's output before it is added, of the sum for the next block ("none", "rms", "layer").  h_dtype: of the stream, y_dtype: of what goes into
+    and comes out of blocks."""
+    return lq_block_config(dim, _NORMS[post], _NORMS[pre], _DTYPES[h_dtype], _DTYPES[y_dtype], 0, eps, res_scale)
+
+
+def lq_block_work_sizes(cfg: lq_block_config, M: int, S: int = 1) -> int:
+    n = C.c_size_t(0)
+    _check(_lib.lq_block_work_sizes(C.byref(cfg), M, S, C.byref(n)), "lq_block_work_sizes")
+    return int(n.value)
+
+
+def _sequences(offsets: Optional[torch.Tensor]) -> int:
+    if offsets is None:
+        return 1
+    assert offsets.is_cuda and offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous() and offsets.shape[0] >= 2, "offsets: sequences + 1 int32"
+    return offsets.shape[0] - 1
+
+
+def _mod(t: Optional[torch.Tensor], S: int, dim: int, what: str) -> lq_mod:
+    if t is None:
+        return lq_mod(None, 0)
+    _rows_arg(t, torch.float32, S, dim, what)
+    return lq_mod(_ptr(t), _ld(t))
+
+
+def _opt_rows(t: Optional[torch.Tensor], dtype, M: int, dim: int, what: str):
+    if t is None:
+        return None, 0
+    _rows_arg(t, dtype, M, dim, what)
+    return _ptr(t), _ld(t)
+
+
+def _opt_vec(t: Optional[torch.Tensor], dim: int, what: str):
+    if t is not None:
+        _dense_arg(t, torch.float32, (dim,), what)
+    return _ptr(t)
+
+
+def lq_block_norm_fwd(cfg: lq_block_config, h: torch.Tensor, y: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                      gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
+                      w_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None, ho: Optional[torch.Tensor] = None,
+                      x: Optional[torch.Tensor] = None, last: bool = False):
+    """(ho, x): ho = res_scale h + gate post(y) w_post (None without y), x = pre(ho) w_pre (1 + scale) + shift (None with last=True).  h, y: M x dim; offsets: int32,
+    the first row of each sequence and the end of the last (rows of no sequence stay as they are in ho and x; None: one sequence); gate, scale, shift: one row of dim fp32
+    values for each sequence (rows may be further apart, as slices of one layer's output); w_post, w_pre: dim fp32.  ho may be h, x may be y."""
+    st = _call.block_norm_fwd(cfg, h, y, offsets, gate, scale, shift, w_post, w_pre, ho, x, last)
+    if st >= 0:
+        _check(st, "lq_block_norm_fwd")
+        return ho, x
+    M, D, S = h.shape[0], cfg.dim, _sequences(offsets)
+    ht, yt = _TORCH[cfg.h_dtype], _TORCH[cfg.y_dtype]
+    assert not (y is None and ho is not None) and not (last and x is not None), "no output without its part"
+    if y is not None and ho is None:
+        ho = torch.empty((M, D), dtype=ht, device=h.device)
+    if x is None and not last:
+        x = torch.empty((M, D), dtype=yt, device=h.device)
+    mods = [_mod(t, S, D, n) for t, n in ((gate, "gate"), (scale, "scale"), (shift, "shift"))]
+    _check(_lib.lq_block_norm_fwd(C.byref(cfg), *_opt_rows(h, ht, M, D, "h"), *_opt_rows(y, yt, M, D, "y"), _ptr(offsets), S, *map(C.byref, mods),
+                                  _opt_vec(w_post, D, "w_post"), _opt_vec(w_pre, D, "w_pre"), *_opt_rows(ho, ht, M, D, "ho"), *_opt_rows(x, yt, M, D, "x"), M,
+                                  _stream()), "lq_block_norm_fwd")
+    return ho, x
+
+
+def lq_block_norm_bwd(cfg: lq_block_config, ho: Optional[torch.Tensor], y: Optional[torch.Tensor], offsets: Optional[torch.Tensor] = None,
+                      gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, w_post: Optional[torch.Tensor] = None,
+                      w_pre: Optional[torch.Tensor] = None, dho: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                      dh: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                      dscale: Optional[torch.Tensor] = None, dshift: Optional[torch.Tensor] = None, dw_post: Optional[torch.Tensor] = None,
+                      dw_pre: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None):
+    """(dh, dy, dgate, dscale, dshift, dw_post, dw_pre) of lq_block_norm_fwd from its result ho (h itself where there was no y), its y and the derivatives with respect to ho
+    and x (either may be None).  dh may be dho, dy may be dx.  Gradients of gate, scale (with shift) and the weights are made where these are given, or where a tensor for them is."""
+    st = _call.block_norm_bwd(cfg, ho, y, offsets, gate, scale, w_post, w_pre, dho, dx, dh, dy, dgate, dscale, dshift, dw_post, dw_pre, work)
+    if st >= 0:
+        _check(st, "lq_block_norm_bwd")
+        return dh, dy, dgate, dscale, dshift, dw_post, dw_pre
+    first = dx if dx is not None else dho
+    assert first is not None, "dho or dx is needed"
+    M, D, S, device = first.shape[0], cfg.dim, _sequences(offsets), first.device
+    ht, yt = _TORCH[cfg.h_dtype], _TORCH[cfg.y_dtype]
+    dh = torch.empty((M, D), dtype=ht, device=device) if dh is None else dh
+    if y is not None:
+        dy = torch.empty((M, D), dtype=yt, device=device) if dy is None else dy
+
+    def wanted(out, given, shape):
+        return torch.empty(shape, dtype=torch.float32, device=device) if out is None and given is not None else out
+    dgate, dw_post = wanted(dgate, gate if y is not None else None, (S, D)), wanted(dw_post, w_post if y is not None else None, (D,))
+    dscale, dshift, dw_pre = wanted(dscale, scale, (S, D)), wanted(dshift, scale, (S, D)), wanted(dw_pre, w_pre, (D,))
+    if work is None:
+        work = torch.empty(lq_block_work_sizes(cfg, M, S), dtype=torch.uint8, device=device)
+    mods = [_mod(t, S, D, n) for t, n in ((gate, "gate"), (scale, "scale"))]
+    out = lq_block_grads(*_opt_rows(dh, ht, M, D, "dh"), *_opt_rows(dy, yt, M, D, "dy"), _mod(dgate, S, D, "dgate"), _mod(dscale, S, D, "dscale"),
+                         _mod(dshift, S, D, "dshift"), _opt_vec(dw_post, D, "dw_post"), _opt_vec(dw_pre, D, "dw_pre"))
+    _check(_lib.lq_block_norm_bwd(C.byref(cfg), *_opt_rows(ho, ht, M, D, "ho"), *_opt_rows(y, yt, M, D, "y"), _ptr(offsets), S, *map(C.byref, mods),
+                                  _opt_vec(w_post, D, "w_post"), _opt_vec(w_pre, D, "w_pre"), *_opt_rows(dho, ht, M, D, "dho"), *_opt_rows(dx, yt, M, D, "dx"),
+                                  C.byref(out), M, _ptr(_blob_arg(work)), work.numel(), _stream()), "lq_block_norm_bwd")
+    return dh, dy, dgate, dscale, dshift, dw_post, dw_pre
+
+
+# ---- AdamW step over many tensors (argument marshalling only) ----------------------------------------------------------
+
+def make_adamw_config(p_dtype: str = "f32", g_dtype: str = "f32", state_bits: int = 32, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                      weight_decay: float = 0.0, seed: int = 0) -> lq_adamw_config:
+    """Types of parameters and gradients; states in 32 or in 8 bits (then rounded at random, from seed)."""
+    return lq_adamw_config(_DTYPES[p_dtype], _DTYPES[g_dtype], state_bits, 0, beta1, beta2, eps, weight_decay, seed, 0)
+
+
+def adamw_states(cfg: lq_adamw_config, p: torch.Tensor):
+    """(m, v, scales) of a parameter that has made no step; scales: None with states in 32 bits."""
+    dtype = torch.float32 if cfg.state_bits == 32 else torch.float8_e4m3fn
+    m, v = (torch.zeros(p.shape, device=p.device).to(dtype) for _ in range(2))
+    return m, v, None if cfg.state_bits == 32 else torch.ones((p.numel() + 255) // 256, 2, device=p.device)
+
+
+def _one(t: torch.Tensor, dtype, what: str):
+    assert t.is_cuda and t.dtype == dtype and t.numel() == 1, f"{what}: one {dtype} CUDA value"
+    return _ptr(t)
+
+
+def lq_adamw_step(cfg: lq_adamw_config, params, grads, m, v, lr, step, scales=None, masters=None, grad_scale: Optional[torch.Tensor] = None) -> None:
+    """One step, in place.  params, grads, m, v: lists of contiguous CUDA tensors of equal sizes (parameters and gradients of cfg's types; states fp32, or float8_e4m3fn with
+    scales: ceil(n / 256) x 2 fp32 of each tensor); masters: None, or fp32 copies that are updated in the parameters' place (None for a tensor without).  lr: a number, or one
+    fp32 CUDA value; step: the number of this step from 1 on, or one int32 CUDA value (both are read by the kernels then, at every replay of a captured step);
+    grad_scale: one fp32 CUDA value that the gradients are multiplied with."""
+    st = _call.adamw_step(cfg, params, grads, m, v, lr, step, scales, masters, grad_scale)
+    if st >= 0:
+        return _check(st, "lq_adamw_step")
+    count = len(params)
+    eight = cfg.state_bits == 8
+    assert len(grads) == len(m) == len(v) == count and (masters is None or len(masters) == count), "lists of the same length"
+    assert not eight or (scales is not None and len(scales) == count), "states in 8 bits have scales"
+    st_dtype = torch.float8_e4m3fn if eight else torch.float32
+    table = (lq_adamw_tensor * count)()
+    for i in range(count):
+        n = params[i].numel()
+        master = None if masters is None else masters[i]
+        for t, dtype in ((params[i], _TORCH[cfg.p_dtype]), (grads[i], _TORCH[cfg.g_dtype]), (m[i], st_dtype), (v[i], st_dtype), (master, torch.float32)):
+            assert t is None or (t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.numel() == n), f"tensor {i}: {n} contiguous {dtype} values"
+        if eight:
+            _dense_arg(scales[i], torch.float32, ((n + 255) // 256, 2), f"scales of tensor {i}")
+        table[i] = lq_adamw_tensor(_ptr(params[i]), _ptr(master), _ptr(grads[i]), _ptr(m[i]), _ptr(v[i]), _ptr(scales[i]) if eight else None, n)
+    args = lq_adamw_args(0.0, 1, None, None, None if grad_scale is None else _one(grad_scale, torch.float32, "grad_scale"))
+    if isinstance(lr, torch.Tensor):
+        args.lr_dev = _one(lr, torch.float32, "lr")
+    else:
+        args.lr = lr
+    if isinstance(step, torch.Tensor):
+        args.step_dev = _one(step, torch.int32, "step")
+    else:
+        args.step = step
+    _check(_lib.lq_adamw_step(C.byref(cfg), table, count, C.byref(args), _stream()), "lq_adamw_step")

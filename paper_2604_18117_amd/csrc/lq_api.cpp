@@ -2,7 +2,11 @@
 // detected here, before any launch, so that all error paths can be exercised without a GPU.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
+#include <new>
+#include <utility>
+#include <vector>
 
 #include "lq_internal.h"
 
@@ -157,6 +161,18 @@ int compute_units()
 }  // namespace lq
 
 using namespace lq;
+
+// A vector for each of S sequences, or none
+template <typename MOD>
+static lq_status mod_check(const MOD* m, const lq_block_config* c, int64_t S, MOD* out)
+{
+    *out = {nullptr, 0};
+    if (!m || !m->p) return LQ_OK;
+    if (S > 1 && (m->ld < c->dim || m->ld >= ((int64_t)1 << 40))) return LQ_ERR_SHAPE;
+    if ((uintptr_t)m->p % 4 != 0) return LQ_ERR_ALIGN;
+    *out = *m;
+    return LQ_OK;
+}
 
 extern "C" {
 
@@ -765,6 +781,252 @@ lq_status lq_qk_norm_rope_bwd(const lq_qk_config* cfg, const lq_heads* q, const 
     t.dw[0] = dwq;
     t.dw[1] = dwk;
     return launch_qk_bwd(cfg, t, M, (uint8_t*)work, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+static lq_status w4_check(const lq_w4_config* c)
+{
+    if (!c) return LQ_ERR_NULL;
+    if (c->flags != 0 || (c->x_dtype != LQ_F32 && c->x_dtype != LQ_BF16) || (c->y_dtype != LQ_F32 && c->y_dtype != LQ_BF16)) return LQ_ERR_UNSUPPORTED;
+    if (c->N < 1 || c->K < 1 || c->N > (1 << 18) || c->K > (1 << 16) || (c->group != 32 && c->group != 64 && c->group != 128)) return LQ_ERR_SHAPE;
+    return LQ_OK;
+}
+static lq_status w4_packed_check(const lq_w4_config* c, const void* packed, size_t packed_bytes)
+{
+    if (!packed) return LQ_ERR_NULL;
+    if (!aligned(packed, 256)) return LQ_ERR_ALIGN;
+    return packed_bytes < w4_packed_bytes(c) ? LQ_ERR_BUFFER_TOO_SMALL : LQ_OK;
+}
+// M rows of `len` values that may start anywhere; the stride of a single row says nothing
+static lq_status any_rows_check(const void* p, int64_t ld, int64_t len, int64_t M, int elem)
+{
+    if (!p) return LQ_ERR_NULL;
+    if (M > 1 && (ld < len || ld >= ((int64_t)1 << 40))) return LQ_ERR_SHAPE;
+    return aligned(p, elem) ? LQ_OK : LQ_ERR_ALIGN;
+}
+static int dtype_bytes(int32_t dtype) { return dtype == LQ_F32 ? 4 : 2; }
+
+lq_status lq_w4_sizes(const lq_w4_config* cfg, size_t* packed_bytes)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK) return st;
+    if (!packed_bytes) return LQ_ERR_NULL;
+    *packed_bytes = w4_packed_bytes(cfg);
+    return LQ_OK;
+}
+
+lq_status lq_w4_pack(const lq_w4_config* cfg, const float* W, void* packed, size_t packed_bytes, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK) return st;
+    if (!W) return LQ_ERR_NULL;
+    if (!aligned(W, 4)) return LQ_ERR_ALIGN;
+    return launch_w4_pack(cfg, W, nullptr, nullptr, (uint8_t*)packed, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_w4_pack_codes(const lq_w4_config* cfg, const int8_t* codes, const float* scales, void* packed, size_t packed_bytes, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK) return st;
+    if (!codes || !scales) return LQ_ERR_NULL;
+    if (!aligned(scales, 4)) return LQ_ERR_ALIGN;
+    return launch_w4_pack(cfg, nullptr, codes, scales, (uint8_t*)packed, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_w4_unpack(const lq_w4_config* cfg, const void* packed, size_t packed_bytes, int8_t* codes, float* scales, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK) return st;
+    if (!aligned(scales, 4)) return LQ_ERR_ALIGN;
+    if (!codes && !scales) return LQ_OK;
+    return launch_w4_unpack(cfg, (const uint8_t*)packed, codes, scales, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+static lq_status w4_batch_check(int64_t M) { return M < 0 || M > (1 << 14) ? LQ_ERR_SHAPE : LQ_OK; }
+
+lq_status lq_w4_fwd(const lq_w4_config* cfg, const void* packed, size_t packed_bytes, const void* X, int64_t ldx, const float* bias, void* Y, int64_t ldy,
+                    int64_t M, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_batch_check(M)) != LQ_OK) return st;
+    if (M == 0) return LQ_OK;  // an empty batch
+    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(X, ldx, cfg->K, M, dtype_bytes(cfg->x_dtype))) != LQ_OK ||
+        (st = any_rows_check(Y, ldy, cfg->N, M, dtype_bytes(cfg->y_dtype))) != LQ_OK)
+        return st;
+    if (!aligned(bias, 4)) return LQ_ERR_ALIGN;
+    return launch_w4_fwd(cfg, (const uint8_t*)packed, X, ldx, bias, Y, ldy, M, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_w4_work_sizes(const lq_w4_config* cfg, int64_t M, size_t* work_bytes)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_batch_check(M)) != LQ_OK) return st;
+    if (!work_bytes) return LQ_ERR_NULL;
+    *work_bytes = w4_work_bytes(cfg, M);
+    return LQ_OK;
+}
+
+lq_status lq_w4_bwd(const lq_w4_config* cfg, const void* packed, size_t packed_bytes, const void* dY, int64_t lddy, void* dX, int64_t lddx, int64_t M, void* work,
+                    size_t work_bytes, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_batch_check(M)) != LQ_OK) return st;
+    if (M == 0) return LQ_OK;  // an empty batch
+    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(dY, lddy, cfg->N, M, dtype_bytes(cfg->y_dtype))) != LQ_OK ||
+        (st = any_rows_check(dX, lddx, cfg->K, M, dtype_bytes(cfg->x_dtype))) != LQ_OK)
+        return st;
+    const size_t need = w4_work_bytes(cfg, M);
+    if (need && !work) return LQ_ERR_NULL;
+    if (need && !aligned(work, 256)) return LQ_ERR_ALIGN;
+    if (work_bytes < need) return LQ_ERR_BUFFER_TOO_SMALL;
+    return launch_w4_bwd(cfg, (const uint8_t*)packed, dY, lddy, dX, lddx, M, (uint8_t*)work, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+static bool norm_known(int32_t n) { return n == LQ_NORM_NONE || n == LQ_NORM_RMS || n == LQ_NORM_LAYER; }
+static lq_status block_check(const lq_block_config* c, int64_t M, int64_t S, bool offsets)
+{
+    if (!c) return LQ_ERR_NULL;
+    if (c->flags != 0 || !norm_known(c->post) || !norm_known(c->pre) || (c->h_dtype != LQ_F32 && c->h_dtype != LQ_BF16) ||
+        (c->y_dtype != LQ_F32 && c->y_dtype != LQ_BF16) || (c->h_dtype == LQ_BF16 && c->y_dtype == LQ_F32))
+        return LQ_ERR_UNSUPPORTED;
+    if ((c->post != LQ_NORM_NONE || c->pre != LQ_NORM_NONE) && !(c->eps > 0.f)) return LQ_ERR_UNSUPPORTED;
+    if (!(c->res_scale - c->res_scale == 0.f)) return LQ_ERR_UNSUPPORTED;  // not finite
+    if (c->dim < 1 || c->dim > 16384 || M < 0 || M > (1 << 24) || S < 1 || S > (1 << 20) || (!offsets && S != 1)) return LQ_ERR_SHAPE;
+    return LQ_OK;
+}
+lq_status lq_block_norm_fwd(const lq_block_config* cfg, const void* h, int64_t ldh, const void* y, int64_t ldy, const int32_t* offsets, int32_t S,
+                            const lq_mod* gate, const lq_mod* scale, const lq_mod* shift, const float* w_post, const float* w_pre, void* ho,
+                            int64_t ldho, void* x, int64_t ldx, int64_t M, void* stream)
+{
+    lq_status st = block_check(cfg, M, S, offsets != nullptr);
+    if (st != LQ_OK) return st;
+    BlockTensors t{};
+    if ((st = mod_check(gate, cfg, S, &t.gate)) != LQ_OK || (st = mod_check(scale, cfg, S, &t.scale)) != LQ_OK || (st = mod_check(shift, cfg, S, &t.shift)) != LQ_OK) return st;
+    if (!aligned(offsets, 4) || !aligned(w_post, 4) || !aligned(w_pre, 4)) return LQ_ERR_ALIGN;
+    if (M == 0) return LQ_OK;  // an empty batch
+    const int he = dtype_bytes(cfg->h_dtype), ye = dtype_bytes(cfg->y_dtype);
+    if ((!y) != (!ho) || (!y && !x)) return LQ_ERR_NULL;
+    if ((st = any_rows_check(h, ldh, cfg->dim, M, he)) != LQ_OK || (y && (st = any_rows_check(y, ldy, cfg->dim, M, ye)) != LQ_OK) ||
+        (ho && (st = any_rows_check(ho, ldho, cfg->dim, M, he)) != LQ_OK) || (x && (st = any_rows_check(x, ldx, cfg->dim, M, ye)) != LQ_OK))
+        return st;
+    t.h = h;
+    t.ldh = ldh;
+    t.y = y;
+    t.ldy = ldy;
+    t.offsets = offsets;
+    t.S = S;
+    t.w_post = w_post;
+    t.w_pre = w_pre;
+    t.ho = ho;
+    t.ldho = ldho;
+    t.x = x;
+    t.ldx = ldx;
+    return launch_block_fwd(cfg, t, M, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+lq_status lq_block_work_sizes(const lq_block_config* cfg, int64_t M, int32_t S, size_t* work_bytes)
+{
+    lq_status st = block_check(cfg, M, S, true);
+    if (st != LQ_OK) return st;
+    if (!work_bytes) return LQ_ERR_NULL;
+    *work_bytes = block_work_bytes(cfg, M, S);
+    return LQ_OK;
+}
+
+lq_status lq_block_norm_bwd(const lq_block_config* cfg, const void* ho, int64_t ldho, const void* y, int64_t ldy, const int32_t* offsets, int32_t S,
+                            const lq_mod* gate, const lq_mod* scale, const float* w_post, const float* w_pre, const void* dho, int64_t lddho,
+                            const void* dx, int64_t lddx, const lq_block_grads* out, int64_t M, void* work, size_t work_bytes, void* stream)
+{
+    lq_status st = block_check(cfg, M, S, offsets != nullptr);
+    if (st != LQ_OK) return st;
+    if (!out) return LQ_ERR_NULL;
+    BlockTensors t{};
+    if ((st = mod_check(gate, cfg, S, &t.gate)) != LQ_OK || (st = mod_check(scale, cfg, S, &t.scale)) != LQ_OK ||
+        (st = mod_check(&out->dgate, cfg, S, &t.dgate)) != LQ_OK || (st = mod_check(&out->dscale, cfg, S, &t.dscale)) != LQ_OK ||
+        (st = mod_check(&out->dshift, cfg, S, &t.dshift)) != LQ_OK)
+        return st;
+    if (!aligned(offsets, 4) || !aligned(w_post, 4) || !aligned(w_pre, 4) || !aligned(out->dw_post, 4) || !aligned(out->dw_pre, 4)) return LQ_ERR_ALIGN;
+    const int he = dtype_bytes(cfg->h_dtype), ye = dtype_bytes(cfg->y_dtype);
+    if (M > 0) {
+        if (!dho && !dx) return LQ_ERR_NULL;
+        if (!y && (out->dy || t.dgate.p || out->dw_post)) return LQ_ERR_NULL;
+        if ((dx && ((st = any_rows_check(dx, lddx, cfg->dim, M, ye)) != LQ_OK || (st = any_rows_check(ho, ldho, cfg->dim, M, he)) != LQ_OK)) ||
+            (dho && (st = any_rows_check(dho, lddho, cfg->dim, M, he)) != LQ_OK) || (y && (st = any_rows_check(y, ldy, cfg->dim, M, ye)) != LQ_OK) ||
+            (out->dh && (st = any_rows_check(out->dh, out->lddh, cfg->dim, M, he)) != LQ_OK) ||
+            (out->dy && (st = any_rows_check(out->dy, out->lddy, cfg->dim, M, ye)) != LQ_OK))
+            return st;
+    }
+    if (t.dgate.p || t.dscale.p || t.dshift.p || out->dw_post || out->dw_pre) {
+        if (!work) return LQ_ERR_NULL;
+        if (!aligned(work, 256)) return LQ_ERR_ALIGN;
+        if (work_bytes < block_work_bytes(cfg, M, S)) return LQ_ERR_BUFFER_TOO_SMALL;
+    }
+    t.h = ho;
+    t.ldh = ldho;
+    t.y = y;
+    t.ldy = ldy;
+    t.offsets = offsets;
+    t.S = S;
+    t.w_post = w_post;
+    t.w_pre = w_pre;
+    t.dho = dho;
+    t.lddho = lddho;
+    t.dx = dx;
+    t.lddx = lddx;
+    t.dh = out->dh;
+    t.lddh = out->lddh;
+    t.dy = out->dy;
+    t.lddy = out->lddy;
+    t.dw_post = out->dw_post;
+    t.dw_pre = out->dw_pre;
+    return launch_block_bwd(cfg, t, M, (uint8_t*)work, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
+}
+
+// Whether the memory that a step writes lies apart.  Tensors mostly come in the order of their addresses, buffer by buffer: then a walk shows it, otherwise they are sorted.
+static bool apart(std::vector<std::pair<uintptr_t, uintptr_t>>& r)
+{
+    if (!std::is_sorted(r.begin(), r.end())) std::sort(r.begin(), r.end());
+    for (size_t i = 1; i < r.size(); ++i)
+        if (r[i].first < r[i - 1].second) return false;
+    return true;
+}
+
+lq_status lq_adamw_step(const lq_adamw_config* cfg, const lq_adamw_tensor* tensors, int32_t count, const lq_adamw_args* args, void* stream)
+{
+    if (!cfg || !args) return LQ_ERR_NULL;
+    if (cfg->flags != 0 || cfg->reserved != 0 || (cfg->p_dtype != LQ_F32 && cfg->p_dtype != LQ_BF16) || (cfg->g_dtype != LQ_F32 && cfg->g_dtype != LQ_BF16) ||
+        (cfg->state_bits != 32 && cfg->state_bits != 8) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps > 0.0) ||
+        !(cfg->weight_decay >= 0.0))
+        return LQ_ERR_UNSUPPORTED;
+    if (count < 0 || count > 65536 || (!args->step_dev && (args->step < 1 || args->step > 0x7FFFFFFF))) return LQ_ERR_SHAPE;
+    if (!args->lr_dev && !(args->lr - args->lr == 0.0)) return LQ_ERR_UNSUPPORTED;  // not finite
+    if (!aligned(args->lr_dev, 4) || !aligned(args->step_dev, 4) || !aligned(args->grad_scale, 4)) return LQ_ERR_ALIGN;
+    if (count == 0) return LQ_OK;
+    if (!tensors) return LQ_ERR_NULL;
+    const bool eight = cfg->state_bits == 8;
+    const int pe = dtype_bytes(cfg->p_dtype), ge = dtype_bytes(cfg->g_dtype), se = eight ? 1 : 4;
+    for (int32_t i = 0; i < count; ++i) {
+        const lq_adamw_tensor& t = tensors[i];
+        if (t.n < 0 || t.n > ((int64_t)1 << 32)) return LQ_ERR_SHAPE;
+        if (t.n == 0) continue;
+        if (!t.p || !t.grad || !t.m || !t.v || (eight && !t.scales)) return LQ_ERR_NULL;
+        if (!aligned(t.p, pe) || !aligned(t.master, 4) || !aligned(t.grad, ge) || !aligned(t.m, se) || !aligned(t.v, se) || !aligned(t.scales, 4)) return LQ_ERR_ALIGN;
+    }
+    try {
+        std::vector<std::pair<uintptr_t, uintptr_t>> written;
+        written.reserve((size_t)count * 5);
+        auto add = [&](const void* p, int64_t bytes) {
+            if (p && bytes) written.emplace_back((uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes);
+        };
+        for (int32_t i = 0; i < count; ++i) add(tensors[i].p, tensors[i].n * pe);
+        for (int32_t i = 0; i < count; ++i) add(tensors[i].master, tensors[i].n * 4);
+        for (int32_t i = 0; i < count; ++i) add(tensors[i].m, tensors[i].n * se);
+        for (int32_t i = 0; i < count; ++i) add(tensors[i].v, tensors[i].n * se);
+        for (int32_t i = 0; eight && i < count; ++i) add(tensors[i].scales, (tensors[i].n + 255) / 256 * 8);
+        if (!apart(written)) return LQ_ERR_SHAPE;
+    } catch (const std::bad_alloc&) {
+        return LQ_ERR_DEVICE;
+    }
+    return launch_adamw(cfg, tensors, count, args, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
 }
 
 }  // extern "C"

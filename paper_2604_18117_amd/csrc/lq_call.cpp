@@ -14,6 +14,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <vector>
 
 #include "lq.h"
 
@@ -22,6 +23,7 @@ namespace {
 constexpr int NOT_HERE = -1;
 PyTypeObject* config_type = nullptr;  // binding.lq_config, a ctypes.Structure laid out as lq_config
 PyTypeObject *adapter_config_type = nullptr, *qk_config_type = nullptr;  // binding.lq_adapter_config, binding.lq_qk_config
+PyTypeObject* block_config_types[3] = {};  // binding.lq_w4_config, binding.lq_block_config, binding.lq_adamw_config
 
 // An ordinary GPU tensor: exactly torch.Tensor or Parameter, strided, with memory of its own.
 const at::Tensor* tensor(PyObject* o)
@@ -420,6 +422,223 @@ PyObject* qk_norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg,
     });
 }
 
+PyObject* set_block_config_types(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 3 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
+        PyErr_SetString(PyExc_TypeError, "three types are needed");
+        return nullptr;
+    }
+    for (int i = 0; i < 3; ++i) {
+        Py_INCREF(a[i]);
+        Py_XDECREF((PyObject*)block_config_types[i]);
+        block_config_types[i] = (PyTypeObject*)a[i];
+    }
+    Py_RETURN_NONE;
+}
+c10::ScalarType type_of(int32_t dtype) { return dtype == LQ_BF16 ? at::kBFloat16 : at::kFloat; }
+
+PyObject* w4_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, packed, X, bias or None, Y
+{
+    return guarded(n, 5, [&] {
+        const ConfigOf<lq_w4_config> c(a[0], block_config_types[0]);
+        const at::Tensor *packed = tensor(a[1]), *X = tensor(a[2]), *bias, *Y = tensor(a[4]);
+        if (!c.p || !blob(packed) || !row_major(X, type_of(c.p->x_dtype), c.p->K) || !optional(a[3], &bias) ||
+            (bias && (!vec(bias, at::kFloat, c.p->N) || bias->dim() != 1)) || !rows(Y, type_of(c.p->y_dtype), X->size(0), c.p->N))
+            return NOT_HERE;
+        const void *pp = packed->data_ptr(), *xp = X->data_ptr();
+        const float* bp = bias ? (const float*)bias->data_ptr() : nullptr;
+        void* yp = Y->data_ptr();
+        const int64_t M = X->size(0), pn = packed->numel(), lx = row_stride(X), ly = row_stride(Y);
+        return on_stream([&](void* s) { return lq_w4_fwd(c.p, pp, (size_t)pn, xp, lx, bp, yp, ly, M, s); });
+    });
+}
+
+PyObject* w4_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, packed, dY, dX, work
+{
+    return guarded(n, 5, [&] {
+        const ConfigOf<lq_w4_config> c(a[0], block_config_types[0]);
+        const at::Tensor *packed = tensor(a[1]), *dY = tensor(a[2]), *dX = tensor(a[3]), *work = tensor(a[4]);
+        if (!c.p || !blob(packed) || !blob(work) || !row_major(dY, type_of(c.p->y_dtype), c.p->N) || !rows(dX, type_of(c.p->x_dtype), dY->size(0), c.p->K))
+            return NOT_HERE;
+        const void *pp = packed->data_ptr(), *yp = dY->data_ptr();
+        void *xp = dX->data_ptr(), *wp = work->data_ptr();
+        const int64_t M = dY->size(0), pn = packed->numel(), wn = work->numel(), ly = row_stride(dY), lx = row_stride(dX);
+        return on_stream([&](void* s) { return lq_w4_bwd(c.p, pp, (size_t)pn, yp, ly, xp, lx, M, wp, (size_t)wn, s); });
+    });
+}
+
+struct RowsArg {
+    void* p = nullptr;
+    int64_t ld = 0;
+};
+// None, or M rows (M < 0: as many as it has)
+bool rows_arg(PyObject* o, c10::ScalarType ty, int64_t* M, int64_t cols, RowsArg* r)
+{
+    const at::Tensor* t;
+    if (!optional(o, &t)) return false;
+    if (!t) return true;
+    if (!row_major(t, ty, cols) || (*M >= 0 && t->size(0) != *M)) return false;
+    *M = t->size(0);
+    *r = {t->data_ptr(), row_stride(t)};
+    return true;
+}
+bool sequences(PyObject* o, const int32_t** p, int64_t* S)
+{
+    const at::Tensor* t;
+    *p = nullptr;
+    *S = 1;
+    if (!optional(o, &t)) return false;
+    if (!t) return true;
+    if (t->scalar_type() != at::kInt || t->dim() != 1 || !t->is_contiguous() || t->size(0) < 2 || t->size(0) > (1 << 21)) return false;
+    *p = (const int32_t*)t->data_ptr();
+    *S = t->size(0) - 1;
+    return true;
+}
+template <typename MOD>
+bool mod_arg(PyObject* o, int64_t S, int64_t dim, MOD* m)
+{
+    RowsArg r;
+    if (!rows_arg(o, at::kFloat, &S, dim, &r)) return false;
+    m->p = (float*)r.p;
+    m->ld = r.ld;
+    return true;
+}
+bool vec_arg(PyObject* o, int64_t dim, float** p)
+{
+    const at::Tensor* t;
+    *p = nullptr;
+    if (!optional(o, &t) || (t && (!vec(t, at::kFloat, dim) || t->dim() != 1))) return false;
+    if (t) *p = (float*)t->data_ptr();
+    return true;
+}
+
+PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, h, y, offsets, gate, scale, shift, w_post, w_pre, ho, x, last
+{
+    return guarded(n, 12, [&] {
+        const ConfigOf<lq_block_config> c(a[0], block_config_types[1]);
+        if (!c.p || a[1] == Py_None) return NOT_HERE;
+        const c10::ScalarType ht = type_of(c.p->h_dtype), yt = type_of(c.p->y_dtype);
+        const int64_t D = c.p->dim;
+        int64_t M = -1, S;
+        RowsArg h, y, ho, x;
+        const int32_t* offsets;
+        lq_mod gate, scale, shift;
+        float *wp, *wr;
+        if (!rows_arg(a[1], ht, &M, D, &h) || !rows_arg(a[2], yt, &M, D, &y) || !rows_arg(a[9], ht, &M, D, &ho) || !rows_arg(a[10], yt, &M, D, &x) ||
+            (a[2] == Py_None) != (a[9] == Py_None) || (a[10] == Py_None) != (a[11] == Py_True) || !sequences(a[3], &offsets, &S) || !mod_arg(a[4], S, D, &gate) ||
+            !mod_arg(a[5], S, D, &scale) || !mod_arg(a[6], S, D, &shift) || !vec_arg(a[7], D, &wp) || !vec_arg(a[8], D, &wr))
+            return NOT_HERE;
+        return on_stream([&](void* s) {
+            return lq_block_norm_fwd(c.p, h.p, h.ld, y.p, y.ld, offsets, (int32_t)S, &gate, &scale, &shift, wp, wr, ho.p, ho.ld, x.p, x.ld, M, s);
+        });
+    });
+}
+
+// cfg, ho, y, offsets, gate, scale, w_post, w_pre, dho, dx, dh, dy, dgate, dscale, dshift, dw_post, dw_pre, work
+PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 18, [&] {
+        const ConfigOf<lq_block_config> c(a[0], block_config_types[1]);
+        const at::Tensor* work = tensor(a[17]);
+        if (!c.p || !blob(work)) return NOT_HERE;
+        const c10::ScalarType ht = type_of(c.p->h_dtype), yt = type_of(c.p->y_dtype);
+        const int64_t D = c.p->dim;
+        int64_t M = -1, S;
+        RowsArg ho, y, dho, dx, dh, dy;
+        const int32_t* offsets;
+        lq_mod gate, scale;
+        lq_block_grads g{};
+        float *wp, *wr;
+        if (!rows_arg(a[8], ht, &M, D, &dho) || !rows_arg(a[9], yt, &M, D, &dx) || M < 0 || !rows_arg(a[1], ht, &M, D, &ho) || !rows_arg(a[2], yt, &M, D, &y) ||
+            !rows_arg(a[10], ht, &M, D, &dh) || !rows_arg(a[11], yt, &M, D, &dy) || !sequences(a[3], &offsets, &S) || !mod_arg(a[4], S, D, &gate) ||
+            !mod_arg(a[5], S, D, &scale) || !vec_arg(a[6], D, &wp) || !vec_arg(a[7], D, &wr) || !mod_arg(a[12], S, D, &g.dgate) || !mod_arg(a[13], S, D, &g.dscale) ||
+            !mod_arg(a[14], S, D, &g.dshift) || !vec_arg(a[15], D, &g.dw_post) || !vec_arg(a[16], D, &g.dw_pre))
+            return NOT_HERE;
+        const bool branch = a[2] != Py_None;
+        // (what the binding would allocate)
+        if (a[10] == Py_None || branch != (a[11] != Py_None) || (branch && a[4] != Py_None && a[12] == Py_None) || (branch && wp && !g.dw_post) ||
+            (a[5] != Py_None && (a[13] == Py_None || a[14] == Py_None)) || (wr && !g.dw_pre))
+            return NOT_HERE;
+        g.dh = dh.p;
+        g.lddh = dh.ld;
+        g.dy = dy.p;
+        g.lddy = dy.ld;
+        void* kp = work->data_ptr();
+        const int64_t kn = work->numel();
+        return on_stream([&](void* s) {
+            return lq_block_norm_bwd(c.p, ho.p, ho.ld, y.p, y.ld, offsets, (int32_t)S, &gate, &scale, wp, wr, dho.p, dho.ld, dx.p, dx.ld, &g, M, kp, (size_t)kn, s);
+        });
+    });
+}
+
+// item i of a list (or tuple); nothing else is looked into
+PyObject* item(PyObject* o, Py_ssize_t i) { return PyList_CheckExact(o) ? PyList_GET_ITEM(o, i) : PyTuple_GET_ITEM(o, i); }
+bool list_of(PyObject* o, Py_ssize_t count)
+{
+    return (PyList_CheckExact(o) && PyList_GET_SIZE(o) == count) || (PyTuple_CheckExact(o) && PyTuple_GET_SIZE(o) == count);
+}
+bool values(PyObject* o, c10::ScalarType ty, int64_t n, void** p)
+{
+    const at::Tensor* t = tensor(o);
+    if (!t || t->scalar_type() != ty || t->numel() != n || !t->is_contiguous()) return false;
+    *p = t->data_ptr();
+    return true;
+}
+
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, params, grads, m, v, lr, step, scales, masters, grad_scale
+{
+    return guarded(n, 10, [&] {
+        const ConfigOf<lq_adamw_config> c(a[0], block_config_types[2]);
+        if (!c.p || !(PyList_CheckExact(a[1]) || PyTuple_CheckExact(a[1]))) return NOT_HERE;
+        const Py_ssize_t count = Py_SIZE(a[1]);
+        const bool eight = c.p->state_bits == 8, masters = a[8] != Py_None;
+        for (int k = 2; k <= 4; ++k)
+            if (!list_of(a[k], count)) return NOT_HERE;
+        if (count > 65536 || (eight && !list_of(a[7], count)) || (masters && !list_of(a[8], count))) return NOT_HERE;
+        lq_adamw_args x{};
+        void* q;
+        if (tensor(a[5])) {
+            if (!values(a[5], at::kFloat, 1, &q)) return NOT_HERE;
+            x.lr_dev = (const float*)q;
+        } else if (PyFloat_CheckExact(a[5])) {
+            x.lr = PyFloat_AS_DOUBLE(a[5]);
+        } else {
+            return NOT_HERE;
+        }
+        x.step = 1;
+        if (tensor(a[6])) {
+            if (!values(a[6], at::kInt, 1, &q)) return NOT_HERE;
+            x.step_dev = (const int32_t*)q;
+        } else if (!integer(a[6], &x.step)) {
+            return NOT_HERE;
+        }
+        if (a[9] != Py_None) {
+            if (!values(a[9], at::kFloat, 1, &q)) return NOT_HERE;
+            x.grad_scale = (const float*)q;
+        }
+        const c10::ScalarType pt = type_of(c.p->p_dtype), gt = type_of(c.p->g_dtype), st = eight ? at::kFloat8_e4m3fn : at::kFloat;
+        std::vector<lq_adamw_tensor> table((size_t)count);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            lq_adamw_tensor& t = table[(size_t)i];
+            const at::Tensor* p = tensor(item(a[1], i));
+            if (!p || p->scalar_type() != pt || !p->is_contiguous()) return NOT_HERE;
+            t = {p->data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, p->numel()};
+            void *g, *s = nullptr, *w = nullptr;
+            if (!values(item(a[2], i), gt, t.n, &g) || !values(item(a[3], i), st, t.n, &t.m) || !values(item(a[4], i), st, t.n, &t.v)) return NOT_HERE;
+            if (masters && item(a[8], i) != Py_None && !values(item(a[8], i), at::kFloat, t.n, &w)) return NOT_HERE;
+            if (eight) {
+                const at::Tensor* sc = tensor(item(a[7], i));
+                if (!dense(sc, at::kFloat, (t.n + 255) / 256, 2)) return NOT_HERE;
+                s = sc->data_ptr();
+            }
+            t.grad = g;
+            t.master = (float*)w;
+            t.scales = (float*)s;
+        }
+        return on_stream([&](void* s) { return lq_adamw_step(c.p, table.data(), (int32_t)count, &x, s); });
+    });
+}
+
 #define FAST(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"set_config_type", set_config_type, METH_O, nullptr},
                          FAST(quantize_act),
@@ -435,6 +654,12 @@ PyMethodDef methods[] = {{"set_config_type", set_config_type, METH_O, nullptr},
                          FAST(adapter_bwd),
                          FAST(qk_norm_rope_fwd),
                          FAST(qk_norm_rope_bwd),
+                         FAST(set_block_config_types),
+                         FAST(w4_fwd),
+                         FAST(w4_bwd),
+                         FAST(block_norm_fwd),
+                         FAST(block_norm_bwd),
+                         FAST(adamw_step),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -261,6 +261,44 @@ size_t qk_work_bytes(const lq_qk_config* c, int64_t M);
 hipError_t launch_qk_fwd(const lq_qk_config* c, const QkTensors& t, int64_t M, hipStream_t s);
 hipError_t launch_qk_bwd(const lq_qk_config* c, const QkTensors& t, int64_t M, uint8_t* work, hipStream_t s);
 
+// Products of a few rows with 4-bit weights (lq_w4.hip).
+size_t w4_packed_bytes(const lq_w4_config* c);
+size_t w4_work_bytes(const lq_w4_config* c, int64_t M);
+hipError_t launch_w4_pack(const lq_w4_config* c, const float* W, const int8_t* codes, const float* scales, uint8_t* packed, hipStream_t s);  // W, or codes and scales
+hipError_t launch_w4_unpack(const lq_w4_config* c, const uint8_t* packed, int8_t* codes, float* scales, hipStream_t s);
+hipError_t launch_w4_fwd(const lq_w4_config* c, const uint8_t* packed, const void* X, int64_t ldx, const float* bias, void* Y, int64_t ldy, int64_t M, hipStream_t s);
+hipError_t launch_w4_bwd(const lq_w4_config* c, const uint8_t* packed, const void* dY, int64_t lddy, void* dX, int64_t lddx, int64_t M, uint8_t* work,
+                         hipStream_t s);
+
+// Norms before and after a block (lq_block.hip).
+struct BlockTensors {
+    const void *h, *y;  // forward: stream and branch; gradient: the forward's h' in h
+    void *ho, *x;
+    const void *dho, *dx;
+    void *dh, *dy;
+    int64_t ldh, ldy, ldho, ldx, lddho, lddx, lddh, lddy;
+    const int32_t* offsets;
+    int S;
+    lq_mod gate, scale, shift;
+    lq_mod_out dgate, dscale, dshift;
+    const float *w_post, *w_pre;
+    float *dw_post, *dw_pre;
+};
+struct BlockArgs {
+    BlockTensors t;
+    int64_t M;
+    int dim, post, pre;
+    int chunk;  // rows of a group of wavefronts (forward), of a workgroup (gradient)
+    int waves;  // of a row
+    float eps, inv_dim, alpha;
+    float* part;  // [chunk + sequence][3][dim] sums
+};
+size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S);
+hipError_t launch_block_fwd(const lq_block_config* c, const BlockTensors& t, int64_t M, hipStream_t s);
+hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int64_t M, uint8_t* work, hipStream_t s);
+
+hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors, int count, const lq_adamw_args* x, hipStream_t s);  // lq_adamw.hip
+
 int compute_units();  // of the current device
 
 // Form of the activation steps with a block-scaled floating-point branch (mxb_act_kernel, mx6_act_kernel; every form sums T in the same

@@ -1,0 +1,182 @@
+"""Products of a few rows with 4-bit weights (lq_w4_*) against the plain 64-bit implementation."""
+import pytest
+import torch
+
+from tests import blocks_ref as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def lq():
+    from paper_2604_18117_amd import binding
+    return binding
+
+
+def make(M, K, N, group, x="bf16", y="bf16", seed=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+    codes = torch.randint(-7, 8, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    scales = normal(N, -(-K // group)) * 0.1  # of both signs
+    X, dY = (normal(M, K) * 2 + 0.5).to(DT[x]), (normal(M, N) * 0.1).to(DT[y])
+    return codes, scales, X, dY, normal(N)
+
+
+def check_all(lq, cfg, packed, codes, scales, X, dY, bias, what=""):
+    xt, yt = X.dtype, dY.dtype
+    ref.check(lq.lq_w4_fwd(cfg, packed, X, bias), ref.w4_fwd(X, codes, scales, cfg.group, bias, yt), what + " forward")
+    ref.check(lq.lq_w4_bwd(cfg, packed, dY), ref.w4_bwd(dY, codes, scales, cfg.group, xt), what + " gradient")
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(1, 1), (16, 128), (17, 129), (40, 300), (33, 31), (5, 64), (160, 1152), (100, 2240)])
+def test_pack_by_the_int_rule(lq, N, K, group):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N)
+    W = torch.randn(N, K, generator=g, device="cuda") * 0.02
+    W[:, : K // 3] = 0.0  # groups of zeros, and groups with some
+    cfg = lq.make_w4_config(N, K, group)
+    want_codes, want_scales = ref.w4_quantise(W.cpu(), group)
+    for packed in (lq.lq_w4_pack(cfg, W), lq.lq_w4_pack(cfg, W, packed=torch.full((lq.lq_w4_sizes(cfg),), 0xFF, dtype=torch.uint8, device="cuda"))):
+        codes, scales = lq.lq_w4_unpack(cfg, packed)
+        assert torch.equal(codes.cpu(), want_codes) and torch.equal(scales.cpu(), want_scales)
+    again = lq.lq_w4_pack_codes(cfg, codes, scales)
+    assert torch.equal(again, packed)
+
+
+def test_codes_beyond_the_range(lq):
+    codes = torch.arange(-128, 128, dtype=torch.int8, device="cuda").view(2, 128)
+    cfg = lq.make_w4_config(2, 128, 32)
+    got, _ = lq.lq_w4_unpack(cfg, lq.lq_w4_pack_codes(cfg, codes, torch.ones(2, 4, device="cuda")))
+    assert torch.equal(got, codes.clamp(-7, 7))
+
+
+@pytest.mark.parametrize("x,y", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("M,K,N,group", [(1, 1, 1, 32), (1, 128, 16, 128), (2, 130, 17, 64), (3, 1152, 100, 64), (1, 2240, 1153, 128), (16, 257, 40, 32), (17, 300, 50, 64),
+                                         (31, 64, 33, 32), (33, 1000, 70, 128), (64, 96, 260, 32), (65, 136, 48, 64), (130, 520, 31, 32), (5, 65, 4608, 64),
+                                         (4, 4608, 300, 64), (7, 40, 13441, 32)])
+def test_sizes(lq, M, K, N, group, x, y):
+    codes, scales, X, dY, bias = make(M, K, N, group, x, y, seed=M + K)
+    cfg = lq.make_w4_config(N, K, group, x, y)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    check_all(lq, cfg, packed, codes, scales, X, dY, bias)
+    ref.check(lq.lq_w4_fwd(cfg, packed, X), ref.w4_fwd(X, codes, scales, group, None, DT[y]), "without a bias")
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,start", [(1, 0), (1, 1), (3, 2), (8, 0), (8, 3)])
+def test_rows_that_start_anywhere(lq, pad, start, x):
+    M, K, N, group = 5, 264, 70, 64
+    codes, scales, X, dY, bias = make(M, K, N, group, x, x)
+    cfg = lq.make_w4_config(N, K, group, x, x)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+
+    def apart(t, fill=float("nan")):
+        big = torch.full((M, t.shape[1] + pad), fill, dtype=t.dtype, device="cuda").flatten()
+        big = torch.cat([big, big[:start]])[start:]
+        v = big.as_strided((M, t.shape[1]), (t.shape[1] + pad, 1))
+        v.copy_(t)
+        return big, v
+    _, Xs = apart(X)
+    _, gs = apart(dY)
+    ybig, Y = apart(torch.zeros_like(dY), 7.0)
+    xbig, dX = apart(torch.zeros_like(X), 7.0)
+    lq.lq_w4_fwd(cfg, packed, Xs, bias, Y=Y)
+    lq.lq_w4_bwd(cfg, packed, gs, dX=dX)
+    assert torch.equal(Y, lq.lq_w4_fwd(cfg, packed, X, bias)) and torch.equal(dX, lq.lq_w4_bwd(cfg, packed, dY))
+    for big, cols in ((ybig, N), (xbig, K)):  # what lies between the rows stays
+        at = torch.arange(big.numel(), device="cuda") % (cols + pad)
+        assert (big[at >= cols] == 7.0).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 2, 6, 20, 70])
+def test_a_row_does_not_depend_on_the_others(lq, M, x):
+    K, N, group = 392, 100, 32
+    codes, scales, X, dY, bias = make(M, K, N, group, x, x)
+    cfg = lq.make_w4_config(N, K, group, x, x)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    Y, dX = lq.lq_w4_fwd(cfg, packed, X, bias), lq.lq_w4_bwd(cfg, packed, dY)
+    assert torch.equal(Y, lq.lq_w4_fwd(cfg, packed, X, bias)) and torch.equal(dX, lq.lq_w4_bwd(cfg, packed, dY))
+    if M < 2:
+        return
+    X2, dY2 = X.clone(), dY.clone()
+    X2[1, 5], X2[1, 7], dY2[1, 3] = float("nan"), float("inf"), float("nan")
+    Y2, dX2 = lq.lq_w4_fwd(cfg, packed, X2, bias), lq.lq_w4_bwd(cfg, packed, dY2)
+    others = torch.arange(M, device="cuda") != 1
+    assert torch.equal(Y[others], Y2[others]) and torch.equal(dX[others], dX2[others])
+    assert torch.isnan(Y2[1]).all() and torch.isnan(dX2[1]).all()
+
+
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_infinities_give_what_the_formula_gives(lq, x):
+    M, K, N, group = 3, 200, 60, 64
+    codes, scales, X, dY, bias = make(M, K, N, group, x, "f32")
+    cfg = lq.make_w4_config(N, K, group, x, "f32")
+    X[0, 70], X[1, 3], X[1, 4] = float("inf"), float("-inf"), float("inf")
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    Y = lq.lq_w4_fwd(cfg, packed, X, bias)
+    W = codes.double() * scales.double().repeat_interleave(group, 1)[:, :K]
+    want = (X.double()[:, None, :] * W[None]).sum(-1) + bias.double()  # inf * 0 and inf - inf are not numbers
+    bad = ~torch.isfinite(want)
+    assert bad[:2].any() and not bad[2].any()
+    assert torch.equal(Y.double()[bad].nan_to_num(nan=3.0), want[bad].nan_to_num(nan=3.0))
+    assert torch.isfinite(Y[~bad]).all()
+
+
+def test_strong_values_in_all_24_bits(lq):
+    """fp32 rows whose strong channels cancel: what the small ones add is left, to the bits of fp32 sums."""
+    K, N, group = 256, 32, 32
+    codes = torch.ones(N, K, dtype=torch.int8, device="cuda")
+    scales = torch.ones(N, K // group, device="cuda")
+    X = torch.zeros(2, K, device="cuda")
+    X[:, 0], X[:, 1], X[0, 2], X[1, 2] = 1.0 + 2.0 ** -23, -1.0, 2.0 ** -20, 3.0
+    cfg = lq.make_w4_config(N, K, group, "f32", "f32")
+    Y = lq.lq_w4_fwd(cfg, lq.lq_w4_pack_codes(cfg, codes, scales), X)
+    # partial sums are at most 4: sums of three terms of 256 values each are off by (768 + 24) 2^-24 of the largest term at worst in general; here only a few values are not
+    # zero, whose terms (8 bits each) add up without a rounding above 2^-22
+    want = torch.tensor([2.0 ** -23 + 2.0 ** -20, 3.0 + 2.0 ** -23], device="cuda", dtype=torch.float64)
+    assert ((Y.double() - want[:, None]).abs() <= 2.0 ** -22).all()
+
+
+def test_empty_batch_and_workspace(lq):
+    cfg = lq.make_w4_config(300, 200, 32)
+    codes, scales, _, _, bias = make(1, 200, 300, 32)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    assert lq.lq_w4_fwd(cfg, packed, torch.zeros(0, 200, dtype=torch.bfloat16, device="cuda"), bias).shape == (0, 300)
+    assert lq.lq_w4_bwd(cfg, packed, torch.zeros(0, 300, dtype=torch.bfloat16, device="cuda")).shape == (0, 200)
+    with pytest.raises(lq.LqError) as e:
+        lq.lq_w4_fwd(cfg, packed[:-256], torch.zeros(1, 200, dtype=torch.bfloat16, device="cuda"), bias)
+    assert e.value.status == lq.LQ_ERR_BUFFER_TOO_SMALL
+
+
+def test_captured_and_replayed_on_a_stream(lq):
+    M, K, N, group = 2, 1152, 700, 64
+    codes, scales, X, dY, bias = make(M, K, N, group, "bf16", "f32")
+    cfg = lq.make_w4_config(N, K, group, "bf16", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    Y, dX = torch.empty(M, N, device="cuda"), torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    work = torch.empty(lq.lq_w4_work_sizes(cfg, M), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        lq.lq_w4_fwd(cfg, packed, X, bias, Y=Y)
+        lq.lq_w4_bwd(cfg, packed, dY, dX=dX, work=work)
+        s.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            lq.lq_w4_fwd(cfg, packed, X, bias, Y=Y)
+            lq.lq_w4_bwd(cfg, packed, dY, dX=dX, work=work)
+    torch.cuda.synchronize()
+    for k in range(4):
+        _, _, X2, dY2, _ = make(M, K, N, group, "bf16", "f32", seed=10 + k)
+        X.copy_(X2)
+        dY.copy_(dY2)
+        want = lq.lq_w4_fwd(cfg, packed, X2, bias), lq.lq_w4_bwd(cfg, packed, dY2)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want[0]) and torch.equal(dX, want[1]), k
