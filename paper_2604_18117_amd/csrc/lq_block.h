@@ -1,0 +1,276 @@
+// What lies between two blocks of a transformer, in one pass over the rows, and its gradient:
+//     h' = alpha h + gate[s] post(y) w_post ;   x = pre(h') w_pre (1 + scale[s]) + shift[s]          (s: the row's sequence)
+// Bound by memory in large batches.  A row belongs to one to sixteen wavefronts; a lane holds the same columns of every row it meets, so that the factors
+//     a = w_pre (1 + scale[s]) ,  b = gate[s] w_post
+// and, in the gradient, the sums over rows stay in registers for as long as the sequence lasts.  Means, variances (of differences from the mean) and everything
+// else are held in fp32; outputs are rounded once.
+#pragma once
+#include <utility>
+
+#include "lq_internal.h"
+
+namespace lq {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum_wave(float v)  // over 64 lanes, in all of them
+{
+    v = add_dpp<0xB1>(v);   // quad_perm [1,0,3,2]
+    v = add_dpp<0x4E>(v);   // quad_perm [2,3,0,1]
+    v = add_dpp<0x141>(v);  // row_half_mirror
+    v = add_dpp<0x140>(v);  // row_mirror
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// Sums over the W wavefronts of a row.  Two sets of slots are used in turn, so that one barrier serves a sum: who writes a set again has passed the barrier of the
+// other one, behind which nobody reads the first.
+template <bool MULTI>
+struct RowSum {
+    float* slot;  // [2][wavefronts of the workgroup][2]
+    int waves, first, wave, W, turn = 0;
+    __device__ __forceinline__ void operator()(float& u, float& v)
+    {
+        u = sum_wave(u);
+        v = sum_wave(v);
+        __builtin_amdgcn_sched_barrier(0);  // (what follows a sum is not begun before it: its values would be held beside all others)
+        if constexpr (MULTI) {
+            float* p = slot + turn * waves * 2;
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) p[wave * 2] = u, p[wave * 2 + 1] = v;
+            __syncthreads();
+            u = v = 0.0f;
+            for (int w = 0; w < W; ++w) u += p[(first + w) * 2], v += p[(first + w) * 2 + 1];
+        }
+    }
+    __device__ __forceinline__ void operator()(float& u)
+    {
+        float v = 0.0f;
+        operator()(u, v);
+    }
+};
+
+// VEC consecutive values in memory.  ANY: of any alignment, and of which only the first `have` may be there (the others are zero and not written).
+template <typename T, int VEC, bool ANY>
+struct Raw {
+    typedef T Value __attribute__((ext_vector_type(VEC)));
+    typedef Value Access __attribute__((aligned(ANY ? sizeof(T) : sizeof(T) * VEC > 16 ? 16 : sizeof(T) * VEC)));
+    Value v;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (T)0.0f;
+    }
+    __device__ __forceinline__ void fetch(const T* p, int have)
+    {
+        if (!ANY || have >= VEC) {
+            v = *(const Access*)p;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = i < have ? p[i] : (T)0.0f;
+        }
+    }
+    __device__ __forceinline__ void get(float (&f)[VEC]) const
+    {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = (float)v[i];
+    }
+    static __device__ __forceinline__ void put(T* p, int have, const float (&f)[VEC])
+    {
+        if (!ANY || have >= VEC) {
+            Value t;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t[i] = (T)f[i];
+            *(Access*)p = t;
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (i < have) p[i] = (T)f[i];
+        }
+    }
+};
+template <int VEC, bool ANY>
+__device__ __forceinline__ void read(const float* p, int have, float (&f)[VEC])
+{
+    Raw<float, VEC, ANY> r;
+    r.fetch(p, have);
+    r.get(f);
+}
+
+// The sequence of a row: how many of the S ends are at or before it, a wavefront looking at 64 of them at a time.  Bounded and inside [0, S] whatever they hold.
+__device__ __forceinline__ int sequence_of(const int32_t* ends, int S, int row)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = S;
+    while (n > 0) {
+        const int step = (n + 63) >> 6, i = lane * step + step - 1;
+        const int k = __popcll(__ballot(i < n && ends[lo + (i < n ? i : 0)] <= row));
+        lo += k * step;
+        n = min(step - 1, n - k * step);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+// Sequence s and its rows from `row` on: [row, end), cut to the limit; s < 0: rows of no sequence.
+struct Segment {
+    int s, end;
+    __device__ __forceinline__ Segment(const BlockTensors& t, int row, int limit)
+    {
+        if (!t.offsets) {
+            s = 0;
+            end = limit;
+            return;
+        }
+        const int start = t.offsets[0];
+        if (row < start) {
+            s = -1;
+            end = min(start, limit);
+            return;
+        }
+        s = sequence_of(t.offsets + 1, t.S, row);
+        end = s < t.S ? min(t.offsets[s + 1], limit) : limit;
+        if (s >= t.S) s = -1;
+        if (end <= row) end = row + 1;  // (ends that do not rise)
+    }
+};
+
+// A lane's NV vectors of columns: the first at `at`, each `step` values from the one before, so that with the row's address in scalar registers one offset serves all.  A
+// vector past the row's end is not read (it is zero) and left out of sums.  ANY: the last one may be there in part.
+template <int VEC, int NV, bool ANY>
+struct Columns {
+    unsigned at, step;
+    int dim;
+    __device__ __forceinline__ Columns(int dim_, int lane, int lanes) : at(lane * VEC), step(lanes * VEC), dim(dim_) {}
+    __device__ __forceinline__ int have(int v) const { return dim - (int)(at + v * step); }
+    __device__ __forceinline__ bool has(int v) const { return have(v) > 0; }
+    __device__ __forceinline__ float counted(int v, float sum) const { return has(v) ? sum : 0.0f; }
+    template <typename T>
+    __device__ __forceinline__ void fetch(const T* row, Raw<T, VEC, ANY> (&r)[NV]) const
+    {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            r[v].clear();
+            if (has(v)) r[v].fetch(row + v * step + at, have(v));
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void put(T* row, int v, const float (&f)[VEC]) const
+    {
+        if (has(v)) Raw<T, VEC, ANY>::put(row + v * step + at, have(v), f);
+    }
+};
+
+// Normalises the values of a row in place; returns 1 / deviation.
+template <int VEC, int NV, bool ANY, bool MULTI>
+__device__ __forceinline__ float normalise(int kind, float (&x)[NV][VEC], const Columns<VEC, NV, ANY>& c, RowSum<MULTI>& sum, const BlockArgs& a)
+{
+    if (kind == LQ_NORM_LAYER) {
+        float m = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float t = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) t += x[v][i];
+            m += c.counted(v, t);
+        }
+        sum(m);
+        m *= a.inv_dim;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[v][i] = ANY && i >= c.have(v) ? 0.0f : x[v][i] - m;
+    }
+    float ss = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) t = fmaf(x[v][i], x[v][i], t);
+        ss += c.counted(v, t);
+    }
+    sum(ss);
+    const float r = 1.0f / sqrtf(fmaf(ss, a.inv_dim, a.eps));
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[v][i] *= r;
+    return r;
+}
+
+// a, b of the header, and shift, of sequence s, at a column
+template <int VEC, bool ANY>
+__device__ __forceinline__ void factor_a(const BlockTensors& t, int at, int have, int s, float (&a)[VEC])
+{
+    float w[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) a[i] = 1.0f;
+    if (t.scale.p) {
+        read<VEC, ANY>(t.scale.p + s * t.scale.ld + at, have, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a[i] = 1.0f + w[i];
+    }
+    if (t.w_pre) {
+        read<VEC, ANY>(t.w_pre + at, have, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) a[i] *= w[i];
+    }
+}
+template <int VEC, bool ANY>
+__device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int have, int s, float (&b)[VEC])
+{
+    float w[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) b[i] = 1.0f;
+    if (t.gate.p) read<VEC, ANY>(t.gate.p + s * t.gate.ld + at, have, b);
+    if (t.w_post) {
+        read<VEC, ANY>(t.w_post + at, have, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) b[i] *= w[i];
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+// Vectors of columns to a lane, and wavefronts to a row
+struct BlockShape {
+    bool any;
+    int NV, W;
+};
+static inline BlockShape block_shape(int dim, bool any, int vec, int most)
+{
+    const int vectors = (dim + vec - 1) / vec, W = (vectors + 64 * most - 1) / (64 * most);
+    return {any, (vectors + 64 * W - 1) / (64 * W), W};
+}
+static inline bool fits(const void* p, int64_t ld, int64_t rows, int bytes, int elem) { return (uintptr_t)p % bytes == 0 && (rows < 2 || ld * elem % bytes == 0); }
+// Whether every row can be read four values at a time
+static inline bool block_fours(const lq_block_config* c, const BlockTensors& t, int64_t M)
+{
+    const int he = c->h_dtype == LQ_F32 ? 4 : 2, ye = c->y_dtype == LQ_F32 ? 4 : 2;
+    bool ok = c->dim % 4 == 0;
+    for (const auto& r : {std::pair<const void*, int64_t>(t.h, t.ldh), {t.ho, t.ldho}, {t.dho, t.lddho}, {t.dh, t.lddh}}) ok = ok && fits(r.first, r.second, M, 4 * he, he);
+    for (const auto& r : {std::pair<const void*, int64_t>(t.y, t.ldy), {t.x, t.ldx}, {t.dx, t.lddx}, {t.dy, t.lddy}}) ok = ok && fits(r.first, r.second, M, 4 * ye, ye);
+    for (const lq_mod& m : {t.gate, t.scale, t.shift}) ok = ok && fits(m.p, m.ld, t.S, 16, 4);
+    return ok && (uintptr_t)t.w_pre % 16 == 0 && (uintptr_t)t.w_post % 16 == 0;
+}
+static inline BlockArgs block_args(const lq_block_config* c, const BlockTensors& t, int64_t M)
+{
+    BlockArgs a{};
+    a.t = t;
+    a.M = M;
+    a.dim = c->dim;
+    a.post = c->post;
+    a.pre = c->pre;
+    a.eps = c->eps;
+    a.inv_dim = 1.0f / (float)c->dim;
+    a.alpha = t.y ? c->res_scale : 1.0f;
+    return a;
+}
+
+}  // namespace lq

@@ -1,0 +1,330 @@
+// Norms before and after a block (lq_block.h): gradient.
+#include "lq_block.h"
+
+namespace lq {
+
+// Gradient.  With n = pre(h'), p = post(y) before their weights, r the reciprocal deviations:
+//     G = dh' + r (dx a - mean(dx a) - n mean(dx a n)) ;  dh = alpha G ;  dy = r_y (G b - mean(G b) - p mean(G b p))       (the plain means with LQ_NORM_LAYER only)
+// and the sums over the rows of a sequence of dx, dx n and G p, from which block_sums makes the gradients of modulation and weights.  A workgroup takes a chunk of rows,
+// its groups of W wavefronts in turn; a and b are in the LDS.  At the end of a sequence or of the chunk the groups' sums are joined in the LDS and written to place chunk + s
+// of the parts, which no other pair of chunk and sequence has (both rise from one pair to the next).
+template <typename TH, typename TY, int VEC, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
+__global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
+{
+    extern __shared__ v4f shared[];
+    __shared__ float slots[64];
+    const BlockTensors& t = a.t;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, W = MULTI ? a.waves : 1, group = wave / W, groups = waves / W;
+    const int padded = (a.dim + VEC - 1) / VEC * VEC;
+    float *la = (float*)shared, *lb = la + padded, *joined = lb + padded;  // a, b; [groups][padded] sums
+    const Columns<VEC, NV, ANY> c(a.dim, threadIdx.x - group * W * 64, W * 64);
+    RowSum<MULTI> sum{slots, waves, group * W, wave, W};
+    int first = blockIdx.x * a.chunk;
+    const int limit = min(first + a.chunk, (int)a.M);
+    const bool has_dx = t.dx, has_y = t.y, has_dho = t.dho;
+    Raw<TH, VEC, ANY> rh[NV], rg[NV];
+    Raw<TY, VEC, ANY> ry[NV], rx[NV];
+    auto request = [&](int m) {
+        if (has_dx) {
+            c.fetch((const TH*)t.h + m * t.ldh, rh);
+            c.fetch((const TY*)t.dx + m * t.lddx, rx);
+        }
+        if (has_y) c.fetch((const TY*)t.y + m * t.ldy, ry);
+        if (has_dho) c.fetch((const TH*)t.dho + m * t.lddho, rg);
+    };
+    auto read_factor = [&](const float* l, int v, float (&f)[VEC]) {  // (past the row's end: the first)
+        read<VEC, false>(l + (c.has(v) ? c.at + v * c.step : 0u), VEC, f);
+    };
+    while (first < limit) {
+        const Segment seg(t, first, limit);
+        if (seg.s < 0) {
+            first = seg.end;
+            continue;
+        }
+        const int last = seg.end - 1;
+        request(min(first + group, last));
+        for (int o = threadIdx.x * VEC; o < padded; o += blockDim.x * VEC) {
+            float f[VEC];
+            factor_a<VEC, ANY>(t, o, a.dim - o, seg.s, f);
+            Raw<float, VEC, false>::put(la + o, VEC, f);
+            factor_b<VEC, ANY>(t, o, a.dim - o, seg.s, f);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) f[i] = ANY && i >= a.dim - o ? 0.0f : f[i];
+            Raw<float, VEC, false>::put(lb + o, VEC, f);
+        }
+        float s1[NV][VEC], s2[NV][VEC], s3[NV][VEC];
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s1[v][i] = s2[v][i] = s3[v][i] = 0.0f;
+        __syncthreads();
+        for (int base = first; base < seg.end; base += groups) {
+            const int row = base + group;
+            const bool on = row < seg.end;  // (of a row: all its wavefronts.  The others take part in the barriers with the last row's values, of which nothing is kept)
+            if (!MULTI && !on) break;
+            asm volatile("" ::: "memory");  // (a and b are read again for every row: kept in registers they would cost a wavefront's)
+            float n[NV][VEC], dx[NV][VEC], g[NV][VEC];
+            Raw<TY, VEC, ANY> py[NV];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (has_dx) {
+                    rh[v].get(n[v]);
+                    rx[v].get(dx[v]);
+                }
+                if (has_dho) rg[v].get(g[v]);
+                else
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[v][i] = 0.0f;
+                py[v] = ry[v];
+            }
+            if (base + groups < seg.end) request(min(row + groups, last));
+            if (has_dx) {
+                float r = 1.0f, u = 0.0f, w = 0.0f;
+                if (a.pre != LQ_NORM_NONE) r = normalise<VEC, NV, ANY, MULTI>(a.pre, n, c, sum, a);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float fa[VEC], tu = 0.0f, tw = 0.0f;
+                    read_factor(la, v, fa);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        if (on) {
+                            s1[v][i] += dx[v][i];
+                            s2[v][i] = fmaf(dx[v][i], n[v][i], s2[v][i]);
+                        }
+                        dx[v][i] *= fa[i];
+                        tu = fmaf(dx[v][i], n[v][i], tu);
+                        tw += dx[v][i];
+                    }
+                    u += c.counted(v, tu);
+                    w += c.counted(v, tw);
+                }
+                if (a.pre != LQ_NORM_NONE) {
+                    sum(u, w);
+                    u *= a.inv_dim * r;
+                    w = a.pre == LQ_NORM_LAYER ? w * a.inv_dim * r : 0.0f;
+                } else {
+                    u = w = 0.0f;
+                }
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) g[v][i] += fmaf(r, dx[v][i], fmaf(-n[v][i], u, -w));
+            }
+            if (t.dh && on) {
+                TH* o = (TH*)t.dh + row * t.lddh;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float d[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) d[i] = a.alpha * g[v][i];
+                    c.put(o, v, d);
+                }
+            }
+            if (has_y) {
+                float p[NV][VEC], r = 1.0f, u = 0.0f, w = 0.0f;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) py[v].get(p[v]);
+                if (POST) r = normalise<VEC, NV, ANY, MULTI>(a.post, p, c, sum, a);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    float fb[VEC], tu = 0.0f, tw = 0.0f;
+                    read_factor(lb, v, fb);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        if (on) s3[v][i] = fmaf(g[v][i], p[v][i], s3[v][i]);
+                        g[v][i] *= fb[i];
+                        if (POST) {
+                            tu = fmaf(g[v][i], p[v][i], tu);
+                            tw += g[v][i];
+                        }
+                    }
+                    u += c.counted(v, tu);
+                    w += c.counted(v, tw);
+                }
+                if (POST) {
+                    sum(u, w);
+                    u *= a.inv_dim * r;
+                    w = a.post == LQ_NORM_LAYER ? w * a.inv_dim * r : 0.0f;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) g[v][i] = fmaf(r, g[v][i], fmaf(-p[v][i], u, -w));
+                }
+                if (t.dy && on) {
+                    TY* o = (TY*)t.dy + row * t.lddy;
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) c.put(o, v, g[v]);
+                }
+            }
+        }
+        if (a.part) {
+            float* out = a.part + (size_t)(blockIdx.x + seg.s) * 3 * a.dim;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                float* mine = joined + group * padded;
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+                    if (c.has(v)) {
+                        const auto& y = k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v];
+                        if (MULTI && groups == 1) Raw<float, VEC, true>::put(out + k * a.dim + c.at + v * c.step, c.have(v), y);
+                        else Raw<float, VEC, false>::put(mine + c.at + v * c.step, VEC, y);
+                    }
+                if (MULTI && groups == 1) continue;
+                __syncthreads();
+                for (int o = threadIdx.x; o < a.dim; o += blockDim.x) {
+                    float y = joined[o];
+                    for (int w = 1; w < groups; ++w) y += joined[w * padded + o];
+                    out[k * a.dim + o] = y;
+                }
+                __syncthreads();
+            }
+        }
+        if (!a.part || (MULTI && groups == 1)) __syncthreads();  // (a and b have been read)
+        first = seg.end;
+    }
+}
+
+// Sums over a sequence's parts in a fixed order; 64 columns of one of the three sums to a workgroup, its wavefronts take parts in turn and are joined in a tree.
+//     dshift = sum dx ;  dscale = w_pre sum dx n ;  dgate = w_post sum G p
+// raw: the last two without the weights, for those of the weights.
+__global__ void __launch_bounds__(1024) block_sums(BlockArgs a, float* raw)
+{
+    __shared__ float sh[16][64];
+    const BlockTensors& t = a.t;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, col = blockIdx.x * 64 + lane;
+    for (int s = blockIdx.z; s < t.S; s += gridDim.z) {
+        int begin = 0, end = (int)a.M;
+        if (t.offsets) {
+            begin = max(t.offsets[s], 0);
+            end = min(t.offsets[s + 1], (int)a.M);
+        }
+        const int c0 = begin / a.chunk, c1 = begin < end ? (end - 1) / a.chunk + 1 : c0;
+        float y = 0.0f;
+        if (col < a.dim) {
+            const float* p = a.part + (size_t)s * 3 * a.dim + k * a.dim + col;
+#pragma unroll 8
+            for (int i = c0 + wave; i < c1; i += waves) y += p[(size_t)i * 3 * a.dim];
+        }
+        sh[wave][lane] = y;
+        __syncthreads();
+        for (int half = waves / 2; half > 0; half /= 2) {
+            if (wave < half) sh[wave][lane] += sh[wave + half][lane];
+            __syncthreads();
+        }
+        if (wave == 0 && col < a.dim) {
+            y = sh[0][lane];
+            const lq_mod_out& o = k == 0 ? t.dshift : k == 1 ? t.dscale : t.dgate;
+            const float* w = k == 0 ? nullptr : k == 1 ? t.w_pre : t.w_post;
+            if (o.p) o.p[s * o.ld + col] = w ? y * w[col] : y;
+            if (raw && k) raw[((size_t)s * 2 + k - 1) * a.dim + col] = y;
+        }
+        __syncthreads();
+    }
+}
+// dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
+__global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const float* raw)
+{
+    __shared__ float sh[16][64];
+    const BlockTensors& t = a.t;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    const lq_mod& f = k == 0 ? t.scale : t.gate;
+    float* out = k == 0 ? t.dw_pre : t.dw_post;
+    float y = 0.0f;
+    if (col < a.dim && out)
+#pragma unroll 4
+        for (int s = wave; s < t.S; s += 16) {
+            const float u = raw[((size_t)s * 2 + k) * a.dim + col];
+            y += f.p ? u * (k == 0 ? 1.0f + f.p[s * f.ld + col] : f.p[s * f.ld + col]) : u;
+        }
+    sh[wave][lane] = y;
+    __syncthreads();
+    for (int half = 8; half > 0; half /= 2) {
+        if (wave < half) sh[wave][lane] += sh[wave + half][lane];
+        __syncthreads();
+    }
+    if (wave == 0 && col < a.dim && out) out[col] = sh[0][lane];
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+// Rows of a workgroup of the gradient, each of which leaves parts of the sums
+static int block_bwd_chunk(int64_t M)
+{
+    const int64_t t = (M + 255) / 256;
+    return (int)(t < 8 ? 8 : t);
+}
+static size_t block_parts(const lq_block_config* c, int64_t M, int64_t S)
+{
+    const int chunk = block_bwd_chunk(M);
+    return (size_t)((M + chunk - 1) / chunk + S) * 3 * c->dim;
+}
+size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
+{
+    return align256(block_parts(c, M, S) * 4) + align256((size_t)S * 2 * c->dim * 4);
+}
+
+template <typename TH, typename TY, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
+static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
+{
+    const int groups = a.waves > 3 ? 1 : 8 / a.waves;
+    const dim3 grid((unsigned)((a.M + a.chunk - 1) / a.chunk)), block(64 * a.waves * groups);
+    const size_t lds = (size_t)(groups > 1 ? groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (more than 64 KB from rows of 8161 values on)
+    if (lds > 65280) {
+        const hipError_t e = allow_lds<block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>>(131072);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>), grid, block, lds, s, a);
+    return hipGetLastError();
+}
+template <typename TH, typename TY, int NV, bool ANY, bool POST>
+static hipError_t block_bwd_run(const BlockArgs& a, hipStream_t s)
+{
+    if constexpr (NV == 5)
+        if (a.waves > 8) return block_bwd_launch<TH, TY, NV, ANY, POST, true, 1024>(a, s);
+    if constexpr (NV >= 3)
+        if (a.waves > 1) return block_bwd_launch<TH, TY, NV, ANY, POST, true, 512>(a, s);
+    return block_bwd_launch<TH, TY, NV, ANY, POST, false, 512>(a, s);
+}
+template <typename TH, typename TY, bool POST>
+static hipError_t block_bwd_vectors(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
+{
+    if (sh.any) return sh.NV <= 2 ? block_bwd_run<TH, TY, 2, true, POST>(a, s) : block_bwd_run<TH, TY, 5, true, POST>(a, s);
+    switch (sh.NV) {
+        case 1: return block_bwd_run<TH, TY, 1, false, POST>(a, s);
+        case 2: return block_bwd_run<TH, TY, 2, false, POST>(a, s);
+        case 3: return block_bwd_run<TH, TY, 3, false, POST>(a, s);
+        case 4: return block_bwd_run<TH, TY, 4, false, POST>(a, s);
+        default: return block_bwd_run<TH, TY, 5, false, POST>(a, s);
+    }
+}
+template <typename TH, typename TY>
+static hipError_t block_bwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
+{
+    return a.t.y && a.post != LQ_NORM_NONE ? block_bwd_vectors<TH, TY, true>(a, sh, s) : block_bwd_vectors<TH, TY, false>(a, sh, s);
+}
+hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int64_t M, uint8_t* work, hipStream_t s)
+{
+    const bool sums = t.dgate.p || t.dscale.p || t.dshift.p || t.dw_pre || t.dw_post, weights = t.dw_pre || t.dw_post;
+    BlockArgs a = block_args(c, t, M);
+    a.chunk = block_bwd_chunk(M);
+    a.part = sums ? (float*)work : nullptr;
+    hipError_t e = hipSuccess;
+    if (M > 0) {
+        const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M), 4, 5);
+        a.waves = sh.W;
+        e = c->h_dtype == LQ_BF16   ? block_bwd_types<__bf16, __bf16>(a, sh, s)
+            : c->y_dtype == LQ_BF16 ? block_bwd_types<float, __bf16>(a, sh, s)
+                                    : block_bwd_types<float, float>(a, sh, s);
+    }
+    if (e != hipSuccess || !sums) return e;
+    float* raw = weights ? (float*)(work + align256(block_parts(c, M, t.S) * 4)) : nullptr;
+    const int64_t each = (M + a.chunk - 1) / a.chunk / t.S;  // parts of a sequence
+    const unsigned cols = (unsigned)((c->dim + 63) / 64);
+    hipLaunchKernelGGL(block_sums, dim3(cols, 3, (unsigned)(t.S < 4096 ? t.S : 4096)), dim3(each >= 32 ? 1024 : 256), 0, s, a, raw);
+    e = hipGetLastError();
+    if (e != hipSuccess || !weights) return e;
+    hipLaunchKernelGGL(block_weight_sums, dim3(cols, 2), dim3(1024), 0, s, a, (const float*)raw);
+    return hipGetLastError();
+}
+
+}  // namespace lq
