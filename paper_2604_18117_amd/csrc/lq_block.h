@@ -118,26 +118,39 @@ __device__ __forceinline__ int sequence_of(const int32_t* ends, int S, int row)
     }
     return __builtin_amdgcn_readfirstlane(lo);
 }
-// Sequence s and its rows from `row` on: [row, end), cut to the limit; s < 0: rows of no sequence.
-struct Segment {
-    int s, end;
-    __device__ __forceinline__ Segment(const BlockTensors& t, int row, int limit)
+// The sequences as a wavefront knows them: up to 64 ends lie in its lanes, so that they cost one round trip, whose load is the first of all.
+struct Sequences {
+    const int32_t* offsets;
+    int S, start, mine;  // first row of the first; lane's end
+    __device__ __forceinline__ Sequences(const BlockTensors& t) : offsets(t.offsets), S(t.S), start(0), mine(0)
     {
-        if (!t.offsets) {
-            s = 0;
-            end = limit;
-            return;
+        const int lane = threadIdx.x & 63;
+        if (!offsets) return;
+        start = offsets[0];
+        if (S <= 64) mine = offsets[1 + min(lane, S - 1)];
+    }
+    // the sequence of `row` (-1: none) and the end of its rows from there on, not past `limit`
+    __device__ __forceinline__ int find(int row, int limit, int& end) const
+    {
+        end = limit;
+        if (!offsets) return 0;
+        const int first = __builtin_amdgcn_readfirstlane(start);
+        if (row < first) {
+            end = min(first, limit);
+            return -1;
         }
-        const int start = t.offsets[0];
-        if (row < start) {
-            s = -1;
-            end = min(start, limit);
-            return;
+        int s, e;
+        if (S <= 64) {
+            s = __popcll(__ballot((int)(threadIdx.x & 63) < S && mine <= row));
+            e = __builtin_amdgcn_readlane(mine, s < 63 ? s : 63);
+        } else {
+            s = sequence_of(offsets + 1, S, row);
+            e = s < S ? __builtin_amdgcn_readfirstlane(offsets[1 + s]) : 0;
         }
-        s = sequence_of(t.offsets + 1, t.S, row);
-        end = s < t.S ? min(t.offsets[s + 1], limit) : limit;
-        if (s >= t.S) s = -1;
+        if (s >= S) return -1;
+        end = min(e, limit);
         if (end <= row) end = row + 1;  // (ends that do not rise)
+        return s;
     }
 };
 

@@ -17,6 +17,7 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
     int row = group * a.chunk;
     const int limit = min(row + a.chunk, (int)a.M);
     if (row >= limit) return;
+    const Sequences sequences(t);
     Raw<TH, VEC, ANY> rh[NV];
     Raw<TY, VEC, ANY> ry[NV];
     auto request = [&](int m) {
@@ -25,9 +26,10 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
     };
     request(row);
     while (row < limit) {
-        const Segment seg(t, row, limit);
-        if (seg.s < 0) {
-            row = seg.end;
+        int end;
+        const int s = sequences.find(row, limit, end);
+        if (s < 0) {
+            row = end;
             if (row < limit) request(row);
             continue;
         }
@@ -38,11 +40,11 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
             for (int i = 0; i < VEC; ++i) fa[v][i] = fb[v][i] = fs[v][i] = 0.0f;
             if (!c.has(v)) continue;
             const int at = c.at + v * c.step;
-            factor_a<VEC, ANY>(t, at, c.have(v), seg.s, fa[v]);
-            factor_b<VEC, ANY>(t, at, c.have(v), seg.s, fb[v]);
-            if (t.shift.p) read<VEC, ANY>(t.shift.p + seg.s * t.shift.ld + at, c.have(v), fs[v]);
+            factor_a<VEC, ANY>(t, at, c.have(v), s, fa[v]);
+            factor_b<VEC, ANY>(t, at, c.have(v), s, fb[v]);
+            if (t.shift.p) read<VEC, ANY>(t.shift.p + s * t.shift.ld + at, c.have(v), fs[v]);
         }
-        for (; row < seg.end; ++row) {
+        for (; row < end; ++row) {
             float h[NV][VEC], y[NV][VEC];
 #pragma unroll
             for (int v = 0; v < NV; ++v) {

@@ -16,12 +16,13 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
     const BlockTensors& t = a.t;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, W = MULTI ? a.waves : 1, group = wave / W, groups = waves / W;
     const int padded = (a.dim + VEC - 1) / VEC * VEC;
-    float *la = (float*)shared, *lb = la + padded, *joined = lb + padded;  // a, b; [groups][padded] sums
+    float *la = (float*)shared, *lb = la + padded, *joined = lb + padded;  // a, b; [3][groups][padded] sums
     const Columns<VEC, NV, ANY> c(a.dim, threadIdx.x - group * W * 64, W * 64);
     RowSum<MULTI> sum{slots, waves, group * W, wave, W};
     int first = blockIdx.x * a.chunk;
     const int limit = min(first + a.chunk, (int)a.M);
     const bool has_dx = t.dx, has_y = t.y, has_dho = t.dho;
+    const Sequences sequences(t);
     Raw<TH, VEC, ANY> rh[NV], rg[NV];
     Raw<TY, VEC, ANY> ry[NV], rx[NV];
     auto request = [&](int m) {
@@ -36,18 +37,17 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
         read<VEC, false>(l + (c.has(v) ? c.at + v * c.step : 0u), VEC, f);
     };
     while (first < limit) {
-        const Segment seg(t, first, limit);
-        if (seg.s < 0) {
-            first = seg.end;
+        int end;
+        const int s = sequences.find(first, limit, end);
+        if (s < 0) {
+            first = end;
             continue;
         }
-        const int last = seg.end - 1;
-        request(min(first + group, last));
         for (int o = threadIdx.x * VEC; o < padded; o += blockDim.x * VEC) {
             float f[VEC];
-            factor_a<VEC, ANY>(t, o, a.dim - o, seg.s, f);
+            factor_a<VEC, ANY>(t, o, a.dim - o, s, f);
             Raw<float, VEC, false>::put(la + o, VEC, f);
-            factor_b<VEC, ANY>(t, o, a.dim - o, seg.s, f);
+            factor_b<VEC, ANY>(t, o, a.dim - o, s, f);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) f[i] = ANY && i >= a.dim - o ? 0.0f : f[i];
             Raw<float, VEC, false>::put(lb + o, VEC, f);
@@ -58,13 +58,14 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) s1[v][i] = s2[v][i] = s3[v][i] = 0.0f;
         __syncthreads();
-        for (int base = first; base < seg.end; base += groups) {
+#pragma unroll 1
+        for (int base = first; base < end; base += groups) {
             const int row = base + group;
-            const bool on = row < seg.end;  // (of a row: all its wavefronts.  The others take part in the barriers with the last row's values, of which nothing is kept)
+            const bool on = row < end;  // (of a row: all its wavefronts.  The others take part in the barriers with the last row's values, of which nothing is kept)
             if (!MULTI && !on) break;
             asm volatile("" ::: "memory");  // (a and b are read again for every row: kept in registers they would cost a wavefront's)
+            request(min(row, end - 1));
             float n[NV][VEC], dx[NV][VEC], g[NV][VEC];
-            Raw<TY, VEC, ANY> py[NV];
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 if (has_dx) {
@@ -75,9 +76,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
                 else
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) g[v][i] = 0.0f;
-                py[v] = ry[v];
             }
-            if (base + groups < seg.end) request(min(row + groups, last));
             if (has_dx) {
                 float r = 1.0f, u = 0.0f, w = 0.0f;
                 if (a.pre != LQ_NORM_NONE) r = normalise<VEC, NV, ANY, MULTI>(a.pre, n, c, sum, a);
@@ -123,7 +122,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
             if (has_y) {
                 float p[NV][VEC], r = 1.0f, u = 0.0f, w = 0.0f;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) py[v].get(p[v]);
+                for (int v = 0; v < NV; ++v) ry[v].get(p[v]);
                 if (POST) r = normalise<VEC, NV, ANY, MULTI>(a.post, p, c, sum, a);
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
@@ -158,29 +157,35 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
             }
         }
         if (a.part) {
-            float* out = a.part + (size_t)(blockIdx.x + seg.s) * 3 * a.dim;
+            float* out = a.part + (size_t)(blockIdx.x + s) * 3 * a.dim;
+            if (MULTI && groups == 1) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                float* mine = joined + group * padded;
+                for (int k = 0; k < 3; ++k)
 #pragma unroll
-                for (int v = 0; v < NV; ++v)
-                    if (c.has(v)) {
-                        const auto& y = k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v];
-                        if (MULTI && groups == 1) Raw<float, VEC, true>::put(out + k * a.dim + c.at + v * c.step, c.have(v), y);
-                        else Raw<float, VEC, false>::put(mine + c.at + v * c.step, VEC, y);
+                    for (int v = 0; v < NV; ++v)
+                        if (c.has(v)) Raw<float, VEC, true>::put(out + k * a.dim + c.at + v * c.step, c.have(v), k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+                        if (c.has(v)) Raw<float, VEC, false>::put(joined + (k * groups + group) * padded + c.at + v * c.step, VEC, k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
+                __syncthreads();
+                for (int o = threadIdx.x * VEC; o < 3 * padded; o += blockDim.x * VEC) {
+                    const int k = o >= 2 * padded ? 2 : o >= padded ? 1 : 0, col = o - k * padded;
+                    float y[VEC], z[VEC];
+                    read<VEC, false>(joined + k * groups * padded + col, VEC, y);
+                    for (int w = 1; w < groups; ++w) {
+                        read<VEC, false>(joined + (k * groups + w) * padded + col, VEC, z);
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) y[i] += z[i];
                     }
-                if (MULTI && groups == 1) continue;
-                __syncthreads();
-                for (int o = threadIdx.x; o < a.dim; o += blockDim.x) {
-                    float y = joined[o];
-                    for (int w = 1; w < groups; ++w) y += joined[w * padded + o];
-                    out[k * a.dim + o] = y;
+                    Raw<float, VEC, true>::put(out + k * a.dim + col, a.dim - col, y);
                 }
-                __syncthreads();
             }
         }
-        if (!a.part || (MULTI && groups == 1)) __syncthreads();  // (a and b have been read)
-        first = seg.end;
+        if (end < limit) __syncthreads();  // (a, b and the sums have been read)
+        first = end;
     }
 }
 
@@ -247,11 +252,12 @@ __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const flo
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Rows of a workgroup of the gradient, each of which leaves parts of the sums
+// Rows of a workgroup of the gradient, each of which leaves parts of the sums: one workgroup to a compute unit is what its registers allow (us by the number of workgroups,
+// 8192 rows of 1152, bf16: 256 31.7, 512 36.9, 768 42.5), in small batches fewer rows than it has wavefronts (300 fp32 rows in 7 sequences, both norms: 4 22.3, 8 23.3)
 static int block_bwd_chunk(int64_t M)
 {
     const int64_t t = (M + 255) / 256;
-    return (int)(t < 8 ? 8 : t);
+    return (int)(t < 4 ? 4 : t);
 }
 static size_t block_parts(const lq_block_config* c, int64_t M, int64_t S)
 {
@@ -268,9 +274,9 @@ static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
 {
     const int groups = a.waves > 3 ? 1 : 8 / a.waves;
     const dim3 grid((unsigned)((a.M + a.chunk - 1) / a.chunk)), block(64 * a.waves * groups);
-    const size_t lds = (size_t)(groups > 1 ? groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (more than 64 KB from rows of 8161 values on)
+    const size_t lds = (size_t)(groups > 1 ? 3 * groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (up to 140 KB)
     if (lds > 65280) {
-        const hipError_t e = allow_lds<block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>>(131072);
+        const hipError_t e = allow_lds<block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>>(143360);
         if (e != hipSuccess) return e;
     }
     hipLaunchKernelGGL((block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>), grid, block, lds, s, a);
