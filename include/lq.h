@@ -475,7 +475,7 @@ lq_status lq_w4_pack_codes(const lq_w4_config *cfg, const int8_t *codes, const f
 /* Their plain views; either may be NULL. */
 lq_status lq_w4_unpack(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, int8_t *codes, float *scales, void *stream);
 
-/* X: M x K, row stride ldx elements (>= K), Y: M x N, row stride ldy; below 2^40; 0 <= M <= 2^14.  bias: N fp32 or NULL.  Y must not overlap X. */
+/* X: M x K, row stride ldx elements (>= K), Y: M x N, row stride ldy; at most 2^22; 0 <= M <= 2^14.  bias: N fp32 or NULL.  Y must not overlap X. */
 lq_status lq_w4_fwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy,
                     int64_t M, void *stream);
 

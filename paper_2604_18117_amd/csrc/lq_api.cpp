@@ -797,10 +797,10 @@ static lq_status w4_packed_check(const lq_w4_config* c, const void* packed, size
     return packed_bytes < w4_packed_bytes(c) ? LQ_ERR_BUFFER_TOO_SMALL : LQ_OK;
 }
 // M rows of `len` values that may start anywhere; the stride of a single row says nothing
-static lq_status any_rows_check(const void* p, int64_t ld, int64_t len, int64_t M, int elem)
+static lq_status any_rows_check(const void* p, int64_t ld, int64_t len, int64_t M, int elem, int64_t most = ((int64_t)1 << 40) - 1)
 {
     if (!p) return LQ_ERR_NULL;
-    if (M > 1 && (ld < len || ld >= ((int64_t)1 << 40))) return LQ_ERR_SHAPE;
+    if (M > 1 && (ld < len || ld > most)) return LQ_ERR_SHAPE;
     return aligned(p, elem) ? LQ_OK : LQ_ERR_ALIGN;
 }
 static int dtype_bytes(int32_t dtype) { return dtype == LQ_F32 ? 4 : 2; }
@@ -849,8 +849,8 @@ lq_status lq_w4_fwd(const lq_w4_config* cfg, const void* packed, size_t packed_b
     lq_status st = w4_check(cfg);
     if (st != LQ_OK || (st = w4_batch_check(M)) != LQ_OK) return st;
     if (M == 0) return LQ_OK;  // an empty batch
-    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(X, ldx, cfg->K, M, dtype_bytes(cfg->x_dtype))) != LQ_OK ||
-        (st = any_rows_check(Y, ldy, cfg->N, M, dtype_bytes(cfg->y_dtype))) != LQ_OK)
+    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(X, ldx, cfg->K, M, dtype_bytes(cfg->x_dtype), 1 << 22)) != LQ_OK ||
+        (st = any_rows_check(Y, ldy, cfg->N, M, dtype_bytes(cfg->y_dtype), 1 << 22)) != LQ_OK)
         return st;
     if (!aligned(bias, 4)) return LQ_ERR_ALIGN;
     return launch_w4_fwd(cfg, (const uint8_t*)packed, X, ldx, bias, Y, ldy, M, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
@@ -871,8 +871,8 @@ lq_status lq_w4_bwd(const lq_w4_config* cfg, const void* packed, size_t packed_b
     lq_status st = w4_check(cfg);
     if (st != LQ_OK || (st = w4_batch_check(M)) != LQ_OK) return st;
     if (M == 0) return LQ_OK;  // an empty batch
-    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(dY, lddy, cfg->N, M, dtype_bytes(cfg->y_dtype))) != LQ_OK ||
-        (st = any_rows_check(dX, lddx, cfg->K, M, dtype_bytes(cfg->x_dtype))) != LQ_OK)
+    if ((st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK || (st = any_rows_check(dY, lddy, cfg->N, M, dtype_bytes(cfg->y_dtype), 1 << 22)) != LQ_OK ||
+        (st = any_rows_check(dX, lddx, cfg->K, M, dtype_bytes(cfg->x_dtype), 1 << 22)) != LQ_OK)
         return st;
     const size_t need = w4_work_bytes(cfg, M);
     if (need && !work) return LQ_ERR_NULL;

@@ -3,6 +3,7 @@
 // Codes are small integers, exact in bf16; group sums and everything after them are held in fp32.  Bound by the read of the codes (half a byte a weight), in
 // small layers by latency.
 #include "lq_internal.h"
+#include <type_traits>
 
 namespace lq {
 
@@ -157,6 +158,19 @@ __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[3])
     }
 }
 
+__device__ __forceinline__ void split4(v4i v, uint2 (&t)[3])  // ... of four, as packed pairs
+{
+    float r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = __int_as_float(v[j]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        t[k] = make_uint2(tops(r[0], r[1]), tops(r[2], r[3]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = k == 0 && __builtin_isinf(r[j]) ? 0.0f : r[j] - cut(r[j]);
+    }
+}
+
 // ---- forward ------------------------------------------------------------------------------------
 
 struct W4Args {
@@ -169,89 +183,162 @@ struct W4Args {
     int64_t ldy;
     int64_t M, N, K;
     int tiles, blocks;
-    int vec;        // rows of X can be read 16 bytes at a time
     int out_f32;
     int splits;     // backward: parts of N
     float* part;
 };
 
-// Eight values of a row of X from k on, as they lie in memory
+constexpr int w4_fwd_lds(bool f32, int mt, int nt)  // bytes of a wavefront: its block of X (of fp32 values three terms), then its sums
+{
+    const int x = (f32 ? 3 : 1) * 16 * mt * 272, sums = mt * nt * 1024;
+    return x > sums ? x : sums;
+}
+
+// Eight values of a row, as they lie in memory (of any alignment: the card reads 16 bytes from wherever they start)
 template <bool F32>
 struct Eight {
-    v4i v[F32 ? 2 : 1];
-    __device__ __forceinline__ void fetch(const void* row, int64_t k, int64_t K, bool vec)
+    typedef v4i Access __attribute__((aligned(2)));
+    static constexpr int H = F32 ? 2 : 1;
+    v4i v[H];
+    __device__ __forceinline__ void read(const char* row, int k)
     {
 #pragma unroll
-        for (int h = 0; h < (F32 ? 2 : 1); ++h) v[h] = v4i{0, 0, 0, 0};
-        if (!row) return;
-        if (vec && k + 8 <= K) {
+        for (int h = 0; h < H; ++h) v[h] = ((const Access*)(row + (size_t)k * (F32 ? 4 : 2)))[h];
+    }
+    // Where a row may end among them: zeros from `end` on.  The row's last eight values are read and moved to their places; with a read of its own for every value, or a branch for
+    // every read, the end of a row cost more than the rest of it.
+    __device__ __forceinline__ void read_end(const char* row, int k, int end)
+    {
+        if (end < 8) {
 #pragma unroll
-            for (int h = 0; h < (F32 ? 2 : 1); ++h) v[h] = ((const v4i*)((const char*)row + k * (F32 ? 4 : 2)))[h];
-        } else {
+            for (int h = 0; h < H; ++h) v[h] = v4i{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (k + i < K) {
+            for (int i = 0; i < 8; ++i)
+                if (k + i < end) {
                     if constexpr (F32) v[i / 4][i % 4] = ((const int*)row)[k + i];
                     else v[0][i / 2] |= (int)((uint32_t)((const uint16_t*)row)[k + i] << (16 * (i & 1)));
                 }
+            return;
+        }
+        const int first = min(k, end - 8), past = min(k - first, 8);
+        read(row, first);
+#pragma unroll
+        for (int step = 8; step >= 1; step /= 2) {
+            const bool on = past & step;
+#pragma unroll
+            for (int d = 0; d < 4 * H; ++d) {
+                int moved;
+                if (!F32 && step == 1) {
+                    moved = (int)((uint32_t)v[0][d] >> 16) | (d < 3 ? v[0][d < 3 ? d + 1 : 0] << 16 : 0);
+                } else {
+                    const int from = d + (F32 ? step : step / 2);
+                    moved = from < 4 * H ? v[from / 4 < H ? from / 4 : 0][from % 4] : 0;
+                }
+                v[d / 4][d % 4] = on ? moved : v[d / 4][d % 4];
             }
         }
     }
-    __device__ __forceinline__ void terms(v4i (&t)[F32 ? 3 : 1]) const
+    __device__ __forceinline__ void values(float (&f)[8]) const
     {
-        if constexpr (F32) {
-            float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = __int_as_float(v[i / 4][i % 4]);
-            split8(f, t);
-        } else {
-            t[0] = v[0];
-        }
+        for (int i = 0; i < 8; ++i)
+            f[i] = __int_as_float(F32 ? v[F32 ? i / 4 : 0][i % 4] : i & 1 ? v[0][i / 2] & (int)0xFFFF0000 : v[0][i / 2] << 16);
     }
 };
 
-// A workgroup makes 16 MT rows of NT tiles; its wavefronts share K out block by block and join their sums in the LDS.
+// A workgroup makes 16 MT rows of NT tiles; its wavefronts share K out block by block and join their sums in the LDS.  A wavefront brings its block of X through LDS of its own: 16 lanes
+// read a row's 256 bytes (32 lanes 512), where the product's order, 16 rows in 16 lanes, is a piece of a cache line in every lane.  The next block is requested ahead of the products of
+// this one.  Rows past M repeat the last one and are not stored.  In the block where rows end, pieces of 16 bytes past the end are zero; the one in which they end is brought value by value.
 template <bool F32, int MT, int NT, int PER>
 __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
 {
-    extern __shared__ float joined[];  // [wavefront][MT][NT][4][64]
-    constexpr int TERMS = F32 ? 3 : 1;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int q = lane >> 4, tile0 = blockIdx.x * NT;
-    const int64_t m0 = (int64_t)blockIdx.y * (16 * MT);
-    const void* row[MT];
+    extern __shared__ v4i shared[];
+    typedef v4i Piece __attribute__((aligned(2)));
+    typedef typename std::conditional<F32, uint32_t, uint16_t>::type Bits;
+    float* joined = (float*)shared;  // [wavefront][MT][NT][4][64]
+    constexpr int TERMS = F32 ? 3 : 1, EB = F32 ? 4 : 2, LANES = 8 * EB, ROWS = 64 / LANES, N = 16 * MT / ROWS, STRIDE = 272, TERM = 16 * MT * STRIDE;  // lanes of a row; rows at a time; bytes of a row and of a term in the LDS
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int q = lane >> 4, tile0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * MT), end = (int)a.K * EB;
+    char* mine = (char*)shared + wave * w4_fwd_lds(F32, MT, NT);
+    const char* X = (const char*)a.X + (int64_t)m0 * a.ldx * EB;
+    const unsigned pitch = (unsigned)a.ldx * EB;
+    const int part = lane % LANES * 16, last = (int)a.M - 1 - m0;
+    unsigned at[N];  // of the lane's rows
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int64_t m = m0 + 16 * mt + (lane & 15);
-        row[mt] = m < a.M ? (const char*)a.X + m * a.ldx * (F32 ? 4 : 2) : nullptr;
-    }
+    for (int i = 0; i < N; ++i) at[i] = (unsigned)min(i * ROWS + lane / LANES, last) * pitch;
     v4f sum[MT][NT];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int t = 0; t < NT; ++t) sum[mt][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v4i next[NT], x[N];
+    float next_sc[NT][PER];
+    auto request = [&](int b) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const size_t o = (size_t)min(tile0 + t, a.tiles - 1) * a.blocks + b;
+            next[t] = ((const v4i*)a.codes)[o * 64 + lane];
+#pragma unroll
+            for (int g = 0; g < PER; ++g) next_sc[t][g] = a.scales[(o * 16 + (lane & 15)) * PER + g];
+        }
+        if (end >= 16) {
+            const unsigned k = (unsigned)min(b * (128 * EB) + part, end - 16);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i * ROWS <= last) x[i] = *(const Piece*)(X + (at[i] + k));  // (the same for the wavefront)
+        }
+    };
+    request(wave);  // (there are no more wavefronts than blocks)
     for (int b = wave; b < a.blocks; b += waves) {
+        const int k0 = b * (128 * EB);
+        if (k0 + 128 * EB > end) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = k0 + part + 16 <= end ? x[i] : v4i{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i * ROWS <= last) {
+                char* to = mine + (i * ROWS + lane / LANES) * STRIDE + part * 2 / EB;
+                if constexpr (F32) {
+                    uint2 t[3];
+                    split4(x[i], t);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) *(uint2*)(to + k * TERM) = t[k];
+                } else {
+                    *(v4i*)to = x[i];
+                }
+            }
+        if (k0 + 128 * EB > end && end % 16) {
+            Bits v[2 * MT];  // eight rows of eight values (f32: of four) at a time
+            const int k = end / 16 * 16 + (lane & 7) * EB;
+#pragma unroll
+            for (int i = 0; i < 2 * MT; ++i) v[i] = k < end ? *(const Bits*)(X + (int64_t)min(8 * i + (lane >> 3), last) * pitch + k) : (Bits)0;
+#pragma unroll
+            for (int i = 0; i < 2 * MT; ++i)
+                if ((lane & 7) * EB < 16) {
+                    char* to = mine + (8 * i + (lane >> 3)) * STRIDE + (k - k0) * 2 / EB;
+                    if constexpr (F32) {
+                        uint2 t[3];
+                        split4(v4i{(int)v[i], 0, 0, 0}, t);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) *(uint16_t*)(to + k * TERM) = (uint16_t)t[k].x;
+                    } else {
+                        *(uint16_t*)to = v[i];
+                    }
+                }
+        }
         v4i code[NT];
         float sc[NT][PER];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const size_t at = (size_t)min(tile0 + t, a.tiles - 1) * a.blocks + b;
-            code[t] = ((const v4i*)a.codes)[at * 64 + lane];
+            code[t] = next[t];
 #pragma unroll
-            for (int g = 0; g < PER; ++g) sc[t][g] = a.scales[(at * 16 + (lane & 15)) * PER + g];
+            for (int g = 0; g < PER; ++g) sc[t][g] = next_sc[t][g];
         }
-        Eight<F32> x[MT][4];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[mt][j].fetch(row[mt], (int64_t)b * 128 + 32 * j + 8 * q, a.K, a.vec);
+        if (b + waves < a.blocks) request(b + waves);
 #pragma unroll
         for (int g = 0; g < PER; ++g) {
             v4f acc[MT][NT];
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) acc[mt][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int j = g * 4 / PER; j < (g + 1) * 4 / PER; ++j) {
                 v4i w[NT];
@@ -260,11 +347,12 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     v4i xt[TERMS];
-                    x[mt][j].terms(xt);
+#pragma unroll
+                    for (int k = 0; k < TERMS; ++k) xt[k] = *(const v4i*)(mine + k * TERM + (16 * mt + (lane & 15)) * STRIDE + (32 * j + 8 * q) * 2);
 #pragma unroll
                     for (int k = TERMS - 1; k >= 0; --k)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) acc[mt][t] = mfma(xt[k], w[t], acc[mt][t]);
+                        for (int t = 0; t < NT; ++t) acc[mt][t] = mfma(xt[k], w[t], j == g * 4 / PER && k == TERMS - 1 ? v4f{0.0f, 0.0f, 0.0f, 0.0f} : acc[mt][t]);
                 }
             }
 #pragma unroll
@@ -275,13 +363,14 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
                     for (int r = 0; r < 4; ++r) sum[mt][t][r] = fmaf(sc[t][g], acc[mt][t][r], sum[mt][t][r]);
         }
     }
+    __syncthreads();
     constexpr int S = MT * NT * 256;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) joined[wave * S + ((mt * NT + t) * 4 + r) * 64 + lane] = sum[mt][t][r];
+            for (int r = 0; r < 4; ++r) joined[wave * (w4_fwd_lds(F32, MT, NT) / 4) + ((mt * NT + t) * 4 + r) * 64 + lane] = sum[mt][t][r];
     __syncthreads();
     // value (mt, t, r, lane): row 16 mt + 4 (lane / 16) + r, channel lane % 16 of tile t
     for (int o = threadIdx.x; o < S; o += blockDim.x) {
@@ -289,7 +378,7 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
         const int64_t m = m0 + 16 * mt + 4 * (l >> 4) + r, n = (int64_t)(tile0 + t) * 16 + (l & 15);
         if (m >= a.M || n >= a.N) continue;
         float y = joined[o];
-        for (int w = 1; w < waves; ++w) y += joined[w * S + o];
+        for (int w = 1; w < waves; ++w) y += joined[w * (w4_fwd_lds(F32, MT, NT) / 4) + o];
         if (a.bias) y += a.bias[n];
         if (a.out_f32) ((float*)a.Y)[m * a.ldy + n] = y;
         else ((__bf16*)a.Y)[m * a.ldy + n] = (__bf16)y;
@@ -298,72 +387,118 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
 
 // ---- gradient ------------------------------------------------------------------------------------
 
-// dX of R rows: a lane's 32 columns of a block, over the 16 channels of a tile in 16 lanes; tiles are dealt to the workgroup's wavefronts and to the parts of N.  The
-// 16 lanes' sums are joined by halving what each keeps, the wavefronts' in the LDS, the parts' by w4_join.
-template <bool F32, int R, int PER>
-__global__ void __launch_bounds__(256) w4_bwd_kernel(W4Args a)
+// Nibble p(r) of dword i from nibble p(i) of dword r, eight by eight (p: the place of a value in a dword): bit by bit of the two numbers, 32 instructions
+__device__ __forceinline__ void turn_nibbles(uint32_t (&d)[8])
 {
-    __shared__ float joined[4][R][128];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, q = lane >> 4;
-    const int block = blockIdx.x, split = blockIdx.y;
-    const int64_t m0 = (int64_t)blockIdx.z * R;
-    float acc[R][32];
 #pragma unroll
-    for (int m = 0; m < R; ++m)
+    for (int r = 0; r < 4; ++r) {
+        const uint32_t x = d[r], y = d[r + 4];
+        d[r] = (x & 0x0F0F0F0Fu) | (y << 4 & 0xF0F0F0F0u);
+        d[r + 4] = (x >> 4 & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+    }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) acc[m][i] = 0.0f;
-    for (int t = split * 4 + wave; t < a.tiles; t += 4 * a.splits) {
-        const size_t at = (size_t)t * a.blocks + block;
-        const v4i code = ((const v4i*)a.codes)[at * 64 + lane];
-        float sc[PER], g[R];
+    for (int k = 0; k < 4; ++k) {
+        const int r = k & 1 | (k & 2) << 1;
+        const uint32_t x = d[r], y = d[r + 2];
+        d[r] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        d[r + 2] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sc[i] = a.scales[(at * 16 + c) * PER + i];
-        const int64_t n = (int64_t)t * 16 + c;
+    for (int r = 0; r < 8; r += 2) {
+        const uint32_t x = d[r], y = d[r + 1];
+        d[r] = __builtin_amdgcn_perm(y, x, 0x06020400u);
+        d[r + 1] = __builtin_amdgcn_perm(y, x, 0x07030501u);
+    }
+}
+
+// dX of 16 rows and a block of 128 columns.  A wavefront takes 32 channels at a time (two tiles), which it brings through LDS of its own so that lane (c, q) holds eight channels
+// 8 q .. + 7 of the eight columns 8 c .. + 7; turned, they are the operands of eight products, product i with the columns 8 c + i.  The channels' scales go into dY (fp32, three terms);
+// where a block has several groups, a product is made for each and a lane keeps that of its own columns.  The wavefronts' sums are joined in the LDS, those of the parts of N by w4_join.
+constexpr int w4_bwd_waves(int per) { return per == 4 ? 4 : 8; }  // (sums for four groups are 128 registers)
+template <bool F32, int PER>
+__global__ void __launch_bounds__(64 * w4_bwd_waves(PER)) w4_bwd_kernel(W4Args a)
+{
+    extern __shared__ v4i shared[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, c = lane & 15, q = lane >> 4;
+    const int block = blockIdx.x, split = blockIdx.y, steps = (a.tiles + 1) / 2;
+    const int64_t m0 = (int64_t)blockIdx.z * 16;
+    const char* row = (const char*)a.X + min(m0 + c, a.M - 1) * a.ldx * (F32 ? 4 : 2);
+    char* mine = (char*)shared + wave * 2176;  // [2 tiles][4][16 channels + 1][16 bytes]: every read finds 64 banks
+    v4f acc[PER][8];
 #pragma unroll
-        for (int m = 0; m < R; ++m) {
-            g[m] = 0.0f;
-            if (n < a.N && m0 + m < a.M) {
-                if constexpr (F32) g[m] = ((const float*)a.X)[(m0 + m) * a.ldx + n];
-                else g[m] = (float)((const __bf16*)a.X)[(m0 + m) * a.ldx + n];
-            }
+    for (int g = 0; g < PER; ++g)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[g][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v4i next[2];
+    float next_sc[8 * PER];
+    Eight<F32> next_dy;
+    auto request = [&](int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) next[t] = ((const v4i*)a.codes)[((size_t)min(2 * s + t, a.tiles - 1) * a.blocks + block) * 64 + lane];
+        const float* sc = a.scales + (((size_t)min(2 * s + (q >> 1), a.tiles - 1) * a.blocks + block) * 16 + 8 * (q & 1)) * PER;
+#pragma unroll
+        for (int i = 0; i < 2 * PER; ++i) {
+            const v4f v = ((const v4f*)sc)[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) next_sc[4 * i + e] = v[e];
         }
+        if ((s + 1) * 32 <= a.N) next_dy.read(row, s * 32 + 8 * q);
+        else next_dy.read_end(row, s * 32 + 8 * q, (int)a.N);
+    };
+    const int first = split * waves + wave, stride = a.splits * waves;
+    if (first < steps) request(first);
+    for (int s = first; s < steps; s += stride) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const v4i w = w4_bf16((uint32_t)code[j]);
+        for (int t = 0; t < 2; ++t) *(v4i*)(mine + t * 1088 + q * 272 + c * 16) = next[t];
+        float dy[8], sc[8 * PER];
+        next_dy.values(dy);
+#pragma unroll
+        for (int i = 0; i < 8 * PER; ++i) sc[i] = next_sc[i];
+        if (s + stride < steps) request(s + stride);
+        uint32_t d[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) d[r] = *(const uint32_t*)(mine + (q >> 1) * 1088 + (c & 3) * 272 + (8 * (q & 1) + r) * 16 + (c >> 2) * 4);
+        turn_nibbles(d);
+        v4i up[PER][3];
+#pragma unroll
+        for (int g = 0; g < PER; ++g) {
             float f[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(i & 1 ? (uint32_t)w[i / 2] & 0xFFFF0000u : (uint32_t)w[i / 2] << 16);
+            for (int i = 0; i < 8; ++i) f[i] = dy[i] * sc[i * PER + g];
+            split8(f, up[g]);
+        }
 #pragma unroll
-            for (int m = 0; m < R; ++m) {
-                const float u = g[m] * sc[j * PER / 4];
+        for (int i = 0; i < 8; ++i) {
+            const v4i w = w4_bf16(d[i]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[m][8 * j + i] = fmaf(u, f[i], acc[m][8 * j + i]);
-            }
+            for (int k = 2; k >= 0; --k)
+#pragma unroll
+                for (int g = 0; g < PER; ++g) acc[g][i] = mfma(up[g][k], w, acc[g][i]);
         }
     }
-#pragma unroll
-    for (int m = 0; m < R; ++m) {
-#pragma unroll
-        for (int half = 16; half >= 2; half /= 2) {
-            const int bit = half / 2;
-            const bool up = c & bit;
-#pragma unroll
-            for (int i = 0; i < half; ++i) {
-                const float give = up ? acc[m][i] : acc[m][i + half], keep = up ? acc[m][i + half] : acc[m][i];
-                acc[m][i] = keep + __shfl_xor(give, bit);
-            }
-        }
-        // two values are left: columns 2 c, 2 c + 1 of the 32
-        const int i = 2 * c;
-        joined[wave][m][32 * (i >> 3) + 8 * q + (i & 7)] = acc[m][0];
-        joined[wave][m][32 * (i >> 3) + 8 * q + (i & 7) + 1] = acc[m][1];
-    }
+    float* joined = (float*)shared;  // [wavefront][16][128]
     __syncthreads();
-    for (int o = threadIdx.x; o < R * 128; o += 256) {
+    // sum r of product i: row 4 q + r, column 8 c + i
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v4f v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = acc[0][4 * h + e][r];
+#pragma unroll
+                for (int g = 1; g < PER; ++g) v[e] = c * PER / 16 == g ? acc[g][4 * h + e][r] : v[e];
+            }
+            *(v4f*)(joined + (wave * 16 + 4 * q + r) * 128 + 8 * c + 4 * h) = v;
+        }
+    __syncthreads();
+    for (int o = threadIdx.x; o < 16 * 128; o += blockDim.x) {
         const int m = o >> 7, k = o & 127;
         const int64_t kk = (int64_t)block * 128 + k;
         if (m0 + m >= a.M || kk >= a.K) continue;
-        const float v = (joined[0][m][k] + joined[1][m][k]) + (joined[2][m][k] + joined[3][m][k]);
+        float v = joined[m * 128 + k];
+        for (int w = 1; w < waves; ++w) v += joined[(w * 16 + m) * 128 + k];
         if (a.part) a.part[((size_t)split * a.M + m0 + m) * a.K + kk] = v;
         else if (a.out_f32) ((float*)a.Y)[(m0 + m) * a.ldy + kk] = v;
         else ((__bf16*)a.Y)[(m0 + m) * a.ldy + kk] = (__bf16)v;
@@ -407,24 +542,43 @@ hipError_t launch_w4_unpack(const lq_w4_config* c, const uint8_t* packed, int8_t
     return hipGetLastError();
 }
 
-template <bool F32, int MT, int NT>
-static void w4_fwd_per(const W4Args& a, int per, dim3 grid, int waves, hipStream_t s)
+template <bool F32, int MT, int NT, int PER>
+static hipError_t w4_fwd_run(const W4Args& a, int waves, hipStream_t s)
 {
-    const size_t lds = (size_t)waves * MT * NT * 1024;
-    if (per == 1) hipLaunchKernelGGL((w4_fwd_kernel<F32, MT, NT, 1>), grid, dim3(64 * waves), lds, s, a);
-    else if (per == 2) hipLaunchKernelGGL((w4_fwd_kernel<F32, MT, NT, 2>), grid, dim3(64 * waves), lds, s, a);
-    else hipLaunchKernelGGL((w4_fwd_kernel<F32, MT, NT, 4>), grid, dim3(64 * waves), lds, s, a);
+    const int lds = waves * w4_fwd_lds(F32, MT, NT);
+    if (lds > 65536) {
+        const hipError_t e = allow_lds<w4_fwd_kernel<F32, MT, NT, PER>>(8 * w4_fwd_lds(F32, MT, NT));
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL((w4_fwd_kernel<F32, MT, NT, PER>), dim3((a.tiles + NT - 1) / NT, (unsigned)((a.M + 16 * MT - 1) / (16 * MT))), dim3(64 * waves), lds, s, a);
+    return hipGetLastError();
 }
-template <bool F32>
-static void w4_fwd_rows(const W4Args& a, int per, hipStream_t s)
+template <bool F32, int MT, int NT>
+static hipError_t w4_fwd_per(const W4Args& a, int per, int waves, hipStream_t s)
 {
-    const int waves = a.blocks < 8 ? a.blocks : 8;
-    if (a.M <= 16) w4_fwd_per<F32, 1, 1>(a, per, dim3(a.tiles, 1), waves, s);
-    else if (a.M <= 32) w4_fwd_per<F32, 2, 1>(a, per, dim3(a.tiles, 1), waves, s);
-    else w4_fwd_per<F32, 4, 2>(a, per, dim3((a.tiles + 1) / 2, (unsigned)((a.M + 63) / 64)), waves, s);
+    return per == 1 ? w4_fwd_run<F32, MT, NT, 1>(a, waves, s) : per == 2 ? w4_fwd_run<F32, MT, NT, 2>(a, waves, s) : w4_fwd_run<F32, MT, NT, 4>(a, waves, s);
+}
+// Rows and channels of a workgroup.  bf16: one tile and up to 16 rows, from more than 16 rows on 32, with two tiles (what is unpacked and what is read of X are shared) where one would leave
+// more than two workgroups to a compute unit (us, one / two tiles: 64 x 2240 -> 11200 16.5 / 12.9, 64 x 1152 -> 1152 4.3 / 5.1).  fp32 rows, whose three terms take three times the LDS: 16 rows
+// and up to three tiles (4 x 4608 -> 13440 19.8 / 14.1 / 17.6, 64 x 2240 -> 11200 - / 30.5 / 27.0, 64 x 1152 -> 1152 - / 7.4 / 8.3).  Eight wavefronts share K out where there are few
+// workgroups, four elsewhere (us, 8 / 4: 16 x 4608 -> 2240 5.2 / 5.9, 64 x 2240 -> 11200 16.6 / 12.9).
+template <bool F32>
+static hipError_t w4_fwd_rows(const W4Args& a, int per, hipStream_t s)
+{
+    const int MT = !F32 && a.M > 16 ? 2 : 1;
+    const int64_t groups = a.tiles * ((a.M + 16 * MT - 1) / (16 * MT));
+    const int NT = F32 ? (groups <= 768 ? 1 : groups <= 1536 ? 2 : 3) : MT == 2 && groups > 512 ? 2 : 1;
+    const int most = groups / NT <= 256 ? 8 : 4, waves = a.blocks < most ? a.blocks : most;
+    if constexpr (F32) {
+        if (NT == 1) return w4_fwd_per<F32, 1, 1>(a, per, waves, s);
+        return NT == 2 ? w4_fwd_per<F32, 1, 2>(a, per, waves, s) : w4_fwd_per<F32, 1, 3>(a, per, waves, s);
+    } else {
+        if (MT == 1) return w4_fwd_per<F32, 1, 1>(a, per, waves, s);
+        return NT == 1 ? w4_fwd_per<F32, 2, 1>(a, per, waves, s) : w4_fwd_per<F32, 2, 2>(a, per, waves, s);
+    }
 }
 
-static W4Args w4_args(const lq_w4_config* c, const uint8_t* packed, const void* in, int64_t ldin, int in_elem, void* out, int64_t ldout, int64_t M)
+static W4Args w4_args(const lq_w4_config* c, const uint8_t* packed, const void* in, int64_t ldin, void* out, int64_t ldout, int64_t M)
 {
     const W4Shape sh = w4_shape(c);
     W4Args a{};
@@ -439,26 +593,21 @@ static W4Args w4_args(const lq_w4_config* c, const uint8_t* packed, const void* 
     a.K = c->K;
     a.tiles = sh.tiles;
     a.blocks = sh.blocks;
-    a.vec = (uintptr_t)in % 16 == 0 && (M < 2 || ldin * in_elem % 16 == 0);
     return a;
 }
 
 hipError_t launch_w4_fwd(const lq_w4_config* c, const uint8_t* packed, const void* X, int64_t ldx, const float* bias, void* Y, int64_t ldy, int64_t M, hipStream_t s)
 {
-    W4Args a = w4_args(c, packed, X, ldx, c->x_dtype == LQ_F32 ? 4 : 2, Y, ldy, M);
+    W4Args a = w4_args(c, packed, X, ldx, Y, ldy, M);
     a.bias = bias;
     a.out_f32 = c->y_dtype == LQ_F32;
-    if (c->x_dtype == LQ_F32) w4_fwd_rows<true>(a, 128 / c->group, s);
-    else w4_fwd_rows<false>(a, 128 / c->group, s);
-    return hipGetLastError();
+    return c->x_dtype == LQ_F32 ? w4_fwd_rows<true>(a, 128 / c->group, s) : w4_fwd_rows<false>(a, 128 / c->group, s);
 }
 
-// Rows of a workgroup of the gradient, and parts of N: two workgroups to a compute unit, each wavefront with two tiles or more
-static int w4_bwd_rows(int64_t M) { return M == 1 ? 1 : M == 2 ? 2 : 4; }
+// Parts of N of the gradient: a workgroup to a compute unit (us by their number, 16 x 2240 -> 13440 / 2 x 1152 -> 6912: 128 15.9 / 9.8, 256 12.8 / 9.0, 512 15.0 / 8.8, 1024 18.1 / 9.4)
 static int w4_bwd_splits(const W4Shape& s, int64_t M)
 {
-    const int R = w4_bwd_rows(M);
-    const int64_t others = (int64_t)s.blocks * ((M + R - 1) / R), want = (512 + others - 1) / others, most = (s.tiles + 7) / 8;
+    const int64_t others = (int64_t)s.blocks * ((M + 15) / 16), want = 256 / others, waves = w4_bwd_waves(s.per), most = ((s.tiles + 1) / 2 + waves - 1) / waves;
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
 size_t w4_work_bytes(const lq_w4_config* c, int64_t M)
@@ -467,31 +616,25 @@ size_t w4_work_bytes(const lq_w4_config* c, int64_t M)
     return splits > 1 ? align256((size_t)splits * M * c->K * 4) : 0;
 }
 
-template <bool F32, int R>
-static void w4_bwd_per(const W4Args& a, int per, dim3 grid, hipStream_t s)
+template <bool F32, int PER>
+static hipError_t w4_bwd_run(const W4Args& a, hipStream_t s)
 {
-    if (per == 1) hipLaunchKernelGGL((w4_bwd_kernel<F32, R, 1>), grid, dim3(256), 0, s, a);
-    else if (per == 2) hipLaunchKernelGGL((w4_bwd_kernel<F32, R, 2>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((w4_bwd_kernel<F32, R, 4>), grid, dim3(256), 0, s, a);
+    constexpr int waves = w4_bwd_waves(PER);
+    hipLaunchKernelGGL((w4_bwd_kernel<F32, PER>), dim3(a.blocks, a.splits, (unsigned)((a.M + 15) / 16)), dim3(64 * waves), waves * 8192, s, a);
+    return hipGetLastError();
 }
 template <bool F32>
-static void w4_bwd_all(const W4Args& a, int per, hipStream_t s)
+static hipError_t w4_bwd_all(const W4Args& a, int per, hipStream_t s)
 {
-    const int R = w4_bwd_rows(a.M);
-    const dim3 grid(a.blocks, a.splits, (unsigned)((a.M + R - 1) / R));
-    if (R == 1) w4_bwd_per<F32, 1>(a, per, grid, s);
-    else if (R == 2) w4_bwd_per<F32, 2>(a, per, grid, s);
-    else w4_bwd_per<F32, 4>(a, per, grid, s);
+    return per == 1 ? w4_bwd_run<F32, 1>(a, s) : per == 2 ? w4_bwd_run<F32, 2>(a, s) : w4_bwd_run<F32, 4>(a, s);
 }
 hipError_t launch_w4_bwd(const lq_w4_config* c, const uint8_t* packed, const void* dY, int64_t lddy, void* dX, int64_t lddx, int64_t M, uint8_t* work, hipStream_t s)
 {
-    W4Args a = w4_args(c, packed, dY, lddy, c->y_dtype == LQ_F32 ? 4 : 2, dX, lddx, M);
+    W4Args a = w4_args(c, packed, dY, lddy, dX, lddx, M);
     a.out_f32 = c->x_dtype == LQ_F32;
     a.splits = w4_bwd_splits(w4_shape(c), M);
     a.part = a.splits > 1 ? (float*)work : nullptr;
-    if (c->y_dtype == LQ_F32) w4_bwd_all<true>(a, 128 / c->group, s);
-    else w4_bwd_all<false>(a, 128 / c->group, s);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = c->y_dtype == LQ_F32 ? w4_bwd_all<true>(a, 128 / c->group, s) : w4_bwd_all<false>(a, 128 / c->group, s);
     if (e != hipSuccess || !a.part) return e;
     hipLaunchKernelGGL(w4_join, dim3((unsigned)((M * c->K + 63) / 64)), dim3(256), 0, s, a);
     return hipGetLastError();

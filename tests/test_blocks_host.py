@@ -63,7 +63,7 @@ def test_w4_arguments(name):
     if name in ("fwd", "bwd"):
         assert _w4(name, X=None) == _w4(name, Y=None) == lq.LQ_ERR_NULL
         assert _w4(name, X=PTR + 1) == _w4(name, Y=PTR + 1) == _w4(name, _wcfg(x_dtype=lq.LQ_F32), X=PTR + 2) == lq.LQ_ERR_ALIGN
-        assert _w4(name, ldx=199) == _w4(name, ldy=99) == _w4(name, ldx=1 << 40) == _w4(name, M=-1) == _w4(name, M=(1 << 14) + 1) == lq.LQ_ERR_SHAPE
+        assert _w4(name, ldx=199) == _w4(name, ldy=99) == _w4(name, ldx=(1 << 22) + 1) == _w4(name, ldy=(1 << 22) + 1) == _w4(name, M=-1) == _w4(name, M=(1 << 14) + 1) == lq.LQ_ERR_SHAPE
         assert _w4(name, M=0, X=None, Y=None, packed=None) == lq.LQ_OK
     if name == "fwd":
         assert _w4(name, bias=PTR + 2) == lq.LQ_ERR_ALIGN
