@@ -544,7 +544,7 @@ lq_status lq_block_norm_bwd(const lq_block_config *cfg, const void *ho, int64_t 
 /* ---- AdamW step over many tensors --------------------------------------------------------------------------------
        g = grad_scale grad ;  m = beta1 m + (1 - beta1) g ;  v = beta2 v + (1 - beta2) g^2
        p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
-   in fp32, every operation rounded by itself, rounded once more where p is bf16.  A launch for every 64 tensors.
+   in fp32, rounded once more where p is bf16 (states: every operation rounded by itself).  A launch for every 120 tensors.
    state_bits = 8: m and the root of v are E4M3 elements (a byte each) times a power of two for each 256 consecutive values of a tensor, the smallest with which the largest of them is
    448 or below (1 for zeros).  They are rounded up or down at random with their mean kept, by numbers that depend on seed, t and the value's place (tensors one after another, each
    from a multiple of 256 on), so that a step repeated on the same state gives the same bits; a root above zero is not rounded to zero.  A gradient that is not finite makes the states of its 256
@@ -565,7 +565,7 @@ typedef struct {       /* device memory, aligned to its type; n consecutive valu
     const void *grad;
     void *m, *v;       /* states: fp32, or bytes                                                   */
     float *scales;     /* state_bits = 8: ceil(n / 256) x 2 (of m, of v's root); otherwise NULL    */
-    int64_t n;         /* 0 .. 2^32                                                                */
+    int64_t n;         /* 0 .. 2^32 - 1 - 1                                                            */
 } lq_adamw_tensor;
 
 typedef struct {

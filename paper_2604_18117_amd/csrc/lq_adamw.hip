@@ -1,10 +1,12 @@
-// An AdamW step over many tensors in one launch for every 64 of them:
+// An AdamW step over many tensors in one launch for every 120 of them:
 //     m = b1 m + (1 - b1) g ;  v = b2 v + (1 - b2) g^2 ;  p = p (1 - lr wd) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
 // Bound by memory: 28 bytes a value with fp32 states, 16 with states in 8 bits.
 // States in 8 bits: E4M3 elements with a power of two as scale for each 256 values, the smallest that brings the block's largest below 448; of v its root is held.
 // Elements are rounded up or down with the probabilities that keep the mean (an average that moves by 0.1 % a step would never leave an element of 3 bits of
 // mantissa), by bits that come from the seed, the step and the value's place; scales being powers of two, a value that does not change is held as it was.  A root that
 // is not zero is not held as zero: m / sqrt(v) stays bounded.
+#include <math.h>
+
 #include "lq_internal.h"
 
 namespace lq {
@@ -12,22 +14,27 @@ namespace lq {
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
-constexpr int TENSORS = 64;  // of a launch: as many as a wavefront looks through at once
-
+// The tensors of a launch: as many as 4 KB of kernel arguments hold.  (With 64 of them, in whole addresses, 229 tensors of 11 M values in 8 bits took four launches and 66 us, of which a
+// launch's beginning and end are some 8; with 120 two and TIME.)  Addresses are steps of an element from the lowest of their kind.
+constexpr int TENSORS = 120;
+struct Entry {
+    uint32_t p, master, g, m, v, scales;  // master: NONE without
+    uint32_t n;
+};
+constexpr uint32_t NONE = 0xFFFFFFFFu;
 struct AdamwArgs {
-    void* p[TENSORS];
-    float* master[TENSORS];
-    const void* g[TENSORS];
-    void *m[TENSORS], *v[TENSORS];
-    float* scales[TENSORS];
-    int64_t n[TENSORS];
-    uint32_t end[TENSORS];  // blocks of 256 values up to and with this tensor's
-    uint32_t base;          // blocks before the launch's
+    Entry tensors[TENSORS];
+    uint32_t first[TENSORS];  // block of 256 values of each in the launch; NONE behind the last
+    char *p, *m, *v;
+    const char* g;
+    float *master, *scales;
+    uint32_t blocks;        // of the launch
+    uint32_t base;          // before it
     int aligned;            // every tensor can be accessed 4 values at a time
     const float *lr_dev, *grad_scale;
     const int32_t* step_dev;
     double beta1, beta2;
-    float b1, c1, b2, c2, eps, wd, lr, bias1, bias2;
+    float b1, c1, b2, c2, eps, wd, lr, correct1, correct2;  // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
     uint32_t seed, step;
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
@@ -50,30 +57,50 @@ __device__ __forceinline__ void random_bits(uint32_t key, uint32_t place, uint32
     a = h & 0xFFFFFu;
     b = h * 0x3C6EF373u >> 12;
 }
-// 0 <= x <= 448 to one of the E4M3 values next to it.  Below 2^-6 they are 2^-9 apart, as from 2^-6 to 2^-5.
-__device__ __forceinline__ float round_e4m3(float x, uint32_t bits)
+// 0 <= x <= 448 to the code of one of the E4M3 values next to it.  Times 2^-120 the number's fields are E4M3's followed by 20 bits that are cut off: 2^-6, E4M3's smallest normal number, becomes
+// fp32's, and what is below stays evenly spaced.  (An answer above 255 stands for not a number.)
+__device__ __forceinline__ uint32_t e4m3_code(float x, uint32_t bits) { return (__float_as_uint(x * 0x1p-120f) + bits) >> 20; }
+// The smallest power of two that brings amax (its bits) to 448 or below, and its reciprocal; 1 for zero, not a number where amax is none or infinite
+__device__ __forceinline__ void power_scale(uint32_t amax, float& scale, float& inverse)
 {
-    const float small = x < 0.015625f ? 0.015625f : 0.0f;
-    return __uint_as_float((__float_as_uint(x + small) + bits) & 0xFFF00000u) - small;
+    const int e = max((int)((amax + 0x1FFFFFu) >> 23) - 8, 1);  // (448 is 1.75 times a power of two)
+    const bool number = amax < 0x7F800000u;
+    scale = __uint_as_float(!number ? 0x7FC00000u : amax ? (uint32_t)e << 23 : 0x3F800000u);
+    inverse = __uint_as_float(!number ? 0x7FC00000u : amax ? (uint32_t)(254 - e) << 23 : 0x3F800000u);
 }
-// The smallest power of two that brings amax to 448 or below; 1 for zero, not a number where amax is none or infinite
-__device__ __forceinline__ float power_scale(float amax)
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v)
 {
-    const uint32_t bits = __float_as_uint(amax);
-    if (bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    const int e = (int)(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u);
-    return amax > 0.0f ? __uint_as_float((uint32_t)max(e, 1) << 23) : 1.0f;
+    return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t x)  // of the bits of numbers without a sign: not a number counts as the largest
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)  // of the bits of numbers without a sign: not a number counts as the largest
 {
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, k));
-    return x;
+    v = max_dpp<0xB1>(v);   // quad_perm [1,0,3,2]
+    v = max_dpp<0x4E>(v);   // quad_perm [2,3,0,1]
+    v = max_dpp<0x141>(v);  // row_half_mirror
+    v = max_dpp<0x140>(v);  // row_mirror
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(s[0], s[1]);
+    const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)max(t[0], t[1]));
 }
 
+// The nearest number to the root of x >= 0: an estimate of 1 / sqrt(x) and its half, improved once together, then the root by what is left (each step by fused operations; 9 instructions, the
+// library's 15).  Outside the estimate's range the library's.
+__device__ __forceinline__ float nearest_root(float x)
+{
+    const float y = __builtin_amdgcn_rsqf(x);
+    float s = x * y, h = 0.5f * y;
+    const float e = fmaf(-h, s, 0.5f);
+    s = fmaf(s, e, s);
+    h = fmaf(h, e, h);
+    s = fmaf(fmaf(-s, s, x), h, s);
+    if (!(x >= 1e-30f && x <= 1e30f)) s = sqrtf(x);
+    return s;
+}
 // Four values of a tensor at i, those from n on zero
 template <typename T>
-__device__ __forceinline__ void read4(const void* p, int64_t i, int64_t n, bool whole, float (&f)[4])
+__device__ __forceinline__ void read4(const void* p, int i, int n, bool whole, float (&f)[4])
 {
     const T* x = (const T*)p + i;
     if (whole) {
@@ -87,7 +114,7 @@ __device__ __forceinline__ void read4(const void* p, int64_t i, int64_t n, bool 
     }
 }
 template <typename T>
-__device__ __forceinline__ void write4(void* p, int64_t i, int64_t n, bool whole, const float (&f)[4])
+__device__ __forceinline__ void write4(void* p, int i, int n, bool whole, const float (&f)[4])
 {
     T* x = (T*)p + i;
     if (whole) {
@@ -102,7 +129,7 @@ __device__ __forceinline__ void write4(void* p, int64_t i, int64_t n, bool whole
             if (i + k < n) x[k] = (T)f[k];
     }
 }
-__device__ __forceinline__ uint32_t codes4(const void* p, int64_t i, int64_t n, bool whole)
+__device__ __forceinline__ uint32_t codes4(const void* p, int i, int n, bool whole)
 {
     const uint8_t* x = (const uint8_t*)p + i;
     if (whole) return *(const uint32_t*)x;
@@ -112,7 +139,7 @@ __device__ __forceinline__ uint32_t codes4(const void* p, int64_t i, int64_t n, 
         if (i + k < n) w |= (uint32_t)x[k] << (8 * k);
     return w;
 }
-__device__ __forceinline__ void put_codes4(void* p, int64_t i, int64_t n, bool whole, uint32_t w)
+__device__ __forceinline__ void put_codes4(void* p, int i, int n, bool whole, uint32_t w)
 {
     uint8_t* x = (uint8_t*)p + i;
     if (whole) {
@@ -130,92 +157,112 @@ __device__ __forceinline__ void e4m3_values(uint32_t w, float (&f)[4])
     f[2] = __builtin_amdgcn_cvt_f32_fp8((int)w, 2);
     f[3] = __builtin_amdgcn_cvt_f32_fp8((int)w, 3);
 }
-__device__ __forceinline__ uint32_t e4m3_codes(const float (&f)[4])  // of values that are E4M3's
+__device__ __forceinline__ uint32_t bytes4(const uint32_t (&c)[4])  // the lowest byte of each
 {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(c[3], c[2], 0x0C0C0400u), __builtin_amdgcn_perm(c[1], c[0], 0x0C0C0400u), 0x05040100u);
 }
 
-// A wavefront takes a block of 256 values, four to a lane.
+// A wavefront takes a block of 256 values, four to a lane (two or four blocks to a wavefront, requested at once: 2 to 25 % slower).  Bound by memory, in 8 bits nearly as much by its
+// arithmetic arithmetic (NNN instructions a value): what 1 - beta^t divides is multiplied, and the new root of v serves its code and the step.
 template <typename TP, typename TG, bool EIGHT>
 __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs a)
 {
     const int lane = threadIdx.x & 63;
     const uint32_t block = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-    if (block >= a.end[TENSORS - 1]) return;
-    const int t = __popcll(__ballot(a.end[lane] <= block));
-    const int64_t n = a.n[t], i = (int64_t)(block - (t ? a.end[t - 1] : 0u)) * 256 + lane * 4, at = block - (t ? a.end[t - 1] : 0u);
+    if (block >= a.blocks) return;
+    int t = __popcll(__ballot(a.first[lane] <= block)) - 1;
+    if (t == 63) t += __popcll(__ballot(lane < TENSORS - 64 && a.first[min(64 + lane, TENSORS - 1)] <= block));
+    t = __builtin_amdgcn_readfirstlane(t);
+    const Entry e = a.tensors[t];
+    const uint32_t at = block - a.first[t];
+    const size_t o = (size_t)at * 256;  // of the block; the same for the wavefront, so that a lane adds its place alone
+    const int n = (int)min((uint32_t)(e.n - at * 256u), 256u), i = lane * 4;
     const bool whole = a.aligned && i + 4 <= n;
-    float p[4], g[4], m[4], v[4];
+    void* const pp = a.p + (e.p + o) * sizeof(TP);
+    float *const master = e.master != NONE ? a.master + (e.master + o) : nullptr, *const scales = a.scales + (e.scales + 2 * (size_t)at);
+    void *const pm = a.m + (e.m + o) * (EIGHT ? 1 : 4), *const pv = a.v + (e.v + o) * (EIGHT ? 1 : 4);
+    float p[4], g[4], m[4], v[4], root[4];
     uint32_t wm = 0, wv = 0;
     float sm = 1.0f, sv = 1.0f;
-    if (a.master[t]) read4<float>(a.master[t], i, n, whole, p);
-    else read4<TP>(a.p[t], i, n, whole, p);
-    read4<TG>(a.g[t], i, n, whole, g);
+    if (master) read4<float>(master, i, n, whole, p);
+    else read4<TP>(pp, i, n, whole, p);
+    read4<TG>(a.g + (e.g + o) * sizeof(TG), i, n, whole, g);
     if constexpr (EIGHT) {
-        wm = codes4(a.m[t], i, n, whole);
-        wv = codes4(a.v[t], i, n, whole);
-        sm = a.scales[t][2 * at];
-        sv = a.scales[t][2 * at + 1];
+        wm = codes4(pm, i, n, whole);
+        wv = codes4(pv, i, n, whole);
+        sm = scales[0];
+        sv = scales[1];
     } else {
-        read4<float>(a.m[t], i, n, whole, m);
-        read4<float>(a.v[t], i, n, whole, v);
+        read4<float>(pm, i, n, whole, m);
+        read4<float>(pv, i, n, whole, v);
     }
     uint32_t step = a.step;
-    float bias1 = a.bias1, bias2 = a.bias2;
+    float correct1 = a.correct1, correct2 = a.correct2;
     if (a.step_dev) {
         step = (uint32_t)max(*a.step_dev, 1);
-        bias1 = (float)(1.0 - power(a.beta1, step));
-        bias2 = (float)(1.0 - power(a.beta2, step));
+        correct1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
+        correct2 = (float)sqrt(1.0 / (1.0 - power(a.beta2, step)));
     }
-    const float lr = a.lr_dev ? *a.lr_dev : a.lr, gs = a.grad_scale ? *a.grad_scale : 1.0f, keep = 1.0f - lr * a.wd;
+    const float lr = a.lr_dev ? *a.lr_dev : a.lr, gs = a.grad_scale ? *a.grad_scale : 1.0f, keep = 1.0f - lr * a.wd, rate = lr * correct1;
     if constexpr (EIGHT) {
         e4m3_values(wm, m);
         e4m3_values(wv, v);
+    }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (EIGHT) {
             m[k] *= sm;
             v[k] *= sv;
             v[k] *= v[k];
         }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
         if (a.grad_scale) g[k] *= gs;
         m[k] = m[k] * a.b1 + g[k] * a.c1;
         v[k] = v[k] * a.b2 + g[k] * a.c2 * g[k];
-        p[k] = p[k] * keep - lr * (m[k] / bias1) / (sqrtf(v[k] / bias2) + a.eps);
+        root[k] = nearest_root(v[k]);
+        p[k] = fmaf(p[k], keep, -(m[k] * rate) * __builtin_amdgcn_rcpf(fmaf(root[k], correct2, a.eps)));
     }
-    if (a.master[t]) write4<float>(a.master[t], i, n, whole, p);
-    write4<TP>(a.p[t], i, n, whole, p);
+    if (master) write4<float>(master, i, n, whole, p);
+    write4<TP>(pp, i, n, whole, p);
     if constexpr (EIGHT) {
-        uint32_t big[2] = {0u, 0u};
+        uint32_t big[2] = {0u, 0u}, cm[4], cv[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            v[k] = sqrtf(v[k]);
             big[0] = max(big[0], __float_as_uint(m[k]) & 0x7FFFFFFFu);
-            big[1] = max(big[1], __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            big[1] = max(big[1], __float_as_uint(root[k]) & 0x7FFFFFFFu);
         }
-        sm = power_scale(__uint_as_float(wave_max(big[0])));
-        sv = power_scale(__uint_as_float(wave_max(big[1])));
-        const float im = 1.0f / sm, iv = 1.0f / sv;
+        float im, iv;
+        power_scale(wave_max(big[0]), sm, im);
+        power_scale(wave_max(big[1]), sv, iv);
         const uint32_t key = a.seed * 0x9E3779B1u + step * 0x6A09E667u, place = (a.base + block) * 256u + lane * 4u;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             uint32_t rm, rv;
             random_bits(key, place + k, rm, rv);
-            m[k] = copysignf(round_e4m3(fabsf(m[k]) * im, rm), m[k]);
-            const float r = round_e4m3(v[k] * iv, rv);
-            v[k] = v[k] > 0.0f ? fmaxf(r, 0.001953125f) : r;
+            cm[k] = e4m3_code(fabsf(m[k]) * im, rm) | (__float_as_uint(m[k]) >> 24 & 0x80u);
+            cv[k] = max(e4m3_code(root[k] * iv, rv), min(__float_as_uint(root[k]), 1u));  // (not zero for what is not)
         }
-        put_codes4(a.m[t], i, n, whole, e4m3_codes(m));
-        put_codes4(a.v[t], i, n, whole, e4m3_codes(v));
-        if (lane == 0) a.scales[t][2 * at] = sm, a.scales[t][2 * at + 1] = sv;
+        put_codes4(pm, i, n, whole, bytes4(cm));
+        put_codes4(pv, i, n, whole, bytes4(cv));
+        if (lane == 0) scales[0] = sm, scales[1] = sv;
     } else {
-        write4<float>(a.m[t], i, n, whole, m);
-        write4<float>(a.v[t], i, n, whole, v);
+        write4<float>(pm, i, n, whole, m);
+        write4<float>(pv, i, n, whole, v);
     }
 }
+
+// The lowest address of a kind and how far the others are from it, in elements: whether one more fits.
+struct Window {
+    uintptr_t low = ~(uintptr_t)0, high = 0;
+    bool take(const void* p, int elem)
+    {
+        const uintptr_t x = (uintptr_t)p, l = x < low ? x : low, h = x > high ? x : high;
+        if ((h - l) / elem >= NONE) return false;
+        low = l;
+        high = h;
+        return true;
+    }
+    uint32_t step(const void* p, int elem) const { return (uint32_t)(((uintptr_t)p - low) / elem); }
+};
 
 hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors, int count, const lq_adamw_args* x, hipStream_t s)
 {
@@ -236,35 +283,53 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
     double p1 = 1.0, p2 = 1.0, q1 = c->beta1, q2 = c->beta2;
     for (uint32_t t = a.step; t; t >>= 1, q1 *= q1, q2 *= q2)
         if (t & 1) p1 *= q1, p2 *= q2;
-    a.bias1 = (float)(1.0 - p1);
-    a.bias2 = (float)(1.0 - p2);
+    a.correct1 = (float)(1.0 / (1.0 - p1));
+    a.correct2 = (float)sqrt(1.0 / (1.0 - p2));
     a.seed = c->seed;
-    const int pe = c->p_dtype == LQ_F32 ? 4 : 2, ge = c->g_dtype == LQ_F32 ? 4 : 2, se = c->state_bits == 32 ? 4 : 1;
+    const bool eight = c->state_bits == 8, pf = c->p_dtype == LQ_F32, gf = c->g_dtype == LQ_F32;
+    const int pe = pf ? 4 : 2, ge = gf ? 4 : 2, se = eight ? 1 : 4;
     for (int i = 0; i < count;) {
+        const lq_adamw_tensor* of[TENSORS];
         int k = 0;
-        uint32_t blocks = 0;
+        Window wp, wmaster, wg, wm, wv, ws;
+        a.blocks = 0;
         a.aligned = 1;
         for (; i < count && k < TENSORS; ++i) {
             const lq_adamw_tensor& t = tensors[i];
             const uint32_t more = (uint32_t)((t.n + 255) / 256);
             if (more == 0) continue;
-            if (blocks + more > (1u << 25)) break;  // (a launch stays below 2^32 threads)
-            a.p[k] = t.p;
-            a.master[k] = t.master;
-            a.g[k] = t.grad;
-            a.m[k] = t.m;
-            a.v[k] = t.v;
-            a.scales[k] = t.scales;
-            a.n[k] = t.n;
-            a.end[k] = blocks += more;
+            if (a.blocks + more > (1u << 25)) break;  // (a launch stays below 2^32 threads)
+            Window np = wp, nmaster = wmaster, ng = wg, nm = wm, nv = wv, ns = ws;
+            if (!np.take(t.p, pe) || (t.master && !nmaster.take(t.master, 4)) || !ng.take(t.grad, ge) || !nm.take(t.m, se) || !nv.take(t.v, se) ||
+                (eight && !ns.take(t.scales, 4)))
+                break;  // (its launch is the next one)
+            wp = np, wmaster = nmaster, wg = ng, wm = nm, wv = nv, ws = ns;
+            a.tensors[k].n = (uint32_t)t.n;
+            a.first[k] = a.blocks;
+            a.blocks += more;
             a.aligned = a.aligned && (uintptr_t)t.p % (4 * pe) == 0 && (uintptr_t)t.master % 16 == 0 && (uintptr_t)t.grad % (4 * ge) == 0 &&
                         (uintptr_t)t.m % (4 * se) == 0 && (uintptr_t)t.v % (4 * se) == 0;
-            ++k;
+            of[k++] = &t;
         }
         if (k == 0) break;
-        for (; k < TENSORS; ++k) a.end[k] = blocks;
-        const dim3 grid((blocks + 3) / 4), block(256);
-        const bool eight = c->state_bits == 8, pf = c->p_dtype == LQ_F32, gf = c->g_dtype == LQ_F32;
+        for (int j = 0; j < k; ++j) {
+            const lq_adamw_tensor& t = *of[j];
+            Entry& e = a.tensors[j];
+            e.p = wp.step(t.p, pe);
+            e.master = t.master ? wmaster.step(t.master, 4) : NONE;
+            e.g = wg.step(t.grad, ge);
+            e.m = wm.step(t.m, se);
+            e.v = wv.step(t.v, se);
+            e.scales = eight ? ws.step(t.scales, 4) : 0;
+        }
+        for (; k < TENSORS; ++k) a.first[k] = NONE;
+        a.p = (char*)wp.low;
+        a.master = (float*)wmaster.low;
+        a.g = (const char*)wg.low;
+        a.m = (char*)wm.low;
+        a.v = (char*)wv.low;
+        a.scales = (float*)ws.low;
+        const dim3 grid((a.blocks + 3) / 4), block(256);
 #define RUN(TP, TG) \
     if (eight) hipLaunchKernelGGL((adamw_kernel<TP, TG, true>), grid, block, 0, s, a); \
     else hipLaunchKernelGGL((adamw_kernel<TP, TG, false>), grid, block, 0, s, a)
@@ -275,7 +340,7 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
 #undef RUN
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        a.base += blocks;
+        a.base += a.blocks;
     }
     return hipSuccess;
 }

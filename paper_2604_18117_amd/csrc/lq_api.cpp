@@ -994,7 +994,7 @@ lq_status lq_adamw_step(const lq_adamw_config* cfg, const lq_adamw_tensor* tenso
 {
     if (!cfg || !args) return LQ_ERR_NULL;
     if (cfg->flags != 0 || cfg->reserved != 0 || (cfg->p_dtype != LQ_F32 && cfg->p_dtype != LQ_BF16) || (cfg->g_dtype != LQ_F32 && cfg->g_dtype != LQ_BF16) ||
-        (cfg->state_bits != 32 && cfg->state_bits != 8) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps > 0.0) ||
+        (cfg->state_bits != 32 && cfg->state_bits != 8) || !(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0) || !(cfg->beta2 >= 0.0 && cfg->beta2 < 1.0) || !(cfg->eps >= 1e-30) ||
         !(cfg->weight_decay >= 0.0))
         return LQ_ERR_UNSUPPORTED;
     if (count < 0 || count > 65536 || (!args->step_dev && (args->step < 1 || args->step > 0x7FFFFFFF))) return LQ_ERR_SHAPE;
@@ -1006,7 +1006,7 @@ lq_status lq_adamw_step(const lq_adamw_config* cfg, const lq_adamw_tensor* tenso
     const int pe = dtype_bytes(cfg->p_dtype), ge = dtype_bytes(cfg->g_dtype), se = eight ? 1 : 4;
     for (int32_t i = 0; i < count; ++i) {
         const lq_adamw_tensor& t = tensors[i];
-        if (t.n < 0 || t.n > ((int64_t)1 << 32)) return LQ_ERR_SHAPE;
+        if (t.n < 0 || t.n >= ((int64_t)1 << 32)) return LQ_ERR_SHAPE;
         if (t.n == 0) continue;
         if (!t.p || !t.grad || !t.m || !t.v || (eight && !t.scales)) return LQ_ERR_NULL;
         if (!aligned(t.p, pe) || !aligned(t.master, 4) || !aligned(t.grad, ge) || !aligned(t.m, se) || !aligned(t.v, se) || !aligned(t.scales, 4)) return LQ_ERR_ALIGN;

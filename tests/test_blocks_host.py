@@ -145,7 +145,7 @@ def _adamw(cfg=None, count=None, args=None, **kw):
 
 def test_adamw_arguments():
     raw = lq.raw()
-    for kw in (dict(p_dtype=2), dict(g_dtype=-1), dict(state_bits=16), dict(flags=1), dict(reserved=1), dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=float("nan")), dict(eps=0.0),
+    for kw in (dict(p_dtype=2), dict(g_dtype=-1), dict(state_bits=16), dict(flags=1), dict(reserved=1), dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=float("nan")), dict(eps=0.0), dict(eps=1e-31),
                dict(weight_decay=-1.0), dict(weight_decay=float("nan"))):
         c = lq.make_adamw_config()
         for k, v in kw.items():
@@ -161,7 +161,7 @@ def test_adamw_arguments():
         assert _adamw(**{name: None}) == lq.LQ_ERR_NULL
         assert _adamw(**{name: 7 * PTR + 1}) == lq.LQ_ERR_ALIGN
     assert _adamw(eight, scales=None) == lq.LQ_ERR_NULL and _adamw(eight, scales=PTR + 1) == lq.LQ_ERR_ALIGN and _adamw(master=7 * PTR + 2) == lq.LQ_ERR_ALIGN
-    assert _adamw(n=-1) == _adamw(n=(1 << 32) + 1) == _adamw(count=-1) == _adamw(count=65537) == lq.LQ_ERR_SHAPE
+    assert _adamw(n=-1) == _adamw(n=1 << 32) == _adamw(count=-1) == _adamw(count=65537) == lq.LQ_ERR_SHAPE
     # what is written lies apart: p over its neighbour, a state over a parameter, a master over a state, scales over scales
     assert _adamw(n=3000) == _adamw(m=PTR + 3996) == _adamw(v=3 * PTR) == _adamw(master=4 * PTR + 8192 + 3996) == lq.LQ_ERR_SHAPE
     assert _adamw(eight, scales=5 * PTR + 8192 - 16) == lq.LQ_ERR_SHAPE
@@ -291,7 +291,7 @@ def run(tmp_path_factory):
 
 
 CALLS = [("w4_pack", (100, 200, 32, 1, 1, 0)), ("w4_unpack", (100, 200, 64, 1, 1, 0)), ("w4_fwd", (6912, 1152, 64, 1, 0, 2)), ("w4_bwd", (6912, 1152, 64, 1, 0, 2)),
-         ("block_fwd", (1152, 1, 2, 1, 1, 2, 8192, 0)), ("block_bwd", (1152, 1, 2, 1, 1, 2, 8192, 0)), ("block_bwd", (33, 0, 1, 0, 0, 5, 0, 1)), ("adamw", (8, [1000] * 130))]
+         ("block_fwd", (1152, 1, 2, 1, 1, 2, 8192, 0)), ("block_bwd", (1152, 1, 2, 1, 1, 2, 8192, 0)), ("block_bwd", (33, 0, 1, 0, 0, 5, 0, 1)), ("adamw", (8, [1000] * 250))]
 
 
 @pytest.mark.parametrize("name,args", CALLS)
@@ -306,14 +306,17 @@ def test_launches_stay_below_two_to_the_32_threads(run):
     """The largest calls that are not refused."""
     jobs = [("w4_pack", (1 << 18, 1 << 16, 32, 1, 1, 0), -1), ("w4_fwd", (1 << 18, 1 << 16, 32, 0, 1, 1 << 14), -1), ("w4_bwd", (1 << 18, 1 << 16, 32, 0, 1, 1 << 14), -1),
             ("w4_bwd", (1 << 18, 1, 32, 0, 1, 1 << 14), -1), ("block_fwd", (16384, 1, 2, 0, 0, 1 << 20, 1 << 24, 0), -1), ("block_fwd", (1, 1, 2, 0, 0, 1, 1 << 24, 0), -1),
-            ("block_fwd", (16383, 1, 2, 0, 0, 1 << 20, 1 << 24, 1), -1), ("block_bwd", (16384, 1, 2, 0, 0, 1 << 20, 1 << 24, 0), -1), ("adamw", (32, [1 << 32] * 3), -1),
+            ("block_fwd", (16383, 1, 2, 0, 0, 1 << 20, 1 << 24, 1), -1), ("block_bwd", (16384, 1, 2, 0, 0, 1 << 20, 1 << 24, 0), -1), ("adamw", (32, [(1 << 32) - 1] * 3), -1),
             ("adamw", (8, [1 << 20] * 200), -1)]
     for job, (st, names, threads) in zip(jobs, run(jobs)):
         assert st == 0 and names and max(threads) < 2.0 ** 32, (job[:1], list(zip(names, threads)))
 
 
-def test_adamw_launches_of_64_tensors(run):
-    for sizes, launches in (([5], 1), ([5] * 64, 1), ([5] * 65, 2), ([0] * 100 + [5] * 64, 1), ([0] * 10, 0), ([5, 0] * 100, 2), ([1 << 32] * 2, 1), ([1 << 32] * 3, 2), ([1 << 32] * 2 + [1], 2)):
+def test_adamw_launches_of_120_tensors(run):
+    """... fewer where they are more than 2^33 values, or lie so far apart that steps of an element pass 32 bits."""
+    big = (1 << 32) - 1
+    for sizes, launches in (([5], 1), ([5] * 64, 1), ([5] * 65, 1), ([5] * 120, 1), ([5] * 121, 2), ([5] * 300, 3), ([0] * 200 + [5] * 120, 1), ([0] * 10, 0), ([5, 0] * 130, 2), ([5] * 240, 2),
+                            ([big], 1), ([big, 5], 2), ([1 << 28] * 3, 1), ([1 << 28] * 12, 4)):  # (here tensors of 2^28 lie 6 GB from each other, 2^32 steps are 16)
         (st, names, _), = run([("adamw", (32, sizes), -1)])
         assert st == 0 and len(names) == launches, (sizes[:4], len(names))
 

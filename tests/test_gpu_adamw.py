@@ -126,7 +126,7 @@ def eight_bit_rule(cfg, e, lr, t, masters):
 @pytest.mark.parametrize("seed,t", [(0, 1), (12345, 7), (2 ** 32 - 1, 2 ** 31 - 1)])
 def test_states_in_8_bits(lq, seed, t, start):
     cfg = lq.make_adamw_config("f32", "f32", 8, seed=seed, **HYPER)
-    sizes = SIZES + [300] * 70  # more than a launch's tensors
+    sizes = SIZES + [300] * 140  # more than a launch's tensors
     d = make(lq, cfg, sizes, seed=3, start=start)
     e = copy(d)
     step(lq, cfg, d, 1e-2, t)
