@@ -15,16 +15,17 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
 
 // The tensors of a launch: as many as 4 KB of kernel arguments hold.  (With 64 of them, in whole addresses, 229 tensors of 11 M values in 8 bits took four launches and 66 us, of which a
-// launch's beginning and end are some 8; with 120 two and TIME.)  Addresses are steps of an element from the lowest of their kind.
-constexpr int TENSORS = 120;
+// launch's beginning and end are some 8; with 120 two and 51.)  Addresses are steps of an element from the lowest of their kind.
+constexpr int TENSORS = 120, FEW = 8;
 struct Entry {
     uint32_t p, master, g, m, v, scales;  // master: NONE without
     uint32_t n;
 };
 constexpr uint32_t NONE = 0xFFFFFFFFu;
+template <int CAP>
 struct AdamwArgs {
-    Entry tensors[TENSORS];
-    uint32_t first[TENSORS];  // block of 256 values of each in the launch; NONE behind the last
+    Entry tensors[CAP];
+    uint32_t first[CAP];    // block of 256 values of each in the launch; NONE behind the last
     char *p, *m, *v;
     const char* g;
     float *master, *scales;
@@ -37,7 +38,7 @@ struct AdamwArgs {
     float b1, c1, b2, c2, eps, wd, lr, correct1, correct2;  // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
     uint32_t seed, step;
 };
-static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+static_assert(sizeof(AdamwArgs<TENSORS>) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ double power(double b, uint32_t t)  // b^t by squaring
 {
@@ -163,15 +164,15 @@ __device__ __forceinline__ uint32_t bytes4(const uint32_t (&c)[4])  // the lowes
 }
 
 // A wavefront takes a block of 256 values, four to a lane (two or four blocks to a wavefront, requested at once: 2 to 25 % slower).  Bound by memory, in 8 bits nearly as much by its
-// arithmetic arithmetic (NNN instructions a value): what 1 - beta^t divides is multiplied, and the new root of v serves its code and the step.
-template <typename TP, typename TG, bool EIGHT>
-__global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs a)
+// arithmetic arithmetic (some 85 instructions a value): what 1 - beta^t divides is multiplied, and the new root of v serves its code and the step.
+template <typename TP, typename TG, bool EIGHT, int CAP>
+__global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs<CAP> a)
 {
     const int lane = threadIdx.x & 63;
     const uint32_t block = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
     if (block >= a.blocks) return;
-    int t = __popcll(__ballot(a.first[lane] <= block)) - 1;
-    if (t == 63) t += __popcll(__ballot(lane < TENSORS - 64 && a.first[min(64 + lane, TENSORS - 1)] <= block));
+    int t = __popcll(__ballot(lane < CAP && a.first[min(lane, CAP - 1)] <= block)) - 1;
+    if (CAP > 64 && t == 63) t += __popcll(__ballot(lane < CAP - 64 && a.first[min(64 + lane, CAP - 1)] <= block));
     t = __builtin_amdgcn_readfirstlane(t);
     const Entry e = a.tensors[t];
     const uint32_t at = block - a.first[t];
@@ -264,9 +265,10 @@ struct Window {
     uint32_t step(const void* p, int elem) const { return (uint32_t)(((uintptr_t)p - low) / elem); }
 };
 
-hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors, int count, const lq_adamw_args* x, hipStream_t s)
+template <int CAP>
+static hipError_t adamw_run(const lq_adamw_config* c, const lq_adamw_tensor* tensors, int count, const lq_adamw_args* x, hipStream_t s)
 {
-    AdamwArgs a{};
+    AdamwArgs<CAP> a{};
     a.lr_dev = x->lr_dev;
     a.grad_scale = x->grad_scale;
     a.step_dev = x->step_dev;
@@ -289,12 +291,12 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
     const bool eight = c->state_bits == 8, pf = c->p_dtype == LQ_F32, gf = c->g_dtype == LQ_F32;
     const int pe = pf ? 4 : 2, ge = gf ? 4 : 2, se = eight ? 1 : 4;
     for (int i = 0; i < count;) {
-        const lq_adamw_tensor* of[TENSORS];
+        const lq_adamw_tensor* of[CAP];
         int k = 0;
         Window wp, wmaster, wg, wm, wv, ws;
         a.blocks = 0;
         a.aligned = 1;
-        for (; i < count && k < TENSORS; ++i) {
+        for (; i < count && k < CAP; ++i) {
             const lq_adamw_tensor& t = tensors[i];
             const uint32_t more = (uint32_t)((t.n + 255) / 256);
             if (more == 0) continue;
@@ -322,7 +324,7 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
             e.v = wv.step(t.v, se);
             e.scales = eight ? ws.step(t.scales, 4) : 0;
         }
-        for (; k < TENSORS; ++k) a.first[k] = NONE;
+        for (; k < CAP; ++k) a.first[k] = NONE;
         a.p = (char*)wp.low;
         a.master = (float*)wmaster.low;
         a.g = (const char*)wg.low;
@@ -331,8 +333,8 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
         a.scales = (float*)ws.low;
         const dim3 grid((a.blocks + 3) / 4), block(256);
 #define RUN(TP, TG) \
-    if (eight) hipLaunchKernelGGL((adamw_kernel<TP, TG, true>), grid, block, 0, s, a); \
-    else hipLaunchKernelGGL((adamw_kernel<TP, TG, false>), grid, block, 0, s, a)
+    if (eight) hipLaunchKernelGGL((adamw_kernel<TP, TG, true, CAP>), grid, block, 0, s, a); \
+    else hipLaunchKernelGGL((adamw_kernel<TP, TG, false, CAP>), grid, block, 0, s, a)
         if (pf && gf) { RUN(float, float); }
         else if (pf) { RUN(float, __bf16); }
         else if (gf) { RUN(__bf16, float); }
@@ -343,6 +345,12 @@ hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors
         a.base += a.blocks;
     }
     return hipSuccess;
+}
+
+// A few tensors: fewer arguments to bring to the card (us, with room for 8 / 120: one tensor of 1152 values 3.9 / 5.3, eight of 0.6 M 5.4 / 5.9)
+hipError_t launch_adamw(const lq_adamw_config* c, const lq_adamw_tensor* tensors, int count, const lq_adamw_args* x, hipStream_t s)
+{
+    return count <= FEW ? adamw_run<FEW>(c, tensors, count, x, s) : adamw_run<TENSORS>(c, tensors, count, x, s);
 }
 
 }  // namespace lq
