@@ -114,10 +114,11 @@ static void block_fwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_
 }
 hipError_t launch_block_fwd(const lq_block_config* c, const BlockTensors& t, int64_t M, hipStream_t s)
 {
-    const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M), 4, 5);
+    const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M));
     BlockArgs a = block_args(c, t, M);
-    // rows one after another while every SIMD has two wavefronts
-    const int64_t chunk = M * sh.W / 2048;
+    // rows one after another while every SIMD has two wavefronts, eight where a row has several, which wait for each other (us by the number of wavefronts: 8192 rows of 1152 1024 16.8, 2048
+    // 15.5, 4096 18.2; 16384 of 2240, fp32 stream and both norms, 2048 97.7, 4096 104.5, 8192 93.8)
+    const int64_t chunk = M * sh.W / (sh.W == 1 ? 2048 : 8192);
     a.chunk = (int)(chunk < 1 ? 1 : chunk > 16 ? 16 : chunk);
     if (c->h_dtype == LQ_BF16) block_fwd_types<__bf16, __bf16>(a, sh, s);
     else if (c->y_dtype == LQ_BF16) block_fwd_types<float, __bf16>(a, sh, s);

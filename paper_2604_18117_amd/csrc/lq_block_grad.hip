@@ -316,7 +316,7 @@ hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int
     a.part = sums ? (float*)work : nullptr;
     hipError_t e = hipSuccess;
     if (M > 0) {
-        const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M), 4, 5);
+        const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M));
         a.waves = sh.W;
         e = c->h_dtype == LQ_BF16   ? block_bwd_types<__bf16, __bf16>(a, sh, s)
             : c->y_dtype == LQ_BF16 ? block_bwd_types<float, __bf16>(a, sh, s)
