@@ -251,18 +251,20 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs<CAP> a)
     }
 }
 
-// The lowest address of a kind and how far the others are from it, in elements: whether one more fits.
+// The lowest address of a kind and how far the others are from it, in elements of 2^log2 bytes: whether one more fits.  (Shifts: a division of the host's costs as much as all else that
+// it does for a pointer.)
 struct Window {
+    int log2;
     uintptr_t low = ~(uintptr_t)0, high = 0;
-    bool take(const void* p, int elem)
+    bool take(const void* p)
     {
         const uintptr_t x = (uintptr_t)p, l = x < low ? x : low, h = x > high ? x : high;
-        if ((h - l) / elem >= NONE) return false;
+        if ((h - l) >> log2 >= NONE) return false;
         low = l;
         high = h;
         return true;
     }
-    uint32_t step(const void* p, int elem) const { return (uint32_t)(((uintptr_t)p - low) / elem); }
+    uint32_t step(const void* p) const { return (uint32_t)(((uintptr_t)p - low) >> log2); }
 };
 
 template <int CAP>
@@ -289,40 +291,40 @@ static hipError_t adamw_run(const lq_adamw_config* c, const lq_adamw_tensor* ten
     a.correct2 = (float)sqrt(1.0 / (1.0 - p2));
     a.seed = c->seed;
     const bool eight = c->state_bits == 8, pf = c->p_dtype == LQ_F32, gf = c->g_dtype == LQ_F32;
-    const int pe = pf ? 4 : 2, ge = gf ? 4 : 2, se = eight ? 1 : 4;
+    const int pl = pf ? 2 : 1, gl = gf ? 2 : 1, sl = eight ? 0 : 2;  // log2 of an element's bytes
     for (int i = 0; i < count;) {
         const lq_adamw_tensor* of[CAP];
         int k = 0;
-        Window wp, wmaster, wg, wm, wv, ws;
+        Window wp{pl}, wmaster{2}, wg{gl}, wm{sl}, wv{sl}, ws{2};
+        uintptr_t odd = 0;  // what keeps four values from being one access
         a.blocks = 0;
-        a.aligned = 1;
         for (; i < count && k < CAP; ++i) {
             const lq_adamw_tensor& t = tensors[i];
             const uint32_t more = (uint32_t)((t.n + 255) / 256);
             if (more == 0) continue;
             if (a.blocks + more > (1u << 25)) break;  // (a launch stays below 2^32 threads)
-            Window np = wp, nmaster = wmaster, ng = wg, nm = wm, nv = wv, ns = ws;
-            if (!np.take(t.p, pe) || (t.master && !nmaster.take(t.master, 4)) || !ng.take(t.grad, ge) || !nm.take(t.m, se) || !nv.take(t.v, se) ||
-                (eight && !ns.take(t.scales, 4)))
+            const Window before[6] = {wp, wmaster, wg, wm, wv, ws};
+            if (!wp.take(t.p) || (t.master && !wmaster.take(t.master)) || !wg.take(t.grad) || !wm.take(t.m) || !wv.take(t.v) || (eight && !ws.take(t.scales))) {
+                wp = before[0], wmaster = before[1], wg = before[2], wm = before[3], wv = before[4], ws = before[5];
                 break;  // (its launch is the next one)
-            wp = np, wmaster = nmaster, wg = ng, wm = nm, wv = nv, ws = ns;
+            }
             a.tensors[k].n = (uint32_t)t.n;
             a.first[k] = a.blocks;
             a.blocks += more;
-            a.aligned = a.aligned && (uintptr_t)t.p % (4 * pe) == 0 && (uintptr_t)t.master % 16 == 0 && (uintptr_t)t.grad % (4 * ge) == 0 &&
-                        (uintptr_t)t.m % (4 * se) == 0 && (uintptr_t)t.v % (4 * se) == 0;
+            odd |= ((uintptr_t)t.p & ((4u << pl) - 1)) | ((uintptr_t)t.master & 15) | ((uintptr_t)t.grad & ((4u << gl) - 1)) | (((uintptr_t)t.m | (uintptr_t)t.v) & ((4u << sl) - 1));
             of[k++] = &t;
         }
         if (k == 0) break;
+        a.aligned = odd == 0;
         for (int j = 0; j < k; ++j) {
             const lq_adamw_tensor& t = *of[j];
             Entry& e = a.tensors[j];
-            e.p = wp.step(t.p, pe);
-            e.master = t.master ? wmaster.step(t.master, 4) : NONE;
-            e.g = wg.step(t.grad, ge);
-            e.m = wm.step(t.m, se);
-            e.v = wv.step(t.v, se);
-            e.scales = eight ? ws.step(t.scales, 4) : 0;
+            e.p = wp.step(t.p);
+            e.master = t.master ? wmaster.step(t.master) : NONE;
+            e.g = wg.step(t.grad);
+            e.m = wm.step(t.m);
+            e.v = wv.step(t.v);
+            e.scales = eight ? ws.step(t.scales) : 0;
         }
         for (; k < CAP; ++k) a.first[k] = NONE;
         a.p = (char*)wp.low;

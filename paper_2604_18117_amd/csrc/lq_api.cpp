@@ -981,14 +981,47 @@ lq_status lq_block_norm_bwd(const lq_block_config* cfg, const void* ho, int64_t 
     return launch_block_bwd(cfg, t, M, (uint8_t*)work, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
 }
 
-// Whether the memory that a step writes lies apart.  Tensors mostly come in the order of their addresses, buffer by buffer: then a walk shows it, otherwise they are sorted.
-static bool apart(std::vector<std::pair<uintptr_t, uintptr_t>>& r)
-{
-    if (!std::is_sorted(r.begin(), r.end())) std::sort(r.begin(), r.end());
-    for (size_t i = 1; i < r.size(); ++i)
-        if (r[i].first < r[i - 1].second) return false;
-    return true;
-}
+// Whether the memory that a step writes lies apart.  Tensors of a kind mostly come in the order of their addresses, and kinds often in memory of their own: then a walk shows it.
+// (Sorting all of them took longer than the step where many tensors are small.)
+struct Spans {
+    typedef std::pair<uintptr_t, uintptr_t> Span;
+    std::vector<Span> all, hulls;
+    std::vector<size_t> kinds;  // where each begins
+    bool rising = true;
+    void begin()                // the next kind
+    {
+        hulls.emplace_back(0, 0);
+        kinds.push_back(all.size());
+    }
+    void add(const void* p, int64_t bytes)
+    {
+        if (!p || bytes == 0) return;
+        const Span s((uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes);
+        Span& hull = hulls.back();
+        if (hull.second == 0) hull.first = s.first;
+        else if (s.first < hull.second) rising = false;
+        hull.second = s.second;
+        all.push_back(s);
+    }
+    static bool apart(const std::vector<Span>& r)  // in order
+    {
+        for (size_t i = 1; i < r.size(); ++i)
+            if (r[i].first < r[i - 1].second) return false;
+        return true;
+    }
+    bool apart()
+    {
+        if (!rising) {
+            std::sort(all.begin(), all.end());
+            return apart(all);
+        }
+        std::sort(hulls.begin(), hulls.end());
+        if (apart(hulls)) return true;
+        for (size_t k = 1; k < kinds.size(); ++k)
+            std::inplace_merge(all.begin(), all.begin() + kinds[k], k + 1 < kinds.size() ? all.begin() + kinds[k + 1] : all.end());
+        return apart(all);
+    }
+};
 
 lq_status lq_adamw_step(const lq_adamw_config* cfg, const lq_adamw_tensor* tensors, int32_t count, const lq_adamw_args* args, void* stream)
 {
@@ -1009,20 +1042,24 @@ lq_status lq_adamw_step(const lq_adamw_config* cfg, const lq_adamw_tensor* tenso
         if (t.n < 0 || t.n >= ((int64_t)1 << 32)) return LQ_ERR_SHAPE;
         if (t.n == 0) continue;
         if (!t.p || !t.grad || !t.m || !t.v || (eight && !t.scales)) return LQ_ERR_NULL;
-        if (!aligned(t.p, pe) || !aligned(t.master, 4) || !aligned(t.grad, ge) || !aligned(t.m, se) || !aligned(t.v, se) || !aligned(t.scales, 4)) return LQ_ERR_ALIGN;
+        const uintptr_t odd = ((uintptr_t)t.p & (pe - 1)) | ((uintptr_t)t.grad & (ge - 1)) | (((uintptr_t)t.m | (uintptr_t)t.v) & (se - 1)) |
+                              (((uintptr_t)t.master | (uintptr_t)t.scales) & 3);
+        if (odd) return LQ_ERR_ALIGN;
     }
     try {
-        std::vector<std::pair<uintptr_t, uintptr_t>> written;
-        written.reserve((size_t)count * 5);
-        auto add = [&](const void* p, int64_t bytes) {
-            if (p && bytes) written.emplace_back((uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes);
-        };
-        for (int32_t i = 0; i < count; ++i) add(tensors[i].p, tensors[i].n * pe);
-        for (int32_t i = 0; i < count; ++i) add(tensors[i].master, tensors[i].n * 4);
-        for (int32_t i = 0; i < count; ++i) add(tensors[i].m, tensors[i].n * se);
-        for (int32_t i = 0; i < count; ++i) add(tensors[i].v, tensors[i].n * se);
-        for (int32_t i = 0; eight && i < count; ++i) add(tensors[i].scales, (tensors[i].n + 255) / 256 * 8);
-        if (!apart(written)) return LQ_ERR_SHAPE;
+        Spans written;
+        written.all.reserve((size_t)count * 5);
+        written.begin();
+        for (int32_t i = 0; i < count; ++i) written.add(tensors[i].p, tensors[i].n * pe);
+        written.begin();
+        for (int32_t i = 0; i < count; ++i) written.add(tensors[i].master, tensors[i].n * 4);
+        written.begin();
+        for (int32_t i = 0; i < count; ++i) written.add(tensors[i].m, tensors[i].n * se);
+        written.begin();
+        for (int32_t i = 0; i < count; ++i) written.add(tensors[i].v, tensors[i].n * se);
+        written.begin();
+        for (int32_t i = 0; eight && i < count; ++i) written.add(tensors[i].scales, (tensors[i].n + 255) / 256 * 8);
+        if (!written.apart()) return LQ_ERR_SHAPE;
     } catch (const std::bad_alloc&) {
         return LQ_ERR_DEVICE;
     }

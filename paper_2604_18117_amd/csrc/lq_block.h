@@ -58,24 +58,30 @@ struct RowSum {
     }
 };
 
-// VEC consecutive values in memory.  ANY: of any alignment, and of which only the first `have` may be there (the others are zero and not written).
+// VEC consecutive values in memory.  ANY: of any alignment, and rows may end among them.
 template <typename T, int VEC, bool ANY>
 struct Raw {
     typedef T Value __attribute__((ext_vector_type(VEC)));
     typedef Value Access __attribute__((aligned(ANY ? sizeof(T) : sizeof(T) * VEC > 16 ? 16 : sizeof(T) * VEC)));
     Value v;
-    __device__ __forceinline__ void clear()
+    __device__ __forceinline__ void fetch(const T* p) { v = *(const Access*)p; }
+    // Where the row of `dim` values may end before or among them: zeros from there on.  ANY: the row's last VEC values are read and moved to their places.
+    __device__ __forceinline__ void fetch_end(const T* row, int at, int dim)
     {
+        if constexpr (!ANY) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = (T)0.0f;
-    }
-    __device__ __forceinline__ void fetch(const T* p, int have)
-    {
-        if (!ANY || have >= VEC) {
-            v = *(const Access*)p;
+            for (int i = 0; i < VEC; ++i) v[i] = (T)0.0f;
+            if (at < dim) fetch(row + at);
+        } else if (dim < VEC) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = at + i < dim ? row[at + i] : (T)0.0f;
         } else {
+            const int first = min(at, dim - VEC), past = min(at - first, VEC);
+            fetch(row + first);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = i < have ? p[i] : (T)0.0f;
+            for (int step = VEC; step >= 1; step /= 2)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = past & step ? (i + step < VEC ? v[i + step < VEC ? i + step : 0] : (T)0.0f) : v[i];
         }
     }
     __device__ __forceinline__ void get(float (&f)[VEC]) const
@@ -83,25 +89,29 @@ struct Raw {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) f[i] = (float)v[i];
     }
-    static __device__ __forceinline__ void put(T* p, int have, const float (&f)[VEC])
+    static __device__ __forceinline__ void put(T* p, const float (&f)[VEC])
     {
-        if (!ANY || have >= VEC) {
-            Value t;
+        Value t;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) t[i] = (T)f[i];
-            *(Access*)p = t;
-        } else {
+        for (int i = 0; i < VEC; ++i) t[i] = (T)f[i];
+        *(Access*)p = t;
+    }
+    static __device__ __forceinline__ void put_end(T* row, int at, int dim, const float (&f)[VEC])
+    {
+        if (at + (ANY ? VEC : 1) <= dim) {
+            put(row + at, f);
+        } else if constexpr (ANY) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
-                if (i < have) p[i] = (T)f[i];
+                if (at + i < dim) row[at + i] = (T)f[i];
         }
     }
 };
 template <int VEC, bool ANY>
-__device__ __forceinline__ void read(const float* p, int have, float (&f)[VEC])
+__device__ __forceinline__ void read(const float* row, int at, int dim, float (&f)[VEC])
 {
     Raw<float, VEC, ANY> r;
-    r.fetch(p, have);
+    r.fetch_end(row, at, dim);
     r.get(f);
 }
 
@@ -154,29 +164,26 @@ struct Sequences {
     }
 };
 
-// A lane's NV vectors of columns: the first at `at`, each `step` values from the one before, so that with the row's address in scalar registers one offset serves all.  A
-// vector past the row's end is not read (it is zero) and left out of sums.  ANY: the last one may be there in part.
+// A lane's NV vectors of columns: the first at `at`, each `step` values from the one before, so that with the row's address in scalar registers one offset serves all.  All but the last
+// are there in every lane; a last one past the row's end is zero and left out of sums.
 template <int VEC, int NV, bool ANY>
 struct Columns {
-    unsigned at, step;
-    int dim;
+    int at, step, dim;
     __device__ __forceinline__ Columns(int dim_, int lane, int lanes) : at(lane * VEC), step(lanes * VEC), dim(dim_) {}
-    __device__ __forceinline__ int have(int v) const { return dim - (int)(at + v * step); }
-    __device__ __forceinline__ bool has(int v) const { return have(v) > 0; }
-    __device__ __forceinline__ float counted(int v, float sum) const { return has(v) ? sum : 0.0f; }
+    __device__ __forceinline__ int have(int v) const { return v < NV - 1 ? VEC : dim - (at + v * step); }
+    __device__ __forceinline__ float counted(int v, float sum) const { return v < NV - 1 || have(v) > 0 ? sum : 0.0f; }
     template <typename T>
     __device__ __forceinline__ void fetch(const T* row, Raw<T, VEC, ANY> (&r)[NV]) const
     {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            r[v].clear();
-            if (has(v)) r[v].fetch(row + v * step + at, have(v));
-        }
+        for (int v = 0; v < NV - 1; ++v) r[v].fetch(row + v * step + at);
+        r[NV - 1].fetch_end(row, (NV - 1) * step + at, dim);
     }
     template <typename T>
     __device__ __forceinline__ void put(T* row, int v, const float (&f)[VEC]) const
     {
-        if (has(v)) Raw<T, VEC, ANY>::put(row + v * step + at, have(v), f);
+        if (v < NV - 1) Raw<T, VEC, ANY>::put(row + v * step + at, f);
+        else Raw<T, VEC, ANY>::put_end(row, v * step + at, dim, f);
     }
 };
 
@@ -219,31 +226,31 @@ __device__ __forceinline__ float normalise(int kind, float (&x)[NV][VEC], const 
 
 // a, b of the header, and shift, of sequence s, at a column
 template <int VEC, bool ANY>
-__device__ __forceinline__ void factor_a(const BlockTensors& t, int at, int have, int s, float (&a)[VEC])
+__device__ __forceinline__ void factor_a(const BlockTensors& t, int at, int dim, int s, float (&a)[VEC])
 {
     float w[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) a[i] = 1.0f;
     if (t.scale.p) {
-        read<VEC, ANY>(t.scale.p + s * t.scale.ld + at, have, w);
+        read<VEC, ANY>(t.scale.p + s * t.scale.ld, at, dim, w);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a[i] = 1.0f + w[i];
     }
     if (t.w_pre) {
-        read<VEC, ANY>(t.w_pre + at, have, w);
+        read<VEC, ANY>(t.w_pre, at, dim, w);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a[i] *= w[i];
     }
 }
 template <int VEC, bool ANY>
-__device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int have, int s, float (&b)[VEC])
+__device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int dim, int s, float (&b)[VEC])
 {
     float w[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) b[i] = 1.0f;
-    if (t.gate.p) read<VEC, ANY>(t.gate.p + s * t.gate.ld + at, have, b);
+    if (t.gate.p) read<VEC, ANY>(t.gate.p + s * t.gate.ld, at, dim, b);
     if (t.w_post) {
-        read<VEC, ANY>(t.w_post + at, have, w);
+        read<VEC, ANY>(t.w_post, at, dim, w);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) b[i] *= w[i];
     }

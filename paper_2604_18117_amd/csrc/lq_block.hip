@@ -36,13 +36,12 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
         float fa[NV][VEC], fb[NV][VEC], fs[NV][VEC];
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) fa[v][i] = fb[v][i] = fs[v][i] = 0.0f;
-            if (!c.has(v)) continue;
             const int at = c.at + v * c.step;
-            factor_a<VEC, ANY>(t, at, c.have(v), s, fa[v]);
-            factor_b<VEC, ANY>(t, at, c.have(v), s, fb[v]);
-            if (t.shift.p) read<VEC, ANY>(t.shift.p + s * t.shift.ld + at, c.have(v), fs[v]);
+            factor_a<VEC, ANY>(t, at, a.dim, s, fa[v]);
+            factor_b<VEC, ANY>(t, at, a.dim, s, fb[v]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) fs[v][i] = 0.0f;
+            if (t.shift.p) read<VEC, ANY>(t.shift.p + s * t.shift.ld, at, a.dim, fs[v]);
         }
         for (; row < end; ++row) {
             float h[NV][VEC], y[NV][VEC];
@@ -94,23 +93,23 @@ static void block_fwd_run(const BlockArgs& a, int W, hipStream_t s)
         }
     hipLaunchKernelGGL((block_fwd_kernel<TH, TY, 4, NV, ANY, POST, false, 256>), dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a);
 }
-template <typename TH, typename TY, bool POST>
+template <typename TH, typename TY, bool ANY, bool POST>
 static void block_fwd_vectors(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
-    if (sh.any) return sh.NV <= 2 ? block_fwd_run<TH, TY, 2, true, POST>(a, sh.W, s) : block_fwd_run<TH, TY, 5, true, POST>(a, sh.W, s);
     switch (sh.NV) {
-        case 1: return block_fwd_run<TH, TY, 1, false, POST>(a, sh.W, s);
-        case 2: return block_fwd_run<TH, TY, 2, false, POST>(a, sh.W, s);
-        case 3: return block_fwd_run<TH, TY, 3, false, POST>(a, sh.W, s);
-        case 4: return block_fwd_run<TH, TY, 4, false, POST>(a, sh.W, s);
-        default: return block_fwd_run<TH, TY, 5, false, POST>(a, sh.W, s);
+        case 1: return block_fwd_run<TH, TY, 1, ANY, POST>(a, sh.W, s);
+        case 2: return block_fwd_run<TH, TY, 2, ANY, POST>(a, sh.W, s);
+        case 3: return block_fwd_run<TH, TY, 3, ANY, POST>(a, sh.W, s);
+        case 4: return block_fwd_run<TH, TY, 4, ANY, POST>(a, sh.W, s);
+        default: return block_fwd_run<TH, TY, 5, ANY, POST>(a, sh.W, s);
     }
 }
 template <typename TH, typename TY>
 static void block_fwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
-    if (a.t.y && a.post != LQ_NORM_NONE) block_fwd_vectors<TH, TY, true>(a, sh, s);
-    else block_fwd_vectors<TH, TY, false>(a, sh, s);
+    const bool post = a.t.y && a.post != LQ_NORM_NONE;
+    if (sh.any) post ? block_fwd_vectors<TH, TY, true, true>(a, sh, s) : block_fwd_vectors<TH, TY, true, false>(a, sh, s);
+    else post ? block_fwd_vectors<TH, TY, false, true>(a, sh, s) : block_fwd_vectors<TH, TY, false, false>(a, sh, s);
 }
 hipError_t launch_block_fwd(const lq_block_config* c, const BlockTensors& t, int64_t M, hipStream_t s)
 {

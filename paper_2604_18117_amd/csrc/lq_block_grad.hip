@@ -34,7 +34,9 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
         if (has_dho) c.fetch((const TH*)t.dho + m * t.lddho, rg);
     };
     auto read_factor = [&](const float* l, int v, float (&f)[VEC]) {  // (past the row's end: the first)
-        read<VEC, false>(l + (c.has(v) ? c.at + v * c.step : 0u), VEC, f);
+        Raw<float, VEC, false> r;
+        r.fetch(l + (c.have(v) > 0 ? c.at + v * c.step : 0));
+        r.get(f);
     };
     while (first < limit) {
         int end;
@@ -45,12 +47,12 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
         }
         for (int o = threadIdx.x * VEC; o < padded; o += blockDim.x * VEC) {
             float f[VEC];
-            factor_a<VEC, ANY>(t, o, a.dim - o, s, f);
-            Raw<float, VEC, false>::put(la + o, VEC, f);
-            factor_b<VEC, ANY>(t, o, a.dim - o, s, f);
+            factor_a<VEC, ANY>(t, o, a.dim, s, f);
+            Raw<float, VEC, false>::put(la + o, f);
+            factor_b<VEC, ANY>(t, o, a.dim, s, f);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) f[i] = ANY && i >= a.dim - o ? 0.0f : f[i];
-            Raw<float, VEC, false>::put(lb + o, VEC, f);
+            Raw<float, VEC, false>::put(lb + o, f);
         }
         float s1[NV][VEC], s2[NV][VEC], s3[NV][VEC];
 #pragma unroll
@@ -163,24 +165,24 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
                 for (int k = 0; k < 3; ++k)
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
-                        if (c.has(v)) Raw<float, VEC, true>::put(out + k * a.dim + c.at + v * c.step, c.have(v), k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
+                        Raw<float, VEC, true>::put_end(out + k * a.dim, c.at + v * c.step, a.dim, k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
             } else {
 #pragma unroll
                 for (int k = 0; k < 3; ++k)
 #pragma unroll
                     for (int v = 0; v < NV; ++v)
-                        if (c.has(v)) Raw<float, VEC, false>::put(joined + (k * groups + group) * padded + c.at + v * c.step, VEC, k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
+                        if (c.have(v) > 0) Raw<float, VEC, false>::put(joined + (k * groups + group) * padded + c.at + v * c.step, k == 0 ? s1[v] : k == 1 ? s2[v] : s3[v]);
                 __syncthreads();
                 for (int o = threadIdx.x * VEC; o < 3 * padded; o += blockDim.x * VEC) {
                     const int k = o >= 2 * padded ? 2 : o >= padded ? 1 : 0, col = o - k * padded;
                     float y[VEC], z[VEC];
-                    read<VEC, false>(joined + k * groups * padded + col, VEC, y);
+                    read<VEC, false>(joined + k * groups * padded, col, padded, y);
                     for (int w = 1; w < groups; ++w) {
-                        read<VEC, false>(joined + (k * groups + w) * padded + col, VEC, z);
+                        read<VEC, false>(joined + (k * groups + w) * padded, col, padded, z);
 #pragma unroll
                         for (int i = 0; i < VEC; ++i) y[i] += z[i];
                     }
-                    Raw<float, VEC, true>::put(out + k * a.dim + col, a.dim - col, y);
+                    Raw<float, VEC, true>::put_end(out + k * a.dim, col, a.dim, y);
                 }
             }
         }
@@ -189,42 +191,73 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
     }
 }
 
-// Sums over a sequence's parts in a fixed order; 64 columns of one of the three sums to a workgroup, its wavefronts take parts in turn and are joined in a tree.
+// Where a sequence's parts begin and end
+__device__ __forceinline__ void parts_of(const BlockArgs& a, int s, int& c0, int& c1)
+{
+    int begin = 0, end = (int)a.M;
+    if (a.t.offsets) {
+        begin = max(a.t.offsets[s], 0);
+        end = min(a.t.offsets[s + 1], (int)a.M);
+    }
+    c0 = begin / a.chunk;
+    c1 = begin < end ? (end - 1) / a.chunk + 1 : c0;
+}
+// Sums over a sequence's parts in a fixed order, 64 columns of one of the three sums to a workgroup:
 //     dshift = sum dx ;  dscale = w_pre sum dx n ;  dgate = w_post sum G p
-// raw: the last two without the weights, for those of the weights.
-__global__ void __launch_bounds__(1024) block_sums(BlockArgs a, float* raw)
+// `team` wavefronts share the parts of a sequence out and are joined in a tree; the workgroup's teams take the sequences from blockIdx.z on in turn.  FUSED (one workgroup sees all sequences): also
+//     dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
+// Otherwise raw: the last two sums without the weights, for block_weight_sums.
+template <bool FUSED>
+__global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float* raw)
 {
     __shared__ float sh[16][64];
     const BlockTensors& t = a.t;
-    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, col = blockIdx.x * 64 + lane;
-    for (int s = blockIdx.z; s < t.S; s += gridDim.z) {
-        int begin = 0, end = (int)a.M;
-        if (t.offsets) {
-            begin = max(t.offsets[s], 0);
-            end = min(t.offsets[s + 1], (int)a.M);
-        }
-        const int c0 = begin / a.chunk, c1 = begin < end ? (end - 1) / a.chunk + 1 : c0;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, col = blockIdx.x * 64 + lane;
+    const int member = wave % team, teams = waves / team;
+    const lq_mod_out& o = k == 0 ? t.dshift : k == 1 ? t.dscale : t.dgate;
+    const lq_mod& f = k == 1 ? t.scale : t.gate;
+    const float* w = k == 0 ? nullptr : k == 1 ? t.w_pre : t.w_post;
+    float* dw = k == 0 ? nullptr : k == 1 ? t.dw_pre : t.dw_post;
+    float total = 0.0f;
+    for (int base = blockIdx.z * teams; base < t.S; base += gridDim.z * teams) {
+        const int s = base + wave / team;
         float y = 0.0f;
-        if (col < a.dim) {
+        if (s < t.S && col < a.dim) {
+            int c0, c1;
+            parts_of(a, s, c0, c1);
             const float* p = a.part + (size_t)s * 3 * a.dim + k * a.dim + col;
 #pragma unroll 8
-            for (int i = c0 + wave; i < c1; i += waves) y += p[(size_t)i * 3 * a.dim];
+            for (int i = c0 + member; i < c1; i += team) y += p[(size_t)i * 3 * a.dim];
         }
-        sh[wave][lane] = y;
-        __syncthreads();
-        for (int half = waves / 2; half > 0; half /= 2) {
-            if (wave < half) sh[wave][lane] += sh[wave + half][lane];
+        if (team > 1) {
+            sh[wave][lane] = y;
             __syncthreads();
+            for (int half = team / 2; half > 0; half /= 2) {
+                if (member < half) sh[wave][lane] += sh[wave + half][lane];
+                __syncthreads();
+            }
+            y = sh[wave][lane];
         }
-        if (wave == 0 && col < a.dim) {
-            y = sh[0][lane];
-            const lq_mod_out& o = k == 0 ? t.dshift : k == 1 ? t.dscale : t.dgate;
-            const float* w = k == 0 ? nullptr : k == 1 ? t.w_pre : t.w_post;
+        if (member == 0 && s < t.S && col < a.dim) {
             if (o.p) o.p[s * o.ld + col] = w ? y * w[col] : y;
-            if (raw && k) raw[((size_t)s * 2 + k - 1) * a.dim + col] = y;
+            if (FUSED) {
+                const float g = f.p ? f.p[s * f.ld + col] : k == 1 ? 0.0f : 1.0f;
+                total = fmaf(k == 1 ? 1.0f + g : g, y, total);
+            } else if (raw && k) {
+                raw[((size_t)s * 2 + k - 1) * a.dim + col] = y;
+            }
         }
+        if (team > 1) __syncthreads();
+    }
+    if (!FUSED || !dw) return;
+    __syncthreads();
+    sh[wave][lane] = total;  // (zero but in the teams' first wavefronts)
+    __syncthreads();
+    for (int half = waves / 2; half > 0; half /= 2) {
+        if (wave < half) sh[wave][lane] += sh[wave + half][lane];
         __syncthreads();
     }
+    if (wave == 0 && col < a.dim) dw[col] = sh[0][lane];
 }
 // dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
 __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const float* raw)
@@ -291,22 +324,23 @@ static hipError_t block_bwd_run(const BlockArgs& a, hipStream_t s)
         if (a.waves > 1) return block_bwd_launch<TH, TY, NV, ANY, POST, true, 512>(a, s);
     return block_bwd_launch<TH, TY, NV, ANY, POST, false, 512>(a, s);
 }
-template <typename TH, typename TY, bool POST>
+template <typename TH, typename TY, bool ANY, bool POST>
 static hipError_t block_bwd_vectors(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
-    if (sh.any) return sh.NV <= 2 ? block_bwd_run<TH, TY, 2, true, POST>(a, s) : block_bwd_run<TH, TY, 5, true, POST>(a, s);
     switch (sh.NV) {
-        case 1: return block_bwd_run<TH, TY, 1, false, POST>(a, s);
-        case 2: return block_bwd_run<TH, TY, 2, false, POST>(a, s);
-        case 3: return block_bwd_run<TH, TY, 3, false, POST>(a, s);
-        case 4: return block_bwd_run<TH, TY, 4, false, POST>(a, s);
-        default: return block_bwd_run<TH, TY, 5, false, POST>(a, s);
+        case 1: return block_bwd_run<TH, TY, 1, ANY, POST>(a, s);
+        case 2: return block_bwd_run<TH, TY, 2, ANY, POST>(a, s);
+        case 3: return block_bwd_run<TH, TY, 3, ANY, POST>(a, s);
+        case 4: return block_bwd_run<TH, TY, 4, ANY, POST>(a, s);
+        default: return block_bwd_run<TH, TY, 5, ANY, POST>(a, s);
     }
 }
 template <typename TH, typename TY>
 static hipError_t block_bwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
-    return a.t.y && a.post != LQ_NORM_NONE ? block_bwd_vectors<TH, TY, true>(a, sh, s) : block_bwd_vectors<TH, TY, false>(a, sh, s);
+    const bool post = a.t.y && a.post != LQ_NORM_NONE;
+    if (sh.any) return post ? block_bwd_vectors<TH, TY, true, true>(a, sh, s) : block_bwd_vectors<TH, TY, true, false>(a, sh, s);
+    return post ? block_bwd_vectors<TH, TY, false, true>(a, sh, s) : block_bwd_vectors<TH, TY, false, false>(a, sh, s);
 }
 hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int64_t M, uint8_t* work, hipStream_t s)
 {
@@ -323,10 +357,18 @@ hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int
                                     : block_bwd_types<float, float>(a, sh, s);
     }
     if (e != hipSuccess || !sums) return e;
-    float* raw = weights ? (float*)(work + align256(block_parts(c, M, t.S) * 4)) : nullptr;
     const int64_t each = (M + a.chunk - 1) / a.chunk / t.S;  // parts of a sequence
+    const int team = each >= 64 ? 16 : each >= 16 ? 4 : 1;
     const unsigned cols = (unsigned)((c->dim + 63) / 64);
-    hipLaunchKernelGGL(block_sums, dim3(cols, 3, (unsigned)(t.S < 4096 ? t.S : 4096)), dim3(each >= 32 ? 1024 : 256), 0, s, a, raw);
+    // a launch of its own for the weights' sums costs 4 us; without it the workgroups of all sequences are one
+    if (weights && t.S * team <= 64) {
+        hipLaunchKernelGGL(block_sums<true>, dim3(cols, 3), dim3(1024), 0, s, a, team, nullptr);
+        return hipGetLastError();
+    }
+    float* raw = weights ? (float*)(work + align256(block_parts(c, M, t.S) * 4)) : nullptr;
+    const int waves = t.S == 1 ? team : 16, teams = waves / team;
+    const int64_t turns = (t.S + teams - 1) / teams;
+    hipLaunchKernelGGL(block_sums<false>, dim3(cols, 3, (unsigned)(turns < 4096 ? turns : 4096)), dim3(64 * waves), 0, s, a, team, raw);
     e = hipGetLastError();
     if (e != hipSuccess || !weights) return e;
     hipLaunchKernelGGL(block_weight_sums, dim3(cols, 2), dim3(1024), 0, s, a, (const float*)raw);

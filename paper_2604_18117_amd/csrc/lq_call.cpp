@@ -577,9 +577,15 @@ bool list_of(PyObject* o, Py_ssize_t count)
 {
     return (PyList_CheckExact(o) && PyList_GET_SIZE(o) == count) || (PyTuple_CheckExact(o) && PyTuple_GET_SIZE(o) == count);
 }
-bool values(PyObject* o, c10::ScalarType ty, int64_t n, void** p)
+// An ordinary tensor of a list, where `like` are the keys of one that has been looked at in full: those of another are enough then.
+const at::Tensor* listed(PyObject* o, const c10::DispatchKeySet& like)
 {
-    const at::Tensor* t = tensor(o);
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.defined() && t.key_set() == like && t.has_storage() ? &t : tensor(o);
+}
+bool values(const at::Tensor* t, c10::ScalarType ty, int64_t n, void** p)
+{
     if (!t || t->scalar_type() != ty || t->numel() != n || !t->is_contiguous()) return false;
     *p = t->data_ptr();
     return true;
@@ -598,7 +604,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, param
         lq_adamw_args x{};
         void* q;
         if (tensor(a[5])) {
-            if (!values(a[5], at::kFloat, 1, &q)) return NOT_HERE;
+            if (!values(tensor(a[5]), at::kFloat, 1, &q)) return NOT_HERE;
             x.lr_dev = (const float*)q;
         } else if (PyFloat_CheckExact(a[5])) {
             x.lr = PyFloat_AS_DOUBLE(a[5]);
@@ -607,27 +613,34 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)  // cfg, param
         }
         x.step = 1;
         if (tensor(a[6])) {
-            if (!values(a[6], at::kInt, 1, &q)) return NOT_HERE;
+            if (!values(tensor(a[6]), at::kInt, 1, &q)) return NOT_HERE;
             x.step_dev = (const int32_t*)q;
         } else if (!integer(a[6], &x.step)) {
             return NOT_HERE;
         }
         if (a[9] != Py_None) {
-            if (!values(a[9], at::kFloat, 1, &q)) return NOT_HERE;
+            if (!values(tensor(a[9]), at::kFloat, 1, &q)) return NOT_HERE;
             x.grad_scale = (const float*)q;
         }
         const c10::ScalarType pt = type_of(c.p->p_dtype), gt = type_of(c.p->g_dtype), st = eight ? at::kFloat8_e4m3fn : at::kFloat;
         std::vector<lq_adamw_tensor> table((size_t)count);
+        c10::DispatchKeySet like;
+        if (count > 0) {
+            const at::Tensor* first = tensor(item(a[1], 0));
+            if (!first) return NOT_HERE;
+            like = first->key_set();
+        }
         for (Py_ssize_t i = 0; i < count; ++i) {
             lq_adamw_tensor& t = table[(size_t)i];
-            const at::Tensor* p = tensor(item(a[1], i));
+            const at::Tensor* p = listed(item(a[1], i), like);
             if (!p || p->scalar_type() != pt || !p->is_contiguous()) return NOT_HERE;
             t = {p->data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, p->numel()};
             void *g, *s = nullptr, *w = nullptr;
-            if (!values(item(a[2], i), gt, t.n, &g) || !values(item(a[3], i), st, t.n, &t.m) || !values(item(a[4], i), st, t.n, &t.v)) return NOT_HERE;
-            if (masters && item(a[8], i) != Py_None && !values(item(a[8], i), at::kFloat, t.n, &w)) return NOT_HERE;
+            if (!values(listed(item(a[2], i), like), gt, t.n, &g) || !values(listed(item(a[3], i), like), st, t.n, &t.m) || !values(listed(item(a[4], i), like), st, t.n, &t.v))
+                return NOT_HERE;
+            if (masters && item(a[8], i) != Py_None && !values(listed(item(a[8], i), like), at::kFloat, t.n, &w)) return NOT_HERE;
             if (eight) {
-                const at::Tensor* sc = tensor(item(a[7], i));
+                const at::Tensor* sc = listed(item(a[7], i), like);
                 if (!dense(sc, at::kFloat, (t.n + 255) / 256, 2)) return NOT_HERE;
                 s = sc->data_ptr();
             }
