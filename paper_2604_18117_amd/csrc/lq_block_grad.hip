@@ -285,16 +285,19 @@ __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const flo
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Rows of a workgroup of the gradient, each of which leaves parts of the sums: one workgroup to a compute unit is what its registers allow (us by the number of workgroups,
-// 8192 rows of 1152, bf16: 256 31.7, 512 36.9, 768 42.5), in small batches fewer rows than it has wavefronts (300 fp32 rows in 7 sequences, both norms: 4 22.3, 8 23.3)
-static int block_bwd_chunk(int64_t M)
+// Groups of W wavefronts of a workgroup, and its rows, of which each leaves parts of the sums: eight wavefronts to a compute unit are what the registers allow (us by the number of
+// workgroups of eight, 8192 rows of 1152, bf16: 256 31.7, 512 36.9, 768 42.5); in small batches a few rows, no more than it has groups (300 fp32 rows in 7 sequences, both norms: 4 22.3,
+// 8 23.3; 8 rows of 4487, four wavefronts each: 1 16.3, 4 25.0)
+static int block_bwd_groups(int W) { return W > 3 ? 1 : 8 / W; }
+static int block_bwd_chunk(const lq_block_config* c, int64_t M)
 {
-    const int64_t t = (M + 255) / 256;
-    return (int)(t < 4 ? 4 : t);
+    const int W = block_shape(c->dim, false).W, groups = block_bwd_groups(W), least = groups < 4 ? groups : 4;
+    const int64_t workgroups = 256 * (W * groups > 4 ? 1 : 2), t = (M + workgroups - 1) / workgroups;
+    return (int)(t < least ? least : t);
 }
 static size_t block_parts(const lq_block_config* c, int64_t M, int64_t S)
 {
-    const int chunk = block_bwd_chunk(M);
+    const int chunk = block_bwd_chunk(c, M);
     return (size_t)((M + chunk - 1) / chunk + S) * 3 * c->dim;
 }
 size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
@@ -305,7 +308,7 @@ size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
 template <typename TH, typename TY, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
 static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
 {
-    const int groups = a.waves > 3 ? 1 : 8 / a.waves;
+    const int groups = block_bwd_groups(a.waves);
     const dim3 grid((unsigned)((a.M + a.chunk - 1) / a.chunk)), block(64 * a.waves * groups);
     const size_t lds = (size_t)(groups > 1 ? 3 * groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (up to 140 KB)
     if (lds > 65280) {
@@ -346,7 +349,7 @@ hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int
 {
     const bool sums = t.dgate.p || t.dscale.p || t.dshift.p || t.dw_pre || t.dw_post, weights = t.dw_pre || t.dw_post;
     BlockArgs a = block_args(c, t, M);
-    a.chunk = block_bwd_chunk(M);
+    a.chunk = block_bwd_chunk(c, M);
     a.part = sums ? (float*)work : nullptr;
     hipError_t e = hipSuccess;
     if (M > 0) {
