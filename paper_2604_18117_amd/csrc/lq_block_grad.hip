@@ -8,11 +8,15 @@ namespace lq {
 // and the sums over the rows of a sequence of dx, dx n and G p, from which block_sums makes the gradients of modulation and weights.  A workgroup takes a chunk of rows,
 // its groups of W wavefronts in turn; a and b are in the LDS.  At the end of a sequence or of the chunk the groups' sums are joined in the LDS and written to place chunk + s
 // of the parts, which no other pair of chunk and sequence has (both rise from one pair to the next).
-template <typename TH, typename TY, int VEC, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
+// TENSORS.  ALL: all inputs and results of rows are there, and read VEC values at a time.  SOME may be missing (the branches cost registers: 8192 rows of 1152, layer norm, 23.2 us where
+// ALL takes 22.7).  LOOSE: any may be missing, and of any alignment.
+enum { ALL, SOME, LOOSE };
+template <typename TH, typename TY, int VEC, int NV, int TENSORS, bool POST, bool MULTI, int THREADS>
 __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
 {
     extern __shared__ v4f shared[];
     __shared__ float slots[64];
+    constexpr bool ANY = TENSORS == LOOSE;
     const BlockTensors& t = a.t;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, W = MULTI ? a.waves : 1, group = wave / W, groups = waves / W;
     const int padded = (a.dim + VEC - 1) / VEC * VEC;
@@ -21,7 +25,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
     RowSum<MULTI> sum{slots, waves, group * W, wave, W};
     int first = blockIdx.x * a.chunk;
     const int limit = min(first + a.chunk, (int)a.M);
-    const bool has_dx = t.dx, has_y = t.y, has_dho = t.dho;
+    const bool has_dx = TENSORS == ALL || t.dx, has_y = TENSORS == ALL || t.y, has_dho = TENSORS == ALL || t.dho, want_dh = TENSORS == ALL || t.dh, want_dy = TENSORS == ALL || t.dy;
     const Sequences sequences(t);
     Raw<TH, VEC, ANY> rh[NV], rg[NV];
     Raw<TY, VEC, ANY> ry[NV], rx[NV];
@@ -111,7 +115,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) g[v][i] += fmaf(r, dx[v][i], fmaf(-n[v][i], u, -w));
             }
-            if (t.dh && on) {
+            if (want_dh && on) {
                 TH* o = (TH*)t.dh + row * t.lddh;
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
@@ -151,7 +155,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
 #pragma unroll
                         for (int i = 0; i < VEC; ++i) g[v][i] = fmaf(r, g[v][i], fmaf(-p[v][i], u, -w));
                 }
-                if (t.dy && on) {
+                if (want_dy && on) {
                     TY* o = (TY*)t.dy + row * t.lddy;
 #pragma unroll
                     for (int v = 0; v < NV; ++v) c.put(o, v, g[v]);
@@ -305,45 +309,47 @@ size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
     return align256(block_parts(c, M, S) * 4) + align256((size_t)S * 2 * c->dim * 4);
 }
 
-template <typename TH, typename TY, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
+template <typename TH, typename TY, int NV, int TENSORS, bool POST, bool MULTI, int THREADS>
 static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
 {
     const int groups = block_bwd_groups(a.waves);
     const dim3 grid((unsigned)((a.M + a.chunk - 1) / a.chunk)), block(64 * a.waves * groups);
     const size_t lds = (size_t)(groups > 1 ? 3 * groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (up to 140 KB)
     if (lds > 65280) {
-        const hipError_t e = allow_lds<block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>>(143360);
+        const hipError_t e = allow_lds<block_bwd_kernel<TH, TY, 4, NV, TENSORS, POST, MULTI, THREADS>>(143360);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((block_bwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>), grid, block, lds, s, a);
+    hipLaunchKernelGGL((block_bwd_kernel<TH, TY, 4, NV, TENSORS, POST, MULTI, THREADS>), grid, block, lds, s, a);
     return hipGetLastError();
 }
-template <typename TH, typename TY, int NV, bool ANY, bool POST>
+template <typename TH, typename TY, int NV, int TENSORS, bool POST>
 static hipError_t block_bwd_run(const BlockArgs& a, hipStream_t s)
 {
     if constexpr (NV == 5)
-        if (a.waves > 8) return block_bwd_launch<TH, TY, NV, ANY, POST, true, 1024>(a, s);
+        if (a.waves > 8) return block_bwd_launch<TH, TY, NV, TENSORS, POST, true, 1024>(a, s);
     if constexpr (NV >= 3)
-        if (a.waves > 1) return block_bwd_launch<TH, TY, NV, ANY, POST, true, 512>(a, s);
-    return block_bwd_launch<TH, TY, NV, ANY, POST, false, 512>(a, s);
+        if (a.waves > 1) return block_bwd_launch<TH, TY, NV, TENSORS, POST, true, 512>(a, s);
+    return block_bwd_launch<TH, TY, NV, TENSORS, POST, false, 512>(a, s);
 }
-template <typename TH, typename TY, bool ANY, bool POST>
+template <typename TH, typename TY, int TENSORS, bool POST>
 static hipError_t block_bwd_vectors(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
     switch (sh.NV) {
-        case 1: return block_bwd_run<TH, TY, 1, ANY, POST>(a, s);
-        case 2: return block_bwd_run<TH, TY, 2, ANY, POST>(a, s);
-        case 3: return block_bwd_run<TH, TY, 3, ANY, POST>(a, s);
-        case 4: return block_bwd_run<TH, TY, 4, ANY, POST>(a, s);
-        default: return block_bwd_run<TH, TY, 5, ANY, POST>(a, s);
+        case 1: return block_bwd_run<TH, TY, 1, TENSORS == ALL ? SOME : TENSORS, POST>(a, s);  // (short rows have registers to spare)
+        case 2: return block_bwd_run<TH, TY, 2, TENSORS == ALL ? SOME : TENSORS, POST>(a, s);
+        case 3: return block_bwd_run<TH, TY, 3, TENSORS, POST>(a, s);
+        case 4: return block_bwd_run<TH, TY, 4, TENSORS, POST>(a, s);
+        default: return block_bwd_run<TH, TY, 5, TENSORS, POST>(a, s);
     }
 }
 template <typename TH, typename TY>
 static hipError_t block_bwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
 {
     const bool post = a.t.y && a.post != LQ_NORM_NONE;
-    if (sh.any) return post ? block_bwd_vectors<TH, TY, true, true>(a, sh, s) : block_bwd_vectors<TH, TY, true, false>(a, sh, s);
-    return post ? block_bwd_vectors<TH, TY, false, true>(a, sh, s) : block_bwd_vectors<TH, TY, false, false>(a, sh, s);
+    const BlockTensors& t = a.t;
+    if (sh.any) return post ? block_bwd_vectors<TH, TY, LOOSE, true>(a, sh, s) : block_bwd_vectors<TH, TY, LOOSE, false>(a, sh, s);
+    if (!t.dx || !t.dho || !t.y || !t.dh || !t.dy) return post ? block_bwd_vectors<TH, TY, SOME, true>(a, sh, s) : block_bwd_vectors<TH, TY, SOME, false>(a, sh, s);
+    return post ? block_bwd_vectors<TH, TY, ALL, true>(a, sh, s) : block_bwd_vectors<TH, TY, ALL, false>(a, sh, s);
 }
 hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int64_t M, uint8_t* work, hipStream_t s)
 {
