@@ -5,10 +5,13 @@ place on its output, queries and keys normalised and rotated by the positions of
 
     activation step -> forward -> adapters -> norm and rotation of queries and keys
 
-Training (``AdaptedQKV.backward``): the gradients of the adapters (and of the norm's weights) from those of the finished queries, keys and values, through
-the frozen projection.
+What comes before it in a block with modulation (``Entrance``): gate, scale and shift of each image from its embedding, a few rows through 4-bit weights, and
+the block before gated, added and normalised in one pass, which gives the projection's rows.
 
-    python -m paper_2604_18117_amd.adapted_qkv            # serves a batch, prints the time of its four calls
+Training (``AdaptedQKV.backward``): the gradients of the adapters (and of the norm's weights) from those of the finished queries, keys and values, through
+the frozen projection; the factors take their steps with ``lq_adamw_step``, bf16 with 32-bit masters.
+
+    python -m paper_2604_18117_amd.adapted_qkv            # serves a batch, prints the time of its six calls
     python -m paper_2604_18117_amd.adapted_qkv --train    # fits two adapters to a shifted layer, prints the loss
 """
 from __future__ import annotations
@@ -91,6 +94,38 @@ class AdaptedQKV:
         return dA, dB, dwq, dwk
 
 
+class Entrance:
+    """The rows that a projection gets from the stream h and the output y of the block before.
+
+    W: 3 dim x emb fp32, the modulation's layer (gate of the block before, scale and shift of the norm); offsets: first row of each image and the end of the last."""
+
+    def __init__(self, W, offsets, bias=None):
+        n, emb = W.shape
+        self.dim, self.bias, self.offsets = n // 3, bias, offsets
+        self.cfg = lq.make_w4_config(n, emb, 64, "f32", "f32")
+        self.packed = lq.lq_w4_pack(self.cfg, W)
+        self.norm = lq.make_block_config(self.dim)
+        self.mod = torch.empty(offsets.shape[0] - 1, n, device="cuda")
+
+    def parts(self, mod):
+        """Views of gate, scale and shift in the layer's rows."""
+        return [mod[:, k * self.dim:(k + 1) * self.dim] for k in range(3)]
+
+    def __call__(self, emb, h, y, X=None):
+        """(h', X): h' = h + gate y in h's place, X its modulated norm."""
+        lq.lq_w4_fwd(self.cfg, self.packed, emb, self.bias, Y=self.mod)
+        gate, scale, shift = self.parts(self.mod)
+        return lq.lq_block_norm_fwd(self.norm, h, y, self.offsets, gate, scale, shift, ho=h, x=X)
+
+    def backward(self, h, y, dh, dX):
+        """(dh, dy, demb).  h: the stream that a call left, dh: the derivative with respect to it from what follows, overwritten; dX: with respect to the rows, overwritten."""
+        gate, scale, _ = self.parts(self.mod)
+        dmod = torch.empty_like(self.mod)
+        dgate, dscale, dshift = self.parts(dmod)
+        lq.lq_block_norm_bwd(self.norm, h, y, self.offsets, gate, scale, dho=dh, dx=dX, dh=dh, dy=dX, dgate=dgate, dscale=dscale, dshift=dshift)
+        return dh, dX, lq.lq_w4_bwd(self.cfg, self.packed, dmod)
+
+
 def layer(dim: int, rank: int, seed: int = 0):
     """A synthetic QKV layer with its branch's factors."""
     g = torch.Generator(device="cuda")
@@ -103,13 +138,16 @@ def serve(images: int = 2, side: int = 64, dim: int = 1152, heads: int = 16, ada
     M = images * side * side
     m = AdaptedQKV(*layer(dim, 32), M, heads, adapters, 32)
     m.B.normal_(std=0.02)
-    X = torch.randn(M, dim, device="cuda").bfloat16()
+    h, y = (torch.randn(M, dim, device="cuda").bfloat16() for _ in range(2))
+    X, emb = torch.empty_like(h), torch.randn(images, dim, device="cuda")
+    enter = Entrance(torch.randn(3 * dim, dim, device="cuda") * 0.02 / math.sqrt(dim), torch.arange(images + 1, dtype=torch.int32, device="cuda") * side * side)
     m.group(torch.arange(images, dtype=torch.int32, device="cuda").repeat_interleave(side * side) - 1)  # the first image has none
     pos, Y = grid_positions(side, side), torch.empty(M, 3 * dim, dtype=torch.bfloat16, device="cuda")
     ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
     for i in range(2 * steps):
         if i == steps:
             ev[0].record()
+        enter(emb, h, y, X)
         m(X, pos, Y)
     ev[1].record()
     torch.cuda.synchronize()
@@ -127,10 +165,12 @@ def train(steps: int = 60, side: int = 16, dim: int = 256, heads: int = 4, rank:
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
     shift = [torch.randn(3 * dim, rank, generator=g, device="cuda") @ torch.randn(rank, dim, generator=g, device="cuda") * 0.01 for _ in range(2)]
-    masters = [m.A.float().requires_grad_(), m.B.float().requires_grad_()]
-    opt = torch.optim.Adam(masters, lr=3e-3)
+    factors = [m.A, m.B]
+    masters = [f.float() for f in factors]
+    adamw = lq.make_adamw_config("bf16", "f32")
+    mean, var, _ = zip(*(lq.adamw_states(adamw, f) for f in factors))
     losses = []
-    for _ in range(steps):
+    for step in range(steps):
         X = torch.randn(M, dim, generator=g, device="cuda").bfloat16()
         target = torch.cat([X[ids == s].float() @ (W + shift[s]).t() for s in range(2)]).bfloat16()
         tq, tk = m.heads_of(target)
@@ -142,11 +182,7 @@ def train(steps: int = 60, side: int = 16, dim: int = 256, heads: int = 4, rank:
         diff = out.float() - target.float()
         losses.append(float((diff * diff).mean()))
         dA, dB, _, _ = m.backward(X, rows, pos, (diff * (2.0 / M)).bfloat16())
-        masters[0].grad, masters[1].grad = dA, dB
-        opt.step()
-        with torch.no_grad():
-            m.A.copy_(masters[0])
-            m.B.copy_(masters[1])
+        lq.lq_adamw_step(adamw, factors, [dA, dB], list(mean), list(var), 3e-3, step + 1, masters=masters)
     return losses
 
 
