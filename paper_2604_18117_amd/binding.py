@@ -1042,7 +1042,7 @@ def make_adamw_config(p_dtype: str = "f32", g_dtype: str = "f32", state_bits: in
 def adamw_states(cfg: lq_adamw_config, p: torch.Tensor):
     """(m, v, scales) of a parameter that has made no step; scales: None with states in 32 bits."""
     dtype = torch.float32 if cfg.state_bits == 32 else torch.float8_e4m3fn
-    m, v = (torch.zeros(p.shape, device=p.device).to(dtype) for _ in range(2))
+    m, v = (torch.zeros(p.shape, dtype=dtype, device=p.device) for _ in range(2))
     return m, v, None if cfg.state_bits == 32 else torch.ones((p.numel() + 255) // 256, 2, device=p.device)
 
 

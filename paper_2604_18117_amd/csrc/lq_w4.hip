@@ -248,7 +248,9 @@ struct Eight {
 
 // A workgroup makes 16 MT rows of NT tiles; its wavefronts share K out block by block and join their sums in the LDS.  A wavefront brings its block of X through LDS of its own: 16 lanes
 // read a row's 256 bytes (32 lanes 512), where the product's order, 16 rows in 16 lanes, is a piece of a cache line in every lane.  The next block is requested ahead of the products of
-// this one.  Rows past M repeat the last one and are not stored.  In the block where rows end, pieces of 16 bytes past the end are zero; the one in which they end is brought value by value.
+// this one (codes two blocks ahead: 64 x 2240 -> 11200 13.4 us for 13.1).  64 x 2240 -> 11200 takes 13-14 us, 2 x 1152 -> 6912 4.0, of which 3.2 are any launch's.  In the first 31 MB come
+// past the L2s, the codes twice, once for each 32 rows; 1.4 wavefronts a SIMD wait 43 % of their cycles, the vector unit has 25 %.  Tried there: 64 rows to a workgroup 16.5, four tiles 16.1; the
+// workgroups of a tile one after another on one XCD, where the second finds the codes, 13.1, but then 48 x 1152 -> 6912 takes 7.1 for 6.3.  Rows past M repeat the last one and are not stored.  In the block where rows end, pieces of 16 bytes past the end are zero; the one in which they end is brought value by value.
 template <bool F32, int MT, int NT, int PER>
 __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
 {
@@ -414,6 +416,7 @@ __device__ __forceinline__ void turn_nibbles(uint32_t (&d)[8])
 // dX of 16 rows and a block of 128 columns.  A wavefront takes 32 channels at a time (two tiles), which it brings through LDS of its own so that lane (c, q) holds eight channels
 // 8 q .. + 7 of the eight columns 8 c .. + 7; turned, they are the operands of eight products, product i with the columns 8 c + i.  The channels' scales go into dY (fp32, three terms);
 // where a block has several groups, a product is made for each and a lane keeps that of its own columns.  The wavefronts' sums are joined in the LDS, those of the parts of N by w4_join.
+// 16 x 2240 -> 13440: 11 us (at 0.9 wavefronts a SIMD, which wait 45 % of their cycles; vector unit 24 %) and 3.5 for the join; 2 x 1152 -> 6912: 6 and 3.9.
 constexpr int w4_bwd_waves(int per) { return per == 4 ? 4 : 8; }  // (sums for four groups are 128 registers)
 template <bool F32, int PER>
 __global__ void __launch_bounds__(64 * w4_bwd_waves(PER)) w4_bwd_kernel(W4Args a)
