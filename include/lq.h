@@ -554,7 +554,7 @@ typedef struct {
     int32_t state_bits;        /* 32 (fp32) | 8                                                       */
     int32_t flags;             /* 0                                                                   */
     double beta1, beta2;       /* in [0, 1)                                                           */
-    double eps, weight_decay;  /* > 0, >= 0                                                           */
+    double eps, weight_decay;  /* >= 1e-30, >= 0                                                      */
     uint32_t seed;             /* of the rounding                                                     */
     uint32_t reserved;         /* 0                                                                   */
 } lq_adamw_config;
@@ -565,7 +565,7 @@ typedef struct {       /* device memory, aligned to its type; n consecutive valu
     const void *grad;
     void *m, *v;       /* states: fp32, or bytes                                                   */
     float *scales;     /* state_bits = 8: ceil(n / 256) x 2 (of m, of v's root); otherwise NULL    */
-    int64_t n;         /* 0 .. 2^32 - 1 - 1                                                            */
+    int64_t n;         /* 0 .. 2^32 - 1                                                            */
 } lq_adamw_tensor;
 
 typedef struct {
@@ -576,7 +576,8 @@ typedef struct {
     const float *grad_scale;    /* device, one value, or NULL for 1                                  */
 } lq_adamw_args;
 
-/* tensors: host, `count` of them (0 .. 65536).  What a call writes must not overlap (LQ_ERR_SHAPE: the same tensor twice, views that share values). */
+/* tensors: host, `count` of them (0 .. 65536).  What a call writes must not overlap (LQ_ERR_SHAPE: the same tensor twice, views that share values), and nothing that it only reads may lie in it; gradients may
+   share memory among themselves. */
 lq_status lq_adamw_step(const lq_adamw_config *cfg, const lq_adamw_tensor *tensors, int32_t count, const lq_adamw_args *args, void *stream);
 
 #ifdef __cplusplus

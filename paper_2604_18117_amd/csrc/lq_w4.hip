@@ -71,11 +71,12 @@ __global__ void __launch_bounds__(64) w4_pack_kernel(const float* W, const int8_
         if (s.per == 1) amax[0] = amax[1] = amax[2] = amax[3] = fmaxf(amax[0], amax[2]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float inv = amax[j] == 0.0f ? 1.0f : 7.0f / amax[j];
+            const float up = amax[j] < 0x1p-100f ? 0x1p100f : 1.0f;  // (below 2^-125 the quotient would be infinite)
+            const float inv = amax[j] == 0.0f ? 1.0f : 7.0f / (amax[j] * up);
             sc[j] = amax[j] == 0.0f ? 1.0f : amax[j] / 7.0f;
             word[j] = 0u;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) word[j] |= w4_nibble((int)fminf(fmaxf(rintf(v[j][i] * inv), -7.0f), 7.0f)) << (8 * (i & 3) + (i & 4));
+            for (int i = 0; i < 8; ++i) word[j] |= w4_nibble((int)fminf(fmaxf(rintf(v[j][i] * up * inv), -7.0f), 7.0f)) << (8 * (i & 3) + (i & 4));
         }
     } else {
 #pragma unroll

@@ -257,3 +257,27 @@ def test_overlapping_tensors_are_refused(lq):
         assert e.value.status == lq.LQ_ERR_SHAPE
         assert all(torch.equal(a, b) for a, b in zip(t, before))
     lq.lq_adamw_step(cfg, [], [], [], [], 1e-3, 1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_values_past_32_bits(lq, bits):
+    """A tensor of more than 2^31 values: its end as a short tensor's (states in 32 bits), or next to it (in 8 bits, whose rounding goes by a value's place)."""
+    n, end = 2 ** 31 + 300, 812
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(0)
+    cfg = lq.make_adamw_config("bf16", "bf16", bits)
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    p[-end:], g[-end:] = torch.randn(end, generator=gen, device="cuda").bfloat16(), torch.randn(end, generator=gen, device="cuda").bfloat16()
+    short, grad = p[-end:].clone(), g[-end:].clone()
+    m, v, scales = lq.adamw_states(cfg, p)
+    sm, sv, ss = lq.adamw_states(cfg, short)
+    for params, grads, a, b, s in ((p, g, m, v, scales), (short, grad, sm, sv, ss)):
+        lq.lq_adamw_step(cfg, [params], [grads], [a], [b], 1e-2, 1, scales=None if s is None else [s])
+    assert torch.equal(p[-end:], short) and not p[:end].any()
+    if bits == 32:
+        assert torch.equal(m[-end:], sm) and torch.equal(v[-end:], sv) and not m[:end].float().any()
+    else:
+        last = scales[-4:].repeat_interleave(256, 0)[:end]  # (the end begins with a block, at 2^31 - 512)
+        for k, (t, want) in enumerate(((m, 0.1 * grad.double()), (v, (0.001 * grad.double().square()).sqrt()))):
+            got = t[-end:].double() * last[:, k]
+            assert (got - want).abs().max() <= 2.0 ** -3 * want.abs().max() * 1.01

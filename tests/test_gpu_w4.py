@@ -48,6 +48,39 @@ def test_pack_by_the_int_rule(lq, N, K, group):
     assert torch.equal(again, packed)
 
 
+def test_pack_groups_of_the_smallest_numbers(lq):
+    """A group whose largest value is below 7 over the largest number: codes within one of the quotient, zeros exact."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    W = torch.randn(16, 128, generator=g, device="cuda")
+    W[:, 5::7] = 0.0
+    W = (W.double() * 2.0 ** -129).float()
+    cfg = lq.make_w4_config(16, 128, 64)
+    codes, scales = lq.lq_w4_unpack(cfg, lq.lq_w4_pack(cfg, W))
+    amax = W.double().abs().view(16, 2, 64).amax(-1)
+    assert not codes[:, 5::7].any()
+    assert (codes.double() - W.double() * 7 / amax.repeat_interleave(64, 1)).abs().max() <= 1.0
+    assert (scales.double() - amax / 7).abs().max() <= 2.0 ** -149
+
+
+def test_codes_past_32_bits(lq):
+    """More than 2^32 bytes of codes: the last channels, and the gradient with respect to some columns."""
+    N, K, group = 2 ** 17 + 5, 2 ** 16, 128
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    codes = torch.randint(-7, 8, (N, K), generator=g, device="cuda", dtype=torch.int8)
+    scales = torch.randn(N, K // group, generator=g, device="cuda")
+    cfg = lq.make_w4_config(N, K, group, "f32", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    X, dY = torch.randn(1, K, generator=g, device="cuda"), torch.randn(1, N, generator=g, device="cuda")
+    rows = torch.cat([torch.arange(40), torch.arange(N - 40, N)]).cuda()
+    ref.check(lq.lq_w4_fwd(cfg, packed, X)[:, rows], ref.w4_fwd(X, codes[rows], scales[rows], group, None, torch.float32), "forward")
+    dX = lq.lq_w4_bwd(cfg, packed, dY)
+    for at in (0, K - 128):
+        part = codes[:, at:at + 128].contiguous(), scales[:, at // group:at // group + 1].contiguous()
+        ref.check(dX[:, at:at + 128], ref.w4_bwd(dY, *part, group, torch.float32), "gradient")
+
+
 def test_codes_beyond_the_range(lq):
     codes = torch.arange(-128, 128, dtype=torch.int8, device="cuda").view(2, 128)
     cfg = lq.make_w4_config(2, 128, 32)
