@@ -479,7 +479,7 @@ lq_status lq_w4_unpack(const lq_w4_config *cfg, const void *packed, size_t packe
 lq_status lq_w4_fwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy,
                     int64_t M, void *stream);
 
-/* Bytes of the gradient's workspace (may be 0).  Host-only. */
+/* Bytes of the gradient's workspace (may be 0); no less for more rows.  Host-only. */
 lq_status lq_w4_work_sizes(const lq_w4_config *cfg, int64_t M, size_t *work_bytes);
 /* work: 256-byte aligned; may be NULL where lq_w4_work_sizes reports 0. */
 lq_status lq_w4_bwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *dY, int64_t lddy, void *dX, int64_t lddx, int64_t M, void *work,
@@ -519,7 +519,7 @@ lq_status lq_block_norm_fwd(const lq_block_config *cfg, const void *h, int64_t l
                             const lq_mod *gate, const lq_mod *scale, const lq_mod *shift, const float *w_post, const float *w_pre, void *ho,
                             int64_t ldho, void *x, int64_t ldx, int64_t M, void *stream);
 
-/* Bytes of the gradient's workspace.  Host-only. */
+/* Bytes of the gradient's workspace; no less for more rows or sequences.  Host-only. */
 lq_status lq_block_work_sizes(const lq_block_config *cfg, int64_t M, int32_t S, size_t *work_bytes);
 
 /* Gradients.  With n = pre(h'), p = post(y) before their weights, dho the derivative of a loss with respect to h' (what comes through the stream) and dx that with respect to x:

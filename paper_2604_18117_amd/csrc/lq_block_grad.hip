@@ -1,4 +1,6 @@
 // Norms before and after a block (lq_block.h): gradient.
+#include <algorithm>
+
 #include "lq_block.h"
 
 namespace lq {
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
         }
         if (a.part) {
             float* out = a.part + (size_t)(blockIdx.x + s) * 3 * a.dim;
-            if (MULTI && groups == 1) {
+            if (groups == 1) {
 #pragma unroll
                 for (int k = 0; k < 3; ++k)
 #pragma unroll
@@ -208,17 +210,17 @@ __device__ __forceinline__ void parts_of(const BlockArgs& a, int s, int& c0, int
     c0 = begin / a.chunk;
     c1 = begin < end ? (end - 1) / a.chunk + 1 : c0;
 }
-// Sums over a sequence's parts in a fixed order, 64 columns of one of the three sums to a workgroup:
+// Sums over a sequence's parts in a fixed order, COLS columns of one of the three sums to a workgroup, 64 / COLS parts at a time to a wavefront:
 //     dshift = sum dx ;  dscale = w_pre sum dx n ;  dgate = w_post sum G p
 // `team` wavefronts share the parts of a sequence out and are joined in a tree; the workgroup's teams take the sequences from blockIdx.z on in turn.  FUSED (one workgroup sees all sequences): also
 //     dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
 // Otherwise raw: the last two sums without the weights, for block_weight_sums.
-template <bool FUSED>
+template <bool FUSED, int COLS>
 __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float* raw)
 {
     __shared__ float sh[16][64];
     const BlockTensors& t = a.t;
-    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, col = blockIdx.x * 64 + lane;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, col = blockIdx.x * COLS + lane % COLS;
     const int member = wave % team, teams = waves / team;
     const lq_mod_out& o = k == 0 ? t.dshift : k == 1 ? t.dscale : t.dgate;
     const lq_mod& f = k == 1 ? t.scale : t.gate;
@@ -233,8 +235,10 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
             parts_of(a, s, c0, c1);
             const float* p = a.part + (size_t)s * 3 * a.dim + k * a.dim + col;
 #pragma unroll 8
-            for (int i = c0 + member; i < c1; i += team) y += p[(size_t)i * 3 * a.dim];
+            for (int i = c0 + member * (64 / COLS) + lane / COLS; i < c1; i += team * (64 / COLS)) y += p[(size_t)i * 3 * a.dim];
         }
+#pragma unroll
+        for (int half = 32; half >= COLS; half /= 2) y += __shfl_xor(y, half);
         if (team > 1) {
             sh[wave][lane] = y;
             __syncthreads();
@@ -244,7 +248,7 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
             }
             y = sh[wave][lane];
         }
-        if (member == 0 && s < t.S && col < a.dim) {
+        if (member == 0 && lane < COLS && s < t.S && col < a.dim) {
             if (o.p) o.p[s * o.ld + col] = w ? y * w[col] : y;
             if (FUSED) {
                 const float g = f.p ? f.p[s * f.ld + col] : k == 1 ? 0.0f : 1.0f;
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
         if (wave < half) sh[wave][lane] += sh[wave + half][lane];
         __syncthreads();
     }
-    if (wave == 0 && col < a.dim) dw[col] = sh[0][lane];
+    if (wave == 0 && lane < COLS && col < a.dim) dw[col] = sh[0][lane];
 }
 // dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
 __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const float* raw)
@@ -291,21 +295,19 @@ __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const flo
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Groups of W wavefronts of a workgroup, and its rows, of which each leaves parts of the sums: eight wavefronts to a compute unit are what the registers allow (us by the number of
-// workgroups of eight, 8192 rows of 1152, bf16: 256 31.7, 512 36.9, 768 42.5); in small batches a few rows, no more than it has groups (300 fp32 rows in 7 sequences, both norms: 4 22.3,
-// 8 23.3; 8 rows of 4487, four wavefronts each: 1 16.3, 4 25.0)
-static int block_bwd_groups(int W) { return W > 3 ? 1 : 8 / W; }
+// Rows of a workgroup, of which each leaves parts of the sums, and its groups of W wavefronts.  One row up to 512 of them (us: 18 rows of 1528 11.5, four at a time 21.3; 64 of 1152 11.2 / 16.5; 500 of
+// 2240, both norms, 21.8 / 25.2; but 1000 of 1152 20.9 / 19.7).  Above, eight wavefronts to a compute unit are what the registers allow (by the number of workgroups of eight, 8192 rows of 1152, bf16:
+// 256 31.7, 512 36.9, 768 42.5), with four rows at least or one to each group.
+constexpr int FEW_ROWS = 512;
+static int block_bwd_groups(int W, int chunk) { return std::min(W > 3 ? 1 : 8 / W, chunk); }
 static int block_bwd_chunk(const lq_block_config* c, int64_t M)
 {
-    const int W = block_shape(c->dim, false).W, groups = block_bwd_groups(W), least = groups < 4 ? groups : 4;
-    const int64_t workgroups = 256 * (W * groups > 4 ? 1 : 2), t = (M + workgroups - 1) / workgroups;
-    return (int)(t < least ? least : t);
+    if (M <= FEW_ROWS) return 1;
+    const int W = block_shape(c->dim, false).W, groups = block_bwd_groups(W, 8), workgroups = 256 * (W * groups > 4 ? 1 : 2);
+    return std::max((int)((M + workgroups - 1) / workgroups), std::min(groups, 4));
 }
-static size_t block_parts(const lq_block_config* c, int64_t M, int64_t S)
-{
-    const int chunk = block_bwd_chunk(c, M);
-    return (size_t)((M + chunk - 1) / chunk + S) * 3 * c->dim;
-}
+// (no chunk leaves more than FEW_ROWS parts and one for each sequence: a workspace serves smaller batches, too)
+static size_t block_parts(const lq_block_config* c, int64_t M, int64_t S) { return (size_t)(std::min<int64_t>(M, FEW_ROWS) + S) * 3 * c->dim; }
 size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
 {
     return align256(block_parts(c, M, S) * 4) + align256((size_t)S * 2 * c->dim * 4);
@@ -314,7 +316,7 @@ size_t block_work_bytes(const lq_block_config* c, int64_t M, int64_t S)
 template <typename TH, typename TY, int NV, int TENSORS, bool POST, bool MULTI, int THREADS>
 static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
 {
-    const int groups = block_bwd_groups(a.waves);
+    const int groups = block_bwd_groups(a.waves, a.chunk);
     const dim3 grid((unsigned)((a.M + a.chunk - 1) / a.chunk)), block(64 * a.waves * groups);
     const size_t lds = (size_t)(groups > 1 ? 3 * groups + 2 : 2) * ((a.dim + 3) / 4 * 4) * 4;  // (up to 140 KB)
     if (lds > 65280) {
@@ -369,17 +371,26 @@ hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int
     }
     if (e != hipSuccess || !sums) return e;
     const int64_t each = (M + a.chunk - 1) / a.chunk / t.S;  // parts of a sequence
-    const int team = each >= 64 ? 16 : each >= 16 ? 4 : 1;
-    const unsigned cols = (unsigned)((c->dim + 63) / 64);
+    // eight parts to a lane, as far as sixteen wavefronts go; from eight parts on pieces of 16 columns, where a wavefront takes four parts at a time (us with the gradient: 300 fp32 rows in 7 sequences
+    // 18.5, by 64 columns 19.0; 64 rows of 1152 11.1 / 11.9)
+    const bool narrow = each >= 8;
+    int team = 1;
+    while (team < 16 && team * (narrow ? 32 : 8) < each) team *= 2;
+    const unsigned cols = (unsigned)((c->dim + 63) / 64), pieces = narrow ? (unsigned)((c->dim + 15) / 16) : cols;
     // a launch of its own for the weights' sums costs 4 us; without it the workgroups of all sequences are one
     if (weights && t.S * team <= 64) {
-        hipLaunchKernelGGL(block_sums<true>, dim3(cols, 3), dim3(1024), 0, s, a, team, nullptr);
+        while (team > 1 && t.S * team > 16) team /= 2;
+        if (narrow) hipLaunchKernelGGL((block_sums<true, 16>), dim3(pieces, 3), dim3(1024), 0, s, a, team, nullptr);
+        else hipLaunchKernelGGL((block_sums<true, 64>), dim3(pieces, 3), dim3(1024), 0, s, a, team, nullptr);
         return hipGetLastError();
     }
     float* raw = weights ? (float*)(work + align256(block_parts(c, M, t.S) * 4)) : nullptr;
-    const int waves = t.S == 1 ? team : 16, teams = waves / team;
-    const int64_t turns = (t.S + teams - 1) / teams;
-    hipLaunchKernelGGL(block_sums<false>, dim3(cols, 3, (unsigned)(turns < 4096 ? turns : 4096)), dim3(64 * waves), 0, s, a, team, raw);
+    int waves = team;
+    while (waves < 16 && waves < team * t.S) waves *= 2;
+    const int64_t teams = waves / team, turns = (t.S + teams - 1) / teams;
+    const dim3 grid(pieces, 3, (unsigned)(turns < 4096 ? turns : 4096));
+    if (narrow) hipLaunchKernelGGL((block_sums<false, 16>), grid, dim3(64 * waves), 0, s, a, team, raw);
+    else hipLaunchKernelGGL((block_sums<false, 64>), grid, dim3(64 * waves), 0, s, a, team, raw);
     e = hipGetLastError();
     if (e != hipSuccess || !weights) return e;
     hipLaunchKernelGGL(block_weight_sums, dim3(cols, 2), dim3(1024), 0, s, a, (const float*)raw);

@@ -616,8 +616,14 @@ static int w4_bwd_splits(const W4Shape& s, int64_t M)
 }
 size_t w4_work_bytes(const lq_w4_config* c, int64_t M)
 {
-    const int splits = M ? w4_bwd_splits(w4_shape(c), M) : 1;
-    return splits > 1 ? align256((size_t)splits * M * c->K * 4) : 0;
+    const W4Shape s = w4_shape(c);
+    int64_t rows = 0;  // of all parts: the most that a batch of up to M needs, so that a workspace serves smaller ones
+    for (int64_t m = 16; m - 16 < M; m += 16) {
+        const int64_t n = m < M ? m : M, splits = w4_bwd_splits(s, n);
+        if (splits == 1) break;  // (more rows have no more parts)
+        if (splits * n > rows) rows = splits * n;
+    }
+    return align256((size_t)rows * c->K * 4);
 }
 
 template <bool F32, int PER>

@@ -376,3 +376,16 @@ def test_the_rounding_rule_of_the_8_bit_states():
         u = r.double() / 2 ** 20 - 0.5
         assert abs(float(u.mean())) <= 5 * (1 / 12) ** 0.5 / 256
         assert abs(float((u[1:] * u[:-1]).mean())) <= 5 / 12 / 256
+
+
+def test_workspaces_serve_smaller_batches():
+    for N, K, group in ((100, 64, 32), (6912, 1152, 64), (13440, 2240, 128), (64, 4608, 64), (700, 128, 128)):
+        cfg = lq.make_w4_config(N, K, group)
+        sizes = [lq.lq_w4_work_sizes(cfg, M) for M in range(0, 2200)]
+        assert sizes == sorted(sizes) and sizes[0] == 0
+    for dim in (63, 1152, 2240, 5000, 16384):
+        cfg = lq.make_block_config(dim)
+        for S in (1, 7):
+            sizes = [lq.lq_block_work_sizes(cfg, M, S) for M in [*range(0, 1100), 2000, 4096, 8191, 8192, 8193, 2 ** 24]]
+            assert sizes == sorted(sizes)
+            assert sizes <= [lq.lq_block_work_sizes(cfg, M, S + 1) for M in [*range(0, 1100), 2000, 4096, 8191, 8192, 8193, 2 ** 24]]

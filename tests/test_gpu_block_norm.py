@@ -92,6 +92,25 @@ def test_sequences(lq, M, offsets, D):
     check_all(lq, make(M, D, offsets, seed=M), "none", "layer")
 
 
+@pytest.mark.parametrize("stream,branch", [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("post,pre", [("none", "layer"), ("rms", "rms"), ("layer", "none")])
+@pytest.mark.parametrize("D", [33, 512, 1152, 1528, 2240, 3600, 4608, 12000])
+def test_several_rows_to_a_workgroup(lq, D, post, pre, stream, branch):
+    """Batches of more than 512 rows: several rows to a group of wavefronts, several groups and sequences to a workgroup."""
+    M = 1300 if D < 4000 else 700
+    check_all(lq, make(M, D, [3, M // 4, M // 4 + 1, M // 4 + 1, M // 2 + 7, M - 10], stream, branch, seed=D), post, pre, alpha=0.75)
+
+
+@pytest.mark.parametrize("D", [200, 1152, 2240, 5000])
+def test_several_rows_to_a_workgroup_in_place(lq, D):
+    d = make(1100, D, [0, 20, 555, 1090], "bf16", "bf16")
+    cfg = config(lq, d, "rms", "layer", 0.5)
+    want = backward(lq, cfg, d, dh=d["dho"].clone(), dy=d["dx"].clone())
+    e = dict(d, dho=d["dho"].clone(), dx=d["dx"].clone())
+    for a, b in zip(backward(lq, cfg, e, dh=e["dho"], dy=e["dx"]), want):
+        assert torch.equal(a, b)
+
+
 def test_many_sequences(lq):
     g = torch.Generator()
     g.manual_seed(0)
