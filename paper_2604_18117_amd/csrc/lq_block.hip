@@ -1,4 +1,6 @@
 // Norms before and after a block (lq_block.h): forward.
+#include <algorithm>
+
 #include "lq_block.h"
 
 namespace lq {
@@ -77,21 +79,37 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
 
 // ---- host ---------------------------------------------------------------------------------------
 
+// Rows of a group, one after another: so many that all groups are on the card at once; where that is more than eight, four for rows of several wavefronts, whose factors come again for every group
+// but which wait for each other (us: 4000 rows of 4608 by 8, 500 groups 40.0, by 4 42.6, by 2 51.4, by 1 65.0; 2000 of 2240, fp32 and both norms, by 2 16.1, by 1 19.6, by 4 17.1; 16384 of them by 4 91.6,
+// by 6 93.6, by 16 97.7), sixteen at most for others (8192 of 1152 by 8 16.8, by 4 15.5, by 2 18.2).
+static int block_fwd_chunk(int64_t M, int W, int waves)  // waves: that a compute unit holds
+{
+    const int64_t groups = 256 * (int64_t)std::max(waves / W, 1), all = (M + groups - 1) / groups;
+    return (int)(all <= 8 ? all : W > 1 && M <= (1 << 20) ? 4 : std::min<int64_t>(all, 16));  // (a launch stays below 2^32 threads)
+}
+template <typename TH, typename TY, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
+static void block_fwd_launch(BlockArgs a, int W, hipStream_t s)
+{
+    constexpr auto kernel = block_fwd_kernel<TH, TY, 4, NV, ANY, POST, MULTI, THREADS>;
+    static const int waves = [] {
+        int n = 0;
+        constexpr int threads = THREADS == 1024 ? 1024 : 256;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) == hipSuccess && n > 0) return n * threads / 64;
+        (void)hipGetLastError();  // (not the launch's)
+        return 8;
+    }();
+    a.chunk = block_fwd_chunk(a.M, W, waves);
+    const int64_t groups = (a.M + a.chunk - 1) / a.chunk;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(MULTI ? groups : (groups + 3) / 4)), dim3(MULTI ? 64 * W : 256), 0, s, a);
+}
 template <typename TH, typename TY, int NV, bool ANY, bool POST>
 static void block_fwd_run(const BlockArgs& a, int W, hipStream_t s)
 {
-    const int64_t groups = (a.M + a.chunk - 1) / a.chunk;
     if constexpr (NV == 5)
-        if (W > 8) {
-            hipLaunchKernelGGL((block_fwd_kernel<TH, TY, 4, NV, ANY, POST, true, 1024>), dim3((unsigned)groups), dim3(64 * W), 0, s, a);
-            return;
-        }
+        if (W > 8) return block_fwd_launch<TH, TY, NV, ANY, POST, true, 1024>(a, W, s);
     if constexpr (NV >= 3)
-        if (W > 1) {
-            hipLaunchKernelGGL((block_fwd_kernel<TH, TY, 4, NV, ANY, POST, true, 512>), dim3((unsigned)groups), dim3(64 * W), 0, s, a);
-            return;
-        }
-    hipLaunchKernelGGL((block_fwd_kernel<TH, TY, 4, NV, ANY, POST, false, 256>), dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a);
+        if (W > 1) return block_fwd_launch<TH, TY, NV, ANY, POST, true, 512>(a, W, s);
+    block_fwd_launch<TH, TY, NV, ANY, POST, false, 256>(a, W, s);
 }
 template <typename TH, typename TY, bool ANY, bool POST>
 static void block_fwd_vectors(const BlockArgs& a, const BlockShape& sh, hipStream_t s)
@@ -114,11 +132,7 @@ static void block_fwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_
 hipError_t launch_block_fwd(const lq_block_config* c, const BlockTensors& t, int64_t M, hipStream_t s)
 {
     const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M));
-    BlockArgs a = block_args(c, t, M);
-    // rows one after another while every SIMD has two wavefronts, eight where a row has several, which wait for each other (us by the number of wavefronts: 8192 rows of 1152 1024 16.8, 2048
-    // 15.5, 4096 18.2; 16384 of 2240, fp32 stream and both norms, 2048 97.7, 4096 104.5, 8192 93.8)
-    const int64_t chunk = M * sh.W / (sh.W == 1 ? 2048 : 8192);
-    a.chunk = (int)(chunk < 1 ? 1 : chunk > 16 ? 16 : chunk);
+    const BlockArgs a = block_args(c, t, M);
     if (c->h_dtype == LQ_BF16) block_fwd_types<__bf16, __bf16>(a, sh, s);
     else if (c->y_dtype == LQ_BF16) block_fwd_types<float, __bf16>(a, sh, s);
     else block_fwd_types<float, float>(a, sh, s);
