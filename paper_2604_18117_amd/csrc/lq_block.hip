@@ -6,7 +6,7 @@
 namespace lq {
 
 // Forward.  A group of W wavefronts takes `chunk` rows one after another, the next row already requested.  MULTI: the group is the workgroup; otherwise a workgroup
-// has four of one wavefront.  8192 rows of 1152, bf16: 15.3 us, 4.9 TB/s; 16384 of 2240, fp32 stream and both norms: 93.5 us, 4.7 TB/s.
+// has four of one wavefront.  8192 rows of 1152, bf16: 15.3 us, 4.9 TB/s; 16384 of 2240, fp32 stream and both norms: 92 us, 4.8 TB/s.
 template <typename TH, typename TY, int VEC, int NV, bool ANY, bool POST, bool MULTI, int THREADS>
 __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
 {

@@ -10,7 +10,7 @@ namespace lq {
 // and the sums over the rows of a sequence of dx, dx n and G p, from which block_sums makes the gradients of modulation and weights.  A workgroup takes a chunk of rows,
 // its groups of W wavefronts in turn; a and b are in the LDS.  At the end of a sequence or of the chunk the groups' sums are joined in the LDS and written to place chunk + s
 // of the parts, which no other pair of chunk and sequence has (both rise from one pair to the next).
-// 8192 rows of 1152, bf16: 26.6 us (4.3 TB/s) and 4.8 for block_sums; the registers allow two wavefronts a SIMD, which wait 38 % of their cycles.  The next row asked for ahead fits into them in bf16
+// 8192 rows of 1152, bf16: 26.5 us (4.3 TB/s) and 4.1 for block_sums; the registers allow two wavefronts a SIMD, which wait 38 % of their cycles.  The next row asked for ahead fits into them in bf16
 // without spills and is slower: 32.0 us for 31.1 in all.
 // TENSORS.  ALL: all inputs and results of rows are there, and read VEC values at a time.  SOME may be missing (the branches cost registers: 8192 rows of 1152, layer norm, 23.2 us where
 // ALL takes 22.7).  LOOSE: any may be missing, and of any alignment.

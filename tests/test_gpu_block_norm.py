@@ -286,6 +286,24 @@ def test_captured_and_replayed_on_a_stream(lq):
             assert torch.equal(a, b), k
 
 
+def test_captured_without_a_call_before(lq):
+    """Forms that nothing else calls: what a first call asks of the runtime is allowed in a capture."""
+    d = make(700, 1021, [0, 333, 700], "f32", "f32")
+    cfg = config(lq, d, "layer", "rms")
+    outs = [torch.zeros_like(d["h"]) for _ in range(4)]
+    sums = [torch.zeros(2, 1021, device="cuda") for _ in range(3)] + [torch.zeros(1021, device="cuda") for _ in range(2)]
+    work = torch.empty(lq.lq_block_work_sizes(cfg, 700, 2), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        forward(lq, cfg, d, ho=outs[0], x=outs[1])
+        backward(lq, cfg, d, **dict(zip(GRADS, outs[2:] + sums)), work=work)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(outs + sums, list(forward(lq, cfg, d)) + list(backward(lq, cfg, d))):
+        assert torch.equal(a, b)
+
+
 def test_offsets_that_do_not_rise_stay_in_bounds(lq):
     """What comes out then is not defined; nothing outside the rows is touched."""
     M, D = 40, 72
