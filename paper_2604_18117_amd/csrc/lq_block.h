@@ -108,10 +108,11 @@ struct Raw {
     }
 };
 template <int VEC, bool ANY>
-__device__ __forceinline__ void read(const float* row, int at, int dim, float (&f)[VEC])
+__device__ __forceinline__ void read(const float* row, int at, int dim, float (&f)[VEC], bool whole = false)  // whole: the row does not end before or among them
 {
     Raw<float, VEC, ANY> r;
-    r.fetch_end(row, at, dim);
+    if (whole) r.fetch(row + at);
+    else r.fetch_end(row, at, dim);
     r.get(f);
 }
 
@@ -226,31 +227,31 @@ __device__ __forceinline__ float normalise(int kind, float (&x)[NV][VEC], const 
 
 // a, b of the header, and shift, of sequence s, at a column
 template <int VEC, bool ANY>
-__device__ __forceinline__ void factor_a(const BlockTensors& t, int at, int dim, int s, float (&a)[VEC])
+__device__ __forceinline__ void factor_a(const BlockTensors& t, int at, int dim, int s, float (&a)[VEC], bool whole = false)
 {
     float w[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) a[i] = 1.0f;
     if (t.scale.p) {
-        read<VEC, ANY>(t.scale.p + s * t.scale.ld, at, dim, w);
+        read<VEC, ANY>(t.scale.p + s * t.scale.ld, at, dim, w, whole);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a[i] = 1.0f + w[i];
     }
     if (t.w_pre) {
-        read<VEC, ANY>(t.w_pre, at, dim, w);
+        read<VEC, ANY>(t.w_pre, at, dim, w, whole);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) a[i] *= w[i];
     }
 }
 template <int VEC, bool ANY>
-__device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int dim, int s, float (&b)[VEC])
+__device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int dim, int s, float (&b)[VEC], bool whole = false)
 {
     float w[VEC];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) b[i] = 1.0f;
-    if (t.gate.p) read<VEC, ANY>(t.gate.p + s * t.gate.ld, at, dim, b);
+    if (t.gate.p) read<VEC, ANY>(t.gate.p + s * t.gate.ld, at, dim, b, whole);
     if (t.w_post) {
-        read<VEC, ANY>(t.w_post, at, dim, w);
+        read<VEC, ANY>(t.w_post, at, dim, w, whole);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) b[i] *= w[i];
     }

@@ -39,11 +39,11 @@ __global__ void __launch_bounds__(THREADS) block_fwd_kernel(BlockArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int at = c.at + v * c.step;
-            factor_a<VEC, ANY>(t, at, a.dim, s, fa[v]);
-            factor_b<VEC, ANY>(t, at, a.dim, s, fb[v]);
+            factor_a<VEC, ANY>(t, at, a.dim, s, fa[v], v < NV - 1);
+            factor_b<VEC, ANY>(t, at, a.dim, s, fb[v], v < NV - 1);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) fs[v][i] = 0.0f;
-            if (t.shift.p) read<VEC, ANY>(t.shift.p + s * t.shift.ld, at, a.dim, fs[v]);
+            if (t.shift.p) read<VEC, ANY>(t.shift.p + s * t.shift.ld, at, a.dim, fs[v], v < NV - 1);
         }
         for (; row < end; ++row) {
             float h[NV][VEC], y[NV][VEC];

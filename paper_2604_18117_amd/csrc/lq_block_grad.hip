@@ -55,9 +55,9 @@ __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
         }
         for (int o = threadIdx.x * VEC; o < padded; o += blockDim.x * VEC) {
             float f[VEC];
-            factor_a<VEC, ANY>(t, o, a.dim, s, f);
+            factor_a<VEC, ANY>(t, o, a.dim, s, f, o + VEC <= a.dim);
             Raw<float, VEC, false>::put(la + o, f);
-            factor_b<VEC, ANY>(t, o, a.dim, s, f);
+            factor_b<VEC, ANY>(t, o, a.dim, s, f, o + VEC <= a.dim);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) f[i] = ANY && i >= a.dim - o ? 0.0f : f[i];
             Raw<float, VEC, false>::put(lb + o, f);
