@@ -565,21 +565,22 @@ static hipError_t w4_fwd_per(const W4Args& a, int per, int waves, hipStream_t s)
 // Rows and channels of a workgroup, and the wavefronts that share K out.  bf16: one tile and up to 16 rows, from more than 16 rows on 32, with two tiles (what is unpacked and what is read of X are
 // shared) where one would leave more than two workgroups to a compute unit, three where two would leave more than the three that it holds (us, one / two tiles: 64 x 2240 -> 11200 16.5 / 13.4,
 // 64 x 1152 -> 1152 4.3 / 5.1; two / three: 64 x 4608 -> 13440 27.3 / 24.0, 64 x 2240 -> 11200 13.4 / 13.9).  Eight wavefronts where there is a workgroup to a compute unit at most, four elsewhere (us, 8 / 4:
-// 16 x 4608 -> 2240 5.2 / 5.9, 64 x 2240 -> 11200 16.6 / 12.9).  fp32 rows, which are split into three terms for every workgroup and take three times the LDS: 16 rows, and up to three tiles that
-// leave one workgroup of eight wavefronts to a compute unit (us, against one tile and four: 16 x 2240 -> 11200 9.5 / 13.3, 6 x 3992 -> 5760 8.7 / 11.4, 64 x 1152 -> 1152 6.1 / 7.0); where more than
-// three would do that, two or three and four wavefronts (33 x 1152 -> 6912, two / three: 8.7 / 9.8; 64 x 2240 -> 11200 29.7 / 26.5).
+// 16 x 4608 -> 2240 5.2 / 5.9, 64 x 2240 -> 11200 16.6 / 12.9).  fp32 rows, which are split into three terms for every workgroup and take three times the LDS: 16 rows, and up to four tiles that
+// leave one workgroup of eight wavefronts to a compute unit (us, against one tile and four: 16 x 2240 -> 11200 9.5 / 13.3, 6 x 3992 -> 5760 8.7 / 11.4, 64 x 1152 -> 1152 6.1 / 7.0; against two and four, 16 x 2240 -> 15000 10.8 / 13.7, 64 x 1152 -> 3456 7.5 / 8.4); where more than
+// four would do that, two or three and four wavefronts (33 x 1152 -> 6912, two / three: 8.7 / 9.8; 64 x 2240 -> 11200 29.7 / 26.5).
 template <bool F32>
 static hipError_t w4_fwd_rows(const W4Args& a, int per, hipStream_t s)
 {
     const int MT = !F32 && a.M > 16 ? 2 : 1;
     const int64_t groups = a.tiles * ((a.M + 16 * MT - 1) / (16 * MT));
     int NT = 1;
-    if (F32) NT = a.blocks >= 8 && groups <= 768 ? (int)((groups + 255) / 256) : groups <= 768 ? 1 : groups <= 1536 ? 2 : 3;
+    if (F32) NT = a.blocks >= 8 && groups <= 1024 ? (int)((groups + 255) / 256) : groups <= 768 ? 1 : groups <= 1536 ? 2 : 3;
     else if (MT == 2) NT = groups <= 512 ? 1 : groups <= 1536 ? 2 : 3;
     const int most = (groups + NT - 1) / NT <= 256 ? 8 : 4, waves = a.blocks < most ? a.blocks : most;
     if constexpr (F32) {
         if (NT == 1) return w4_fwd_per<F32, 1, 1>(a, per, waves, s);
-        return NT == 2 ? w4_fwd_per<F32, 1, 2>(a, per, waves, s) : w4_fwd_per<F32, 1, 3>(a, per, waves, s);
+        if (NT == 2) return w4_fwd_per<F32, 1, 2>(a, per, waves, s);
+        return NT == 3 ? w4_fwd_per<F32, 1, 3>(a, per, waves, s) : w4_fwd_per<F32, 1, 4>(a, per, waves, s);
     } else {
         if (MT == 1) return w4_fwd_per<F32, 1, 1>(a, per, waves, s);
         if (NT == 1) return w4_fwd_per<F32, 2, 1>(a, per, waves, s);

@@ -101,10 +101,10 @@ def test_sizes(lq, M, K, N, group, x, y):
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("M,K,N,x", [(40, 140, 3003, "bf16"), (40, 140, 10007, "bf16"), (40, 140, 25001, "bf16"), (70, 1100, 1000, "bf16"), (20, 1100, 2503, "f32"), (20, 1100, 5007, "f32"),
+@pytest.mark.parametrize("M,K,N,x", [(40, 140, 3003, "bf16"), (40, 140, 10007, "bf16"), (40, 140, 25001, "bf16"), (70, 1100, 1000, "bf16"), (20, 1100, 2503, "f32"), (20, 1100, 5007, "f32"), (20, 1100, 7007, "f32"), (3, 1100, 14333, "f32"),
                                      (20, 140, 5007, "f32"), (20, 140, 10007, "f32"), (20, 140, 15001, "f32"), (16, 1100, 4090, "f32")])
 def test_forms(lq, M, K, N, x, group):
-    """One, two and three tiles to a workgroup, the last one with fewer, by four and eight wavefronts."""
+    """One to four tiles to a workgroup, the last one with fewer, by four and eight wavefronts."""
     codes, scales, X, dY, bias = make(M, K, N, group, x, "f32", seed=N)
     cfg = lq.make_w4_config(N, K, group, x, "f32")
     check_all(lq, cfg, lq.lq_w4_pack_codes(cfg, codes, scales), codes, scales, X, dY, bias)
