@@ -618,6 +618,7 @@ hipError_t launch_w4_fwd(const lq_w4_config* c, const uint8_t* packed, const voi
 static int w4_bwd_splits(const W4Shape& s, int64_t M)
 {
     const int64_t others = (int64_t)s.blocks * ((M + 15) / 16), want = 256 / others, waves = w4_bwd_waves(s.per), most = ((s.tiles + 1) / 2 + waves - 1) / waves;
+    if (most <= 2) return 1;  // (two steps of a wavefront cost less than a second launch: 3 x 359 -> 256 4.5 us for 6.2)
     return (int)(want < 1 ? 1 : want < most ? want : most);
 }
 size_t w4_work_bytes(const lq_w4_config* c, int64_t M)
