@@ -481,7 +481,7 @@ lq_status lq_w4_fwd(const lq_w4_config *cfg, const void *packed, size_t packed_b
 
 /* Bytes of the gradient's workspace (may be 0); no less for more rows.  Host-only. */
 lq_status lq_w4_work_sizes(const lq_w4_config *cfg, int64_t M, size_t *work_bytes);
-/* work: 256-byte aligned; may be NULL where lq_w4_work_sizes reports 0. */
+/* work: 256-byte aligned; may be NULL where lq_w4_work_sizes reports 0.  dX must not overlap dY. */
 lq_status lq_w4_bwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *dY, int64_t lddy, void *dX, int64_t lddx, int64_t M, void *work,
                     size_t work_bytes, void *stream);
 
@@ -528,7 +528,7 @@ lq_status lq_block_work_sizes(const lq_block_config *cfg, int64_t M, int32_t S, 
        dshift[s] = sum dx ,  dscale[s] = w_pre sum dx n ,  dgate[s] = w_post sum G p    over the rows of s (zeros for a sequence without rows)
        dw_pre = sum dx (1 + scale[s]) n ,  dw_post = sum G gate[s] p                     over all rows of sequences
    ho: the forward's h'.  dho or dx may be NULL (zero): without dx, h' is not looked at; without y, dy, dgate and dw_post must be NULL.  dh, dy and every gradient of modulation and
-   weights may be NULL.  dh may be dho, dy may be dx (same pointer and stride).  work: 256-byte aligned.  Sums are fixed in their order: repeated calls give identical bits. */
+   weights may be NULL.  dh may be dho, dy may be dx (same pointer and stride); outputs must not overlap otherwise.  work: 256-byte aligned.  Sums are fixed in their order: repeated calls give identical bits. */
 typedef struct {
     void *dh;
     int64_t lddh;
