@@ -269,6 +269,7 @@ static inline BlockShape block_shape(int dim, bool any)
 {
     const int vectors = (dim + 3) / 4;
     BlockShape s{any, 0, (vectors + 319) / 320};
+    if (s.W > 8) s.W = 16;  // (1024 threads have 128 registers each, of which every vector takes some 30)
     s.NV = (vectors + 64 * s.W - 1) / (64 * s.W);
     const int more = (vectors + 64 * (s.W + 1) - 1) / (64 * (s.W + 1));
     if (s.W > 1 && s.W < 8 && vectors * 10 < s.NV * 64 * s.W * 9 && more >= 3 && more * (s.W + 1) < s.NV * s.W) s.NV = more, ++s.W;

@@ -105,7 +105,7 @@ static void block_fwd_launch(BlockArgs a, int W, hipStream_t s)
 template <typename TH, typename TY, int NV, bool ANY, bool POST>
 static void block_fwd_run(const BlockArgs& a, int W, hipStream_t s)
 {
-    if constexpr (NV == 5)
+    if constexpr (NV == 3 || NV == 4)
         if (W > 8) return block_fwd_launch<TH, TY, NV, ANY, POST, true, 1024>(a, W, s);
     if constexpr (NV >= 3)
         if (W > 1) return block_fwd_launch<TH, TY, NV, ANY, POST, true, 512>(a, W, s);

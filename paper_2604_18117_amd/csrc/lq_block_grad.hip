@@ -329,7 +329,7 @@ static hipError_t block_bwd_launch(const BlockArgs& a, hipStream_t s)
 template <typename TH, typename TY, int NV, int TENSORS, bool POST>
 static hipError_t block_bwd_run(const BlockArgs& a, hipStream_t s)
 {
-    if constexpr (NV == 5)
+    if constexpr (NV == 3 || NV == 4)
         if (a.waves > 8) return block_bwd_launch<TH, TY, NV, TENSORS, POST, true, 1024>(a, s);
     if constexpr (NV >= 3)
         if (a.waves > 1) return block_bwd_launch<TH, TY, NV, TENSORS, POST, true, 512>(a, s);
