@@ -259,20 +259,21 @@ __device__ __forceinline__ void factor_b(const BlockTensors& t, int at, int dim,
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Vectors of four columns to a lane (up to five), and wavefronts to a row: the fewest, or one more where lanes would be idle otherwise (us, 16384 rows of 2240, fp32 stream and both norms / bf16
-// and one: two wavefronts with five vectors, 12 % of them past the end, 102.8 / 67.6, three with three 93.8 / 63.9; 8192 rows of 4608: four with five 66.0, six with three 70.7)
+// Vectors of four columns to a lane (up to five), and wavefronts to a row: the fewest; `wide` (forward, small batches): one more where lanes would be idle otherwise (us, 16384 rows of 2240, fp32 stream and both norms / bf16
+// and one: two wavefronts with five vectors, 12 % of them past the end, 102.8 / 67.6, three with three 93.8 / 63.9; 8192 rows of 4608: four with five 66.0, six with three 70.7;
+// gradient of 8192 rows of 2240: two with five 67.0, three with three 73.7, of 500 24.0 / 21.2)
 struct BlockShape {
     bool any;
     int NV, W;
 };
-static inline BlockShape block_shape(int dim, bool any)
+static inline BlockShape block_shape(int dim, bool any, bool wide)
 {
     const int vectors = (dim + 3) / 4;
     BlockShape s{any, 0, (vectors + 319) / 320};
     if (s.W > 8) s.W = 16;  // (1024 threads have 128 registers each, of which every vector takes some 30)
     s.NV = (vectors + 64 * s.W - 1) / (64 * s.W);
     const int more = (vectors + 64 * (s.W + 1) - 1) / (64 * (s.W + 1));
-    if (s.W > 1 && s.W < 8 && vectors * 10 < s.NV * 64 * s.W * 9 && more >= 3 && more * (s.W + 1) < s.NV * s.W) s.NV = more, ++s.W;
+    if (wide && s.W > 1 && s.W < 8 && vectors * 10 < s.NV * 64 * s.W * 9 && more >= 3 && more * (s.W + 1) < s.NV * s.W) s.NV = more, ++s.W;
     return s;
 }
 static inline bool fits(const void* p, int64_t ld, int64_t rows, int bytes, int elem) { return (uintptr_t)p % bytes == 0 && (rows < 2 || ld * elem % bytes == 0); }

@@ -131,7 +131,7 @@ static void block_fwd_types(const BlockArgs& a, const BlockShape& sh, hipStream_
 }
 hipError_t launch_block_fwd(const lq_block_config* c, const BlockTensors& t, int64_t M, hipStream_t s)
 {
-    const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M));
+    const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M), true);
     const BlockArgs a = block_args(c, t, M);
     if (c->h_dtype == LQ_BF16) block_fwd_types<__bf16, __bf16>(a, sh, s);
     else if (c->y_dtype == LQ_BF16) block_fwd_types<float, __bf16>(a, sh, s);

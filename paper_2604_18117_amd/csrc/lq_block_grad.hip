@@ -303,7 +303,7 @@ static int block_bwd_groups(int W, int chunk) { return std::min(W > 3 ? 1 : 8 / 
 static int block_bwd_chunk(const lq_block_config* c, int64_t M)
 {
     if (M <= FEW_ROWS) return 1;
-    const int W = block_shape(c->dim, false).W, groups = block_bwd_groups(W, 8), workgroups = 256 * (W * groups > 4 ? 1 : 2);
+    const int W = block_shape(c->dim, false, false).W, groups = block_bwd_groups(W, 8), workgroups = 256 * (W * groups > 4 ? 1 : 2);
     return std::max((int)((M + workgroups - 1) / workgroups), std::min(groups, 4));
 }
 // (no chunk leaves more than FEW_ROWS parts and one for each sequence: a workspace serves smaller batches, too)
@@ -363,7 +363,7 @@ hipError_t launch_block_bwd(const lq_block_config* c, const BlockTensors& t, int
     a.part = sums ? (float*)work : nullptr;
     hipError_t e = hipSuccess;
     if (M > 0) {
-        const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M));
+        const BlockShape sh = block_shape(c->dim, !block_fours(c, t, M), M <= FEW_ROWS);
         a.waves = sh.W;
         e = c->h_dtype == LQ_BF16   ? block_bwd_types<__bf16, __bf16>(a, sh, s)
             : c->y_dtype == LQ_BF16 ? block_bwd_types<float, __bf16>(a, sh, s)
