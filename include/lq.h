@@ -527,6 +527,7 @@ lq_status lq_block_work_sizes(const lq_block_config *cfg, int64_t M, int32_t S, 
        dh = res_scale G ,  dy = (post's gradient at y) (G gate[s] w_post)
        dshift[s] = sum dx ,  dscale[s] = w_pre sum dx n ,  dgate[s] = w_post sum G p    over the rows of s (zeros for a sequence without rows)
        dw_pre = sum dx (1 + scale[s]) n ,  dw_post = sum G gate[s] p                     over all rows of sequences
+   (The modulation of a sequence without rows is not used, whatever it holds.)
    ho: the forward's h'.  dho or dx may be NULL (zero): without dx, h' is not looked at; without y, dy, dgate and dw_post must be NULL.  dh, dy and every gradient of modulation and
    weights may be NULL.  dh may be dho, dy may be dx (same pointer and stride); outputs must not overlap otherwise.  work: 256-byte aligned.  Sums are fixed in their order: repeated calls give identical bits. */
 typedef struct {

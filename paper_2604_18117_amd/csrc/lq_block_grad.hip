@@ -214,7 +214,8 @@ __device__ __forceinline__ void parts_of(const BlockArgs& a, int s, int& c0, int
 //     dshift = sum dx ;  dscale = w_pre sum dx n ;  dgate = w_post sum G p
 // `team` wavefronts share the parts of a sequence out and are joined in a tree; the workgroup's teams take the sequences from blockIdx.z on in turn.  FUSED (one workgroup sees all sequences): also
 //     dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
-// Otherwise raw: the last two sums without the weights, for block_weight_sums.
+// Otherwise raw: the last two sums without the weights, for block_weight_sums.  The modulation of a sequence without rows, and the weights beside it, are not used: whatever they hold, it adds nothing
+// (times a sum of zero, an infinity would be no number).
 template <bool FUSED, int COLS>
 __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float* raw)
 {
@@ -230,9 +231,11 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
     for (int base = blockIdx.z * teams; base < t.S; base += gridDim.z * teams) {
         const int s = base + wave / team;
         float y = 0.0f;
+        bool rows = false;
         if (s < t.S && col < a.dim) {
             int c0, c1;
             parts_of(a, s, c0, c1);
+            rows = c0 < c1;
             const float* p = a.part + (size_t)s * 3 * a.dim + k * a.dim + col;
 #pragma unroll 8
             for (int i = c0 + member * (64 / COLS) + lane / COLS; i < c1; i += team * (64 / COLS)) y += p[(size_t)i * 3 * a.dim];
@@ -249,9 +252,9 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
             y = sh[wave][lane];
         }
         if (member == 0 && lane < COLS && s < t.S && col < a.dim) {
-            if (o.p) o.p[s * o.ld + col] = w ? y * w[col] : y;
+            if (o.p) o.p[s * o.ld + col] = rows && w ? y * w[col] : y;
             if (FUSED) {
-                const float g = f.p ? f.p[s * f.ld + col] : k == 1 ? 0.0f : 1.0f;
+                const float g = rows && f.p ? f.p[s * f.ld + col] : k == 1 ? 0.0f : 1.0f;
                 total = fmaf(k == 1 ? 1.0f + g : g, y, total);
             } else if (raw && k) {
                 raw[((size_t)s * 2 + k - 1) * a.dim + col] = y;
@@ -274,15 +277,17 @@ __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const flo
 {
     __shared__ float sh[16][64];
     const BlockTensors& t = a.t;
-    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = blockIdx.x * 64 + lane;
     const lq_mod& f = k == 0 ? t.scale : t.gate;
     float* out = k == 0 ? t.dw_pre : t.dw_post;
     float y = 0.0f;
     if (col < a.dim && out)
 #pragma unroll 4
         for (int s = wave; s < t.S; s += 16) {
-            const float u = raw[((size_t)s * 2 + k) * a.dim + col];
-            y += f.p ? u * (k == 0 ? 1.0f + f.p[s * f.ld + col] : f.p[s * f.ld + col]) : u;
+            int c0, c1;
+            parts_of(a, s, c0, c1);
+            const float u = raw[((size_t)s * 2 + k) * a.dim + col], g = f.p ? f.p[s * f.ld + col] : k == 0 ? 0.0f : 1.0f;
+            y += c0 < c1 ? u * (k == 0 ? 1.0f + g : g) : 0.0f;
         }
     sh[wave][lane] = y;
     __syncthreads();

@@ -317,3 +317,36 @@ def test_offsets_that_do_not_rise_stay_in_bounds(lq):
         assert (big[[0, -1]] == 7.0).all()
         backward(lq, cfg, d, dy=big[1:-1], dgate=sums[1:-1])
         assert (big[[0, -1]] == 7.0).all() and (sums[[0, -1]] == 7.0).all()
+
+
+@pytest.mark.parametrize("M,offsets", [
+    (12, [0, 5, 5, 12]), (4000, [0, 1000, 1000, 4000, 4000]),                       # weights' sums with those of the sequences
+    (390, [3 * (i // 2) for i in range(261)]), (3000, [30 * (i - i % 3) // 3 for i in range(301)]),  # ... in a launch of their own
+    (9, [0, 0, 9, 9, 9]), (0, [0, 0, 0])])
+@pytest.mark.parametrize("D", [40, 1153])
+def test_modulation_of_sequences_without_rows_is_not_used(lq, D, M, offsets):
+    """Rows of modulation that belong to nothing (unused places of a batch of fixed size) may hold anything: their own gradients are zeros, and no other value sees them."""
+    d = make(M, D, offsets, "f32", "bf16")
+    cfg = config(lq, d, "rms", "layer")
+    empty = (d["offsets"][1:] == d["offsets"][:-1])
+    assert empty.any()
+    want = [list(forward(lq, cfg, d)), list(backward(lq, cfg, d))]
+    e = {k: v.clone() if k in ("gate", "scale", "shift") else v for k, v in d.items()}
+    for k, v in (("gate", float("inf")), ("scale", float("nan")), ("shift", float("nan"))):
+        e[k][empty] = v
+    got = [list(forward(lq, cfg, e)), list(backward(lq, cfg, e))]
+    inside = slice(offsets[0], offsets[-1])
+    for a, b in zip(got[0] + got[1][:2], want[0] + want[1][:2]):
+        assert torch.equal(a[inside], b[inside])
+    for k, a, b in zip(GRADS[2:], got[1][2:], want[1][2:]):
+        assert torch.equal(a, b), k
+    for t in got[1][2:5]:
+        assert (t[empty] == 0).all()
+
+
+def test_gradients_of_sequences_without_rows_are_zeros_whatever_the_weights(lq):
+    d = make(20, 72, [0, 8, 8, 20], "f32", "f32")
+    cfg = config(lq, d, "rms", "layer")
+    d["w_post"][3], d["w_pre"][5] = float("inf"), float("nan")
+    for t in backward(lq, cfg, d)[2:5]:
+        assert (t[1] == 0).all()
