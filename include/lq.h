@@ -545,7 +545,8 @@ lq_status lq_block_norm_bwd(const lq_block_config *cfg, const void *ho, int64_t 
 /* ---- AdamW step over many tensors --------------------------------------------------------------------------------
        g = grad_scale grad ;  m = beta1 m + (1 - beta1) g ;  v = beta2 v + (1 - beta2) g^2
        p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
-   in fp32, rounded once more where p is bf16 (states: every operation rounded by itself).  A launch for every 120 tensors.
+   in fp32, rounded once more where p is bf16 (states: every operation rounded by itself); lr weight_decay p is taken off p with the step, so that no decay is too small for the factor.
+   A launch for every 120 tensors.
    state_bits = 8: m and the root of v are E4M3 elements (a byte each) times a power of two for each 256 consecutive values of a tensor, the smallest with which the largest of them is
    448 or below (1 for zeros).  They are rounded up or down at random with their mean kept, by numbers that depend on seed, t and the value's place (tensors one after another, each
    from a multiple of 256 on), so that a step repeated on the same state gives the same bits; a root above zero is not rounded to zero.  A gradient that is not finite makes the states of its 256

@@ -22,6 +22,22 @@ struct Entry {
     uint32_t n;
 };
 constexpr uint32_t NONE = 0xFFFFFFFFu;
+// 1 - lr wd as keep - rest: in fp32 by itself it has none of a decay below 2^-25, and 1e-6 as 1.013e-6, so that what keep lacks is taken off p with the step.  (keep is below the true factor and rest
+// below zero: of an infinite parameter both are infinities of one sign, and it stays.  rest is zero where nothing decays.)
+struct Decay {
+    float keep, rest;
+};
+__host__ __device__ static inline Decay decay_of(float decay)
+{
+    Decay d = {1.0f - decay, 0.0f};
+    if (decay == 0.0f) return d;
+    d.rest = decay - (1.0f - d.keep);
+    if (d.rest >= 0.0f && d.keep > 0.0f) {
+        d.keep = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, d.keep) - 1u);  // (the number below)
+        d.rest = decay - (1.0f - d.keep);
+    }
+    return d;
+}
 template <int CAP>
 struct AdamwArgs {
     Entry tensors[CAP];
@@ -36,6 +52,7 @@ struct AdamwArgs {
     const int32_t* step_dev;
     double beta1, beta2;
     float b1, c1, b2, c2, eps, wd, lr, correct1, correct2;  // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    Decay decay;            // of lr
     uint32_t seed, step;
 };
 static_assert(sizeof(AdamwArgs<TENSORS>) <= 4096, "kernel arguments");
@@ -183,7 +200,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs<CAP> a)
     void* const pp = a.p + (e.p + o) * sizeof(TP);
     float *const master = e.master != NONE ? a.master + (e.master + o) : nullptr, *const scales = a.scales + (e.scales + 2 * (size_t)at);
     void *const pm = a.m + (e.m + o) * (EIGHT ? 1 : 4), *const pv = a.v + (e.v + o) * (EIGHT ? 1 : 4);
-    float p[4], g[4], m[4], v[4], root[4];
+    float p[4], g[4], m[4], v[4], root[4], step_of[4];
     uint32_t wm = 0, wv = 0;
     float sm = 1.0f, sv = 1.0f;
     if (master) read4<float>(master, i, n, whole, p);
@@ -205,7 +222,9 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs<CAP> a)
         correct1 = (float)(1.0 / (1.0 - power(a.beta1, step)));
         correct2 = (float)sqrt(1.0 / (1.0 - power(a.beta2, step)));
     }
-    const float lr = a.lr_dev ? *a.lr_dev : a.lr, gs = a.grad_scale ? *a.grad_scale : 1.0f, keep = 1.0f - lr * a.wd, rate = lr * correct1;
+    const float lr = a.lr_dev ? *a.lr_dev : a.lr, gs = a.grad_scale ? *a.grad_scale : 1.0f, rate = lr * correct1;
+    Decay d = a.decay;
+    if (a.lr_dev) d = decay_of(lr * a.wd);
     if constexpr (EIGHT) {
         e4m3_values(wm, m);
         e4m3_values(wv, v);
@@ -221,8 +240,14 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwArgs<CAP> a)
         m[k] = m[k] * a.b1 + g[k] * a.c1;
         v[k] = v[k] * a.b2 + g[k] * a.c2 * g[k];
         root[k] = nearest_root(v[k]);
-        p[k] = fmaf(p[k], keep, -(m[k] * rate) * __builtin_amdgcn_rcpf(fmaf(root[k], correct2, a.eps)));
+        step_of[k] = (m[k] * rate) * __builtin_amdgcn_rcpf(fmaf(root[k], correct2, a.eps));
     }
+    if (__builtin_amdgcn_readfirstlane(__float_as_int(d.rest)) != 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) step_of[k] = fmaf(p[k], d.rest, step_of[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) p[k] = fmaf(p[k], d.keep, -step_of[k]);
     if (master) write4<float>(master, i, n, whole, p);
     write4<TP>(pp, i, n, whole, p);
     if constexpr (EIGHT) {
@@ -284,6 +309,7 @@ static hipError_t adamw_run(const lq_adamw_config* c, const lq_adamw_tensor* ten
     a.eps = (float)c->eps;
     a.wd = (float)c->weight_decay;
     a.lr = (float)x->lr;
+    a.decay = decay_of(a.lr * a.wd);
     a.step = (uint32_t)x->step;
     double p1 = 1.0, p2 = 1.0, q1 = c->beta1, q2 = c->beta2;
     for (uint32_t t = a.step; t; t >>= 1, q1 *= q1, q2 *= q2)

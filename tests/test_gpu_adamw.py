@@ -281,3 +281,38 @@ def test_values_past_32_bits(lq, bits):
         for k, (t, want) in enumerate(((m, 0.1 * grad.double()), (v, (0.001 * grad.double().square()).sqrt()))):
             got = t[-end:].double() * last[:, k]
             assert (got - want).abs().max() <= 2.0 ** -3 * want.abs().max() * 1.01
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr,decay", [(1e-4, 0.01), (1e-5, 0.01), (3e-4, 0.1), (1e-3, 1e-5), (1e-2, 0.5)])
+def test_weight_decay_keeps_small_factors(lq, lr, decay, bits):
+    """lr weight_decay down to 1e-8: what is taken from a parameter is that part of it, to the bits of fp32, before the one rounding of the result.  lr and weight_decay are rounded, and their
+    product, and its product with the parameter (4 e, e = 2^-24); the step's own part is off by 14 e of itself and 5 e of the sizes that its average is made of."""
+    e, n, t = 2.0 ** -24, 70001, 7
+    cfg = lq.make_adamw_config("f32", "f32", bits, weight_decay=decay)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    for device_lr in (False, True):
+        for size in (0.0, 1e-3):
+            p, g = torch.randn(n, generator=gen, device="cuda"), torch.randn(n, generator=gen, device="cuda") * size
+            m, v, scales = lq.adamw_states(cfg, p)
+            old = p.double()
+            lq.lq_adamw_step(cfg, [p], [g], [m], [v], torch.full((1,), lr, device="cuda") if device_lr else lr, t, scales=None if scales is None else [scales])
+            mean = 0.1 * g.double() / (1 - 0.9 ** t)
+            step = lr * mean / ((0.001 * g.double().square() / (1 - 0.999 ** t)).sqrt() + 1e-8)
+            want = old - lr * decay * old - step
+            off = ref.SLACK * e * (4 * lr * decay * old.abs() + 20 * step.abs())
+            bad = ~((p.double() - want).abs() <= off + e * (want.abs() + off))
+            assert not bad.any(), (device_lr, size, int(bad.sum()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("decay", [0.0, 0.01])
+def test_parameters_that_are_infinite_stay_so(lq, decay, bits):
+    """Masked places of a parameter, with gradients of zero."""
+    cfg = lq.make_adamw_config("f32", "f32", bits, weight_decay=decay)
+    p = torch.ones(300, device="cuda")
+    p[5], p[290] = float("-inf"), float("inf")
+    m, v, scales = lq.adamw_states(cfg, p)
+    lq.lq_adamw_step(cfg, [p], [torch.zeros_like(p)], [m], [v], 1e-2, 1, scales=None if scales is None else [scales])
+    assert float(p[5]) == float("-inf") and float(p[290]) == float("inf") and torch.isfinite(p).sum() == 298
