@@ -103,8 +103,9 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)  // of the bits of numb
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)max(t[0], t[1]));
 }
 
-// The nearest number to the root of x >= 0: an estimate of 1 / sqrt(x) and its half, improved once together, then the root by what is left (each step by fused operations; 9 instructions, the
-// library's 15).  Outside the estimate's range the library's.
+// The nearest number to the root of x >= 0 by Goldschmidt's iteration with a last step by the residual: from an estimate y of 1 / sqrt(x), s = x y and h = y / 2 go to the root and to half of its reciprocal
+// together (e = 1/2 - h s; s += s e; h += h e), then s += (x - s^2) h, each step by fused operations (9 instructions, the library's 15).  Outside the estimate's range the
+// library's.
 __device__ __forceinline__ float nearest_root(float x)
 {
     const float y = __builtin_amdgcn_rsqf(x);

@@ -316,3 +316,49 @@ def test_parameters_that_are_infinite_stay_so(lq, decay, bits):
     m, v, scales = lq.adamw_states(cfg, p)
     lq.lq_adamw_step(cfg, [p], [torch.zeros_like(p)], [m], [v], 1e-2, 1, scales=None if scales is None else [scales])
     assert float(p[5]) == float("-inf") and float(p[290]) == float("inf") and torch.isfinite(p).sum() == 298
+
+
+def roots_at_a_step(count, seed, t, c2):
+    """fp32 gradients g for which the cut part of the nearest root of v = fl(fl(g c2) g), beside the random number that its place is rounded with, decides by its last bit: (g, codes that
+    a right root gives, how many of them go up).  In every second place the root's lowest 20 bits and the random number make 2^20, in the others 2^20 - 1."""
+    _, bits = ref.random_bits(seed, t, count)
+    f, i32 = torch.float32, torch.int32
+    gen = torch.Generator().manual_seed(seed)
+    top = torch.randint(0, 8, (count,), generator=gen)           # mantissa's first three bits
+    e = torch.randint(-5, 8, (count,), generator=gen)            # roots in [2^-5, 2^8): E4M3's normal numbers
+    up = torch.arange(count) % 2 == 0
+    low = (2 ** 20 - bits - (~up).long()).clamp(min=0)
+    low = torch.where(low > 2 ** 20 - 1, torch.zeros_like(low), low)
+    root = (((e + 127) << 23) | (top << 20) | low).to(i32).view(f)
+    c = torch.tensor(c2, dtype=f)
+    near = (root.double() / float(c) ** 0.5).to(f)
+    g, hit = torch.zeros(count, dtype=f), torch.zeros(count, dtype=torch.bool)
+    for k in range(-6, 7):  # the gradient whose v has this nearest root
+        x = (near.view(i32) + k).view(f)
+        r = (x * c * x).double().sqrt().to(f)
+        found = (r == root) & ~hit
+        g, hit = torch.where(found, x, g), hit | found
+    g = torch.where(hit, g, torch.ones_like(g))
+    r = (g * c * g).double().sqrt().to(f)
+    return g, r, bits, hit, up
+
+
+@pytest.mark.parametrize("size", [0, -40, 40, -52, 52])
+@pytest.mark.parametrize("c2", [1.0, 0.25 + 2.0 ** -7, 0.001])
+def test_roots_are_the_nearest_numbers(lq, c2, size):
+    """The held root of v where its last bit decides which way it is rounded: a root that is one bit too small is seen in one half of the places, one that is too large in the other.  Gradients
+    times 2^size, which the blocks' scales take up."""
+    blocks, seed, t = 2000, 77, 3
+    n = blocks * 256
+    cfg = lq.make_adamw_config("f32", "f32", 8, beta1=0.0, beta2=1.0 - c2, seed=seed)
+    c2 = 1.0 - cfg.beta2
+    g, root, bits, hit, up = roots_at_a_step(n, seed, t, c2)
+    assert float(hit.double().mean()) > 0.4 and float((hit & up).double().mean()) > 0.15 and float((hit & ~up).double().mean()) > 0.15
+    last = g.view(blocks, 256)[:, -1]
+    last.copy_((torch.full((blocks,), 448.0, dtype=torch.float64) / c2 ** 0.5 * 0.99).float())  # a large value: every block's scale is 1
+    root = (g * torch.tensor(c2, dtype=torch.float32) * g).double().sqrt().float()
+    p = torch.zeros(n, device="cuda")
+    m, v, scales = lq.adamw_states(cfg, p)
+    lq.lq_adamw_step(cfg, [p], [g.cuda() * 2.0 ** size], [m], [v], 1e-3, t, scales=[scales])
+    assert (scales[:, 1] == 2.0 ** size).all()
+    assert torch.equal(v.float().cpu().double(), ref.e4m3_random(root, bits))
