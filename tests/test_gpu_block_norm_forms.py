@@ -1,0 +1,107 @@
+"""Gradients of the norms before and after a block where tensors are missing or not wanted, and where rows cannot be read four values at a time, at widths of one to five vectors a
+lane and of several wavefronts: the kernels that these calls take are others than those of whole calls.  Against the plain 64-bit implementation."""
+import ctypes as C
+
+import pytest
+import torch
+
+from tests import blocks_ref as ref
+from tests.test_gpu_block_norm import EPS, GRADS, backward, check_all, config, forward, make
+
+pytestmark = pytest.mark.gpu
+TYPES = [("bf16", "bf16"), ("f32", "bf16"), ("f32", "f32")]
+WIDTHS = [600, 883, 1021, 1152, 1153, 1279, 2239, 2240, 4607]
+MISSING = [("dho",), ("dx",), ("y",), ("y", "dho"), ("y", "dx")]
+
+
+@pytest.fixture(scope="module")
+def lq():
+    from paper_2604_18117_amd import binding
+    return binding
+
+
+def cuts(M):
+    return [2, M // 4, M // 4, M // 2 + 1, M - 3]
+
+
+def gradients(d, post, pre, alpha):
+    return ref.block_bwd(d["h"], d["y"], d["offsets"], d["gate"], d["scale"], d["w_post"], d["w_pre"], d["dho"], d["dx"], post, pre, EPS, alpha, d["h"].dtype,
+                         d["yt"])
+
+
+@pytest.mark.parametrize("stream,branch", TYPES)
+@pytest.mark.parametrize("post,pre", [("none", "layer"), ("rms", "layer"), ("layer", "rms")])
+@pytest.mark.parametrize("M", [50, 1300])
+@pytest.mark.parametrize("D", WIDTHS)
+def test_gradients_without_a_tensor(lq, D, M, post, pre, stream, branch):
+    d = make(M, D, cuts(M), stream, branch, seed=D)
+    cfg = config(lq, d, post, pre, 0.75)
+    for keys in MISSING:
+        e = dict(d, yt=d["y"].dtype, **{k: None for k in keys})
+        keep = dict(dh=torch.full_like(d["h"], 7.0), dy=None if e["y"] is None else torch.full_like(d["y"], 7.0))
+        got = dict(zip(GRADS, backward(lq, cfg, e, **keep)))
+        want = gradients(e, post, pre, 0.75)
+        rows = want["rows"]
+        others = torch.ones(M, dtype=torch.bool, device="cuda")
+        others[rows] = False
+        for k in GRADS:
+            if k in ("dh", "dy") and got[k] is not None:
+                ref.check(got[k][rows], want[k], f"{k} without {keys}")
+                assert (got[k][others] == 7.0).all(), (k, keys)
+            elif k in want and got[k] is not None:
+                ref.check(got[k], want[k], f"{k} without {keys}")
+            elif got[k] is not None:
+                assert (got[k] == 0).all(), (k, keys)
+
+
+@pytest.mark.parametrize("stream,branch", TYPES)
+@pytest.mark.parametrize("D", [600, 1152, 1153, 2240])
+@pytest.mark.parametrize("M", [50, 1300])
+def test_gradients_that_are_not_wanted(lq, M, D, stream, branch):
+    """dh, dy or sums left out, through the C interface."""
+    d = make(M, D, cuts(M), stream, branch, seed=D)
+    cfg = config(lq, d, "rms", "layer", 0.75)
+    S = len(cuts(M)) - 1
+    whole = dict(zip(GRADS, backward(lq, cfg, d, dh=torch.full_like(d["h"], 7.0), dy=torch.full_like(d["y"], 7.0))))
+    p = lambda t: t.data_ptr()  # noqa: E731
+    mod = lambda t: lq.lq_mod(None, 0) if t is None else lq.lq_mod(p(t), t.stride(0))  # noqa: E731
+    work = torch.empty(lq.lq_block_work_sizes(cfg, M, S), dtype=torch.uint8, device="cuda")
+    for left in (("dh",), ("dy",), ("dh", "dy"), ("dgate", "dscale", "dshift", "dw_post", "dw_pre"), ("dgate", "dw_pre"), ("dh", "dscale", "dshift", "dw_post")):
+        o = {k: None if k in left else torch.full_like(t, 7.0) for k, t in whole.items()}
+        out = lq.lq_block_grads(None if o["dh"] is None else p(o["dh"]), D, None if o["dy"] is None else p(o["dy"]), D, mod(o["dgate"]), mod(o["dscale"]), mod(o["dshift"]),
+                                None if o["dw_post"] is None else p(o["dw_post"]), None if o["dw_pre"] is None else p(o["dw_pre"]))
+        st = lq.raw().lq_block_norm_bwd(C.byref(cfg), p(d["h"]), D, p(d["y"]), D, p(d["offsets"]), S, C.byref(mod(d["gate"])), C.byref(mod(d["scale"])), p(d["w_post"]),
+                                        p(d["w_pre"]), p(d["dho"]), D, p(d["dx"]), D, C.byref(out), M, p(work), work.numel(), torch.cuda.current_stream().cuda_stream)
+        assert st == lq.LQ_OK
+        want = gradients(dict(d, yt=d["y"].dtype), "rms", "layer", 0.75)
+        for k, t in o.items():
+            if t is None:
+                continue
+            if k in ("dh", "dy"):
+                ref.check(t[want["rows"]], want[k], f"{k} without {left}")
+                assert (t[:2] == 7.0).all() and (t[M - 3:] == 7.0).all(), (k, left)
+            else:
+                ref.check(t, want[k], f"{k} without {left}")
+
+
+@pytest.mark.parametrize("stream,branch", TYPES)
+@pytest.mark.parametrize("post,pre", [("none", "layer"), ("rms", "rms"), ("layer", "layer")])
+@pytest.mark.parametrize("M", [50, 1300])
+@pytest.mark.parametrize("D", [515, 770, 883, 1021, 1153, 1279, 1527, 2239, 3601, 10241])
+def test_odd_widths(lq, D, M, post, pre, stream, branch):
+    M = M if D < 4000 else min(M, 700)
+    check_all(lq, make(M, D, cuts(M), stream, branch, seed=D), post, pre, alpha=0.75)
+
+
+@pytest.mark.parametrize("stream,branch", TYPES)
+@pytest.mark.parametrize("D", [1152, 2240])
+def test_rows_at_odd_places(lq, D, stream, branch):
+    """Rows of a width that is a multiple of four, one value from an aligned place: the kernels of any alignment with no row's end among four values."""
+    M = 600
+    d = make(M, D, cuts(M), stream, branch, seed=D)
+
+    def moved(t):
+        big = torch.full((M, D + 1), float("nan"), dtype=t.dtype, device="cuda")
+        big[:, 1:] = t
+        return big[:, 1:]
+    check_all(lq, dict(d, **{k: moved(d[k]) for k in ("h", "y", "dx", "dho")}), "rms", "layer", 0.75)
