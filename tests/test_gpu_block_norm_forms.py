@@ -105,3 +105,42 @@ def test_rows_at_odd_places(lq, D, stream, branch):
         big[:, 1:] = t
         return big[:, 1:]
     check_all(lq, dict(d, **{k: moved(d[k]) for k in ("h", "y", "dx", "dho")}), "rms", "layer", 0.75)
+
+
+def exact_rows(M, D, mean, seed):
+    """fp32 rows of whole numbers whose sums, means and differences from the mean are all exact in 24 bits: M x D (a power of two, so that the mean is the sum times one), deviations
+    around 1."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    x = (torch.randn(M, D, generator=g, device="cuda") * 1.5).round() + mean
+    assert D & (D - 1) == 0 and float(x.abs().sum(1).max()) < 2 ** 24
+    return x
+
+
+@pytest.mark.parametrize("D", [256, 1024, 2048])
+def test_variance_of_rows_with_a_large_mean(lq, D):
+    """Differences from the mean being exact, 1 / deviation is off by half of what a sum of D squares can be in any order, (D + 8) 2^-24, and by the root, the division and the mean of the
+    squares, 4 2^-24; the row by one product more, and its rounding.  (Squares less the mean's square are off by 4096^2 2^-24 of variances around 2.)"""
+    M, e = 9, 2.0 ** -24
+    rel = (0.5 * (D + 8) + 6) * e
+    h, y = exact_rows(M, D, 4096.0, D), exact_rows(M, D, -4096.0, D + 1)
+
+    def normed(x):
+        x = x.double()
+        x = x - x.mean(1, keepdim=True)
+        r = 1.0 / (x.square().mean(1, keepdim=True) + EPS).sqrt()
+        return x * r, r
+    cfg = lq.make_block_config(D, "none", "layer", EPS, 1.0, "f32", "f32")
+    (n, r), (p, ry) = normed(h), normed(y)
+    _, x = lq.lq_block_norm_fwd(cfg, h)
+    assert ((x.double() - n).abs() <= (rel + 2 * e) * n.abs()).all()
+    both = lq.make_block_config(D, "layer", "none", EPS, 1.0, "f32", "f32")
+    ho, _ = lq.lq_block_norm_fwd(both, torch.zeros_like(h), y)
+    assert ((ho.double() - p).abs() <= (rel + 2 * e) * p.abs()).all()
+    # gradients: of h through the first norm, of y through the second
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    d = torch.randn(M, D, generator=g, device="cuda")
+    for name, got, v, s in (("dh", lq.lq_block_norm_bwd(cfg, h, None, dx=d)[0], n, r), ("dy", lq.lq_block_norm_bwd(both, torch.zeros_like(h), y, dho=d)[1], p, ry)):
+        value, off = ref.norm_grad("layer", v, s, rel * v.abs(), torch.full_like(s, rel), d.double(), torch.zeros_like(v))
+        ref.check(got, ref.rounded(value, off, torch.float32), name)
