@@ -487,7 +487,7 @@ lq_status lq_w4_bwd(const lq_w4_config *cfg, const void *packed, size_t packed_b
 
 /* ---- Norms before and after a block, with its gate, residual scale and modulation ---------------------------------
    What lies between two blocks, row by row; s is the row's sequence:
-       h' = res_scale h + gate[s] post(y) w_post              (without a branch y: h' = h, which is not written)
+       h' = res_scale h + gate[s] post(y) w_post              (without a branch y: h' = h, which is not written, whatever res_scale is)
        x  = pre(h') w_pre (1 + scale[s]) + shift[s]            (from h' before its rounding)
    LQ_NORM_NONE: z;  LQ_NORM_RMS: z / sqrt(mean(z^2) + eps);  LQ_NORM_LAYER: (z - mean z) / sqrt(var z + eps), var the mean of squared differences.
    Everything is held in fp32 and rounded once.  Not a number stays in its row (and in the gradients of its sequence). */
@@ -524,11 +524,12 @@ lq_status lq_block_work_sizes(const lq_block_config *cfg, int64_t M, int32_t S, 
 
 /* Gradients.  With n = pre(h'), p = post(y) before their weights, dho the derivative of a loss with respect to h' (what comes through the stream) and dx that with respect to x:
        G = dho + (pre's gradient at h') (dx w_pre (1 + scale[s]))
-       dh = res_scale G ,  dy = (post's gradient at y) (G gate[s] w_post)
+       dh = res_scale G (G where the forward had no y) ,  dy = (post's gradient at y) (G gate[s] w_post)
        dshift[s] = sum dx ,  dscale[s] = w_pre sum dx n ,  dgate[s] = w_post sum G p    over the rows of s (zeros for a sequence without rows)
        dw_pre = sum dx (1 + scale[s]) n ,  dw_post = sum G gate[s] p                     over all rows of sequences
    (The modulation of a sequence without rows is not used, whatever it holds.)
-   ho: the forward's h'.  dho or dx may be NULL (zero): without dx, h' is not looked at; without y, dy, dgate and dw_post must be NULL.  dh, dy and every gradient of modulation and
+   ho: the forward's h'.  y: the forward's; NULL says that it had none, that is h' = h and dh = G (a forward with a branch needs its y here, also for dh alone).  dho or dx may be NULL (zero): without dx,
+   h' is not looked at; without y, dy, dgate and dw_post must be NULL.  dh, dy and every gradient of modulation and
    weights may be NULL.  dh may be dho, dy may be dx (same pointer and stride); outputs must not overlap otherwise.  work: 256-byte aligned.  Sums are fixed in their order: repeated calls give identical bits. */
 typedef struct {
     void *dh;

@@ -975,7 +975,7 @@ def lq_block_norm_fwd(cfg: lq_block_config, h: torch.Tensor, y: Optional[torch.T
                       gate: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, shift: Optional[torch.Tensor] = None,
                       w_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None, ho: Optional[torch.Tensor] = None,
                       x: Optional[torch.Tensor] = None, last: bool = False):
-    """(ho, x): ho = res_scale h + gate post(y) w_post (None without y), x = pre(ho) w_pre (1 + scale) + shift (None with last=True).  h, y: M x dim; offsets: int32,
+    """(ho, x): ho = res_scale h + gate post(y) w_post (None without y, where the sum is h itself, not scaled), x = pre(ho) w_pre (1 + scale) + shift (None with last=True).  h, y: M x dim; offsets: int32,
     the first row of each sequence and the end of the last (rows of no sequence stay as they are in ho and x; None: one sequence); gate, scale, shift: one row of dim fp32
     values for each sequence (rows may be further apart, as slices of one layer's output); w_post, w_pre: dim fp32.  ho may be h, x may be y."""
     st = _call.block_norm_fwd(cfg, h, y, offsets, gate, scale, shift, w_post, w_pre, ho, x, last)
@@ -1003,7 +1003,7 @@ def lq_block_norm_bwd(cfg: lq_block_config, ho: Optional[torch.Tensor], y: Optio
                       dscale: Optional[torch.Tensor] = None, dshift: Optional[torch.Tensor] = None, dw_post: Optional[torch.Tensor] = None,
                       dw_pre: Optional[torch.Tensor] = None, work: Optional[torch.Tensor] = None):
     """(dh, dy, dgate, dscale, dshift, dw_post, dw_pre) of lq_block_norm_fwd from its result ho (h itself where there was no y), its y and the derivatives with respect to ho
-    and x (either may be None).  dh may be dho, dy may be dx.  Gradients of gate, scale (with shift) and the weights are made where these are given, or where a tensor for them is."""
+    and x (either may be None).  y=None says that the forward had none: dh is then not scaled by res_scale.  dh may be dho, dy may be dx.  Gradients of gate, scale (with shift) and the weights are made where these are given, or where a tensor for them is."""
     st = _call.block_norm_bwd(cfg, ho, y, offsets, gate, scale, w_post, w_pre, dho, dx, dh, dy, dgate, dscale, dshift, dw_post, dw_pre, work)
     if st >= 0:
         _check(st, "lq_block_norm_bwd")

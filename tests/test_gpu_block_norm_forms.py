@@ -107,6 +107,25 @@ def test_rows_at_odd_places(lq, D, stream, branch):
     check_all(lq, dict(d, **{k: moved(d[k]) for k in ("h", "y", "dx", "dho")}), "rms", "layer", 0.75)
 
 
+@pytest.mark.parametrize("mods", [("gate", "scale", "shift"), ()])
+@pytest.mark.parametrize("D", [200, 1152, 1153])
+@pytest.mark.parametrize("M", [40, 600])
+def test_without_a_branch_there_is_no_residual_scale(lq, M, D, mods):
+    """Without y the sum is h itself, whatever res_scale is, and the gradient with respect to h is not scaled either: the first norm of a model with the configuration of the others."""
+    d = dict(make(M, D, cuts(M), "f32", "bf16", seed=D, mods=mods), y=None)
+    cfg = lq.make_block_config(D, "rms", "layer", EPS, 0.5, "f32", "bf16")
+    none, x = forward(lq, cfg, d)
+    want = ref.block_fwd(d["h"], None, d["offsets"], d["gate"], d["scale"], d["shift"], d["w_post"], d["w_pre"], "rms", "layer", EPS, 1.0, torch.bfloat16)
+    rows = want["rows"]
+    assert none is None
+    ref.check(x[rows], want["x"], "x")
+    for keys in ((), ("dho",), ("dx",)):
+        e = dict(d, yt=torch.bfloat16, **{k: None for k in keys})
+        got, grads = dict(zip(GRADS, backward(lq, cfg, e))), gradients(e, "rms", "layer", 1.0)
+        ref.check(got["dh"][rows], grads["dh"], f"dh without {keys}")
+        assert got["dy"] is None and got["dgate"] is None and got["dw_post"] is None
+
+
 def exact_rows(M, D, mean, seed):
     """fp32 rows of whole numbers whose sums, means and differences from the mean are all exact in 24 bits: M x D (a power of two, so that the mean is the sum times one), deviations
     around 1."""
