@@ -172,6 +172,14 @@ __device__ __forceinline__ void split4(v4i v, uint2 (&t)[3])  // ... of four, as
     }
 }
 
+// Between a wavefront's stores to its LDS and other lanes' loads of them or stores over them, and between loads and the next stores: neither moves across.  (The LDS takes a wavefront's accesses in their order, so that this is no
+// instruction.)
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---- forward ------------------------------------------------------------------------------------
 
 struct W4Args {
@@ -312,6 +320,7 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
                 }
             }
         if (k0 + 128 * EB > end && end % 16) {
+            wave_lds_order();  // (the zeros of that piece were another lane's)
             Bits v[2 * MT];  // eight rows of eight values (f32: of four) at a time
             const int k = end / 16 * 16 + (lane & 7) * EB;
 #pragma unroll
@@ -330,6 +339,7 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
                     }
                 }
         }
+        wave_lds_order();
         v4i code[NT];
         float sc[NT][PER];
 #pragma unroll
@@ -365,6 +375,7 @@ __global__ void __launch_bounds__(512) w4_fwd_kernel(W4Args a)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) sum[mt][t][r] = fmaf(sc[t][g], acc[mt][t][r], sum[mt][t][r]);
         }
+        wave_lds_order();
     }
     __syncthreads();
     constexpr int S = MT * NT * 256;
@@ -454,6 +465,7 @@ __global__ void __launch_bounds__(64 * w4_bwd_waves(PER)) w4_bwd_kernel(W4Args a
     for (int s = first; s < steps; s += stride) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) *(v4i*)(mine + t * 1088 + q * 272 + c * 16) = next[t];
+        wave_lds_order();
         float dy[8], sc[8 * PER];
         next_dy.values(dy);
 #pragma unroll
@@ -462,6 +474,7 @@ __global__ void __launch_bounds__(64 * w4_bwd_waves(PER)) w4_bwd_kernel(W4Args a
         uint32_t d[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) d[r] = *(const uint32_t*)(mine + (q >> 1) * 1088 + (c & 3) * 272 + (8 * (q & 1) + r) * 16 + (c >> 2) * 4);
+        wave_lds_order();
         turn_nibbles(d);
         v4i up[PER][3];
 #pragma unroll
