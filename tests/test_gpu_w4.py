@@ -223,3 +223,79 @@ def test_captured_and_replayed_on_a_stream(lq):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(Y, want[0]) and torch.equal(dX, want[1]), k
+
+
+def normal24(rows, cols, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(rows, cols, generator=g, device="cuda")
+
+
+FORMS = [(256, 32), (1100, 2007), (1100, 5007), (1100, 9007), (1100, 14333), (140, 3003), (140, 14333), (140, 30001), (4608, 300)]  # one to four tiles to a workgroup, by four and eight wavefronts
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K,N", FORMS)
+def test_all_24_bits_of_rows(lq, K, N, group):
+    """Strong channels that cancel leave what is 2^-18 of them to 2^-22 (a third term left out would cost 2^-18): every partial sum is a multiple of 2^-23 below 2 and so exact in 24 bits.  A row
+    with one channel alone is that channel's value to the last bit, times a code that is a power of two, then times the scale with one rounding."""
+    M = 3
+    codes = torch.ones(N, K, dtype=torch.int8, device="cuda")
+    cfg = lq.make_w4_config(N, K, group, "f32", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, codes, torch.ones(N, -(-K // group), device="cuda"))
+    X = torch.zeros(M, K, device="cuda")
+    strong = 1.0 + 2.0 ** -10 + 2.0 ** -18 + 2.0 ** -23
+    for m, (a, b, c, d) in enumerate(((0, 1, 2, 3), (0, K - 1, K // 2, 5), (K - 2, K // 3, 7, 70))):
+        X[m, a], X[m, b], X[m, c], X[m, d] = strong, -1.0, -(2.0 ** -10), 2.0 ** -20
+    want = 2.0 ** -18 + 2.0 ** -20 + 2.0 ** -23
+    assert ((lq.lq_w4_fwd(cfg, packed, X).double() - want).abs() <= 2.0 ** -22).all()
+    scales = normal24(N, -(-K // group), 5) * 0.1
+    codes = torch.tensor([1, -1, 2, -2, 4, -4], dtype=torch.int8, device="cuda")[torch.arange(N * K, device="cuda") % 6].view(N, K)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    at = torch.tensor([K - 1, K // 2, 3], device="cuda")
+    X.zero_()
+    X[torch.arange(M, device="cuda"), at] = normal24(1, M, 6)[0]
+    got = lq.lq_w4_fwd(cfg, packed, X)
+    for m in range(M):
+        want = (X[m, at[m]].double() * codes[:, at[m]].double() * scales[:, at[m] // group].double()).float()
+        assert torch.equal(got[m], want), m
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(2, 6912, 1152), (3, 359, 256), (16, 13441, 300), (5, 64, 64), (1, 33, 4608), (20, 2000, 130)])
+def test_all_24_bits_of_gradients(lq, M, N, K, group):
+    """The same of dY, in one launch and in parts of N; a bf16 dY times the scale is a number of 24 bits too."""
+    codes = torch.ones(N, K, dtype=torch.int8, device="cuda")
+    cfg = lq.make_w4_config(N, K, group, "f32", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, codes, torch.ones(N, -(-K // group), device="cuda"))
+    dY = torch.zeros(M, N, device="cuda")
+    strong = 1.0 + 2.0 ** -10 + 2.0 ** -18 + 2.0 ** -23
+    for m in range(M):
+        a, b, c, d = ((0, 1, 2, 3), (0, N - 1, N // 2, 5), (N - 2, N // 3, 7, 30))[m % 3]
+        dY[m, a], dY[m, b], dY[m, c], dY[m, d] = strong, -1.0, -(2.0 ** -10), 2.0 ** -20
+    want = 2.0 ** -18 + 2.0 ** -20 + 2.0 ** -23
+    assert ((lq.lq_w4_bwd(cfg, packed, dY).double() - want).abs() <= 2.0 ** -22).all()
+    scales = normal24(N, -(-K // group), 5) * 0.1
+    codes = torch.tensor([1, -1, 2, -2, 4, -4], dtype=torch.int8, device="cuda")[torch.arange(N * K, device="cuda") % 6].view(N, K)
+    at = (torch.arange(M, device="cuda") * 97 + 11) % N
+    for y in ("f32", "bf16"):
+        cfg = lq.make_w4_config(N, K, group, "f32", y)
+        packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+        dY = torch.zeros(M, N, dtype=DT[y], device="cuda")
+        dY[torch.arange(M, device="cuda"), at] = normal24(1, M, 6)[0].to(DT[y])
+        got = lq.lq_w4_bwd(cfg, packed, dY)
+        each = scales[at].repeat_interleave(group, 1)[:, :K]
+        up = (dY[torch.arange(M, device="cuda"), at].double()[:, None] * each.double()).float()  # the one rounding
+        assert torch.equal(got, (up.double() * codes[at].double()).float()), y
+
+
+@pytest.mark.parametrize("M,K,N", [(2, 1152, 6912), (16, 2240, 13441), (3, 4608, 300), (40, 1100, 5007)])
+def test_rounding_errors_of_random_rows(lq, M, K, N):
+    """n sums of numbers of random signs are off by some sqrt(n) of a rounding of the result's size (in the 2-norm over all results), not by n: rows in one term of three would be off by 2^-9."""
+    codes, scales, X, dY, _ = make(M, K, N, 64, "f32", "f32", seed=N)
+    X = X - 0.5  # (no mean: results are of the size of a random sum)
+    cfg = lq.make_w4_config(N, K, 64, "f32", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    for got, (want, _), n in ((lq.lq_w4_fwd(cfg, packed, X), ref.w4_fwd(X, codes, scales, 64, None, torch.float32), K),
+                              (lq.lq_w4_bwd(cfg, packed, dY), ref.w4_bwd(dY, codes, scales, 64, torch.float32), N)):
+        assert float((got.double() - want).norm() / want.norm()) <= ref.U * (3 * n + 24) ** 0.5
