@@ -63,7 +63,7 @@ typedef enum {
     LQ_ERR_ALIGN = 4,            /* a pointer or stride is not aligned as documented     */
     LQ_ERR_BUFFER_TOO_SMALL = 5, /* caller's buffer smaller than lq_*_sizes reports       */
     LQ_ERR_DEVICE = 6,           /* the HIP runtime rejected a launch                    */
-    LQ_ERR_STALE_BLOB = 7        /* lq_verify_blob, lq_adapter_verify_plan: the blob's header belongs to another configuration, token count or layout version */
+    LQ_ERR_STALE_BLOB = 7        /* lq_verify_blob, lq_adapter_verify_plan, lq_w4_verify: the blob's header belongs to another configuration, token count or layout version */
 } lq_status;
 
 typedef enum { LQ_BLOB_PACKED = 1, LQ_BLOB_ACT = 2 } lq_blob_kind;
@@ -474,6 +474,10 @@ lq_status lq_w4_pack(const lq_w4_config *cfg, const float *W, void *packed, size
 lq_status lq_w4_pack_codes(const lq_w4_config *cfg, const int8_t *codes, const float *scales, void *packed, size_t packed_bytes, void *stream);
 /* Their plain views; either may be NULL. */
 lq_status lq_w4_unpack(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, int8_t *codes, float *scales, void *stream);
+
+/* Packed weights start with a 256-byte header that holds N, K and group.  The calls do not read it (that would synchronise): weights of another layer that are large enough give wrong results.  This is
+   the explicit check: it copies the header to the host and therefore SYNCHRONISES `stream`.  LQ_ERR_STALE_BLOB for anything but weights that lq_w4_pack or lq_w4_pack_codes made for these three. */
+lq_status lq_w4_verify(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, void *stream);
 
 /* X: M x K, row stride ldx elements (>= K), Y: M x N, row stride ldy; at most 2^22; 0 <= M <= 2^14.  bias: N fp32 or NULL.  Y must not overlap X. */
 lq_status lq_w4_fwd(const lq_w4_config *cfg, const void *packed, size_t packed_bytes, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy,

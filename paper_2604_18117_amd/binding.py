@@ -156,7 +156,7 @@ EXPORTS = ["lq_status_string", "lq_packed_sizes", "lq_pack_weights", "lq_verify_
            "lq_calib_unpack", "lq_rot_sizes", "lq_rot_init", "lq_rot_step", "lq_rot_step_static", "lq_rot_apply", "lq_rot_unpack",
            "lq_adapter_plan_sizes", "lq_adapter_plan", "lq_adapter_verify_plan", "lq_adapter_sizes", "lq_adapter_fwd", "lq_adapter_bwd",
            "lq_qk_norm_rope_fwd", "lq_qk_work_sizes", "lq_qk_norm_rope_bwd",
-           "lq_w4_sizes", "lq_w4_pack", "lq_w4_pack_codes", "lq_w4_unpack", "lq_w4_fwd", "lq_w4_work_sizes", "lq_w4_bwd",
+           "lq_w4_sizes", "lq_w4_pack", "lq_w4_pack_codes", "lq_w4_unpack", "lq_w4_verify", "lq_w4_fwd", "lq_w4_work_sizes", "lq_w4_bwd",
            "lq_block_norm_fwd", "lq_block_work_sizes", "lq_block_norm_bwd", "lq_adamw_step"]
 
 _lib.lq_calib_sizes.argtypes = [C.POINTER(lq_config), C.POINTER(C.c_size_t)]
@@ -211,6 +211,7 @@ _lib.lq_w4_sizes.argtypes = [_W4, C.POINTER(C.c_size_t)]
 _lib.lq_w4_pack.argtypes = [_W4, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lq_w4_pack_codes.argtypes = [_W4, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lq_w4_unpack.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.lq_w4_verify.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.lq_w4_fwd.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
 _lib.lq_w4_work_sizes.argtypes = [_W4, C.c_int64, C.POINTER(C.c_size_t)]
 _lib.lq_w4_bwd.argtypes = [_W4, C.c_void_p, C.c_size_t, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_size_t, C.c_void_p]
@@ -889,6 +890,11 @@ def lq_w4_unpack(cfg: lq_w4_config, packed: torch.Tensor):
     scales = torch.empty((cfg.N, -(-cfg.K // cfg.group)), dtype=torch.float32, device=packed.device)
     _check(_lib.lq_w4_unpack(C.byref(cfg), _ptr(_blob_arg(packed)), packed.numel(), _ptr(codes), _ptr(scales), _stream()), "lq_w4_unpack")
     return codes, scales
+
+
+def lq_w4_verify(cfg: lq_w4_config, packed: torch.Tensor) -> None:
+    """Raises LqError(LQ_ERR_STALE_BLOB) when `packed` is not weights of cfg's N, K and group.  Synchronises the stream."""
+    _check(_lib.lq_w4_verify(C.byref(cfg), _ptr(_blob_arg(packed)), packed.numel(), _stream()), "lq_w4_verify")
 
 
 def lq_w4_fwd(cfg: lq_w4_config, packed: torch.Tensor, X: torch.Tensor, bias: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -841,6 +841,19 @@ lq_status lq_w4_unpack(const lq_w4_config* cfg, const void* packed, size_t packe
     return launch_w4_unpack(cfg, (const uint8_t*)packed, codes, scales, (hipStream_t)stream) == hipSuccess ? LQ_OK : LQ_ERR_DEVICE;
 }
 
+lq_status lq_w4_verify(const lq_w4_config* cfg, const void* packed, size_t packed_bytes, void* stream)
+{
+    lq_status st = w4_check(cfg);
+    if (st != LQ_OK || (st = w4_packed_check(cfg, packed, packed_bytes)) != LQ_OK) return st;
+    BlobTag got;
+    if (hipMemcpyAsync(&got, packed, sizeof(got), hipMemcpyDeviceToHost, (hipStream_t)stream) != hipSuccess) return LQ_ERR_DEVICE;
+    if (hipStreamSynchronize((hipStream_t)stream) != hipSuccess) return LQ_ERR_DEVICE;
+    const BlobTag want = w4_tag(cfg);
+    for (int i = 0; i < 8; ++i)
+        if (got.w[i] != want.w[i]) return LQ_ERR_STALE_BLOB;
+    return LQ_OK;
+}
+
 static lq_status w4_batch_check(int64_t M) { return M < 0 || M > (1 << 14) ? LQ_ERR_SHAPE : LQ_OK; }
 
 lq_status lq_w4_fwd(const lq_w4_config* cfg, const void* packed, size_t packed_bytes, const void* X, int64_t ldx, const float* bias, void* Y, int64_t ldy,

@@ -261,7 +261,12 @@ size_t qk_work_bytes(const lq_qk_config* c, int64_t M);
 hipError_t launch_qk_fwd(const lq_qk_config* c, const QkTensors& t, int64_t M, hipStream_t s);
 hipError_t launch_qk_bwd(const lq_qk_config* c, const QkTensors& t, int64_t M, uint8_t* work, hipStream_t s);
 
-// Products of a few rows with 4-bit weights (lq_w4.hip).
+// Products of a few rows with 4-bit weights (lq_w4.hip).  Packed weights start with a header of the blobs' kind, which lq_w4_verify compares with a configuration.
+constexpr uint32_t W4_KIND = 4, W4_VERSION = 1;
+static inline BlobTag w4_tag(const lq_w4_config* c)
+{
+    return {{BLOB_MAGIC, W4_VERSION, W4_KIND, (uint32_t)c->group, 0, 0, (uint32_t)c->N, (uint32_t)c->K}};
+}
 size_t w4_packed_bytes(const lq_w4_config* c);
 size_t w4_work_bytes(const lq_w4_config* c, int64_t M);
 hipError_t launch_w4_pack(const lq_w4_config* c, const float* W, const int8_t* codes, const float* scales, uint8_t* packed, hipStream_t s);  // W, or codes and scales

@@ -12,6 +12,7 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
 // ---- layout -------------------------------------------------------------------------------------
+// header: BLOB_HEADER bytes, w4_tag and zeros
 // codes:  [tile of 16 channels][block of 128 of K][lane = n%16 + 16 q][16 bytes]: dword j of lane (n, q) holds k = 32 j + 8 q .. + 7 of the block, so that product
 //         j of the matrix core takes 32 consecutive k, which belong to one group.  Value i < 4 of a dword is the low nibble of byte i, value 4 + i its high
 //         nibble; a nibble is sign and magnitude.  What lies past N or K is zero.
@@ -28,8 +29,10 @@ static size_t w4_code_bytes(const W4Shape& s) { return (size_t)s.tiles * s.block
 size_t w4_packed_bytes(const lq_w4_config* c)
 {
     const W4Shape s = w4_shape(c);
-    return w4_code_bytes(s) + (size_t)s.tiles * s.blocks * 16 * s.per * 4;
+    return BLOB_HEADER + w4_code_bytes(s) + (size_t)s.tiles * s.blocks * 16 * s.per * 4;
 }
+static const uint8_t* w4_codes(const uint8_t* packed) { return packed + BLOB_HEADER; }
+static const float* w4_scales(const uint8_t* packed, const W4Shape& s) { return (const float*)(packed + BLOB_HEADER + w4_code_bytes(s)); }
 
 // ---- packing ------------------------------------------------------------------------------------
 
@@ -46,9 +49,11 @@ __device__ __forceinline__ int w4_code(uint32_t dword, int i)
 
 // A wavefront packs a block of a tile.  W: values, quantised by the INT family's rule (scale = amax / 7, code = rint(v 7 / amax), 1 for a group of zeros); or codes
 // and scales that are there.
-__global__ void __launch_bounds__(64) w4_pack_kernel(const float* W, const int8_t* codes, const float* scales, W4Shape s, uint8_t* out, float* sout)
+__global__ void __launch_bounds__(64) w4_pack_kernel(const float* W, const int8_t* codes, const float* scales, W4Shape s, BlobTag tag, uint32_t* header, uint8_t* out, float* sout)
 {
+    static_assert(BLOB_HEADER == 64 * 4, "a dword to a lane");
     const int tile = blockIdx.x / s.blocks, block = blockIdx.x % s.blocks, lane = threadIdx.x, q = lane >> 4;
+    if (blockIdx.x == 0) header[lane] = lane < 8 ? tag.w[lane & 7] : 0u;
     const int64_t n = (int64_t)tile * 16 + (lane & 15), k0 = (int64_t)block * 128 + 8 * q;
     const int groups = (int)((s.K + 128 / s.per - 1) / (128 / s.per));
     uint32_t word[4];
@@ -548,14 +553,15 @@ __global__ void __launch_bounds__(256) w4_join(W4Args a)
 hipError_t launch_w4_pack(const lq_w4_config* c, const float* W, const int8_t* codes, const float* scales, uint8_t* packed, hipStream_t s)
 {
     const W4Shape sh = w4_shape(c);
-    hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)(sh.tiles * sh.blocks)), dim3(64), 0, s, W, codes, scales, sh, packed, (float*)(packed + w4_code_bytes(sh)));
+    hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)(sh.tiles * sh.blocks)), dim3(64), 0, s, W, codes, scales, sh, w4_tag(c), (uint32_t*)packed, (uint8_t*)w4_codes(packed),
+                       (float*)w4_scales(packed, sh));
     return hipGetLastError();
 }
 
 hipError_t launch_w4_unpack(const lq_w4_config* c, const uint8_t* packed, int8_t* codes, float* scales, hipStream_t s)
 {
     const W4Shape sh = w4_shape(c);
-    hipLaunchKernelGGL(w4_unpack_kernel, dim3((unsigned)(sh.tiles * sh.blocks)), dim3(64), 0, s, packed, (const float*)(packed + w4_code_bytes(sh)), sh, codes, scales);
+    hipLaunchKernelGGL(w4_unpack_kernel, dim3((unsigned)(sh.tiles * sh.blocks)), dim3(64), 0, s, w4_codes(packed), w4_scales(packed, sh), sh, codes, scales);
     return hipGetLastError();
 }
 
@@ -605,8 +611,8 @@ static W4Args w4_args(const lq_w4_config* c, const uint8_t* packed, const void* 
 {
     const W4Shape sh = w4_shape(c);
     W4Args a{};
-    a.codes = packed;
-    a.scales = (const float*)(packed + w4_code_bytes(sh));
+    a.codes = w4_codes(packed);
+    a.scales = w4_scales(packed, sh);
     a.X = in;
     a.ldx = ldin;
     a.Y = out;

@@ -74,6 +74,13 @@ def test_w4_arguments(name):
         assert _w4(name, big, ldy=4096, work=None) == lq.LQ_ERR_NULL and _w4(name, big, ldy=4096, work=PTR + 64) == lq.LQ_ERR_ALIGN
 
 
+def test_w4_verify_arguments():
+    f, c = lq.raw().lq_w4_verify, C.byref(_wcfg())
+    assert f(None, PTR, BIG, None) == f(c, None, BIG, None) == lq.LQ_ERR_NULL
+    assert f(c, PTR + 128, BIG, None) == lq.LQ_ERR_ALIGN and f(c, PTR, lq.lq_w4_sizes(_wcfg()) - 1, None) == lq.LQ_ERR_BUFFER_TOO_SMALL
+    assert f(C.byref(_wcfg(group=16)), PTR, BIG, None) == lq.LQ_ERR_SHAPE and f(C.byref(_wcfg(flags=1)), PTR, BIG, None) == lq.LQ_ERR_UNSUPPORTED
+
+
 def _bcfg(**kw):
     c = lq.make_block_config(64, "rms", "layer", h_dtype="f32")
     for k, v in kw.items():

@@ -299,3 +299,27 @@ def test_rounding_errors_of_random_rows(lq, M, K, N):
     for got, (want, _), n in ((lq.lq_w4_fwd(cfg, packed, X), ref.w4_fwd(X, codes, scales, 64, None, torch.float32), K),
                               (lq.lq_w4_bwd(cfg, packed, dY), ref.w4_bwd(dY, codes, scales, 64, torch.float32), N)):
         assert float((got.double() - want).norm() / want.norm()) <= ref.U * (3 * n + 24) ** 0.5
+
+
+def test_weights_of_another_layer_are_told(lq):
+    """lq_w4_verify: another N, K or group, other memory, another kind of packed weights; the weights depend on nothing else of the configuration."""
+    codes, scales, X, _, _ = make(2, 256, 512, 64)
+    cfg = lq.make_w4_config(512, 256, 64)
+    packed = lq.lq_w4_pack_codes(cfg, codes, scales)
+    for x in ("bf16", "f32"):
+        for y in ("bf16", "f32"):
+            lq.lq_w4_verify(lq.make_w4_config(512, 256, 64, x, y), packed)
+    lq.lq_w4_verify(cfg, lq.lq_w4_pack(cfg, torch.randn(512, 256, device="cuda")))
+    same = [lq.make_w4_config(512, 256, 128), lq.make_w4_config(256, 512, 64), lq.make_w4_config(511, 256, 64), lq.make_w4_config(512, 255, 64), lq.make_w4_config(16, 128, 32)]
+    for other in same:
+        assert lq.lq_w4_sizes(other) <= packed.numel()
+        with pytest.raises(lq.LqError) as e:
+            lq.lq_w4_verify(other, packed)
+        assert e.value.status == lq.LQ_ERR_STALE_BLOB
+    for blob in (torch.zeros_like(packed), torch.full_like(packed, 0xFF), packed[256:].clone().resize_(packed.numel())):
+        with pytest.raises(lq.LqError) as e:
+            lq.lq_w4_verify(cfg, blob)
+        assert e.value.status == lq.LQ_ERR_STALE_BLOB
+    with pytest.raises(lq.LqError) as e:
+        lq.lq_w4_verify(cfg, packed[:-256])
+    assert e.value.status == lq.LQ_ERR_BUFFER_TOO_SMALL
