@@ -97,7 +97,10 @@ class AdaptedQKV:
 class Entrance:
     """The rows that a projection gets from the stream h and the output y of the block before.
 
-    W: 3 dim x emb fp32, the modulation's layer (gate of the block before, scale and shift of the norm); offsets: first row of each image and the end of the last."""
+    W: 3 dim x emb fp32, the modulation's layer (gate of the block before, scale and shift of the norm); offsets: first row of each image and the end of the last.
+
+    A call's modulation (one row of 3 dim fp32 values for each image) is needed again by its gradient: ``mod`` holds the last call's, in memory of its own unless a call is given some.  With
+    several calls before their backward, on one stream or on several, the program keeps each call's and hands it to its backward."""
 
     def __init__(self, W, offsets, bias=None):
         n, emb = W.shape
@@ -105,22 +108,29 @@ class Entrance:
         self.cfg = lq.make_w4_config(n, emb, 64, "f32", "f32")
         self.packed = lq.lq_w4_pack(self.cfg, W)
         self.norm = lq.make_block_config(self.dim)
-        self.mod = torch.empty(offsets.shape[0] - 1, n, device="cuda")
+        self.mod, self.open, self.alone = None, 0, False  # of the last call; calls without a backward so far; whether the last one was made with none before it
 
     def parts(self, mod):
         """Views of gate, scale and shift in the layer's rows."""
         return [mod[:, k * self.dim:(k + 1) * self.dim] for k in range(3)]
 
-    def __call__(self, emb, h, y, X=None):
-        """(h', X): h' = h + gate y in h's place, X its modulated norm."""
-        lq.lq_w4_fwd(self.cfg, self.packed, emb, self.bias, Y=self.mod)
+    def __call__(self, emb, h, y, X=None, mod=None):
+        """(h', X): h' = h + gate y in h's place, X its modulated norm.  mod: memory for the modulation."""
+        self.mod = lq.lq_w4_fwd(self.cfg, self.packed, emb, self.bias, Y=mod)
+        self.open, self.alone = self.open + 1, self.open == 0
         gate, scale, shift = self.parts(self.mod)
         return lq.lq_block_norm_fwd(self.norm, h, y, self.offsets, gate, scale, shift, ho=h, x=X)
 
-    def backward(self, h, y, dh, dX):
-        """(dh, dy, demb).  h: the stream that a call left, dh: the derivative with respect to it from what follows, overwritten; dX: with respect to the rows, overwritten."""
-        gate, scale, _ = self.parts(self.mod)
-        dmod = torch.empty_like(self.mod)
+    def backward(self, h, y, dh, dX, mod=None):
+        """(dh, dy, demb).  h: the stream that a call left, dh: the derivative with respect to it from what follows, overwritten; dX: with respect to the rows, overwritten; mod: that call's
+        modulation, which may be left out for the last call where no earlier one was without a backward."""
+        if mod is None:
+            if not self.alone:
+                raise ValueError("not the only call without a backward: its modulation is needed")
+            mod = self.mod
+        self.open = max(self.open - 1, 0)
+        gate, scale, _ = self.parts(mod)
+        dmod = torch.empty_like(mod)
         dgate, dscale, dshift = self.parts(dmod)
         lq.lq_block_norm_bwd(self.norm, h, y, self.offsets, gate, scale, dho=dh, dx=dX, dh=dh, dy=dX, dgate=dgate, dscale=dscale, dshift=dshift)
         return dh, dX, lq.lq_w4_bwd(self.cfg, self.packed, dmod)
@@ -139,7 +149,7 @@ def serve(images: int = 2, side: int = 64, dim: int = 1152, heads: int = 16, ada
     m = AdaptedQKV(*layer(dim, 32), M, heads, adapters, 32)
     m.B.normal_(std=0.02)
     h, y = (torch.randn(M, dim, device="cuda").bfloat16() for _ in range(2))
-    X, emb = torch.empty_like(h), torch.randn(images, dim, device="cuda")
+    X, emb, mod = torch.empty_like(h), torch.randn(images, dim, device="cuda"), torch.empty(images, 3 * dim, device="cuda")
     enter = Entrance(torch.randn(3 * dim, dim, device="cuda") * 0.02 / math.sqrt(dim), torch.arange(images + 1, dtype=torch.int32, device="cuda") * side * side)
     m.group(torch.arange(images, dtype=torch.int32, device="cuda").repeat_interleave(side * side) - 1)  # the first image has none
     pos, Y = grid_positions(side, side), torch.empty(M, 3 * dim, dtype=torch.bfloat16, device="cuda")
@@ -147,7 +157,7 @@ def serve(images: int = 2, side: int = 64, dim: int = 1152, heads: int = 16, ada
     for i in range(2 * steps):
         if i == steps:
             ev[0].record()
-        enter(emb, h, y, X)
+        enter(emb, h, y, X, mod)
         m(X, pos, Y)
     ev[1].record()
     torch.cuda.synchronize()

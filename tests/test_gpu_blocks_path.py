@@ -153,3 +153,38 @@ def test_steps_follow_the_formula(lq):
             for name, got in (("p", p1), ("m", m1), ("v", v1)):
                 value, off = want[name]
                 ref.check(got, (value, off + 2.0 ** -24 * (value.abs() + off)), f"{name} of step {t}")
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_entrance_with_two_batches_under_way(lq, given):
+    """Two calls before their gradients: each backward takes the modulation of its own call."""
+    from paper_2604_18117_amd import adapted_qkv as ex
+    images, rows, dim, emb = 3, 11, 100, 48
+    rnd, M = normal(2), images * rows
+    enter = ex.Entrance(rnd(3 * dim, emb) * 0.05, torch.arange(images + 1, dtype=torch.int32, device="cuda") * rows, rnd(3 * dim))
+    batches = []
+    for _ in range(2):
+        e, h, y, dh, dx = rnd(images, emb), *(rnd(M, dim).bfloat16() for _ in range(4))
+        mod = torch.empty(images, 3 * dim, device="cuda") if given else None
+        h0 = h.clone()
+        enter(e, h, y, mod=mod)
+        batches.append((e, h0, h, y, dh, dx, enter.mod))
+        assert not given or enter.mod is mod
+    with pytest.raises(ValueError):  # whose?
+        enter.backward(batches[0][2], batches[0][3], batches[0][4].clone(), batches[0][5].clone())
+    got = []
+    for _, _, h, y, dh, dx, mod in reversed(batches):
+        got.insert(0, enter.backward(h, y, dh.clone(), dx.clone(), mod=mod))
+        with pytest.raises(ValueError):  # the other call's is not the last one
+            enter.backward(h, y, dh.clone(), dx.clone())
+    for (e, h0, h, y, dh, dx, mod), have in zip(batches, got):
+        alone = ex.Entrance(torch.zeros(3 * dim, emb, device="cuda"), enter.offsets, enter.bias)
+        alone.packed = enter.packed
+        again = h0.clone()
+        alone(e, again, y)
+        assert torch.equal(again, h) and torch.equal(alone.mod, mod)
+        for _ in range(2):
+            for a, b in zip(have, alone.backward(again, y, dh.clone(), dx.clone())):
+                assert torch.equal(a, b)
+    with pytest.raises(ValueError):  # a call's modulation without a call
+        ex.Entrance(torch.zeros(3 * dim, emb, device="cuda"), enter.offsets).backward(h, y, dh, dx)
