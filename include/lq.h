@@ -453,7 +453,8 @@ lq_status lq_qk_norm_rope_bwd(const lq_qk_config *cfg, const lq_heads *q, const 
    The layers beside the large projections: conditioning vectors, single tokens.
        Y[m,n]  = bias[n] + sum_k X[m,k] c[n,k] s[n, k / group]
        dX[m,k] = sum_n dY[m,n] s[n, k / group] c[n,k]                    (the weights are not trained)
-   c: integers -7 .. 7, s: fp32.  Codes enter the products exactly, fp32 rows with all 24 bits; sums are held in fp32 and rounded once.  A row's result does not depend on what
+   c: integers -7 .. 7, s: fp32.  Codes enter the products exactly, fp32 rows with all 24 bits (numbers below 2^-110, to whose last bits bf16 does not reach, to 2^-133); sums, those of a group before its
+   scale among them, are held in fp32 and rounded once.  A row's result does not depend on what
    the other rows hold; infinities and NaN stay in their row.  Sums are fixed in their order: repeated calls give identical bits.  Any N, K; rows may start anywhere (16-byte
    aligned rows are read faster). */
 typedef struct {

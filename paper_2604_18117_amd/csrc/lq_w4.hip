@@ -146,8 +146,8 @@ __device__ __forceinline__ v4f mfma(v4i a, v4i b, v4f c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
-// An fp32 number as three bf16 terms, each the leading bits of what the ones before leave: all 24 bits of it.  Of an infinity the first term is one and nothing
-// is left.
+// An fp32 number as three bf16 terms, each the leading bits of what the ones before leave: all 24 bits of it from 2^-110 on, below that all down to 2^-133, bf16's smallest number.  Of an infinity the
+// first term is one and nothing is left.
 __device__ __forceinline__ float cut(float x) { return __uint_as_float(__float_as_uint(x) & 0xFFFF0000u); }
 __device__ __forceinline__ uint32_t tops(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
 __device__ __forceinline__ void split8(const float (&v)[8], v4i (&t)[3])

@@ -323,3 +323,19 @@ def test_weights_of_another_layer_are_told(lq):
     with pytest.raises(lq.LqError) as e:
         lq.lq_w4_verify(cfg, packed[:-256])
     assert e.value.status == lq.LQ_ERR_BUFFER_TOO_SMALL
+
+
+@pytest.mark.parametrize("e", [-100, -109, -111, -118, -125, -130])
+def test_rows_of_the_smallest_numbers(lq, e):
+    """One channel to a row: the value itself from 2^-110 on; below, what three bf16 terms hold of it, which cut off less than 2^-133."""
+    K, N, M = 256, 48, 16
+    cfg = lq.make_w4_config(N, K, 64, "f32", "f32")
+    packed = lq.lq_w4_pack_codes(cfg, torch.ones(N, K, dtype=torch.int8, device="cuda"), torch.ones(N, K // 64, device="cuda"))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(-e)
+    v = ((1 + torch.rand(M, generator=g, device="cuda").double()) * 2.0 ** e).float()
+    X, dY, rows = torch.zeros(M, K, device="cuda"), torch.zeros(M, N, device="cuda"), torch.arange(M, device="cuda")
+    X[rows, rows * 7], dY[rows, rows * 3] = v, v
+    off = 0.0 if e >= -110 else 2.0 ** -133
+    for got in (lq.lq_w4_fwd(cfg, packed, X), lq.lq_w4_bwd(cfg, packed, dY)):
+        assert ((got.double() - v.double()[:, None]).abs() <= off).all()
