@@ -13,7 +13,8 @@ namespace lq {
 // 8192 rows of 1152, bf16: 26.5 us (4.3 TB/s) and 4.1 for block_sums; the registers allow two wavefronts a SIMD, which wait 38 % of their cycles.  The next row asked for ahead fits into them in bf16
 // without spills and is slower: 32.0 us for 31.1 in all.
 // TENSORS.  ALL: all inputs and results of rows are there, and read VEC values at a time.  SOME may be missing (the branches cost registers: 8192 rows of 1152, layer norm, 23.2 us where
-// ALL takes 22.7).  LOOSE: any may be missing, and of any alignment.
+// ALL takes 22.7).  LOOSE: any may be missing, and of any alignment.  SOME and LOOSE of one wavefront with four or five vectors, a bf16 branch and POST have 133 to 345 registers in scratch (8192 rows of
+// 1152: without dh' 124 us, rows of 1153 136, ALL 32).
 enum { ALL, SOME, LOOSE };
 template <typename TH, typename TY, int VEC, int NV, int TENSORS, bool POST, bool MULTI, int THREADS>
 __global__ void __launch_bounds__(THREADS) block_bwd_kernel(BlockArgs a)
