@@ -217,6 +217,9 @@ __device__ __forceinline__ void parts_of(const BlockArgs& a, int s, int& c0, int
 //     dw_pre = sum over sequences of (1 + scale) sum dx n ;  dw_post = sum of gate sum G p
 // Otherwise raw: the last two sums without the weights, for block_weight_sums.  The modulation of a sequence without rows, and the weights beside it, are not used: whatever they hold, it adds nothing
 // (times a sum of zero, an infinity would be no number).
+// In raw such a sequence has a zero with a sign, which no sum that begins with one without is: block_weight_sums need not look at the offsets (us with them / without, gradient of
+// 1000 rows of 1152 in 100 sequences 27.6 / 25.7, of 8192 in 1000 98.1 / 78.3).
+constexpr uint32_t NO_ROWS = 0x80000000u;
 template <bool FUSED, int COLS>
 __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float* raw)
 {
@@ -258,7 +261,7 @@ __global__ void __launch_bounds__(1024) block_sums(BlockArgs a, int team, float*
                 const float g = rows && f.p ? f.p[s * f.ld + col] : k == 1 ? 0.0f : 1.0f;
                 total = fmaf(k == 1 ? 1.0f + g : g, y, total);
             } else if (raw && k) {
-                raw[((size_t)s * 2 + k - 1) * a.dim + col] = y;
+                raw[((size_t)s * 2 + k - 1) * a.dim + col] = rows ? y : __uint_as_float(NO_ROWS);
             }
         }
         if (team > 1) __syncthreads();
@@ -278,17 +281,15 @@ __global__ void __launch_bounds__(1024) block_weight_sums(BlockArgs a, const flo
 {
     __shared__ float sh[16][64];
     const BlockTensors& t = a.t;
-    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = blockIdx.x * 64 + lane;
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
     const lq_mod& f = k == 0 ? t.scale : t.gate;
     float* out = k == 0 ? t.dw_pre : t.dw_post;
     float y = 0.0f;
     if (col < a.dim && out)
 #pragma unroll 4
         for (int s = wave; s < t.S; s += 16) {
-            int c0, c1;
-            parts_of(a, s, c0, c1);
             const float u = raw[((size_t)s * 2 + k) * a.dim + col], g = f.p ? f.p[s * f.ld + col] : k == 0 ? 0.0f : 1.0f;
-            y += c0 < c1 ? u * (k == 0 ? 1.0f + g : g) : 0.0f;
+            y += __float_as_uint(u) == NO_ROWS ? 0.0f : u * (k == 0 ? 1.0f + g : g);
         }
     sh[wave][lane] = y;
     __syncthreads();
